@@ -313,6 +313,126 @@ pard_status pard_set_attention_split_cap(pard_ctx* ctx, int32_t cap);
  * PARD_ERR_ARG for a null context or another value. */
 pard_status pard_set_share_wait(pard_ctx* ctx, int32_t ns);
 
+/* ---- A decode step over a TREE of drafted tokens ----------------------------
+ *
+ * The paper drafts one chain of K candidates a sequence.  These operators
+ * verify several candidates a position: a tree whose node 0 is the last
+ * emitted token and whose other nodes are drafted tokens, each hung on the
+ * node that it follows.  One step:
+ *   pard_tree_plan      masks, positions and cache slots of the nodes
+ *   (each layer)        pard_qk_norm_rope, pard_tree_attention
+ *   pard_sample         one token a node from its logits
+ *   pard_tree_commit    the path that the drawn tokens lead through; its keys
+ *                       and values become the sequence's next cache entries
+ * Drawing every node's token from the target and following the child that
+ * carries it emits exactly what autoregressive sampling would (a greedy or
+ * deterministic draft needs no rejection step for that).
+ *
+ * They take no context: all device memory is the caller's, work is enqueued
+ * on `stream`, and calls on different streams share nothing but what the
+ * caller shares.  Types: PARD_BF16, PARD_F16 (and PARD_F32 for logits).
+ * Caches are paged, 16 tokens a page: page p holds [n_kv_heads][16][head_dim]
+ * entries at p * page_stride (so a pool [layer][K|V][page][kv_head][16][hd] as
+ * pard_kv_pool_bytes describes it fits, with any page stride that is a
+ * multiple of 8 and no smaller than a page).  d_page_table [batch][max_pages]
+ * lists a sequence's pages in order; d_ctx_len [batch] counts its committed
+ * tokens and d_n_nodes [batch] its tree's nodes (0..width; others are
+ * clamped).  Node i's keys and values lie at position d_ctx_len + i.  A page
+ * id outside [0, n_pages), a position past the table and a slot outside the
+ * pool are never accessed: their keys count as masked, their rows are not
+ * written.  Entries of arrays past a sequence's nodes may hold anything.
+ * Pointers to 16-bit data must be 16-byte aligned and row strides multiples of
+ * 8 entries. */
+enum { PARD_BF16 = 0, PARD_F16 = 1, PARD_F32 = 2 };
+
+/* The plan of a verify pass over trees of up to `width` (<= 256) nodes.
+ * d_parents [batch][width]: the node that each node follows, which must
+ * precede it; -1: none (it follows the committed tokens).  A node with another
+ * parent is dead, and so are those that hang on it.  Outputs, [batch][width]:
+ * d_mask [..][ceil(width / 64)] bit j of word w set where node 64 w + j is the
+ * node itself or one of its ancestors; d_pos its position in its own branch,
+ * d_ctx_len + its ancestors; d_slots its cache slot, page * 16 + offset.  Dead
+ * and unused nodes get mask 0, position 0 and slot -1. */
+pard_status pard_tree_plan(const int32_t* d_parents, const int32_t* d_n_nodes, const int32_t* d_ctx_len,
+                           const int32_t* d_page_table, int32_t batch, int32_t width, int32_t max_pages,
+                           int32_t n_pages, uint64_t* d_mask, int32_t* d_pos, int64_t* d_slots, void* stream);
+
+/* RMS norm of each query and key head, rotary positions, and the cache write,
+ * from the rows of a QKV projection: d_qkv [n_tokens][qkv_stride], a row's
+ * query heads, key heads, value heads in order.
+ *   x' = x * rsqrt(mean(x^2) + eps) * gain      d_q_gain, d_k_gain [head_dim], null: no norm
+ *   (a, b) -> amplitude * (a cos t - b sin t, a sin t + b cos t),  t = d_pos * d_inv_freq[i]
+ * on the first rot_dim (a multiple of 16, at most head_dim; 0: none) entries of
+ * a query or key head, in pairs (i, i + rot_dim / 2), or (2i, 2i + 1) where
+ * `interleaved`.  Scaling for long contexts is a matter of d_inv_freq
+ * [rot_dim / 2] and amplitude.  Angles are exact for any position.  Queries go
+ * to d_q [n_tokens][q_stride], keys and values to their caches at d_slots
+ * (page * 16 + offset; negative or past the pool: not written), rounded once
+ * to `dtype`.  head_dim 64 or 128.  No output may overlap d_qkv. */
+pard_status pard_qk_norm_rope(const void* d_qkv, int64_t qkv_stride, int32_t dtype, int32_t n_tokens,
+                              int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, const void* d_q_gain,
+                              const void* d_k_gain, float eps, const int32_t* d_pos, const int64_t* d_slots,
+                              const float* d_inv_freq, int32_t rot_dim, int32_t interleaved, float amplitude,
+                              void* d_q, int64_t q_stride, void* d_k_cache, void* d_v_cache, int64_t page_stride,
+                              int32_t n_pages, void* stream);
+
+/* Attention of each tree node over its sequence's committed keys and the tree
+ * keys that its mask row names:
+ *   o = sum_j softmax_j(scale q . k_j) v_j
+ * d_q [batch * width][q_stride], query heads of head_dim (64 or 128) entries;
+ * query head h reads key/value head h / (n_q_heads / n_kv_heads).  d_mask
+ * [batch][width][ceil(width / 64)] as pard_tree_plan writes it, or any other
+ * (bits at or past a sequence's nodes are ignored).  d_out [batch][width]
+ * [n_q_heads][head_dim]: zero for a node that sees no key and for unused
+ * nodes.  Masked keys and values may hold infinities or NaN.  Scores and sums
+ * are held in 32 bits; probabilities are rounded to `dtype` before they
+ * multiply the values.  d_workspace: pard_tree_attention_workspace_bytes (0:
+ * invalid arguments), which the call neither reads nor needs afterwards; calls
+ * that may overlap on the GPU need one each. */
+size_t pard_tree_attention_workspace_bytes(int32_t batch, int32_t width, int32_t n_q_heads, int32_t n_kv_heads,
+                                           int32_t head_dim);
+pard_status pard_tree_attention(const void* d_q, int64_t q_stride, int32_t dtype, int32_t batch, int32_t width,
+                                int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, const void* d_k_cache,
+                                const void* d_v_cache, int64_t page_stride, int32_t n_pages,
+                                const int32_t* d_page_table, int32_t max_pages, const int32_t* d_ctx_len,
+                                const int32_t* d_n_nodes, const uint64_t* d_mask, float scale, void* d_out,
+                                void* d_workspace, size_t workspace_bytes, void* stream);
+
+/* One token for each row of logits [rows][row_stride] (vocab <= 262144 entries
+ * each), drawn with a given number d_u in [0, 1) from softmax(z / temperature)
+ * after three cuts, in this order (each array [rows], null: off):
+ *   d_top_k  > 0: the k largest (equal logits: lowest index first);
+ *   d_top_p  < 1: of those, the shortest run from the largest down whose mass
+ *                 reaches p times theirs;
+ *   d_min_p  in [0, 1]: those with at least min_p times the largest's probability.
+ * The largest entry is always kept.  d_token is the lowest index at which the
+ * kept entries' mass, summed in index order, exceeds u times their total;
+ * d_logprob its log-probability among the kept.  temperature 0 (d_temperature
+ * null: 1): the largest logit, lowest index first, log-probability 0.  NaN
+ * counts as -infinity; a row without an entry above that gives token -1 and
+ * -infinity.  Weights e^((z - max) / T) are summed as whole multiples of
+ * 2^-40: results do not depend on any order of summation. */
+pard_status pard_sample(const void* d_logits, int64_t row_stride, int32_t dtype, int32_t rows, int32_t vocab,
+                        const float* d_u, const float* d_temperature, const int32_t* d_top_k, const float* d_top_p,
+                        const float* d_min_p, int32_t* d_token, float* d_logprob, void* stream);
+
+/* Walks each tree from node 0 along the drawn tokens d_sampled [batch][width]:
+ * from a node to its lowest child whose d_tokens entry is the token drawn at
+ * the node, until none is.  The path's keys and values move, in every layer of
+ * the pool, to positions d_ctx_len + 0, 1, ... (in place; other rows keep what
+ * they hold).  d_pool's layers lie layer_stride entries apart, a layer's keys
+ * and values kv_stride, pages page_stride.  Outputs: d_accept_len [batch] (nodes
+ * on the path after node 0), d_emitted [batch][width] (the tokens drawn along
+ * the path, accept_len + 1 of them, then -1) and d_new_len [batch] (d_ctx_len +
+ * path nodes; the last emitted token's keys are not in the cache yet).  A tree
+ * without nodes emits nothing.  d_new_len must not be d_ctx_len. */
+pard_status pard_tree_commit(const int32_t* d_sampled, const int32_t* d_tokens, const int32_t* d_parents,
+                             const int32_t* d_n_nodes, const int32_t* d_ctx_len, const int32_t* d_page_table,
+                             int32_t batch, int32_t width, int32_t max_pages, void* d_pool, int64_t layer_stride,
+                             int64_t kv_stride, int64_t page_stride, int32_t n_layers, int32_t n_kv_heads,
+                             int32_t head_dim, int32_t n_pages, int32_t* d_accept_len, int32_t* d_emitted,
+                             int32_t* d_new_len, void* stream);
+
 /* Thread-local message for the last failing call ("" if none). */
 const char* pard_last_error(void);
 
