@@ -284,6 +284,13 @@ def test_attention_widest_tree_and_long_context(tree, dtype, hd):
     check_attention(tree, dtype, 8, 2, hd, [20011, 3], [3, 2], 3, seed=4, spread=2.0)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("Hq,Hkv,hd,width", [(32, 32, 128, 3), (32, 32, 64, 5), (64, 16, 128, 40), (96, 24, 64, 33)])
+def test_attention_many_tiles_a_cta(tree, dtype, Hq, Hkv, hd, width):
+    """Ranges of a dozen tiles and more, of several units: every stage of the ring is used again and again."""
+    check_attention(tree, dtype, Hq, Hkv, hd, [5000, 1777, 3, 2900], [width, width - 1, width, 2], width, seed=width)
+
+
 def test_attention_many_short_sequences(tree):
     rs = np.random.RandomState(8)
     lens, nodes = [int(x) for x in rs.randint(0, 200, 70)], [int(x) for x in rs.randint(0, 10, 70)]
