@@ -387,8 +387,11 @@ pard_status pard_qk_norm_rope(const void* d_qkv, int64_t qkv_stride, int32_t dty
  * nodes.  Masked keys and values may hold infinities or NaN.  Scores and sums
  * are held in 32 bits; probabilities are rounded to `dtype` before they
  * multiply the values.  d_workspace: pard_tree_attention_workspace_bytes (0:
- * invalid arguments), which the call neither reads nor needs afterwards; calls
- * that may overlap on the GPU need one each. */
+ * invalid arguments) bytes that are zero before the first call; each call
+ * leaves them fit for the next, of any sizes that they are enough for.  Calls
+ * that may overlap on the GPU need one each.  Should a wait inside the kernel
+ * ever run out (2 s), the output is NaN, and so is that of later calls until
+ * the workspace is zeroed again. */
 size_t pard_tree_attention_workspace_bytes(int32_t batch, int32_t width, int32_t n_q_heads, int32_t n_kv_heads,
                                            int32_t head_dim);
 pard_status pard_tree_attention(const void* d_q, int64_t q_stride, int32_t dtype, int32_t batch, int32_t width,

@@ -67,6 +67,8 @@ struct TreeAttnArgs {
   void* workspace;
 };
 size_t tree_attention_workspace(int batch, int width, int n_q_heads, int n_kv_heads, int head_dim);
+// places of the work ranges that a pass may have: below 2^31
+int64_t tree_attention_places(int batch, int width, int n_q_heads, int n_kv_heads, int max_pages);
 void launch_tree_attention(const TreeAttnArgs& a, cudaStream_t s);
 
 struct SampleArgs {

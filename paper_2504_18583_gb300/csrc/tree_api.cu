@@ -122,6 +122,8 @@ pard_status pard_tree_attention(const void* d_q, int64_t q_stride, int32_t dtype
       !aligned16(d_workspace))
     return refuse(PARD_ERR_ARG, "rows, caches, output and workspace must start on 16-byte boundaries");
   if (!std::isfinite(scale)) return refuse(PARD_ERR_ARG, "the scale must be finite");
+  if (tree_attention_places(batch, width, n_q_heads, n_kv_heads, max_pages) >= ((int64_t)1 << 31))
+    return refuse(PARD_ERR_SHAPE, "more than 2^31 tiles of 128 keys: shorter page tables or a smaller batch");
   if (workspace_bytes < tree_attention_workspace(batch, width, n_q_heads, n_kv_heads, head_dim))
     return refuse(PARD_ERR_ARG, "workspace smaller than pard_tree_attention_workspace_bytes");
   const TreeAttnArgs a{d_q, d_k_cache, d_v_cache, q_stride, page_stride, d_page_table, d_ctx_len, d_n_nodes, d_mask,

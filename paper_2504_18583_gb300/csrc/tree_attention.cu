@@ -4,12 +4,15 @@
 //
 // A unit is one sequence's key/value head with up to 128 or 256 query vectors
 // (nodes x the query heads that share the head) and its keys in tiles of 128.
-// All units' tiles, in order, are cut into one even range a CTA (one CTA an SM,
-// persistent): contexts may differ by any factor, the host need not know them,
-// and no SM waits for a long sequence.  A range that begins or ends inside a
-// unit leaves a partial (unnormalised O, maximum, sum, all in 32 bits) in the
-// workspace; the combine kernel joins a unit's partials in tile order, so
-// results do not depend on timing.
+// Each CTA (one an SM) works out its share from the sequences' lengths, which
+// the host need not know.  A unit that is split between CTAs costs its
+// partials' way through L2 (kSplit tiles' time), so units stay whole where they
+// can: with no more units than CTAs, each CTA takes one equal part of one unit,
+// the parts no longer than they must be; with more, all units' tiles, in order,
+// are cut into one even range a CTA, and a cut near a unit's end moves there.
+// A part leaves a partial (unnormalised O, maximum, sum, all in 32 bits) in the
+// workspace; the last of a unit's CTAs to arrive joins them in tile order, so no
+// CTA waits for another and results do not depend on timing.
 //
 // Roles: warp 0 loads (TMA boxes of one page's 16 tokens x 64 entries: a tile
 // of eight pages lands as the 128-byte-swizzled operand that the products
@@ -45,17 +48,15 @@ namespace {
 constexpr int kTile = 128;                      // keys a tile, rows a score tile
 constexpr int kTilePages = kTile / kPageTok;
 constexpr int kTaThreads = 384;
+constexpr int kStart = 2, kSplit = 6;           // what a unit's start, and splitting it, costs in tiles
+constexpr int kSeqCache = 64;                   // sequences whose lengths a CTA keeps at hand
 constexpr int kMaxGrid = 160;                   // workspace slots are sized for this many CTAs
 constexpr float kLazy = 8.0f;                   // growth of a maximum, in powers of two, that is let pass
 
 __host__ __device__ constexpr int stage_bytes(int hd) { return kTile * hd * 2; }
-__host__ __device__ constexpr int stages(int hd, int blocks) { return (hd == 128 ? 7 : 14) - (hd == 128 ? blocks : 2 * blocks); }
-__host__ __device__ constexpr int bar_bytes(int hd, int blocks) { return (8 * (3 * stages(hd, blocks) + 10) + 16 + 8 * stages(hd, blocks) + 127) / 128 * 128; }
-__host__ __device__ constexpr int smem_bytes(int hd, int blocks) {
-  return 1024 + (blocks + stages(hd, blocks)) * stage_bytes(hd) + bar_bytes(hd, blocks);
-}
-static_assert(smem_bytes(128, 1) <= 227 * 1024 && smem_bytes(128, 2) <= 227 * 1024, "shared memory of one CTA");
-static_assert(smem_bytes(64, 1) <= 227 * 1024 && smem_bytes(64, 2) <= 227 * 1024, "shared memory of one CTA");
+// tiles of keys, and of values, in flight: what shared memory holds beside the queries
+__host__ __device__ constexpr int k_stages(int hd, int blocks) { return hd == 128 ? (blocks == 1 ? 3 : 2) : (blocks == 1 ? 6 : 5); }
+__host__ __device__ constexpr int v_stages(int hd, int blocks) { return hd == 128 ? 3 : (blocks == 1 ? 6 : 5); }
 
 template <typename T> struct Num;
 template <> struct Num<__nv_bfloat16> {
@@ -83,19 +84,6 @@ __host__ __device__ constexpr uint32_t idesc16(uint32_t fmt, int M, int N, bool 
   return (1u << 4) | (fmt << 7) | (fmt << 10) | ((flip ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) |
          ((uint32_t)(M >> 4) << 24);
 }
-// Descriptor of a 128-byte-swizzled operand whose N (or M) entries are
-// contiguous: 64 of them a 128-byte row, eight K rows an atom; atoms 1024 bytes
-// apart along K, `chunk` bytes along N.
-__device__ __forceinline__ uint64_t sw128_flip_desc(uint32_t addr, uint32_t chunk) {
-  uint64_t d = 0;
-  d |= (uint64_t)((addr & 0x3FFFFu) >> 4);
-  d |= (uint64_t)(chunk >> 4) << 16;
-  d |= (uint64_t)(1024 >> 4) << 32;
-  d |= (uint64_t)1 << 46;
-  d |= (uint64_t)2 << 61;
-  return d;
-}
-
 __device__ __forceinline__ void umma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
   umma_bf16(d, a, b, idesc, accumulate);  // the descriptor names the type
 }
@@ -140,11 +128,56 @@ __device__ __forceinline__ void tm_st32(uint32_t addr, const uint32_t* r) {
       : "memory");
 }
 __device__ __forceinline__ void tm_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// ... after which registers hold what was loaded: nothing moves their uses before it
+template <int N>
+__device__ __forceinline__ void tm_landed(uint32_t* r) {
+  tm_wait_ld();
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+r"(r[i]));
+}
 __device__ __forceinline__ void tm_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+// two 32-bit floats at a time
+__device__ __forceinline__ uint64_t pair_of(uint32_t x, uint32_t y) {
+  uint64_t p;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "r"(x), "r"(y));
+  return p;
+}
+__device__ __forceinline__ float2 floats_of(uint64_t p) {
+  uint32_t x, y;
+  asm("mov.b64 {%0, %1}, %2;" : "=r"(x), "=r"(y) : "l"(p));
+  return make_float2(__uint_as_float(x), __uint_as_float(y));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+// This row's accumulator times alpha, 16 columns a turn: the scores stay in
+// their registers meanwhile.
+template <int HD>
+__device__ __forceinline__ void scale_row(uint32_t o_addr, float alpha) {
+#pragma unroll 1
+  for (int c = 0; c < HD; c += 16) {
+    uint32_t o[16];
+    tmem_ld16(o_addr + c, o);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::"r"(o[0]),
+        "r"(o[1]), "r"(o[2]), "r"(o[3]), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7]), "r"(o[8]), "r"(o[9]), "r"(o[10]),
+        "r"(o[11]), "r"(o[12]), "r"(o[13]), "r"(o[14]), "r"(o[15]), "r"(o_addr + c)
+        : "memory");
+  }
 }
 // Two 16-bit values with infinities and NaN replaced by zero.
 template <typename T>
@@ -154,19 +187,26 @@ __device__ __forceinline__ uint32_t finite_of(uint32_t v) {
   if ((v >> 16 & e) == e) v &= 0x0000FFFFu;
   return v;
 }
-// A bounded wait that all lanes of a warp leave with the same answer.
+// A bounded wait that all lanes of a warp leave with the same answer.  (Counted
+// and not timed: the loop is inlined some twenty times, and what a CTA runs once
+// it waits for, instruction by instruction.  Each try suspends the warp for a
+// while by itself.)
+constexpr int kTries = 1 << 22;
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort) {
-  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort));
+  bool done = mbar_try_wait(bar, parity);
+#pragma unroll 1
+  for (int i = 0; !done && i < kTries && !*abort; ++i) done = mbar_try_wait(bar, parity);
+  return __all_sync(0xffffffffu, done);
 }
 
 // Keys, tiles and row blocks of a sequence.
 struct Seq {
   int ctx, nodes, keys, plain, tiles, blocks;  // plain: keys that every node sees
 };
-__device__ __forceinline__ Seq seq_of(const TreeAttnArgs& a, int b, int rows_per_block) {
+__device__ __forceinline__ Seq seq_of(const TreeAttnArgs& a, int ctx, int nodes, int rows_per_block) {
   Seq s;
-  s.nodes = min(max(a.n_nodes[b], 0), a.width);
-  s.ctx = max(a.ctx_len[b], 0);
+  s.nodes = min(max(nodes, 0), a.width);
+  s.ctx = max(ctx, 0);
   const int64_t end = (int64_t)s.ctx + s.nodes, most = (int64_t)a.max_pages * kPageTok;
   s.keys = (int)(end < most ? end : most);
   s.plain = min(s.ctx, s.keys);
@@ -174,50 +214,84 @@ __device__ __forceinline__ Seq seq_of(const TreeAttnArgs& a, int b, int rows_per
   s.blocks = (s.nodes * (a.n_q_heads / a.n_kv_heads) + rows_per_block - 1) / rows_per_block;
   return s;
 }
-__device__ __forceinline__ int64_t seq_cost(const TreeAttnArgs& a, const Seq& s) {
-  return (int64_t)a.n_kv_heads * s.blocks * s.tiles;
+// Ranges count a unit as kStart tiles more than it has: what its queries,
+// first loads and epilogue cost.  (All of them together stay below 2^31: the
+// caller has checked.)
+__device__ __forceinline__ int seq_cost(const TreeAttnArgs& a, const Seq& s) {
+  return s.tiles ? a.n_kv_heads * s.blocks * (s.tiles + kStart) : 0;
 }
-__device__ __forceinline__ int64_t range_at(int c, int64_t total, int grid) { return c * total / grid; }
-
-// A CTA's walk over its range: one segment (part of a unit) after the other.
-struct Walk {
-  int64_t left;        // tiles to go
-  int b, off;          // sequence, and tile within all of its units
-  Seq s;
-  int head, block, t0, t1;
-  __device__ __forceinline__ bool next(const TreeAttnArgs& a, int rows_per_block) {
-    if (left <= 0) return false;
-    while (off >= seq_cost(a, s)) {  // the first call's off lies inside its sequence
-      ++b;
-      off = 0;
-      s = seq_of(a, b, rows_per_block);
-    }
-    const int unit = off / s.tiles;
-    t0 = off - unit * s.tiles;
-    t1 = (int)min((int64_t)s.tiles, t0 + left);
-    head = unit / s.blocks;
-    block = unit - head * s.blocks;
-    off += t1 - t0;
-    left -= t1 - t0;
-    return true;
+// Parts of a unit of so many tiles where a part has `most`: one that is longer
+// by less than a split costs stays whole.
+__device__ __forceinline__ int parts_of(int tiles, int most) {
+  // (the quotient in floating point is exact: half a unit off any whole number)
+  return tiles <= most + kSplit ? 1 : (int)__fdividef((float)(tiles + most) - 0.5f, (float)most);
+}
+// Where CTA c's range begins: floor(total c / grid).
+struct Ranges {
+  int total, grid, each, rest;
+  __device__ __forceinline__ void set(int n, int g) {
+    total = n;
+    grid = g;
+    each = n / g;
+    rest = n - each * g;
+  }
+  __device__ __forceinline__ int at(int c) const { return c * each + c * rest / grid; }
+  // a cut at place x of a unit of `len` places: near an end it moves there
+  static __device__ __forceinline__ int cut(int x, int len) {
+    return x <= kSplit ? 0 : x >= len - kSplit ? len : x;
   }
 };
 
-// Order in which a segment's n tiles are loaded (K and V are an item each).
-// Two query blocks: K0 V0 K1 V1 ...; one: K0 K1 V0 K2 V1 ..., the order in
-// which two alternating tiles are consumed.
-template <int BLOCKS> __device__ __forceinline__ int item_k(int j) { return BLOCKS == 2 ? 2 * j : (j ? 2 * j - 1 : 0); }
-template <int BLOCKS> __device__ __forceinline__ int item_v(int j, int n) {
-  return BLOCKS == 2 ? 2 * j + 1 : (j < n - 1 ? 2 * j + 2 : 2 * n - 1);
-}
-// which tile item i is of, and whether it is its values
-template <int BLOCKS> __device__ __forceinline__ int tile_of(int i, int n, bool& v) {
-  if (BLOCKS == 2) { v = i & 1; return i >> 1; }
-  if (i == 0) { v = false; return 0; }
-  if (i == 2 * n - 1) { v = true; return n - 1; }
-  v = !(i & 1);
-  return v ? (i - 2) >> 1 : (i + 1) >> 1;
-}
+// A warp's walk over its CTA's share: one segment (part of a unit) after the
+// other.  It lies in shared memory: held in registers, it made the softmax's
+// scores spill.
+struct Walk {
+  int left;            // places to go; in the one-part form 1, then 0
+  int b, off;          // sequence, and place within all of its units
+  int at;              // place of the whole pass that off counts from
+  Seq s;
+  int head, block, t0, t1;
+  int count, me, c0;   // the unit's contributors, this CTA's place among them, the first of them
+  __device__ __forceinline__ void load(const TreeAttnArgs& a, const int2* cache, int rows_per_block) {
+    const int2 v = b < kSeqCache ? cache[b] : make_int2(a.ctx_len[b], a.n_nodes[b]);
+    s = seq_of(a, v.x, v.y, rows_per_block);
+  }
+  __device__ __noinline__ bool next(const TreeAttnArgs& a, const int2* cache, int rows_per_block, const Ranges& ranges,
+                                    bool one_part) {
+    if (one_part) return left-- > 0;
+    while (left > 0) {
+      for (int cost = seq_cost(a, s); off >= cost; cost = seq_cost(a, s)) {  // the first call's off lies inside its sequence
+        at += cost;
+        ++b;
+        off = 0;
+        load(a, cache, rows_per_block);
+      }
+      const int len = s.tiles + kStart, unit = off / len, y = off - unit * len;
+      const int x0 = Ranges::cut(y, len), x1 = y + left < len ? Ranges::cut(y + left, len) : len;
+      const int u0 = at + off - y;  // place of the unit in the whole pass
+      head = unit / s.blocks;
+      block = unit - head * s.blocks;
+      const int step = min(len - y, left);
+      off += step;
+      left -= step;
+      t0 = max(0, x0 - kStart);
+      t1 = x1 - kStart;
+      if (t1 <= t0) continue;
+      count = 1;
+      me = 0;
+      c0 = blockIdx.x;
+      if (t0 > 0 || t1 < s.tiles) {  // who else has a part of it
+        while (c0 > 0 && ranges.at(c0) > u0 && Ranges::cut(ranges.at(c0) - u0, len) > 0) --c0;
+        int c1 = blockIdx.x;
+        while (c1 + 1 < ranges.grid && ranges.at(c1 + 1) < u0 + len && Ranges::cut(ranges.at(c1 + 1) - u0, len) < len) ++c1;
+        count = c1 - c0 + 1;
+        me = (int)blockIdx.x - c0;
+      }
+      return true;
+    }
+    return false;
+  }
+};
 
 // 32 of a row's allowed columns, from the mask bits of its node: column 0 is
 // key `key`; bits of the context are set, those past the nodes clear.
@@ -234,170 +308,409 @@ __device__ __forceinline__ uint32_t allowed32(const uint32_t* row, int words32, 
   return some >= 32 ? m : some <= 0 ? 0u : m & ((1u << some) - 1u);
 }
 
-struct Partial {  // of one slot, rows = 128 * blocks: O as [HD / 4][rows] float4, then maxima, sums
+// A slot holds one partial, rows = 128 * blocks: O as [HD / 4][rows] float4,
+// then each softmax group's maxima and sums.  Before the slots: arrivals at a
+// unit, by the CTA that has its first tile, for each group.
+struct Partial {
   float* base;
   int rows;
   __device__ __forceinline__ float4* o(int c4, int row) const { return reinterpret_cast<float4*>(base) + (size_t)c4 * rows + row; }
-  __device__ __forceinline__ float* max_of(int hd, int row) const { return base + (size_t)hd * rows + row; }
-  __device__ __forceinline__ float* sum_of(int hd, int row) const { return base + (size_t)(hd + 1) * rows + row; }
+  __device__ __forceinline__ float2* stats(int hd, int g, int row) const {
+    return reinterpret_cast<float2*>(base + (size_t)hd * rows) + (size_t)g * rows + row;
+  }
 };
-__host__ __device__ constexpr size_t slot_floats(int hd, int blocks) { return (size_t)(hd + 2) * kTile * blocks; }
-constexpr size_t kStatusBytes = kMaxGrid * 4;
+__host__ __device__ constexpr size_t slot_floats(int hd, int blocks) { return (size_t)(hd + 4) * kTile * blocks; }
+constexpr int kStalledWord = 2 * kMaxGrid;       // after the arrivals: a wait has run out in some call
+constexpr size_t kArriveBytes = (kStalledWord + 4) * sizeof(uint32_t);
 __device__ __forceinline__ Partial slot_of(const TreeAttnArgs& a, int slot, int hd, int blocks) {
-  return Partial{reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(a.workspace) + kStatusBytes) +
+  return Partial{reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(a.workspace) + kArriveBytes) +
                      (size_t)slot * slot_floats(hd, blocks),
                  kTile * blocks};
 }
+__device__ __forceinline__ uint32_t ld_acquire(const uint32_t* p) {
+  uint32_t v;
+  asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ void fence_gpu() { asm volatile("fence.acq_rel.gpu;" ::: "memory"); }
+__device__ __forceinline__ uint32_t arrive_acq_rel(uint32_t* p) {
+  uint32_t old;
+  asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(old) : "l"(p) : "memory");
+  return old;
+}
+
+// Adds the infinities and NaN of the values at positions [from, end), tree
+// nodes', back to a row that sees them: to the output, or to a partial.  (In
+// the joined output they go on top of the sum, where they stay what they are.)
+template <typename T, int HD>
+__device__ __noinline__ void patch_row(const TreeAttnArgs& a, int b, int head, const Seq& s, int from, int end,
+                                       const uint32_t* mrow, int col0, int cols, T* out, Partial part, int row) {
+  for (int pos = from; pos < end; ++pos) {
+    const int node = pos - s.ctx, page = page_of(a.page_table + (size_t)b * a.max_pages, pos, a.max_pages, a.n_pages);
+    if (page < 0 || !(mrow[node >> 5] >> (node & 31) & 1)) continue;
+    const T* v = reinterpret_cast<const T*>(a.v_cache) + page * a.page_stride + ((int64_t)head * kPageTok + pos % kPageTok) * HD;
+#pragma unroll 1
+    for (int c = col0; c < col0 + cols; ++c) {
+      const float x = Num<T>::get(v + c);
+      if (fabsf(x) < INFINITY) continue;
+      if (out) {
+        const uint32_t y = Num<T>::pack(Num<T>::get(out + c) + x, 0.f);
+        *reinterpret_cast<uint16_t*>(out + c) = (uint16_t)y;
+      } else {
+        reinterpret_cast<float*>(part.o(c / 4, row))[c % 4] += x;
+      }
+    }
+  }
+}
+
+// What a CTA keeps in shared memory behind the operands.
+template <int NK, int NV>
+struct Control {
+  uint64_t k_full[NK], k_empty[NK], v_full[NV], v_empty[NV];
+  uint64_t fixed[NV];      // a stage's values are fit for the product
+  uint64_t s_full[2];      // scores of a group are in tensor memory
+  uint64_t p_full[2];      // its probabilities are, and O is scaled
+  uint64_t o_full[2];      // a segment's last product is done
+  uint64_t ready[2];       // the group has read O and laid out its queries
+  uint64_t pair, met[2];   // the two groups meet, a group's warps do
+  uint64_t drain;          // every product is done
+  uint32_t tmem, last_in[2], odd[NV];  // odd: a stage's tree values held infinities or NaN
+  int abort_flag, start_b, start_off;
+  int sum[kTaThreads / 32], units[kTaThreads / 32], most[kTaThreads / 32];
+  int2 seq[kSeqCache];
+  Walk walk[kTaThreads / 32];
+  uint16_t slots[2][kMaxGrid];
+};
+
+// Joins a unit's partials, in order, for one group's rows and columns.  Threads
+// take rows (32, 64 or 128 of them) and share a row's columns out; the loads of
+// four partials' four pieces go out together.  It runs once a unit: its code
+// comes from L2 as its data do, so it is kept short.
+template <typename T, int HD, int BLOCKS>
+__device__ __noinline__ void join(const TreeAttnArgs& a, const uint16_t* slots, int count, int g, int t, int row0, int rows,
+                                  int c4_0, int n_c4, T* unit_out, int unit_row0) {
+  const int span = rows <= 32 ? 32 : rows <= 64 ? 64 : 128, row = t & (span - 1), step = kTile / span;
+  if (row >= rows) return;
+  const int group = a.n_q_heads / a.n_kv_heads, r = unit_row0 + row, node = r / group;
+  T* out = unit_out + ((int64_t)node * a.n_q_heads + (r - node * group)) * HD + c4_0 * 4;
+#pragma unroll 1
+  for (int c = t / span; c < n_c4; c += 4 * step) {
+    float4 acc[4];
+    float m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+    for (int i0 = 0; i0 < count; i0 += 4) {
+      float4 v[4][4];
+      float2 st[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        st[i] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[i][e] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (i0 + i < count) {
+          const Partial p = slot_of(a, slots[i0 + i], HD, BLOCKS);
+          st[i] = *p.stats(HD, g, row0 + row);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[i][e] = *p.o(c4_0 + min(c + e * step, n_c4 - 1), row0 + row);
+        }
+      }
+      const float top = fmaxf(fmaxf(m, fmaxf(st[0].x, st[1].x)), fmaxf(st[2].x, st[3].x)), base = top == -INFINITY ? 0.f : top;
+      const float old = ex2(m - base);
+      m = top;
+      l *= old;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { acc[e].x *= old; acc[e].y *= old; acc[e].z *= old; acc[e].w *= old; }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float w = ex2(st[i].x - base);
+        l = fmaf(st[i].y, w, l);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          acc[e].x = fmaf(v[i][e].x, w, acc[e].x);
+          acc[e].y = fmaf(v[i][e].y, w, acc[e].y);
+          acc[e].z = fmaf(v[i][e].z, w, acc[e].z);
+          acc[e].w = fmaf(v[i][e].w, w, acc[e].w);
+        }
+      }
+    }
+    const float inv = l > 0.f ? 1.0f / l : 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      uint2 p;
+      p.x = Num<T>::pack(acc[e].x * inv, acc[e].y * inv);
+      p.y = Num<T>::pack(acc[e].z * inv, acc[e].w * inv);
+      if (c + e * step < n_c4) *reinterpret_cast<uint2*>(out + (c + e * step) * 4) = p;
+    }
+  }
+}
+
+template <int HD, int BLOCKS>
+constexpr int smem_bytes() {
+  return (BLOCKS + k_stages(HD, BLOCKS) + v_stages(HD, BLOCKS)) * stage_bytes(HD) +
+         (int)sizeof(Control<k_stages(HD, BLOCKS), v_stages(HD, BLOCKS)>);
+}
+static_assert(smem_bytes<128, 1>() <= 227 * 1024 && smem_bytes<128, 2>() <= 227 * 1024, "shared memory of one CTA");
+static_assert(smem_bytes<64, 1>() <= 227 * 1024 && smem_bytes<64, 2>() <= 227 * 1024, "shared memory of one CTA");
 
 }  // namespace
 
 template <typename T, int HD, int BLOCKS>
 __global__ void __launch_bounds__(kTaThreads, 1)
-    tree_attention_kernel(const TreeAttnArgs a, const __grid_constant__ CUtensorMap kmap,
+    tree_attention_kernel(const __grid_constant__ TreeAttnArgs a, const __grid_constant__ CUtensorMap kmap,
                           const __grid_constant__ CUtensorMap vmap) {
-  constexpr int NS = stages(HD, BLOCKS), kStage = stage_bytes(HD), kChunks = HD / 64, kChunkBytes = kTile * 128;
-  constexpr int kRows = kTile * BLOCKS;
+  constexpr int NK = k_stages(HD, BLOCKS), NV = v_stages(HD, BLOCKS), kStage = stage_bytes(HD);
+  constexpr int kChunks = HD / 64, kChunkBytes = kTile * 128, kRows = kTile * BLOCKS;
   constexpr uint32_t kIdescS = idesc16(Num<T>::kFormat, kTile, kTile, false);
   constexpr uint32_t kIdescO = idesc16(Num<T>::kFormat, kTile, HD, true);
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t* qbuf = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint8_t* ring = qbuf + BLOCKS * kStage;
-  uint64_t* full = reinterpret_cast<uint64_t*>(ring + NS * kStage);
-  uint64_t* fixed = full + NS;     // [NS], by tiles: a tile's values are fit for the product
-  uint64_t* empty = fixed + NS;
-  uint64_t* s_full = empty + NS;   // [2] scores of a group are in tensor memory
-  uint64_t* p_full = s_full + 2;   // [2] probabilities are, and O is scaled
-  uint64_t* o_full = p_full + 2;   // [2] a segment's last product is done
-  uint64_t* ready = o_full + 2;    // [2] the group has read O and laid out its queries
-  uint64_t* pair = ready + 2;      // the two groups meet
-  uint64_t* drain = pair + 1;      // every product is done
-  uint32_t* misc = reinterpret_cast<uint32_t*>(drain + 1);
-  uint32_t* tmem_slot = misc;
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 1);
-  int* start_b = reinterpret_cast<int*>(misc + 2);
-  int* start_off = start_b + 1;
-  uint32_t* odd = misc + 4;        // [NS][2], by tiles: its tree values held infinities or NaN
+  extern __shared__ __align__(1024) uint8_t qbuf[];  // queries, then the rings
+  uint8_t* kring = qbuf + BLOCKS * kStage;
+  uint8_t* vring = kring + NK * kStage;
+  Control<NK, NV>& sh = *reinterpret_cast<Control<NK, NV>*>(vring + NV * kStage);
+  volatile int* abort_flag = &sh.abort_flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int group = a.n_q_heads / a.n_kv_heads;
+  const int group = a.n_q_heads / a.n_kv_heads, grid = gridDim.x;
 
   // ---- this CTA's range -------------------------------------------------------
-  __shared__ int64_t s_sum[kTaThreads / 32];
-  int64_t total = 0;
-  for (int b0 = 0; b0 < a.batch; b0 += kTaThreads)
-    if (b0 + tid < a.batch) total += seq_cost(a, seq_of(a, b0 + tid, kRows));
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-  if (lane == 0) s_sum[warp] = total;
+  if (warp == 1) tmem_alloc(&sh.tmem, 512);
   if (tid == 0) {
-    for (int i = 0; i < NS; ++i) { mbar_init(full + i, 1); mbar_init(fixed + i, 2); mbar_init(empty + i, 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(s_full + i, 1); mbar_init(p_full + i, 4); mbar_init(o_full + i, 1); mbar_init(ready + i, 4); }
-    mbar_init(pair, 8);
-    mbar_init(drain, 1);
+    tma_prefetch_desc(&kmap);
+    tma_prefetch_desc(&vmap);
+#pragma unroll 1
+    for (int i = 0; i < NK; ++i) { mbar_init(sh.k_full + i, 1); mbar_init(sh.k_empty + i, 1); }
+#pragma unroll 1
+    for (int i = 0; i < NV; ++i) { mbar_init(sh.v_full + i, 1); mbar_init(sh.v_empty + i, 1); mbar_init(sh.fixed + i, 1); }
+#pragma unroll 1
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(sh.s_full + i, 1); mbar_init(sh.p_full + i, 4);
+      mbar_init(sh.o_full + i, 1); mbar_init(sh.ready + i, 4); mbar_init(sh.met + i, 4);
+    }
+    mbar_init(&sh.pair, 8);
+    mbar_init(&sh.drain, 1);
     fence_barrier_init();
     *abort_flag = 0;
   }
-  __syncthreads();
-  total = 0;
-  for (int i = 0; i < kTaThreads / 32; ++i) total += s_sum[i];
-  const int64_t lo = range_at(blockIdx.x, total, gridDim.x), hi = range_at(blockIdx.x + 1, total, gridDim.x);
-  if (tid == 0) reinterpret_cast<uint32_t*>(a.workspace)[blockIdx.x] = 0;  // status: raised where a wait runs out
-  pdl_trigger();
-  if (lo >= hi) return;
-  int64_t run = 0;
-  for (int b0 = 0; b0 < a.batch && run <= lo; b0 += kTaThreads) {
-    const int64_t cost = b0 + tid < a.batch ? seq_cost(a, seq_of(a, b0 + tid, kRows)) : 0;
-    int64_t inc = cost;
+  const uint32_t stalled = reinterpret_cast<const volatile uint32_t*>(a.workspace)[kStalledWord];
+  // The share's form and, in ranges, this CTA's first place: two rounds over the
+  // sequences, their sum and then the place in it; both are one round of a
+  // single step for up to 384.
+  Ranges ranges;
+  int lo = 0, hi = 0, units = 0, longest = 0;
+#pragma unroll 1
+  for (int round = 0; round < 2; ++round) {
+    int run = 0;
+#pragma unroll 1
+    for (int b0 = 0; b0 < a.batch; b0 += kTaThreads) {
+      const int b = b0 + tid;
+      int2 v = make_int2(0, 0);
+      if (b < a.batch) v = make_int2(a.ctx_len[b], a.n_nodes[b]);
+      if (b < kSeqCache) sh.seq[b] = v;
+      const Seq s = seq_of(a, v.x, v.y, kRows);
+      const int cost = b < a.batch ? seq_cost(a, s) : 0;
+      int inc = cost;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int t = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += t;
+      }
+      const int u = __reduce_add_sync(0xffffffffu, cost ? a.n_kv_heads * s.blocks : 0);
+      const int most = __reduce_max_sync(0xffffffffu, cost ? s.tiles : 0);
+      if (lane == 31) { sh.sum[warp] = inc; sh.units[warp] = u; sh.most[warp] = most; }
+      __syncthreads();
+      int step = 0;
+#pragma unroll 1
+      for (int i = 0; i < kTaThreads / 32; ++i) {
+        if (i < warp) inc += sh.sum[i];
+        step += sh.sum[i];
+        units += sh.units[i];
+        longest = max(longest, sh.most[i]);
+      }
+      inc += run;
+      run += step;
+      if (a.batch <= kTaThreads) {
+        ranges.set(run, grid);
+        lo = ranges.at(blockIdx.x);
+        hi = ranges.at(blockIdx.x + 1);
+        round = 1;
+      }
+      if (round && inc > lo && inc - cost <= lo) { sh.start_b = b; sh.start_off = lo - (inc - cost); }
+      __syncthreads();
+    }
+    if (!round) {
+      ranges.set(run, grid);
+      lo = ranges.at(blockIdx.x);
+      hi = ranges.at(blockIdx.x + 1);
+    }
+  }
+  const bool one_part = a.batch <= kSeqCache && units <= grid;
+  Walk& w = sh.walk[warp];
+  if (one_part) {
+    // the fewest tiles a part that the CTAs are enough for; two sequences a lane
+    static_assert(kSeqCache == 64, "two sequences a lane");
+    int tiles[2], mine[2];
+    const int all_tiles = ranges.total - units * kStart;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int b = 2 * lane + e;
+      const Seq s = b < a.batch ? seq_of(a, sh.seq[b].x, sh.seq[b].y, kRows) : Seq{};
+      tiles[e] = s.tiles;
+      mine[e] = s.tiles ? a.n_kv_heads * s.blocks : 0;
+    }
+    // (a unit's parts are less than one more than its tiles / most)
+    int least = max(1, all_tiles / grid), most = max(least, min(longest, all_tiles / (grid - units + 1) + 1));
+#pragma unroll 1
+    while (least < most) {
+      const int mid = (least + most) / 2;
+      const int need = __reduce_add_sync(0xffffffffu, mine[0] * parts_of(tiles[0], mid) + mine[1] * parts_of(tiles[1], mid));
+      if (need <= grid) most = mid; else least = mid + 1;
+    }
+    int inc = 0;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) { mine[e] *= parts_of(tiles[e], most); inc += mine[e]; }
+    const int own = inc;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int64_t t = __shfl_up_sync(0xffffffffu, inc, o);
+      const int t = __shfl_up_sync(0xffffffffu, inc, o);
       if (lane >= o) inc += t;
     }
-    __syncthreads();
-    if (lane == 31) s_sum[warp] = inc;
-    __syncthreads();
-    for (int i = 0; i < kTaThreads / 32; ++i) {
-      if (i < warp) inc += s_sum[i];
+    if (lane == 0) w.left = 0;  // more CTAs than parts
+    __syncwarp();
+    int before = inc - own;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int at = (int)blockIdx.x - before;
+      if (at >= 0 && at < mine[e]) {
+        const int parts = parts_of(tiles[e], most), unit = at / parts;
+        w.left = 1;
+        w.b = 2 * lane + e;
+        w.load(a, sh.seq, kRows);
+        w.head = unit / w.s.blocks;
+        w.block = unit - w.head * w.s.blocks;
+        w.count = parts;
+        w.me = at - unit * parts;
+        w.c0 = (int)blockIdx.x - w.me;
+        w.t0 = w.me * w.s.tiles / parts;
+        w.t1 = (w.me + 1) * w.s.tiles / parts;
+      }
+      before += mine[e];
     }
-    inc += run;
-    if (inc > lo && inc - cost <= lo) { *start_b = b0 + tid; *start_off = (int)(lo - (inc - cost)); }
-    for (int i = 0; i < kTaThreads / 32; ++i) run += s_sum[i];
+  } else if (lane == 0) {
+    w.left = hi - lo;  // 0: more CTAs than places
+    w.b = hi > lo ? sh.start_b : 0;
+    w.off = hi > lo ? sh.start_off : 0;
+    w.at = lo - w.off;
+    w.load(a, sh.seq, kRows);
   }
-  if (warp == 1) tmem_alloc(tmem_slot, 512);
-  if (tid == 0) { tma_prefetch_desc(&kmap); tma_prefetch_desc(&vmap); }
+  __syncwarp();
+  const bool had_part = w.left > 0;
+  // the warp's next segment
+  auto next = [&]() -> bool {
+    __syncwarp();
+    bool some = false;
+    if (lane == 0) some = w.next(a, sh.seq, kRows, ranges, one_part);
+    return __shfl_sync(0xffffffffu, (int)some, 0);
+  };
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = *tmem_slot;
-  Walk w;
-  w.left = hi - lo;
-  w.b = *start_b;
-  w.off = *start_off;
-  w.s = seq_of(a, w.b, kRows);
-  int item0 = 0;  // items of the segments before this one
+  const uint32_t tmem = sh.tmem;
+  int tile0 = 0;  // tiles of the segments before this one
   bool ok = true;
 
-  if (warp == 0) {
-    // ---- loads ------------------------------------------------------------------
-    int issued = 0;
-    while (ok && w.next(a, kRows)) {
-      const int n = w.t1 - w.t0;
+  if (warp == 0 || warp == 2) {
+    // ---- loads: keys by one warp, values by another --------------------------------
+    // Page ids are fetched 32 pages (four tiles) at a time, a block ahead of
+    // their use: a load from the table would be on every copy's path.
+    const bool v = warp == 2;
+    uint64_t *full = v ? sh.v_full : sh.k_full, *empty = v ? sh.v_empty : sh.k_empty;
+    uint8_t* to0 = v ? vring : kring;
+    const CUtensorMap* map = v ? &vmap : &kmap;
+    const int ns = v ? NV : NK;
+    int st = 0, phase = 0, issued = 0;  // stages are used in turn
+    while (ok && next()) {
+      const int n = w.t1 - w.t0, head = w.head, page0 = w.t0 * kTilePages;
       const int32_t* row = a.page_table + (size_t)w.b * a.max_pages;
       const int last_page = (w.s.keys - 1) / kPageTok;
-      for (int i = 0; i < 2 * n && ok; ++i) {
-        bool v;
-        const int j = tile_of<BLOCKS>(i, n, v);
-        const int item = item0 + i, st = item % NS;
-        const int p0 = (w.t0 + j) * kTilePages, pages = min(kTilePages, last_page - p0 + 1);
-        int page = 0;
-        if (lane < kTilePages * kChunks) {
-          const int q = lane / kChunks;
-          if (q < pages) {
-            page = row[p0 + q];
-            if ((uint32_t)page >= (uint32_t)a.n_pages) page = a.n_pages;  // out of the tensor: reads as zeros
-          }
+      auto fetch = [&](int block) {
+        const int p = page0 + 32 * block + lane;
+        const int page = p <= last_page ? row[p] : 0;
+        return (uint32_t)page < (uint32_t)a.n_pages ? page : a.n_pages;  // out of the tensor: reads as zeros
+      };
+      int have = fetch(0), after = n > 4 ? fetch(1) : 0;
+#pragma unroll 1
+      for (int j = 0; j < n; ++j) {
+        const int pages = min(kTilePages, last_page - page0 - j * kTilePages + 1);
+        if (j > 0 && (j & 3) == 0) {
+          have = after;
+          if (j + 4 < n) after = fetch(j / 4 + 1);
         }
-        ok = warp_wait(empty + st, ((item / NS) & 1) ^ 1, abort_flag);
+        int page[kTilePages];
+#pragma unroll
+        for (int q = 0; q < kTilePages; ++q) page[q] = __shfl_sync(0xffffffffu, have, (j & 3) * kTilePages + q);
+        ok = warp_wait(empty + st, phase ^ 1, abort_flag);
         if (!ok) break;
-        if (elect_one()) mbar_arrive_expect_tx(full + st, (uint32_t)pages * kChunks * kPageTok * 128);
+        if (elect_one()) {
+          mbar_arrive_expect_tx(full + st, (uint32_t)pages * kChunks * kPageTok * 128);
+          uint8_t* to = to0 + st * kStage;
+#pragma unroll
+          for (int q = 0; q < kTilePages; ++q)
+            if (q < pages) {
+#pragma unroll
+              for (int c = 0; c < kChunks; ++c)
+                tma_load_4d(to + c * kChunkBytes + q * kPageTok * 128, map, full + st, c * 64, 0, head, page[q]);
+            }
+        }
         __syncwarp();
-        const int q = lane / kChunks, c = lane % kChunks;
-        if (lane < pages * kChunks)
-          tma_load_4d(ring + st * kStage + c * kChunkBytes + q * kPageTok * 128, v ? &vmap : &kmap, full + st, c * 64, 0,
-                      w.head, page);
-        __syncwarp();
-        issued = item + 1;
+        ++issued;
+        if (++st == ns) { st = 0; phase ^= 1; }
       }
-      item0 += 2 * n;
     }
-    if (!ok) {  // let the copies in flight land before the CTA goes
+    if (!ok) {  // copies in flight write this CTA's shared memory: they land before it goes
       *abort_flag = 1;
-      for (int it = max(0, issued - NS); it < issued; ++it) mbar_drain(full + it % NS, (it / NS) & 1);
+      for (int i = max(0, issued - ns); i < issued; ++i) mbar_drain(full + i % ns, (i / ns) & 1);
     }
   } else if (warp == 1) {
     // ---- products ---------------------------------------------------------------
-    uint32_t ph_p[2] = {0, 0}, ph_ready = 0;
-    const uint32_t q_addr = smem_u32(qbuf), r_addr = smem_u32(ring);
-    auto wait_full = [&](uint64_t* bars, int item) { ok = ok && warp_wait(bars + item % NS, (item / NS) & 1, abort_flag); };
-    auto scores = [&](int g, int item) {
-      const uint32_t qa = q_addr + (BLOCKS == 2 ? g * kStage : 0), kb = r_addr + (item % NS) * kStage;
+    uint32_t ph_p = 0, ph_ready = 0;
+    const uint32_t q_addr = smem_u32(qbuf), k_addr = smem_u32(kring), v_addr = smem_u32(vring);
+    auto wait_k = [&](int i) { ok = ok && warp_wait(sh.k_full + i % NK, (i / NK) & 1, abort_flag); };
+    auto wait_v = [&](int i) { ok = ok && warp_wait(sh.fixed + i % NV, (i / NV) & 1, abort_flag); };
+    // Operand addresses go through a shuffle, which tells the compiler that they
+    // are the warp's and not a lane's, and steps add constants to a
+    // descriptor's low word: an issue then costs little beside its product.
+    auto uniform = [](uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); };
+    // Shared-memory descriptors, 128-byte swizzle.  Queries and keys: 128-byte
+    // rows along K, eight-row atoms 1024 bytes apart.  Values: 64 of a key's
+    // entries a row (N is contiguous), atoms of eight keys 1024 bytes apart along
+    // K, the next 64 entries a chunk further.
+    constexpr uint64_t kDescK = (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+    constexpr uint64_t kDescV = (uint64_t)(kChunkBytes >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+    auto scores = [&](int g, int i) {
+      const uint32_t qa = uniform((q_addr + (BLOCKS == 2 ? g * kStage : 0)) >> 4), kb = uniform((k_addr + (i % NK) * kStage) >> 4);
+      const uint32_t d = uniform(tmem + g * kTile);
       if (elect_one()) {
 #pragma unroll
         for (int k = 0; k < HD / 16; ++k) {
-          const uint32_t at = (k / 4) * kChunkBytes + (k % 4) * 32;
-          umma_ss(tmem + g * kTile, sw128_desc(qa + at), sw128_desc(kb + at), kIdescS, k > 0);
+          const uint32_t at = ((k / 4) * kChunkBytes + (k % 4) * 32) >> 4;
+          umma_ss(d, kDescK | (qa + at), kDescK | (kb + at), kIdescS, k > 0);
         }
-        umma_commit(s_full + g);
+        umma_commit(sh.s_full + g);
       }
       __syncwarp();
     };
-    auto outputs = [&](int g, int item, bool first, int keys) {
-      const uint32_t vb = r_addr + (item % NS) * kStage;
+    auto outputs = [&](int g, int i, bool first, int keys) {  // O += P V
+      const uint32_t vb = uniform((v_addr + (i % NV) * kStage) >> 4);
+      const uint32_t o = uniform(tmem + 2 * kTile + g * HD), p = uniform(tmem + g * kTile);
       // keys past the end have probability 0: whole steps of 16 are left out
-      const int steps = min(kTile / 16, (keys + 15) / 16);
+      const int steps = __shfl_sync(0xffffffffu, (keys + 15) / 16, 0);
+      ok = ok && warp_wait(sh.p_full + g, ph_p >> g & 1, abort_flag);
+      if (!ok) return;
+      ph_p ^= 1u << g;
+      tc_fence_after();
       if (elect_one()) {
-        for (int k = 0; k < steps; ++k)
-          umma_ts(tmem + 2 * kTile + g * HD, tmem + g * kTile + k * 8, sw128_flip_desc(vb + k * 2048, kChunkBytes), kIdescO,
-                  !(first && k == 0));
+#pragma unroll
+        for (int k = 0; k < kTile / 16; ++k)
+          if (k < steps) umma_ts(o, p + k * 8, kDescV | (vb + k * 128), kIdescO, !first || k > 0);
       }
       __syncwarp();
     };
@@ -405,102 +718,100 @@ __global__ void __launch_bounds__(kTaThreads, 1)
       if (elect_one()) umma_commit(bar);
       __syncwarp();
     };
-    auto wait_p = [&](int g) {
-      ok = ok && warp_wait(p_full + g, ph_p[g], abort_flag);
-      ph_p[g] ^= 1;
-      tc_fence_after();
-    };
-    while (ok && w.next(a, kRows)) {
-      const int n = w.t1 - w.t0;
-      auto left = [&](int j) { return w.s.keys - (w.t0 + j) * kTile; };
-      ok = ok && warp_wait(ready + 0, ph_ready, abort_flag) && warp_wait(ready + 1, ph_ready, abort_flag);
+    while (ok && next()) {
+      const int n = w.t1 - w.t0, keys0 = w.s.keys - w.t0 * kTile;  // from the first tile on
+      ok = warp_wait(sh.ready + 0, ph_ready, abort_flag) && warp_wait(sh.ready + 1, ph_ready, abort_flag);
       ph_ready ^= 1;
       tc_fence_after();
-      wait_full(full, item0 + item_k<BLOCKS>(0));
-      if (!ok) break;
-      scores(0, item0 + item_k<BLOCKS>(0));
-      if (BLOCKS == 2) {
-        scores(1, item0 + item_k<BLOCKS>(0));
-        commit(empty + (item0 + item_k<BLOCKS>(0)) % NS);
-        for (int j = 0; j < n && ok; ++j) {
-          const int iv = item0 + item_v<BLOCKS>(j, n), ik = item0 + item_k<BLOCKS>(j + 1);
+      if (BLOCKS == 2) {  // step j: each group takes tile j, and the scores of the next
+#pragma unroll 1
+        for (int j = -1; j < n && ok; ++j) {
+          const int i = tile0 + j;
           const bool more = j + 1 < n;
-          wait_full(fixed, item0 / 2 + j);
-          if (more) wait_full(full, ik);
+          if (j >= 0) wait_v(i);
+          if (more) wait_k(i + 1);
+          if (!ok) break;
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
-            wait_p(g);
+            if (j >= 0) outputs(g, i, j == 0, keys0 - j * kTile);
             if (!ok) break;
-            outputs(g, iv, j == 0, left(j));
-            if (more) scores(g, ik); else commit(o_full + g);
+            if (more) scores(g, i + 1); else commit(sh.o_full + g);
           }
           if (!ok) break;
-          commit(empty + iv % NS);
-          if (more) commit(empty + ik % NS);
+          if (j >= 0) commit(sh.v_empty + i % NV);
+          if (more) commit(sh.k_empty + (i + 1) % NK);
         }
-      } else {
-        commit(empty + (item0 + item_k<BLOCKS>(0)) % NS);
-        if (n > 1) {
-          const int ik = item0 + item_k<BLOCKS>(1);
-          wait_full(full, ik);
-          if (!ok) break;
-          scores(1, ik);
-          commit(empty + ik % NS);
-        }
-        for (int j = 0; j < n && ok; ++j) {
-          const int g = j & 1, iv = item0 + item_v<BLOCKS>(j, n);
-          wait_full(fixed, item0 / 2 + j);
-          wait_p(g);
-          if (!ok) break;
-          outputs(g, iv, j < 2, left(j));
-          commit(empty + iv % NS);
-          if (j + 2 < n) {
-            const int ik = item0 + item_k<BLOCKS>(j + 2);
-            wait_full(full, ik);
+      } else {  // group j & 1 takes tile j, and the scores of its next, j + 2
+#pragma unroll 1
+        for (int j = -2; j < n && ok; ++j) {
+          const int g = j & 1, i = tile0 + j;
+          if (j >= 0) {
+            wait_v(i);
+            if (ok) outputs(g, i, j < 2, keys0 - j * kTile);
             if (!ok) break;
-            scores(g, ik);
-            commit(empty + ik % NS);
+            commit(sh.v_empty + i % NV);
+          }
+          if (j + 2 < n) {
+            wait_k(i + 2);
+            if (!ok) break;
+            scores(g, i + 2);
+            commit(sh.k_empty + (i + 2) % NK);
           }
         }
         if (!ok) break;
-        commit(o_full + 0);
-        commit(o_full + 1);
+        commit(sh.o_full + 0);
+        commit(sh.o_full + 1);
       }
-      item0 += 2 * n;
+      tile0 += n;
     }
     if (!ok) *abort_flag = 1;
     // products in flight read shared memory and write tensor memory: let them end
-    commit(drain);
-    mbar_drain(drain, 0);
-  } else if (warp < 4) {
-    // ---- values of tiles that reach past the context -------------------------------
-    while (ok && w.next(a, kRows)) {
+    commit(&sh.drain);
+    mbar_drain(&sh.drain, 0);
+  } else if (warp == 3) {
+    // ---- values of tiles that reach past the context --------------------------------
+    // and, first, the rows of unused nodes, which are zero
+    const size_t row16 = (size_t)a.n_q_heads * HD / 8;  // 16-byte pieces of a node
+#pragma unroll 1
+    for (int b = 0; b < a.batch; ++b) {
+      const int nodes = min(max(b < kSeqCache ? sh.seq[b].y : a.n_nodes[b], 0), a.width);
+      uint4* at = reinterpret_cast<uint4*>(a.out) + ((size_t)b * a.width + nodes) * row16;
+#pragma unroll 1
+      for (size_t i = blockIdx.x * 32 + lane; i < (a.width - nodes) * row16; i += grid * 32) at[i] = make_uint4(0, 0, 0, 0);
+    }
+    while (ok && next()) {
       const int n = w.t1 - w.t0;
-      for (int j = 0; j < n && ok; ++j) {
-        const int item = item0 + item_v<BLOCKS>(j, n), st = item % NS, vc = item0 / 2 + j;
-        ok = warp_wait(full + st, (item / NS) & 1, abort_flag);
+#pragma unroll 1
+      for (int j = 0; j < n; ++j) {
+        const int st = (tile0 + j) % NV;
+        ok = warp_wait(sh.v_full + st, ((tile0 + j) / NV) & 1, abort_flag);
         if (!ok) break;
         const int k0 = (w.t0 + j) * kTile;
         if (k0 + kTile > w.s.plain) {
           const int first = max(0, w.s.plain - k0), end = w.s.keys - k0;
+          const int used = min(kTile, (end + 15) & ~15);  // the products take steps of 16 keys
           constexpr int kPieces = HD / 8;
           bool any = false;
-          for (int p = first * kPieces + tid - 64; p < kTile * kPieces; p += 64) {
+#pragma unroll 4
+          for (int p = first * kPieces + lane; p < used * kPieces; p += 32) {
             const int r = p / kPieces, c = p % kPieces;
-            uint4* at = reinterpret_cast<uint4*>(ring + st * kStage + (c / 8) * kChunkBytes + r * 128 + (((c % 8) ^ (r & 7)) << 4));
-            if (r >= end) { *at = make_uint4(0, 0, 0, 0); continue; }
+            uint4* at = reinterpret_cast<uint4*>(vring + st * kStage + (c / 8) * kChunkBytes + r * 128 + (((c % 8) ^ (r & 7)) << 4));
             const uint4 v = *at;
-            const uint4 f = make_uint4(finite_of<T>(v.x), finite_of<T>(v.y), finite_of<T>(v.z), finite_of<T>(v.w));
-            if (f.x != v.x || f.y != v.y || f.z != v.z || f.w != v.w) { *at = f; any = true; }
+            const uint4 f = r >= end ? make_uint4(0, 0, 0, 0)
+                                     : make_uint4(finite_of<T>(v.x), finite_of<T>(v.y), finite_of<T>(v.z), finite_of<T>(v.w));
+            if (f.x != v.x || f.y != v.y || f.z != v.z || f.w != v.w) {
+              *at = f;
+              any |= r < end;
+            }
           }
           fence_proxy_async_all();
           any = __any_sync(0xffffffffu, any);
-          if (lane == 0) odd[2 * (vc % NS) + warp - 2] = any;
+          if (lane == 0) sh.odd[st] = any;
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(fixed + vc % NS);
+        if (lane == 0) mbar_arrive(sh.fixed + st);
       }
-      item0 += 2 * n;
+      tile0 += n;
     }
     if (!ok) *abort_flag = 1;
   } else {
@@ -509,76 +820,102 @@ __global__ void __launch_bounds__(kTaThreads, 1)
     const uint32_t my = tmem + ((uint32_t)((warp & 3) * 32) << 16);
     const uint32_t s_addr = my + g * kTile, o_addr = my + 2 * kTile + g * HD;
     const float sl2 = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1e-30f);  // a masked score stays -inf at scale 0
-    const uint32_t sign = a.scale < 0.f ? 0x80008000u : 0u;  // a negative scale turns the queries' signs
-    uint32_t ph_s = 0, ph_o = 0, ph_pair = 0;
+    uint32_t ph_s = 0, ph_o = 0, ph_pair = 0, ph_met = 0;
     auto meet = [&] {  // both groups, 256 threads
       __syncwarp();
-      if (lane == 0) mbar_arrive(pair);
-      ok = warp_wait(pair, ph_pair, abort_flag);
+      if (lane == 0) mbar_arrive(&sh.pair);
+      ok = warp_wait(&sh.pair, ph_pair, abort_flag);
       ph_pair ^= 1;
     };
-    while (ok && w.next(a, kRows)) {
-      const int n = w.t1 - w.t0, row0 = w.block * kRows, live = w.s.nodes * group - row0;
+    auto group_meet = [&] {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(sh.met + g);
+      ok = warp_wait(sh.met + g, ph_met, abort_flag);
+      ph_met ^= 1;
+    };
+    while (ok && next()) {
+      const int n = w.t1 - w.t0;
+      const int row_base = w.block * kRows + (BLOCKS == 2 ? g * kTile : 0);  // row of the unit that lane 0 of the group has
+      const int row = row_base + t, rows = w.s.nodes * group;
       // queries into shared memory, swizzled; one block: each group lays out half
       {
-        constexpr int kPieces = HD / 8, kMine = BLOCKS == 2 ? kTile : kTile / 2;
-        uint8_t* dst = qbuf + (BLOCKS == 2 ? g * kStage : 0);
-        const T* q = reinterpret_cast<const T*>(a.q) + (int64_t)w.b * a.width * a.q_stride + (int64_t)w.head * group * HD;
-        for (int p = t; p < kMine * kPieces; p += kTile) {
-          const int r = p / kPieces + (BLOCKS == 2 ? 0 : g * kMine), c = p % kPieces;
-          const int gr = r + (BLOCKS == 2 ? g * kTile : 0);  // row of the unit's block
-          uint4 v = make_uint4(0, 0, 0, 0);
-          if (gr < live) {
-            const int node = (row0 + gr) / group, h = (row0 + gr) - node * group;
-            v = *reinterpret_cast<const uint4*>(q + (int64_t)node * a.q_stride + h * HD + c * 8);
-            v.x ^= sign; v.y ^= sign; v.z ^= sign; v.w ^= sign;
-          }
-          *reinterpret_cast<uint4*>(dst + (c / 8) * kChunkBytes + r * 128 + (((c % 8) ^ (r & 7)) << 4)) = v;
+        constexpr int kPieces = HD / 8, kMine = BLOCKS == 2 ? kTile : kTile / 2, kStep = kTile / kPieces;
+        // row / group as a product: exact for the rows of 256 nodes x 4096 heads
+        const uint32_t magic = group > 1 ? 0xFFFFFFFFu / (uint32_t)group + 1 : 0;
+        const uint32_t sign = a.scale < 0.f ? 0x80008000u : 0u;  // a negative scale turns the queries' signs
+        const int c = t % kPieces, r0 = t / kPieces + (BLOCKS == 2 ? 0 : g * kMine);
+        const T* q = reinterpret_cast<const T*>(a.q) + (int64_t)w.b * a.width * a.q_stride + (int64_t)w.head * group * HD + c * 8;
+        uint8_t* dst = qbuf + (BLOCKS == 2 ? g * kStage : 0) + (c / 8) * kChunkBytes;
+        uint4 v[kMine / kStep];  // all loads are out before the first is stored
+#pragma unroll
+        for (int i = 0; i < kMine / kStep; ++i) {
+          const int r = row_base + r0 + i * kStep, node = magic ? (int)__umulhi((uint32_t)r, magic) : r;
+          v[i] = make_uint4(0, 0, 0, 0);
+          if (r < rows) v[i] = *reinterpret_cast<const uint4*>(q + (int64_t)node * a.q_stride + (r - node * group) * HD);
+        }
+#pragma unroll
+        for (int i = 0; i < kMine / kStep; ++i) {
+          const int r = r0 + i * kStep;
+          v[i].x ^= sign; v[i].y ^= sign; v[i].z ^= sign; v[i].w ^= sign;
+          *reinterpret_cast<uint4*>(dst + r * 128 + (((c % 8) ^ (r & 7)) << 4)) = v[i];
         }
         fence_proxy_async_all();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(ready + g);
+        if (lane == 0) mbar_arrive(sh.ready + g);
       }
-      const int row = row0 + (BLOCKS == 2 ? g * kTile : 0) + t;  // of the unit
       const int node = min(row / group, w.s.nodes - 1);
       const uint32_t* mrow = reinterpret_cast<const uint32_t*>(a.mask + ((size_t)w.b * a.width + node) * a.words);
-      const int32_t* pages = a.page_table + (size_t)w.b * a.max_pages;
-      const int n_pg = (w.s.keys + kPageTok - 1) / kPageTok;
-      const int j0 = BLOCKS == 2 ? 0 : g, jn = BLOCKS == 2 ? 1 : 2;
       auto page_flag = [&](int j) -> uint32_t {  // this lane's page of tile j is one of the pool
         const int p = (w.t0 + j) * kTilePages + lane;
-        return lane >= kTilePages || p >= n_pg || (uint32_t)pages[p] < (uint32_t)a.n_pages;
+        if (lane >= kTilePages || p * kPageTok >= w.s.keys) return 1;
+        return (uint32_t)a.page_table[(size_t)w.b * a.max_pages + p] < (uint32_t)a.n_pages;
       };
       float m_ref = -INFINITY, sum = 0.f;
       bool patch = false;  // values that the rows who see them get back in the epilogue
+      const int j0 = BLOCKS == 2 ? 0 : g, jn = BLOCKS == 2 ? 1 : 2;
       uint32_t flag = j0 < n ? page_flag(j0) : 1u;
+#pragma unroll 1
       for (int j = j0; j < n; j += jn) {
         const uint32_t flags = __ballot_sync(0xffffffffu, flag);
         if (j + jn < n) flag = page_flag(j + jn);
-        ok = warp_wait(s_full + g, ph_s, abort_flag);
+        const int k0 = (w.t0 + j) * kTile;
+        const bool tail = k0 + kTile > w.s.plain;
+        const bool masked = tail || flags != 0xFFFFFFFFu;
+        uint32_t allow[4] = {0, 0, 0, 0};
+        if (masked) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            allow[c] = allowed32(mrow, 2 * a.words, k0 + 32 * c, w.s) &
+                       (((flags >> (2 * c)) & 1 ? 0xFFFFu : 0u) | ((flags >> (2 * c + 1)) & 1 ? 0xFFFF0000u : 0u));
+        }
+        ok = warp_wait(sh.s_full + g, ph_s, abort_flag);
         if (!ok) break;
         ph_s ^= 1;
         tc_fence_after();
+        if (masked) {
+          // masked scores become -inf where they lie, 32 columns a turn
+#pragma unroll 1
+          for (int c = 0; c < 4; ++c) {
+            const uint32_t m = c < 2 ? (c ? allow[1] : allow[0]) : (c == 2 ? allow[2] : allow[3]);
+            uint32_t x[32];
+            tm_ld32(s_addr + 32 * c, x);
+            tm_landed<32>(x);
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (!(m >> i & 1)) x[i] = 0xFF800000u;
+            tm_st32(s_addr + 32 * c, x);
+          }
+          tm_wait_st();
+        }
         uint32_t v[kTile];
 #pragma unroll
         for (int c = 0; c < 4; ++c) tm_ld32(s_addr + 32 * c, v + 32 * c);
-        tm_wait_ld();
-        const int k0 = (w.t0 + j) * kTile;
-        const bool tail = k0 + kTile > w.s.plain;
-        if (tail || flags != 0xFFFFFFFFu) {
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            uint32_t m = allowed32(mrow, 2 * a.words, k0 + 32 * c, w.s);
-            m &= ((flags >> (2 * c)) & 1 ? 0xFFFFu : 0u) | ((flags >> (2 * c + 1)) & 1 ? 0xFFFF0000u : 0u);
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (!(m >> i & 1)) v[32 * c + i] = 0xFF800000u;
-          }
-        }
+        tm_landed<kTile>(v);
         float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int i = 0; i < kTile; ++i) mx[i & 3] = fmaxf(mx[i & 3], __uint_as_float(v[i]));
+        for (int i = 0; i < kTile; i += 2)
+          mx[i >> 1 & 3] = fmaxf(fmaxf(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), mx[i >> 1 & 3]);
         const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * sl2;
         if (j == j0) {
           m_ref = top;
@@ -587,50 +924,44 @@ __global__ void __launch_bounds__(kTaThreads, 1)
           const float alpha = m_new == m_ref ? 1.0f : ex2(m_ref - m_new);
           m_ref = m_new;
           sum *= alpha;
-#pragma unroll
-          for (int c = 0; c < HD / 32; ++c) {
-            uint32_t o[32];
-            tm_ld32(o_addr + 32 * c, o);
-            tm_wait_ld();
-#pragma unroll
-            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
-            tm_st32(o_addr + 32 * c, o);
-          }
+          scale_row<HD>(o_addr, alpha);
         }
         const float base = m_ref == -INFINITY ? 0.f : m_ref;
-        float acc[4] = {0.f, 0.f, 0.f, 0.f};
+        const uint64_t scale2 = pair_of(__float_as_uint(sl2), __float_as_uint(sl2));
+        const uint64_t base2 = pair_of(__float_as_uint(-base), __float_as_uint(-base));
+        uint64_t acc[2] = {0, 0};
+        // in place: the pair at 2 i becomes entry i
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          uint32_t p[32];
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            const float x = ex2(fmaf(__uint_as_float(v[64 * h + 2 * i]), sl2, -base));
-            const float y = ex2(fmaf(__uint_as_float(v[64 * h + 2 * i + 1]), sl2, -base));
-            acc[2 * (i & 1)] += x;
-            acc[2 * (i & 1) + 1] += y;
-            p[i] = Num<T>::pack(x, y);
+          for (int i = 32 * h; i < 32 * h + 32; ++i) {
+            const float2 e = floats_of(fma2(pair_of(v[2 * i], v[2 * i + 1]), scale2, base2));
+            const float x = ex2(e.x), y = ex2(e.y);
+            acc[i & 1] = add2(acc[i & 1], pair_of(__float_as_uint(x), __float_as_uint(y)));
+            v[i] = Num<T>::pack(x, y);
           }
-          tm_st32(s_addr + 32 * h, p);
+          tm_st32(s_addr + 32 * h, v + 32 * h);
         }
         tm_wait_st();
-        sum += (acc[0] + acc[1]) + (acc[2] + acc[3]);
+        const float2 acc2 = floats_of(add2(acc[0], acc[1]));
+        sum += acc2.x + acc2.y;
         if (tail) {  // the stage is not refilled before this group's probabilities are used
-          const int vc = item0 / 2 + j;
-          ok = warp_wait(fixed + vc % NS, (vc / NS) & 1, abort_flag);
+          const int st = (tile0 + j) % NV;
+          ok = warp_wait(sh.fixed + st, ((tile0 + j) / NV) & 1, abort_flag);
           if (!ok) break;
-          patch |= (odd[2 * (vc % NS)] | odd[2 * (vc % NS) + 1]) != 0;
+          patch |= sh.odd[st] != 0;
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(p_full + g);
+        if (lane == 0) mbar_arrive(sh.p_full + g);
       }
       if (!ok) break;
-      ok = warp_wait(o_full + g, ph_o, abort_flag);
+      ok = warp_wait(sh.o_full + g, ph_o, abort_flag);
       if (!ok) break;
       ph_o ^= 1;
       tc_fence_after();
       // ---- epilogue: a group's own accumulator, or half the columns of both groups' ----
-      float m_row = m_ref, l_row = sum, w0 = 1.f, w1 = 0.f;
+      float w0 = 1.f, w1 = 0.f;
       if (BLOCKS == 1) {
         float4* ml = reinterpret_cast<float4*>(qbuf);  // the queries have been read
         ml[g * kTile + t] = make_float4(m_ref, sum, patch ? 1.f : 0.f, 0.f);
@@ -638,162 +969,159 @@ __global__ void __launch_bounds__(kTaThreads, 1)
         if (!ok) break;
         const float4 x = ml[t], y = ml[kTile + t];
         patch = x.z + y.z > 0.f;
-        m_row = fmaxf(x.x, y.x);
-        w0 = x.x == -INFINITY ? 0.f : ex2(x.x - m_row);
-        w1 = y.x == -INFINITY ? 0.f : ex2(y.x - m_row);
-        l_row = x.y * w0 + y.y * w1;
+        m_ref = fmaxf(x.x, y.x);
+        w0 = x.x == -INFINITY ? 0.f : ex2(x.x - m_ref);
+        w1 = y.x == -INFINITY ? 0.f : ex2(y.x - m_ref);
+        sum = x.y * w0 + y.y * w1;
       }
       constexpr int kCols = BLOCKS == 2 ? HD : HD / 2;
-      const int col0 = BLOCKS == 2 ? 0 : g * kCols;
-      const bool whole = w.t0 == 0 && w.t1 == w.s.tiles, on = row < w.s.nodes * group;
-      const float inv = whole ? (l_row > 0.f ? 1.0f / l_row : 0.f) : 1.f;
-      const int in_block = (BLOCKS == 2 ? g * kTile : 0) + t;
-      const Partial part = slot_of(a, 2 * blockIdx.x + (w.t0 > 0 ? 0 : 1), HD, BLOCKS);
-      T* out = reinterpret_cast<T*>(a.out) +
-               (((int64_t)w.b * a.width + node) * a.n_q_heads + (int64_t)w.head * group + (row - node * group)) * HD;
+      const int col0 = BLOCKS == 2 ? 0 : g * kCols, in_block = (BLOCKS == 2 ? g * kTile : 0) + t;
+      const bool whole = w.t0 == 0 && w.t1 == w.s.tiles, on = row < rows;
+      // A unit's contributors are consecutive CTAs.  All but the last to arrive
+      // leave their partial; that one joins them, in tile order.  Where two share
+      // a unit, the owner of its first tile looks before it leaves its own: in
+      // ranges it came to the unit last of all its work, the other has arrived as
+      // a rule, and the two are joined straight from tensor memory.
+      const int count = whole ? 1 : w.count, me = w.me, c0 = w.c0;
+      uint32_t* arrived = reinterpret_cast<uint32_t*>(a.workspace) + 2 * c0 + g;
+      const Partial mine = slot_of(a, 2 * blockIdx.x + (w.t0 > 0 ? 0 : 1), HD, BLOCKS);
+      bool two = false;
+      if (count == 2 && me == 0) {
+        if (t == 0) sh.last_in[g] = ld_acquire(arrived) == 1;
+        group_meet();
+        if (!ok) break;
+        two = sh.last_in[g];
+      }
+      const Partial other = slot_of(a, 2 * (c0 + 1), HD, BLOCKS);
+      float x_mine = 1.f, x_other = 0.f, inv = sum > 0.f ? 1.0f / sum : 0.f;
+      if (two) {
+        fence_gpu();
+        const float2 st = *other.stats(HD, g, in_block);
+        const float top = fmaxf(m_ref, st.x), base = top == -INFINITY ? 0.f : top;
+        x_mine = ex2(m_ref - base);
+        x_other = ex2(st.x - base);
+        const float l = fmaf(st.y, x_other, sum * x_mine);  // all as join() would
+        inv = l > 0.f ? 1.0f / l : 0.f;
+      }
+      {
+        T* out = reinterpret_cast<T*>(a.out) +
+                 (((int64_t)w.b * a.width + node) * a.n_q_heads + (int64_t)w.head * group + (row - node * group)) * HD;
+#pragma unroll 1
+        for (int c = col0; c < col0 + kCols; c += 32) {
+          float4 v[8];
+          if (two && on) {
 #pragma unroll
-      for (int c = 0; c < kCols / 32; ++c) {
-        uint32_t o[32];
-        if (BLOCKS == 2) {
-          tm_ld32(o_addr + 32 * c, o);
-          tm_wait_ld();
-        } else {
-          uint32_t o1[32];
-          tm_ld32(my + 2 * kTile + col0 + 32 * c, o);
-          tm_ld32(my + 2 * kTile + HD + col0 + 32 * c, o1);
-          tm_wait_ld();
-          // a group without a tile has written nothing there
+            for (int i = 0; i < 8; ++i) v[i] = *other.o(c / 4 + i, in_block);
+          }
+          uint32_t o[32];
+          if (BLOCKS == 2) {
+            tm_ld32(o_addr + c, o);
+            tm_landed<32>(o);
+          } else {
+            uint32_t o1[32];
+            tm_ld32(my + 2 * kTile + c, o);
+            tm_ld32(my + 2 * kTile + HD + c, o1);
+            tm_landed<32>(o);
+            tm_landed<32>(o1);
+            // a group without a tile has written nothing there
 #pragma unroll
-          for (int i = 0; i < 32; ++i)
-            o[i] = __float_as_uint((n > 1 ? __uint_as_float(o1[i]) * w1 : 0.f) + __uint_as_float(o[i]) * w0);
-        }
-        if (patch && on) {
-          for (int i = 0; i < w.s.nodes; ++i) {
-            const int pos = w.s.ctx + i;
-            if (pos < w.t0 * kTile || pos >= min(w.t1 * kTile, w.s.keys) || !(mrow[i >> 5] >> (i & 31) & 1)) continue;
-            const int page = pages[pos / kPageTok];
-            if ((uint32_t)page >= (uint32_t)a.n_pages) continue;
-            const T* vp = reinterpret_cast<const T*>(a.v_cache) + page * a.page_stride +
-                          ((int64_t)w.head * kPageTok + pos % kPageTok) * HD + col0 + 32 * c;
+            for (int i = 0; i < 32; ++i)
+              o[i] = __float_as_uint((n > 1 ? __uint_as_float(o1[i]) * w1 : 0.f) + __uint_as_float(o[i]) * w0);
+          }
+          if (two) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              const float x = Num<T>::get(vp + e);
-              if (!(fabsf(x) < INFINITY)) o[e] = __float_as_uint(__uint_as_float(o[e]) + x);
+            for (int i = 0; i < 8; ++i) {
+              o[4 * i] = __float_as_uint(fmaf(v[i].x, x_other, __uint_as_float(o[4 * i]) * x_mine));
+              o[4 * i + 1] = __float_as_uint(fmaf(v[i].y, x_other, __uint_as_float(o[4 * i + 1]) * x_mine));
+              o[4 * i + 2] = __float_as_uint(fmaf(v[i].z, x_other, __uint_as_float(o[4 * i + 2]) * x_mine));
+              o[4 * i + 3] = __float_as_uint(fmaf(v[i].w, x_other, __uint_as_float(o[4 * i + 3]) * x_mine));
             }
           }
-        }
-        if (!on) continue;
-        if (whole) {
+          if (on && (whole || two)) {
 #pragma unroll
-          for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * inv);
+            for (int i = 0; i < 4; ++i) {
+              uint4 p;
+              p.x = Num<T>::pack(__uint_as_float(o[8 * i]) * inv, __uint_as_float(o[8 * i + 1]) * inv);
+              p.y = Num<T>::pack(__uint_as_float(o[8 * i + 2]) * inv, __uint_as_float(o[8 * i + 3]) * inv);
+              p.z = Num<T>::pack(__uint_as_float(o[8 * i + 4]) * inv, __uint_as_float(o[8 * i + 5]) * inv);
+              p.w = Num<T>::pack(__uint_as_float(o[8 * i + 6]) * inv, __uint_as_float(o[8 * i + 7]) * inv);
+              *reinterpret_cast<uint4*>(out + c + 8 * i) = p;
+            }
+          } else if (on) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            uint4 p;
-            p.x = Num<T>::pack(__uint_as_float(o[8 * i]), __uint_as_float(o[8 * i + 1]));
-            p.y = Num<T>::pack(__uint_as_float(o[8 * i + 2]), __uint_as_float(o[8 * i + 3]));
-            p.z = Num<T>::pack(__uint_as_float(o[8 * i + 4]), __uint_as_float(o[8 * i + 5]));
-            p.w = Num<T>::pack(__uint_as_float(o[8 * i + 6]), __uint_as_float(o[8 * i + 7]));
-            *reinterpret_cast<uint4*>(out + col0 + 32 * c + 8 * i) = p;
+            for (int i = 0; i < 8; ++i)
+              *mine.o(c / 4 + i, in_block) = make_float4(__uint_as_float(o[4 * i]), __uint_as_float(o[4 * i + 1]),
+                                                         __uint_as_float(o[4 * i + 2]), __uint_as_float(o[4 * i + 3]));
           }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            *part.o((col0 + 32 * c) / 4 + i, in_block) =
-                make_float4(__uint_as_float(o[4 * i]), __uint_as_float(o[4 * i + 1]), __uint_as_float(o[4 * i + 2]),
-                            __uint_as_float(o[4 * i + 3]));
         }
+        if (patch && on)
+          patch_row<T, HD>(a, w.b, w.head, w.s, max(w.t0 * kTile, w.s.ctx), min(w.t1 * kTile, w.s.keys), mrow, col0, kCols,
+                           whole || two ? out : nullptr, mine, in_block);
       }
-      if (!whole && on && (BLOCKS == 2 || g == 0)) {
-        *part.max_of(HD, in_block) = m_row;
-        *part.sum_of(HD, in_block) = l_row;
+      if (two) {
+        if (t == 0) *arrived = 0;  // both have arrived: as the next call wants it
+      } else if (!whole) {
+        *mine.stats(HD, g, in_block) = make_float2(m_ref, sum);
+        // written before the group meets, read after, and written again only when
+        // all of it has been through another tile
+#pragma unroll 1
+        for (int i = t; i < count; i += kTile)
+          sh.slots[g][i] = (uint16_t)(2 * (c0 + i) + (i == 0 ? 1 : 0));
+        fence_gpu();
+        group_meet();
+        if (!ok) break;
+        if (t == 0) sh.last_in[g] = arrive_acq_rel(arrived) == (uint32_t)count - 1;
+        group_meet();
+        if (!ok) break;
+        if (sh.last_in[g]) {
+          fence_gpu();
+          if (t == 0) *arrived = 0;
+          T* unit = reinterpret_cast<T*>(a.out) + ((int64_t)w.b * a.width * a.n_q_heads + (int64_t)w.head * group) * HD;
+          const int live = min(kTile, rows - row_base);
+          join<T, HD, BLOCKS>(a, sh.slots[g], count, g, t, in_block - t, live, col0 / 4, kCols / 4, unit, row_base);
+        }
       }
       if (BLOCKS == 1) {  // the queries' place holds the sums, and each group reads both accumulators
         meet();
         if (!ok) break;
       }
-      item0 += 2 * n;
+      tile0 += n;
     }
     if (!ok) *abort_flag = 1;
   }
   tc_fence_before();
   __syncthreads();
-  if (tid == 0 && *abort_flag) reinterpret_cast<uint32_t*>(a.workspace)[blockIdx.x] = 1;
   if (warp == 1) tmem_dealloc(tmem, 512);
-}
-
-// Joins the partials of units that several CTAs shared, in tile order, and
-// zeroes the rows of unused nodes.  A lane takes a row, a warp HD / 32 groups
-// of four columns.  A stalled pipeline in any CTA turns the output into NaN:
-// never into numbers that look right.
-constexpr int kCombineThreads = 256, kCombineRows = 32;
-
-template <typename T, int HD, int BLOCKS>
-__global__ void __launch_bounds__(kCombineThreads) tree_combine_kernel(const TreeAttnArgs a, int grid) {
-  constexpr int kRows = kTile * BLOCKS, kC4 = HD / 32;
-  __shared__ int64_t s_sum[2][kCombineThreads / 32];
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int b = blockIdx.z, head = blockIdx.y, group = a.n_q_heads / a.n_kv_heads;
-  const int row = blockIdx.x * kCombineRows + lane;
-  int64_t total = 0, before = 0;
-  for (int i = tid; i < a.batch; i += kCombineThreads) {
-    const int64_t c = seq_cost(a, seq_of(a, i, kRows));
-    total += c;
-    if (i < b) before += c;
-  }
-  const Seq s = seq_of(a, b, kRows);
-  pdl_wait();
-  const int stalled = __syncthreads_or(tid < grid && reinterpret_cast<const uint32_t*>(a.workspace)[tid] != 0);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    total += __shfl_xor_sync(0xffffffffu, total, o);
-    before += __shfl_xor_sync(0xffffffffu, before, o);
-  }
-  if (lane == 0) { s_sum[0][warp] = total; s_sum[1][warp] = before; }
-  __syncthreads();
-  total = before = 0;
-  for (int i = 0; i < kCombineThreads / 32; ++i) { total += s_sum[0][i]; before += s_sum[1][i]; }
-  if (row >= a.width * group) return;
-  const int node = row / group;
-  T* out = reinterpret_cast<T*>(a.out) +
-           (((int64_t)b * a.width + node) * a.n_q_heads + (int64_t)head * group + (row - node * group)) * HD;
-  float4 acc[kC4];
-  float scale = 0.f;
-#pragma unroll
-  for (int e = 0; e < kC4; ++e) acc[e] = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (stalled) {
-    scale = __int_as_float(0x7FC00000);
-  } else if (node < s.nodes) {
-    const int block = row / kRows, r = row % kRows;
-    const int64_t t0 = before + (int64_t)(head * s.blocks + block) * s.tiles;
-    const int first = (int)(((t0 + 1) * grid - 1) / total), last = (int)(((t0 + s.tiles) * grid - 1) / total);
-    if (first == last) return;  // written whole
-    float m = -INFINITY, l = 0.f;
-    for (int c = first; c <= last; ++c) {
-      if (range_at(c, total, grid) == range_at(c + 1, total, grid)) continue;  // a CTA without a tile
-      m = fmaxf(m, *slot_of(a, 2 * c + (c == first ? 1 : 0), HD, BLOCKS).max_of(HD, r));
-    }
-    for (int c = first; c <= last; ++c) {
-      if (range_at(c, total, grid) == range_at(c + 1, total, grid)) continue;
-      const Partial p = slot_of(a, 2 * c + (c == first ? 1 : 0), HD, BLOCKS);
-      const float mc = *p.max_of(HD, r), w = mc == -INFINITY ? 0.f : ex2(mc - m);
-      l = fmaf(*p.sum_of(HD, r), w, l);
-#pragma unroll
-      for (int e = 0; e < kC4; ++e) {
-        const float4 v = *p.o(warp * kC4 + e, r);
-        acc[e].x = fmaf(v.x, w, acc[e].x);
-        acc[e].y = fmaf(v.y, w, acc[e].y);
-        acc[e].z = fmaf(v.z, w, acc[e].z);
-        acc[e].w = fmaf(v.w, w, acc[e].w);
+  if (*abort_flag || stalled) {
+    // A wait ran out, now or in an earlier call with this workspace (whose
+    // arrivals are then not to be trusted): every unit of the range becomes NaN,
+    // never numbers that look right, until the workspace is zeroed again.
+    if (tid == 0) {
+      reinterpret_cast<volatile uint32_t*>(a.workspace)[kStalledWord] = 1;
+      w.left = one_part ? had_part : hi - lo;
+      if (!one_part) {
+        w.b = hi > lo ? sh.start_b : 0;
+        w.off = hi > lo ? sh.start_off : 0;
+        w.at = lo - w.off;
+        w.load(a, sh.seq, kRows);
       }
     }
-    scale = l > 0.f ? 1.0f / l : 0.f;
-  }
-#pragma unroll
-  for (int e = 0; e < kC4; ++e) {
-    uint2 p;
-    p.x = Num<T>::pack(acc[e].x * scale, acc[e].y * scale);
-    p.y = Num<T>::pack(acc[e].z * scale, acc[e].w * scale);
-    *reinterpret_cast<uint2*>(out + (warp * kC4 + e) * 4) = p;
+    __syncthreads();
+    const Walk& u = sh.walk[0];
+    while (true) {
+      __syncthreads();
+      if (tid == 0) sh.odd[0] = sh.walk[0].next(a, sh.seq, kRows, ranges, one_part);
+      __syncthreads();
+      if (!sh.odd[0]) break;
+#pragma unroll 1
+      for (int r = u.block * kRows + tid; r < min((u.block + 1) * kRows, u.s.nodes * group); r += kTaThreads) {
+        const int node = r / group;
+        T* out = reinterpret_cast<T*>(a.out) +
+                 (((int64_t)u.b * a.width + node) * a.n_q_heads + (int64_t)u.head * group + (r - node * group)) * HD;
+#pragma unroll 1
+        for (int e = 0; e < HD; e += 2) *reinterpret_cast<uint32_t*>(out + e) = 0x7FFF7FFFu;
+      }
+    }
   }
 }
 
@@ -832,7 +1160,7 @@ int query_blocks(int width, int group) { return width * group <= kTile ? 1 : 2; 
 
 template <typename T, int HD, int BLOCKS>
 void run_attention(const TreeAttnArgs& a, cudaStream_t s) {
-  constexpr int smem = smem_bytes(HD, BLOCKS);
+  constexpr int smem = smem_bytes<HD, BLOCKS>();
   auto* kernel = tree_attention_kernel<T, HD, BLOCKS>;
   static const cudaError_t configured = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (configured != cudaSuccess) throw configured;
@@ -841,21 +1169,10 @@ void run_attention(const TreeAttnArgs& a, cudaStream_t s) {
     if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) n = 1;
     return n;
   }();
-  const int grid = sms < kMaxGrid ? sms : kMaxGrid, group = a.n_q_heads / a.n_kv_heads;
+  const int grid = sms < kMaxGrid ? sms : kMaxGrid;
   const CUtensorMap km = cache_map(a, a.k_cache), vm = cache_map(a, a.v_cache);
   kernel<<<grid, kTaThreads, smem, s>>>(a, km, vm);
-  cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess) throw e;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((a.width * group + kCombineRows - 1) / kCombineRows, a.n_kv_heads, a.batch);
-  cfg.blockDim = dim3(kCombineThreads);
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, tree_combine_kernel<T, HD, BLOCKS>, a, grid);
+  const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) throw e;
 }
 
@@ -871,8 +1188,14 @@ void run_typed(const TreeAttnArgs& a, cudaStream_t s) {
 
 }  // namespace
 
+int64_t tree_attention_places(int batch, int width, int n_q_heads, int n_kv_heads, int max_pages) {
+  const int group = n_q_heads / n_kv_heads, rows = kTile * query_blocks(width, group);
+  const int64_t blocks = ((int64_t)width * group + rows - 1) / rows, tiles = ((int64_t)max_pages * kPageTok + kTile - 1) / kTile;
+  return batch * blocks * n_kv_heads * (tiles + kStart);
+}
+
 size_t tree_attention_workspace(int, int width, int n_q_heads, int n_kv_heads, int head_dim) {
-  return kStatusBytes + 2 * kMaxGrid * slot_floats(head_dim, query_blocks(width, n_q_heads / n_kv_heads)) * sizeof(float);
+  return kArriveBytes + 2 * kMaxGrid * slot_floats(head_dim, query_blocks(width, n_q_heads / n_kv_heads)) * sizeof(float);
 }
 
 void launch_tree_attention(const TreeAttnArgs& a, cudaStream_t s) {

@@ -169,11 +169,23 @@ def qk_norm_rope(qkv, n_q_heads: int, n_kv_heads: int, pos, slots, k_cache, v_ca
 
 
 def tree_attention_workspace(batch: int, width: int, n_q_heads: int, n_kv_heads: int, head_dim: int, device="cuda"):
-    """A workspace for tree_attention calls of these sizes, one at a time."""
+    """A workspace for tree_attention calls of these sizes (or smaller), one at a time."""
     n = lib().pard_tree_attention_workspace_bytes(batch, width, n_q_heads, n_kv_heads, head_dim)
     if n == 0:
         raise ValueError("tree_attention does not support these sizes")
-    return torch.empty(n, dtype=torch.uint8, device=device)
+    return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+_workspaces = {}  # (device, stream): what calls without a workspace of their own use, one after the other
+
+
+def _workspace(dev: int, st: int, n: int):
+    if torch.cuda.is_current_stream_capturing():  # a graph may run beside later calls: its calls have their own
+        return torch.zeros(n, dtype=torch.uint8, device=dev)
+    ws = _workspaces.get((dev, st))
+    if ws is None or ws.numel() < n:
+        ws = _workspaces[dev, st] = torch.zeros(n, dtype=torch.uint8, device=dev)
+    return ws
 
 
 def tree_attention(q, k_cache, v_cache, page_table, ctx_len, n_nodes, mask, scale: Optional[float] = None, out=None,
@@ -184,7 +196,8 @@ def tree_attention(q, k_cache, v_cache, page_table, ctx_len, n_nodes, mask, scal
     q [B, N, Hq, hd] bf16 or fp16 (nodes may lie apart, as columns of a QKV
     projection do); caches [pages, Hkv, 16, hd]; page_table [B, P], ctx_len [B],
     n_nodes [B] int32; mask [B, N, ceil(N / 64)] int64 of tree_plan; scale:
-    1 / sqrt(hd) unless given.  Returns [B, N, Hq, hd]."""
+    1 / sqrt(hd) unless given; workspace: of tree_attention_workspace (without
+    one, calls share one a stream).  Returns [B, N, Hq, hd]."""
     st = _stream(q)
     dtype, dev = q.dtype, q.get_device()
     if q.dim() != 4 or dtype not in _CODE:
@@ -202,8 +215,7 @@ def tree_attention(q, k_cache, v_cache, page_table, ctx_len, n_nodes, mask, scal
     P = page_table.shape[-1]
     L = lib()
     if workspace is None:
-        need = L.pard_tree_attention_workspace_bytes(B, N, Hq, Hkv, hd)
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        workspace = _workspace(dev, st, L.pard_tree_attention_workspace_bytes(B, N, Hq, Hkv, hd))
     if out is None:
         out = torch.empty((B, N, Hq, hd), dtype=dtype, device=q.device)
     code = L.pard_tree_attention(
@@ -211,7 +223,7 @@ def tree_attention(q, k_cache, v_cache, page_table, ctx_len, n_nodes, mask, scal
         _want("page_table", page_table, _I32, (B, P), dev), P, _want("ctx_len", ctx_len, _I32, (B,), dev),
         _want("n_nodes", n_nodes, _I32, (B,), dev), _want("mask", mask, _I64, (B, N, (N + 63) // 64), dev),
         hd ** -0.5 if scale is None else scale, _want("out", out, dtype, (B, N, Hq, hd), dev), workspace.data_ptr(),
-        workspace.nbytes, st)
+        workspace.numel(), st)
     if code:
         _check(code, "pard_tree_attention")
     return out
