@@ -1,8 +1,10 @@
-"""Build libpard.so in-tree with nvcc for sm_103a (GB300).
+"""Build libpard.so in-tree with nvcc for sm_103a (GB300), and the module
+that calls its tree operators on torch tensors.
 
 Translation units are compiled in parallel and linked into
-``paper_2504_18583_gb300/libpard.so``.  A rebuild happens only when a source
-or header is newer than the library.
+``paper_2504_18583_gb300/libpard.so``; ``csrc/torch_binding.cpp`` becomes
+``_tree_ops*.so`` beside it, compiled by the host compiler against the running
+torch.  A rebuild happens only when a source or header is newer than they are.
 """
 from __future__ import annotations
 
@@ -12,12 +14,15 @@ import glob
 import os
 import shutil
 import subprocess
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libpard.so")
+BINDING_SRC = os.path.join(CSRC, "torch_binding.cpp")
+BINDING = os.path.join(PKG, "_tree_ops" + sysconfig.get_config_var("EXT_SUFFIX"))
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr",
@@ -41,13 +46,13 @@ def _sources():
 
 def _deps():
     return _sources() + glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(CSRC, "*.cuh")) + \
-        glob.glob(os.path.join(ROOT, "include", "*.h")) + [os.path.abspath(__file__)]
+        glob.glob(os.path.join(ROOT, "include", "*.h")) + [BINDING_SRC, os.path.abspath(__file__)]
 
 
 def up_to_date() -> bool:
-    if not os.path.exists(LIB):
+    if not (os.path.exists(LIB) and os.path.exists(BINDING)):
         return False
-    t = os.path.getmtime(LIB)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(BINDING))
     return all(os.path.getmtime(p) <= t for p in _deps())
 
 
@@ -81,8 +86,10 @@ def _compile_and_link(verbose: bool, extra_flags) -> str:
             print(r.stdout, r.stderr)
         return obj
 
-    with cf.ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 4)) as ex:
+    with cf.ThreadPoolExecutor(max_workers=min(12, os.cpu_count() or 4)) as ex:
+        binding = ex.submit(_compile_binding)
         objs = list(ex.map(compile_one, _sources()))
+        binding_obj = binding.result()
     tmp = LIB + ".tmp"
     r = subprocess.run([cc, *ARCH, "-shared", "-o", tmp, *objs, "-lcuda"], capture_output=True, text=True)
     if r.returncode != 0:
@@ -93,7 +100,40 @@ def _compile_and_link(verbose: bool, extra_flags) -> str:
         if r.returncode != 0:
             raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
     os.replace(tmp, LIB)
+    _link_binding(binding_obj)
     return LIB
+
+
+def _run(cmd, what):
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"{what} failed:\n{r.stdout}\n{r.stderr}")
+
+
+def _torch_dir():
+    import torch
+    return os.path.dirname(os.path.abspath(torch.__file__)), int(torch._C._GLIBCXX_USE_CXX11_ABI)
+
+
+def _compile_binding() -> str:
+    tdir, abi = _torch_dir()
+    obj = os.path.join(BUILD, "torch_binding.o")
+    cuda = os.path.dirname(os.path.dirname(nvcc()))
+    _run(["g++", "-O2", "-std=c++20", "-fPIC", "-w", f"-D_GLIBCXX_USE_CXX11_ABI={abi}",
+          "-I" + os.path.join(ROOT, "include"), "-I" + os.path.join(tdir, "include"),
+          "-I" + os.path.join(tdir, "include", "torch", "csrc", "api", "include"),
+          "-I" + os.path.join(cuda, "include"), "-I" + sysconfig.get_paths()["include"],
+          "-c", BINDING_SRC, "-o", obj], "g++ on torch_binding.cpp")
+    return obj
+
+
+def _link_binding(obj: str) -> None:
+    tdir, _ = _torch_dir()
+    tmp = BINDING + ".tmp"
+    _run(["g++", "-shared", "-o", tmp, obj, "-L" + PKG, "-l:libpard.so", "-L" + os.path.join(tdir, "lib"), "-lc10",
+          "-lc10_cuda", "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath,$ORIGIN", "-Wl,--allow-shlib-undefined"],
+         "link of the torch binding")
+    os.replace(tmp, BINDING)
 
 
 if __name__ == "__main__":

@@ -12,18 +12,24 @@
 // over 1e5 entries move a draw's boundaries by 1e-7 each).
 //
 // What bounds it: HBM for many rows (each logit is read once and stays in
-// shared memory), dependent steps for few.  A cluster of up to eight CTAs holds
-// a row, an index range each.  Sorting is avoided: one histogram over
-// max z - z (1024 bins, counts and the sums of the places within a bin, which
-// give a bin's mass to 1e-5) finds the bins that the cuts fall into, and only
-// entries that can matter are sorted:
-//   A  top-k set:   the bins up to the k-th entry hold at most 2048 entries: one
-//                   CTA sorts them and does all the rest;
-//   B  top-p only:  the same with the bins up to the nucleus' end, and the
-//                   exact sum of all weights;
-//   C  otherwise:   exact sums around the cut's bin, whose entries alone are
-//                   sorted (a bin of more than 2048 entries, ties as a rule: by
-//                   bisection over (z, i)); then one pass draws in index order.
+// shared memory) and, next to it, instructions: a row of 128256 entries is 200
+// of them a lane, so a pass over all entries is kept to what it must do.  For
+// few rows, dependent steps.  A cluster of up to eight CTAs holds a row, an
+// index range each.  Nothing is sorted but the entries that a cut can depend on:
+//   A  top-k: any k entries bound the k-th from below; the threads' largest
+//      entries (4096 a row) are counted into 1024 bins over max z - z, and the
+//      entries up to the k-th one's bin, a few more than k, go to one CTA, which
+//      sorts them and does the rest;
+//   B  top-p alone: the same counts, and one in eight of the other entries,
+//      guess the masses; one pass then has the exact mass of what is kept for
+//      sure and of all, and the entries between the guess's bounds by finer bins;
+//      the entries of the bin that the cut falls into are sorted;
+//   C  whatever these do not cover (more than 2048 entries to sort, ties, extreme
+//      temperatures, a guess that failed): a histogram of all entries, exact
+//      masses around the cut's bin, and, in a bin of more than 2048 entries,
+//      bisection over (z, i).
+// The draw is a scan in index order: masses of CTAs, then of warps' ranges, then
+// of the one range that the target falls into.
 #include <cuda_fp16.h>
 
 #include "common.cuh"
@@ -45,23 +51,41 @@ static_assert(kBins == 2 * kSmpThreads && kList == 4 * kSmpThreads, "bins and en
 
 struct Exchange {  // what a CTA tells its cluster; two, used in turn
   float top, low;
-  int top_at;
+  int n;
   unsigned long long a, b, c;
+};
+
+// Whole weights rint(w 2^40) summed in 32-bit halves at full rate: a sum with
+// 1.5 * 2^23 leaves a whole number in the low bits, which add as integers (a
+// lane has at most 64 weights of a row: the halves stay within 32 bits).
+struct Halves {
+  int hi = 0, lo = 0;
+  static constexpr float kMagic = 12582912.0f;  // 1.5 * 2^23
+  __device__ __forceinline__ void add(float w) {
+    const float a = fmaf(w, 1048576.0f, kMagic), h = a - kMagic;          // rint(w 2^20)
+    const float b = fmaf(fmaf(w, 1048576.0f, -h), 1048576.0f, kMagic);    // the rest, in 2^-40
+    hi += __float_as_int(a) - 0x4B400000;
+    lo += __float_as_int(b) - 0x4B400000;
+  }
+  __device__ __forceinline__ unsigned long long total() const { return (unsigned long long)((long long)hi * 1048576 + lo); }
 };
 
 struct SmpShared {
   uint64_t list[kList];
-  uint32_t count[kBins], place[kBins];
+  union {
+    struct { uint32_t count[kBins], place[kBins], extra[kBins]; };
+    unsigned long long mass[kBins];
+  };
   Exchange ex[2];
-  unsigned long long warp64[kSmpWarps];
+  unsigned long long warp64[kSmpWarps], above[kSmpWarps], part[3][kSmpWarps];
+  int first[kSmpMaxCluster + 1];
   float warp_top[kSmpWarps], warp_low[kSmpWarps];
-  int warp_at[kSmpWarps];
   uint32_t warp_cnt[kSmpWarps];
   float warp_mass[kSmpWarps];
-  int n_list, found;
+  int n_list, found, over;
   int bin_k, bin_p;
   uint32_t before_k;
-  float mass_k;
+  float mass_k, warp_var[kSmpWarps];
   unsigned long long reply;  // the leader's answer to its cluster
   int again;
 };
@@ -122,43 +146,61 @@ struct Row {
   int rank, size;  // place in the cluster
   int tid, lane, warp;
   int turn;        // which exchange is next
-  float top, temp, scale, range, log_min_p;
+  float top, temp, inv_temp, scale, range, log_min_p;
+  bool tame;       // finite, and far from the ends of the exponents' range
 
   __device__ float z(int i) const { return clean(to_f32(buf[i])); }
   __device__ float dist(float v) const { return v == top ? 0.f : top - v; }
   __device__ int bin(float d) const { return min(kBins - 1, (int)(d * scale)); }
-  __device__ float expo(float v) const { return v == top ? 0.f : __fdiv_rn(v - top, temp); }
+  // (v - top) / temp, correctly rounded: the reciprocal's product and one
+  // correction by its exact remainder (Markstein, IBM J. Res. Dev. 34, 1990),
+  // where nothing over- or underflows on the way, else the division
+  __device__ float expo(float v) const {
+    const float d = v - top;
+    if (!tame) return v == top ? 0.f : __fdiv_rn(d, temp);
+    const float q = d * inv_temp;
+    return fmaf(fmaf(-q, temp, d), inv_temp, q);
+  }
   __device__ float weight(float v) const { return v == -INFINITY ? 0.f : expf(expo(v)); }
   // w >= min_p, told by the exponents: next to 1 the weights have no bits left
   __device__ bool likely(float v) const { return expo(v) >= log_min_p; }
   __device__ unsigned long long whole(float w) const { return (unsigned long long)__float2ll_rn(w * kWeightOne); }
   __device__ unsigned long long mass(float v) const { return dist(v) > range ? 0ull : whole(weight(v)); }
+  // place among the bins, as a real number; more than kBins: no weight
+  __device__ float place(float v) const { return (top - v) * scale; }
 
-  // sums of three 64-bit values over the CTA
-  __device__ void block_sum(unsigned long long (&v)[3]) {
+  // a word of every CTA of the cluster, summed: a lane reads one
+  __device__ int cluster_int(const int* mine) {
+    return (int)__reduce_add_sync(0xffffffffu, lane < size ? ld_cluster32(mapa_shared(mine, lane)) : 0u);
+  }
+  __device__ unsigned long long cluster_sum64(const unsigned long long* mine) {
+    return warp_sum64(lane < size ? ld_cluster64(mapa_shared(mine, lane)) : 0ull);
+  }
+  // the warps' values that lie in shared memory: all of them, and those before this one
+  __device__ unsigned long long warps_total(const unsigned long long* of, unsigned long long* before) {
+    const unsigned long long x = lane < kSmpWarps ? of[lane] : 0ull;
+    *before = warp_sum64(lane < warp ? x : 0ull);
+    return warp_sum64(x);
+  }
+  // sums of three 64-bit values over the cluster
+  __device__ void cluster_total(unsigned long long (&v)[3]) {
 #pragma unroll
     for (int e = 0; e < 3; ++e) {
-      const unsigned long long w = warp_sum64(v[e]);
-      __syncthreads();
-      if (lane == 0) sh.warp64[warp] = w;
-      __syncthreads();
-      unsigned long long t = 0;
-      for (int i = 0; i < kSmpWarps; ++i) t += sh.warp64[i];
-      v[e] = t;
+      v[e] = warp_sum64(v[e]);
+      if (lane == 0) sh.part[e][warp] = v[e];
     }
-  }
-  // and over the cluster
-  __device__ void cluster_total(unsigned long long (&v)[3]) {
-    block_sum(v);
+    __syncthreads();
     Exchange* mine = &sh.ex[turn];
-    if (tid == 0) { mine->a = v[0]; mine->b = v[1]; mine->c = v[2]; }
-    cluster_sync();
-    v[0] = v[1] = v[2] = 0;
-    for (int r = 0; r < size; ++r) {
-      v[0] += ld_cluster64(mapa_shared(&mine->a, r));
-      v[1] += ld_cluster64(mapa_shared(&mine->b, r));
-      v[2] += ld_cluster64(mapa_shared(&mine->c, r));
+    if (warp == 0) {
+      unsigned long long b, t[3];
+#pragma unroll
+      for (int e = 0; e < 3; ++e) t[e] = warps_total(sh.part[e], &b);
+      if (lane == 0) { mine->a = t[0]; mine->b = t[1]; mine->c = t[2]; }
     }
+    cluster_sync();
+    v[0] = cluster_sum64(&mine->a);
+    v[1] = cluster_sum64(&mine->b);
+    v[2] = cluster_sum64(&mine->c);
     turn ^= 1;
   }
 
@@ -184,23 +226,59 @@ struct Row {
   // The leader's list takes the other CTAs' entries; returns the total.  A
   // cluster_sync lies between collect() and this.
   __device__ int pull() {
-    int total = min(sh.n_list, kList);
-    for (int r = 1; r < size; ++r) {
-      const int c = min((int)ld_cluster32(mapa_shared(&sh.n_list, r)), kList - total);
-      const uint32_t from = mapa_shared(sh.list, r);
-      for (int i = tid; i < c; i += kSmpThreads) sh.list[total + i] = ld_cluster64(from + 8 * i);
-      total += c;
+    const int c = lane < size ? min((int)ld_cluster32(mapa_shared(&sh.n_list, lane)), kList) : 0;
+    int inc = c;
+#pragma unroll
+    for (int o = 1; o < kSmpMaxCluster; o <<= 1) {
+      const int t = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += t;
+    }
+    if (warp == 0 && lane <= kSmpMaxCluster) sh.first[lane] = lane < kSmpMaxCluster ? inc - c : inc;
+    const int total = min(__shfl_sync(0xffffffffu, inc, kSmpMaxCluster - 1), kList);
+    __syncthreads();
+    const int own = sh.first[1];
+    for (int i = own + tid; i < total; i += kSmpThreads) {
+      int r = 1;
+#pragma unroll
+      for (int e = 2; e < kSmpMaxCluster; ++e) r += i >= sh.first[e];
+      sh.list[i] = ld_cluster64(mapa_shared(sh.list, r) + 8 * (i - sh.first[r]));
     }
     __syncthreads();
     return total;
   }
-  // Sorts the list's first m entries, ascending; returns the padded length.
-  __device__ int sort(int m) {
-    int len = 2;
+  // Sorts the list's first m entries, ascending: bitonic, an entry a thread in
+  // registers (steps within a warp are shuffles) for up to 512, else in place.
+  __device__ void sort(int m) {
+    int len = 32;
     while (len < m) len <<= 1;
+    if (len <= kSmpThreads) {
+      uint64_t x = tid < m ? sh.list[tid] : ~0ull;
+#pragma unroll 1
+      for (int k = 2; k <= len; k <<= 1)
+#pragma unroll 1
+        for (int j = k >> 1; j > 0; j >>= 1) {
+          uint64_t y;
+          if (j >= 32) {
+            __syncthreads();
+            sh.list[tid] = x;
+            __syncthreads();
+            y = sh.list[tid ^ j];
+          } else {
+            y = __shfl_xor_sync(0xffffffffu, x, j);
+          }
+          const bool low = ((tid & j) == 0) == ((tid & k) == 0);  // this thread keeps the smaller
+          x = low ? (x < y ? x : y) : (x < y ? y : x);
+        }
+      __syncthreads();
+      sh.list[tid] = x;
+      __syncthreads();
+      return;
+    }
     for (int i = m + tid; i < len; i += kSmpThreads) sh.list[i] = ~0ull;
     __syncthreads();
+#pragma unroll 1
     for (int k = 2; k <= len; k <<= 1)
+#pragma unroll 1
       for (int j = k >> 1; j > 0; j >>= 1) {
         for (int t = tid; t < len / 2; t += kSmpThreads) {
           const int i = 2 * t - (t & (j - 1)), p = i + j;
@@ -209,18 +287,18 @@ struct Row {
         }
         __syncthreads();
       }
-    return len;
   }
-  // Of four consecutive weights a thread: what lies before the thread's first.
-  __device__ unsigned long long scan_before(const unsigned long long (&v)[4]) {
+  // Of four consecutive weights a thread: what lies before the thread's first,
+  // and the total.
+  __device__ unsigned long long scan_before(const unsigned long long (&v)[4], unsigned long long* total) {
     const unsigned long long own = v[0] + v[1] + v[2] + v[3];
     const unsigned long long inc = warp_scan64(own, lane);
     __syncthreads();
     if (lane == 31) sh.warp64[warp] = inc;
     __syncthreads();
-    unsigned long long before = inc - own;
-    for (int i = 0; i < warp; ++i) before += sh.warp64[i];
-    return before;
+    unsigned long long before;
+    *total = warps_total(sh.warp64, &before);
+    return before + inc - own;
   }
 
   // Smallest key whose entries up to it (at or before `most`) reach `bar`:
@@ -246,10 +324,10 @@ struct Row {
     Exchange* mine = &sh.ex[turn];
     if (tid == 0) mine->a = (unsigned long long)zl << 32 | zh;
     cluster_sync();
-    for (int r = 0; r < size; ++r) {
-      const unsigned long long v = ld_cluster64(mapa_shared(&mine->a, r));
-      zl = min(zl, (uint32_t)(v >> 32));
-      zh = max(zh, (uint32_t)v);
+    {
+      const unsigned long long v = ld_cluster64(mapa_shared(&mine->a, lane < size ? lane : 0));
+      zl = __reduce_min_sync(0xffffffffu, min(zl, (uint32_t)(v >> 32)));
+      zh = __reduce_max_sync(0xffffffffu, max(zh, (uint32_t)v));
     }
     turn ^= 1;
     // over z, then over the index among the entries of that z
@@ -263,6 +341,139 @@ struct Row {
       if (reaches((uint64_t)zl << 32 | mid, by_mass, bar, most)) ih = mid; else il = mid + 1;
     }
     return (uint64_t)zl << 32 | il;
+  }
+  // Sorts the list's m entries and returns the last that a nucleus keeps, of
+  // which `before` lies before the list: the last whose mass before it is below
+  // the bar, or the first.
+  __device__ uint64_t cut_list(int m, unsigned long long before, double bar) {
+    sort(m);
+    unsigned long long W[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int i = 4 * tid + e;
+      W[e] = i < m ? whole(weight(key_z(sh.list[i]))) : 0ull;
+    }
+    unsigned long long all;
+    before += scan_before(W, &all);
+    if (tid == 0) sh.found = 1;
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int i = 4 * tid + e;
+      if (i < m && (double)before < bar) atomicMax(&sh.found, i + 1);
+      before += W[e];
+    }
+    __syncthreads();
+    return sh.list[sh.found - 1];
+  }
+  // The whole rest of a row whose first k entries are among the list's m: the
+  // leader sorts them, cuts and draws.
+  __device__ void finish_list(int m, int k, bool need_p, float p, double u, int32_t* token, float* logprob) {
+    sort(m);
+    unsigned long long W[4];
+    bool fits[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int i = 4 * tid + e;
+      const bool in = i < m && i < k;
+      const float v = in ? key_z(sh.list[i]) : -INFINITY;
+      W[e] = whole(weight(v));
+      fits[e] = in && likely(v);
+    }
+    unsigned long long all;  // the top-k's mass
+    unsigned long long before = scan_before(W, &all);
+    const double bar = (double)p * (double)all;
+    // kept entries are a prefix: the weights fall along the list
+    int kept = 1;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int i = 4 * tid + e;
+      if (fits[e] && (!need_p || (double)before < bar)) kept = max(kept, i + 1);
+      before += W[e];
+    }
+    if (tid == 0) sh.found = 1;
+    __syncthreads();
+    kept = __reduce_max_sync(0xffffffffu, kept);
+    if (lane == 0) atomicMax(&sh.found, kept);
+    __syncthreads();
+    const int m2 = sh.found;
+    __syncthreads();
+    // the kept entries in index order: (index, z's key)
+    for (int i = tid; i < m2; i += kSmpThreads) {
+      const uint64_t key = sh.list[i];
+      sh.list[i] = key << 32 | key >> 32;
+    }
+    sort(m2);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int i = 4 * tid + e;
+      W[e] = i < m2 ? whole(weight(key_z(sh.list[i] << 32))) : 0ull;
+    }
+    unsigned long long S, upto = scan_before(W, &S);
+    const double t = u * (double)S;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int i = 4 * tid + e;
+      const double was = (double)upto;
+      upto += W[e];
+      if (i < m2 && (double)upto > t && (i == 0 || was <= t)) {
+        *token = (int)(sh.list[i] >> 32);
+        *logprob = -log1pf((float)(S - W[e]) / (float)W[e]);
+      }
+    }
+  }
+  __device__ unsigned long long kept_mass(int i, uint64_t last) const {
+    const float v = z(i);
+    if (dist(v) > range || entry_key(v, lo + i) > last) return 0ull;
+    return likely(v) ? whole(weight(v)) : 0ull;
+  }
+  // The draw in index order, of kept entries (key up to `last`, likely enough);
+  // `own`: the mass of this warp's range [w0, w1), the same in all its lanes.
+  __device__ void draw(int w0, int w1, unsigned long long own, uint64_t last, double u, int32_t* token, float* logprob) {
+    __syncthreads();
+    if (lane == 0) sh.warp64[warp] = own;
+    __syncthreads();
+    unsigned long long before;
+    const unsigned long long mine = warps_total(sh.warp64, &before);
+    Exchange* e = &sh.ex[turn];
+    if (tid == 0) e->a = mine;
+    cluster_sync();
+    const unsigned long long of = lane < size ? ld_cluster64(mapa_shared(&e->a, lane)) : 0ull;
+    const unsigned long long S = warp_sum64(of);
+    before += warp_sum64(lane < rank ? of : 0ull);
+    const double t = u * (double)S;
+    // the warp whose range passes the target (u < 1 keeps it below S)
+    if (own && (double)before <= t && (double)(before + own) > t) {
+#pragma unroll 1
+      for (int i0 = w0; i0 < w1; i0 += 128) {
+        unsigned long long W[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int i = i0 + 32 * q + lane;
+          W[q] = i < w1 ? kept_mass(i, last) : 0ull;
+        }
+        const unsigned long long four = warp_sum64(W[0] + W[1] + W[2] + W[3]);
+        if ((double)(before + four) <= t) {
+          before += four;
+          continue;
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const unsigned long long inc = before + warp_scan64(W[q], lane);
+          const uint32_t past = __ballot_sync(0xffffffffu, (double)inc > t);
+          if (past) {
+            if (lane == __ffs(past) - 1) {
+              *token = lo + i0 + 32 * q + lane;
+              *logprob = -log1pf((float)(S - W[q]) / (float)W[q]);
+            }
+            break;
+          }
+          before = __shfl_sync(0xffffffffu, inc, 31);
+        }
+        break;
+      }
+    }
+    cluster_sync();  // no CTA leaves while another reads its shared memory
   }
   __device__ bool reaches(uint64_t key, bool by_mass, double bar, uint64_t most) {
     key = key < most ? key : most;
@@ -296,13 +507,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
   constexpr int kPer = 16 / (int)sizeof(T);
   const int pieces = (n - head) / kPer;
 
-  float top = -INFINITY, low = INFINITY;
-  int top_at = 0x7FFFFFFF;
-  auto see = [&](float v, int i) {
-    v = clean(v);
-    if (v > top || (v == top && i < top_at)) { top = v; top_at = i; }
-    if (v > -INFINITY) low = fminf(low, v);
-  };
+  float top = -INFINITY;  // a NaN is no maximum
   {
     const uint4* s4 = reinterpret_cast<const uint4*>(src + head);
     uint4* d4 = reinterpret_cast<uint4*>(buf + head);
@@ -320,7 +525,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
         d4[p] = v[e];
         const T* q = reinterpret_cast<const T*>(&v[e]);
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) see(to_f32(q[j]), lo + head + p * kPer + j);
+        for (int j = 0; j < kPer; ++j) top = fmaxf(top, to_f32(q[j]));
       }
     }
     const int tail = n - head - pieces * kPer;
@@ -328,35 +533,49 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
       const int i = tid < head ? tid : n - tail + (tid - head);
       const T v = src[i];
       buf[i] = v;
-      see(to_f32(v), lo + i);
+      top = fmaxf(top, to_f32(v));
     }
   }
-  for (int i = tid; i < kBins; i += kSmpThreads) sh.count[i] = sh.place[i] = 0;
-  // the row's largest entry (its lowest index) and smallest finite one
-  warp_argmax(top, top_at);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) low = fminf(low, __shfl_xor_sync(0xffffffffu, low, o));
-  if (lane == 0) { sh.warp_top[warp] = top; sh.warp_at[warp] = top_at; sh.warp_low[warp] = low; }
+  for (int i = tid; i < kBins; i += kSmpThreads) sh.count[i] = sh.place[i] = sh.extra[i] = 0;
+  // the row's largest entry
+  const float thread_top = top;
+  top = warp_max(top);
+  if (lane == 0) sh.warp_top[warp] = top;
   __syncthreads();
-  for (int i = 0; i < kSmpWarps; ++i) {
-    argmax_merge(top, top_at, sh.warp_top[i], sh.warp_at[i]);
-    low = fminf(low, sh.warp_low[i]);
-  }
-  if (tid == 0) { sh.ex[0].top = top; sh.ex[0].top_at = top_at; sh.ex[0].low = low; }
+  top = warp_max(sh.warp_top[lane % kSmpWarps]);
+  if (tid == 0) sh.ex[0].top = top;
   cluster_sync();
-#pragma unroll 1
-  for (int r = 0; r < size; ++r) {
-    const float t = __uint_as_float(ld_cluster32(mapa_shared(&sh.ex[0].top, r)));
-    argmax_merge(top, top_at, t, (int)ld_cluster32(mapa_shared(&sh.ex[0].top_at, r)));
-    low = fminf(low, __uint_as_float(ld_cluster32(mapa_shared(&sh.ex[0].low, r))));
+  {
+    const float t = lane < size ? __uint_as_float(ld_cluster32(mapa_shared(&sh.ex[0].top, lane))) : -INFINITY;
+    top = warp_max(t);
   }
   const float temp = a.temperature ? a.temperature[row] : 1.0f;
-  if (top == -INFINITY || !(temp > 0.f)) {  // nothing to draw from, or the largest entry
+  // whatever follows, the row gets an answer
+  if (rank == 0 && tid == 0) {
+    a.token[row] = -1;
+    a.logprob[row] = -INFINITY;
+  }
+  if (top == -INFINITY) {  // nothing to draw from
+    cluster_sync();        // no CTA leaves while another reads its shared memory
+    return;
+  }
+  if (!(temp > 0.f)) {  // the largest entry's lowest index
+    int at = 0x7FFFFFFF;
+    for (int i = n - 1 - tid; i >= 0; i -= kSmpThreads)
+      if (to_f32(buf[i]) == top) at = lo + i;
+    at = __reduce_min_sync(0xffffffffu, at);
+    if (tid == 0) sh.found = 0x7FFFFFFF;
+    __syncthreads();
+    if (lane == 0) atomicMin(&sh.found, at);
+    __syncthreads();
+    if (tid == 0) sh.ex[1].n = sh.found;
+    cluster_sync();
     if (rank == 0 && tid == 0) {
-      a.token[row] = top == -INFINITY ? -1 : top_at;
-      a.logprob[row] = top == -INFINITY ? -INFINITY : 0.f;
+      for (int r = 0; r < size; ++r) at = min(at, (int)ld_cluster32(mapa_shared(&sh.ex[1].n, r)));
+      a.token[row] = at;
+      a.logprob[row] = 0.f;
     }
-    cluster_sync();  // no CTA leaves while another reads its shared memory
+    cluster_sync();
     return;
   }
   const float p = a.top_p ? a.top_p[row] : 1.0f;
@@ -365,11 +584,243 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
   const double u = (double)fminf(fmaxf(a.u[row], 0.f), 0.99999994f);
   const int k = a.top_k ? a.top_k[row] : 0;
   bool need_k = k > 0 && k < a.vocab, need_p = p < 1.0f;
-  const float range = fminf(kRange * temp, top - low);
-  Row<T> R{sh, buf, lo, n, rank, size, tid, lane, warp, 1, top, temp, range > 1e-30f ? kBins / range : 0.f, range, log_min_p};
+  const float inv_temp = 1.0f / temp;
+  const bool tame = top < INFINITY && temp > 1e-12f && temp < 1e12f;
+  float range = kRange * temp;
+  Row<T> R{sh, buf, lo, n, rank, size, tid, lane, warp, 1, top, temp, inv_temp, kBins / range, range, log_min_p, tame};
 
   uint64_t last = ~0ull;  // the last entry that top-k and top-p keep
-  if (need_k || need_p) {
+  const int per_warp = (n + 32 * kSmpWarps - 1) / (32 * kSmpWarps) * 32;
+  const int w0 = min(n, warp * per_warp), w1 = min(n, w0 + per_warp);
+  bool general = need_k || need_p;
+  if (general && tame) {
+    // ---- A, B: few entries can matter; a guess finds them ------------------------
+    // Counted: each thread's largest entry.  Any k of them bound the k-th entry
+    // of the row from below; of the rest, entries as large as the 256th of them
+    // are few, and are counted too where top-p asks for masses, with one in eight
+    // of the others.
+    float var = 0.f;
+    const float own_place = R.place(thread_top);
+    if (own_place < (float)kBins) atomicAdd(&sh.count[(int)own_place], 1u);
+    if (tid == 0) { sh.bin_k = kBins; sh.bin_p = kBins; sh.over = 0; sh.n_list = 0; }
+    cluster_sync();
+    uint32_t cnt[2] = {0, 0};
+    // this thread's two bins of all CTAs, their loads together
+    auto gather = [&](const uint32_t* of, uint32_t (&to)[2]) {
+      uint2 c[kSmpMaxCluster];
+#pragma unroll
+      for (int r = 0; r < kSmpMaxCluster; ++r) c[r] = r < size ? ld_cluster32x2(mapa_shared(of + 2 * tid, r)) : make_uint2(0, 0);
+#pragma unroll
+      for (int r = 0; r < kSmpMaxCluster; ++r) { to[0] += c[r].x; to[1] += c[r].y; }
+    };
+    gather(sh.count, cnt);
+    // first bins up to which the counts, or the masses, reach a bar
+    auto first_bin = [&](bool lo_reaches, bool hi_reaches, int* where) {
+      const int at = lo_reaches ? 2 * tid : hi_reaches ? 2 * tid + 1 : kBins;
+      const int first = __reduce_min_sync(0xffffffffu, at);
+      if (lane == 0 && first < kBins) atomicMin(where, first);
+    };
+    {
+      uint32_t ci = cnt[0] + cnt[1];
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t t = __shfl_up_sync(0xffffffffu, ci, o);
+        if (lane >= o) ci += t;
+      }
+      if (lane == 31) sh.warp_cnt[warp] = ci;
+      __syncthreads();
+      ci += __reduce_add_sync(0xffffffffu, lane < warp ? sh.warp_cnt[lane] : 0);
+      const uint32_t want = need_k ? (uint32_t)k : 256u;
+      first_bin(ci - cnt[1] >= want, ci >= want, &sh.bin_k);
+      __syncthreads();
+    }
+    float m_all = 0.f, mi = 0.f, m_last = 0.f;
+    if (!need_k) {
+      const float heavy = (float)min(sh.bin_k + 1, kBins);
+#pragma unroll 4
+      for (int i = tid, j = 0; i < n; i += kSmpThreads, ++j) {
+        const float v = to_f32(buf[i]), t = R.place(v);
+        if (t >= heavy && (j & 7)) continue;
+        if (t < (float)kBins) atomicAdd(t < heavy ? &sh.place[(int)t] : &sh.extra[(int)t], 1u);
+      }
+      cluster_sync();
+      if (tid == 0) sh.bin_k = kBins;
+      uint32_t ex[2] = {0, 0}, smp[2] = {0, 0};
+      gather(sh.place, ex);
+      gather(sh.extra, smp);
+      // (of each run of 8 x 512 entries the first 512 were looked at)
+      const int runs = per_cta / (8 * kSmpThreads), seen = runs * kSmpThreads + min(kSmpThreads, per_cta - runs * 8 * kSmpThreads);
+      const float step = range / (kBins * temp), each = (float)per_cta / (float)seen;
+      float ms[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float w = __expf(-(2 * tid + e + 0.5f) * step);
+        ms[e] = (ex[e] + each * smp[e]) * w;
+        var += each * each * smp[e] * w * w;
+      }
+      mi = ms[0] + ms[1];
+      m_last = ms[1];
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const float tm = __shfl_up_sync(0xffffffffu, mi, o);
+        if (lane >= o) mi += tm;
+      }
+      var = warp_sum(var);
+      if (lane == 31) { sh.warp_mass[warp] = mi; sh.warp_var[warp] = var; }
+      __syncthreads();
+      const float m = lane < kSmpWarps ? sh.warp_mass[lane] : 0.f;
+      mi += warp_sum(lane < warp ? m : 0.f);
+      m_all = warp_sum(m);
+      var = warp_sum(lane < kSmpWarps ? sh.warp_var[lane] : 0.f);
+      const float slack = 5.f * sqrtf(var) + 0.004f * m_all, bar0 = p * m_all;
+      first_bin(mi - m_last >= bar0 - slack, mi >= bar0 - slack, &sh.bin_k);
+      first_bin(mi - m_last >= bar0 + slack, mi >= bar0 + slack, &sh.bin_p);
+      __syncthreads();
+    }
+    // Top-k: places before `inner` are the candidates.  Top-p: places before
+    // `inner` are kept for sure, those from `outer` on are not.
+    const float inner = need_k ? (float)min(sh.bin_k + 1, kBins) : (float)min(sh.bin_k, kBins - 1);
+    const float outer = (float)min(sh.bin_p + 1, kBins);
+    const bool guess = !need_k || sh.bin_k < kBins;
+    const float finer = kBins / (outer - inner);
+    auto fine_bin = [&](float t) { return min(kBins - 1, (int)((t - inner) * finer)); };
+    cluster_sync();  // the counts have been read: their place is taken again below
+    if (guess && need_k) {
+      if (tid == 0) sh.n_list = 0;
+      __syncthreads();
+#pragma unroll 4
+      for (int i = tid; i < n; i += kSmpThreads) {
+        const float v = to_f32(buf[i]);
+        if (R.place(v) < inner) {
+          const int at = atomicAdd(&sh.n_list, 1);
+          if (at < kList) sh.list[at] = entry_key(v, lo + i);
+        }
+      }
+      __syncthreads();
+      cluster_sync();
+      if (R.cluster_int(&sh.n_list) <= kList) {
+        const int m = rank == 0 ? R.pull() : 0;
+        cluster_sync();  // the others leave: only the leader goes on
+        if (rank == 0) R.finish_list(m, k, need_p, p, u, a.token + row, a.logprob + row);
+        return;
+      }
+      cluster_sync();
+    } else if (guess) {
+      // the exact masses before `inner` and of all, and the entries between
+      if (tid == 0) sh.n_list = 0;
+      for (int i = tid; i < kBins; i += kSmpThreads) sh.mass[i] = 0;
+      __syncthreads();
+      Halves all, sure;
+      unsigned long long between = 0;
+#pragma unroll 4
+      for (int i = w0 + lane; i < w1; i += 32) {
+        const float v = to_f32(buf[i]), t = R.place(v);
+        if (!(t <= (float)kBins)) continue;
+        const float w = R.weight(v);
+        all.add(w);
+        if (t < inner) {
+          sure.add(w);
+        } else if (t < outer) {
+          const int at = atomicAdd(&sh.n_list, 1);
+          if (at < kList) sh.list[at] = entry_key(v, lo + i);
+          const unsigned long long W = R.whole(w);
+          between += W;
+          atomicAdd(&sh.mass[fine_bin(t)], W);
+        }
+      }
+      const unsigned long long mine = warp_sum64(sure.total());
+      if (lane == 0) sh.above[warp] = mine;
+      unsigned long long v[3] = {all.total(), sure.total(), between};
+      __syncthreads();
+      if (tid == 0) sh.over = sh.n_list > kList;
+      R.cluster_total(v);
+      const double bar = (double)p * (double)v[0];
+      bool fits = (double)v[1] < bar && (double)(v[1] + v[2]) >= bar;
+      fits &= R.cluster_int(&sh.over) == 0;
+      if (fits) {
+        // the fine bin that the cut falls into, exactly
+        unsigned long long f[2] = {0, 0};
+#pragma unroll
+        for (int r = 0; r < kSmpMaxCluster; ++r)
+          if (r < size) {
+            f[0] += ld_cluster64(mapa_shared(&sh.mass[2 * tid], r));
+            f[1] += ld_cluster64(mapa_shared(&sh.mass[2 * tid + 1], r));
+          }
+        const unsigned long long inc = warp_scan64(f[0] + f[1], lane);
+        if (lane == 31) sh.warp64[warp] = inc;
+        __syncthreads();
+        unsigned long long before;
+        R.warps_total(sh.warp64, &before);
+        before += v[1] + inc - f[0] - f[1];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          if ((double)before < bar && (double)(before + f[e]) >= bar) { sh.found = 2 * tid + e; sh.reply = before; }
+          before += f[e];
+        }
+        __syncthreads();
+        const int fine = sh.found, n_mine = sh.n_list;
+        const unsigned long long m_before = sh.reply;
+        // its entries, in front of the list (each thread's own first: they move down)
+        uint64_t keep[kList / kSmpThreads];
+        bool in[kList / kSmpThreads];
+#pragma unroll
+        for (int e = 0; e < kList / kSmpThreads; ++e) {
+          const int i = e * kSmpThreads + tid;
+          keep[e] = i < n_mine ? sh.list[i] : ~0ull;
+          const float t = R.place(key_z(keep[e]));
+          in[e] = i < n_mine && fine_bin(t) == fine;
+        }
+        cluster_sync();  // all have read n_list, mass and over
+        if (tid == 0) sh.n_list = 0;
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < kList / kSmpThreads; ++e)
+          if (in[e]) sh.list[atomicAdd(&sh.n_list, 1)] = keep[e];
+        cluster_sync();
+        fits = R.cluster_int(&sh.n_list) <= kList;
+        if (fits) {
+          if (rank == 0) {
+            const uint64_t key = R.cut_list(R.pull(), m_before, bar);
+            if (tid == 0) sh.reply = key;
+          }
+          cluster_sync();
+          last = ld_cluster64(mapa_shared(&sh.reply, 0));
+          general = false;
+          if (log_min_p == -INFINITY) {
+            // kept: what was sure, and the entries between up to the cut
+#pragma unroll
+            for (int e = 0; e < kList / kSmpThreads; ++e)
+              if (e * kSmpThreads + tid < n_mine && keep[e] <= last)
+                atomicAdd(&sh.above[((int)(uint32_t)keep[e] - lo) / per_warp], R.mass(key_z(keep[e])));
+            __syncthreads();
+            R.draw(w0, w1, sh.above[warp], last, u, a.token + row, a.logprob + row);
+            return;
+          }
+        }
+      }
+      cluster_sync();
+    }
+  }
+  if (general) {
+    // ---- C: any k, any ties, any range -------------------------------------------
+    if (tid == 0) sh.found = 0;
+    for (int i = tid; i < kBins; i += kSmpThreads) sh.count[i] = sh.place[i] = 0;
+    float low = INFINITY;
+    for (int i = tid; i < n; i += kSmpThreads) {
+      const float v = R.z(i);
+      if (v > -INFINITY) low = fminf(low, v);
+    }
+    low = -warp_max(-low);
+    if (lane == 0) sh.warp_top[warp] = low;
+    __syncthreads();
+    low = -warp_max(-sh.warp_top[lane % kSmpWarps]);
+    Exchange* mine = &sh.ex[R.turn];
+    if (tid == 0) mine->low = low;
+    cluster_sync();
+    for (int r = 0; r < size; ++r) low = fminf(low, __uint_as_float(ld_cluster32(mapa_shared(&mine->low, r))));
+    R.turn ^= 1;
+    range = R.range = fminf(kRange * temp, top - low);
+    R.scale = range > 1e-30f ? kBins / range : 0.f;
     // ---- histogram over the distance from the largest entry ------------------
     for (int i = tid; i < n; i += kSmpThreads) {
       const float d = R.dist(R.z(i));
@@ -441,92 +892,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
     const int bin_k = sh.bin_k;
     int bin_p = sh.bin_p;
     if (need_k && bin_p > bin_k) bin_p = bin_k;
-    // entries up to a bin, from the thread that holds it
-    const int few_bin = need_k ? bin_k : min(bin_p + 2, kBins - 1);
-    if (tid == 0) sh.found = 0;
-    __syncthreads();
-    if ((few_bin >> 1) == tid) sh.found = (int)cc[few_bin & 1];
-    __syncthreads();
-    const int few = sh.found;
-    if ((need_k || need_p) && few <= kList) {
-      // ---- A, B: one CTA sorts all that can be kept ----------------------------
-      unsigned long long sums[3] = {0, 0, 0};
-      R.collect(0, few_bin, ~0ull);
-      if (!need_k) {
-        for (int i = tid; i < n; i += kSmpThreads) sums[0] += R.mass(R.z(i));
-        R.cluster_total(sums);
-      } else {
-        cluster_sync();
-      }
-      if (rank == 0) {
-        const int m = R.pull();
-        R.sort(m);
-        unsigned long long W[4];
-        bool fits[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int i = 4 * tid + e;
-          const bool in = i < m && (!need_k || i < k);
-          const float v = in ? key_z(sh.list[i]) : -INFINITY;
-          W[e] = R.whole(R.weight(v));
-          fits[e] = in && R.likely(v);
-        }
-        unsigned long long before = R.scan_before(W);
-        unsigned long long all = 0;  // the list's mass: the top-k's
-        for (int i = 0; i < kSmpWarps; ++i) all += sh.warp64[i];
-        const double bar = (double)p * (double)(need_k ? all : sums[0]);
-        const int limit = need_k ? min(m, k) : m;
-        const bool short_list = need_p && !need_k && (double)all < bar;
-        // kept entries are a prefix: the weights fall along the list
-        int kept = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int i = 4 * tid + e;
-          if (i < limit && (i == 0 || ((!need_p || (double)before < bar) && fits[e]))) kept = i + 1;
-          before += W[e];
-        }
-        if (tid == 0) { sh.found = 1; sh.again = short_list; }
-        __syncthreads();
-        atomicMax(&sh.found, kept);
-        __syncthreads();
-        const int m2 = sh.found;
-        if (!short_list) {
-          // the kept entries in index order: (index, z's key)
-          __syncthreads();
-          for (int i = tid; i < m2; i += kSmpThreads) {
-            const uint64_t key = sh.list[i];
-            sh.list[i] = key << 32 | key >> 32;
-          }
-          R.sort(m2);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int i = 4 * tid + e;
-            W[e] = i < m2 ? R.whole(R.weight(key_z(sh.list[i] << 32))) : 0ull;
-          }
-          unsigned long long upto = R.scan_before(W);
-          unsigned long long S = 0;
-          for (int i = 0; i < kSmpWarps; ++i) S += sh.warp64[i];
-          const double t = u * (double)S;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int i = 4 * tid + e;
-            const double was = (double)upto;
-            upto += W[e];
-            if (i < m2 && (double)upto > t && (i == 0 || was <= t)) {
-              a.token[row] = (int)(sh.list[i] >> 32);
-              a.logprob[row] = -log1pf((float)(S - W[e]) / (float)W[e]);
-            }
-          }
-        }
-      }
-      cluster_sync();
-      if (need_k || !ld_cluster32(mapa_shared(&sh.again, 0))) {
-        cluster_sync();
-        return;
-      }
-      cluster_sync();
-    }
-    // ---- C: the last entry of the top-k, then that of the nucleus --------------
+    // the last entry of the top-k, then that of the nucleus;
     // answers: the leader sorts a bin's entries and replies with a key
     if (need_k) {
       __syncthreads();
@@ -576,25 +942,8 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
         R.collect(bin_p, bin_p, most);
         cluster_sync();
         if (rank == 0) {
-          const int m = R.pull();
-          R.sort(m);
-          unsigned long long W[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int i = 4 * tid + e;
-            W[e] = i < m ? R.whole(R.weight(key_z(sh.list[i]))) : 0ull;
-          }
-          unsigned long long before = v[1] + R.scan_before(W);
-          if (tid == 0) sh.found = 1;
-          __syncthreads();
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int i = 4 * tid + e;
-            if (i < m && (double)before < bar) atomicMax(&sh.found, i + 1);
-            before += W[e];
-          }
-          __syncthreads();
-          if (tid == 0) sh.reply = sh.list[sh.found - 1];
+          const uint64_t key = R.cut_list(R.pull(), v[1], bar);
+          if (tid == 0) sh.reply = key;
         }
         cluster_sync();
         last = ld_cluster64(mapa_shared(&sh.reply, 0));
@@ -604,53 +953,21 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
     }
   }
   // ---- the draw, in index order: warps own consecutive ranges ------------------
-  const int per_warp = (n + 32 * kSmpWarps - 1) / (32 * kSmpWarps) * 32;
-  const int w0 = min(n, warp * per_warp), w1 = min(n, w0 + per_warp);
-  auto kept_mass = [&](int i) -> unsigned long long {
-    const float v = R.z(i);
-    if (R.dist(v) > range || entry_key(v, lo + i) > last) return 0ull;
-    return R.likely(v) ? R.whole(R.weight(v)) : 0ull;
-  };
   unsigned long long own = 0;
-  for (int i = w0 + lane; i < w1; i += 32) own += kept_mass(i);
-  own = warp_sum64(own);
-  __syncthreads();
-  if (lane == 0) sh.warp64[warp] = own;
-  __syncthreads();
-  unsigned long long mine = 0, before_warp = 0;
-  for (int i = 0; i < kSmpWarps; ++i) {
-    if (i == warp) before_warp = mine;
-    mine += sh.warp64[i];
-  }
-  Exchange* e = &sh.ex[R.turn];
-  if (tid == 0) e->a = mine;
-  cluster_sync();
-  unsigned long long S = 0, before = 0;
-  for (int r = 0; r < size; ++r) {
-    const unsigned long long v = ld_cluster64(mapa_shared(&e->a, r));
-    if (r < rank) before += v;
-    S += v;
-  }
-  const double t = u * (double)S;
-  before += before_warp;
-  // the first warp whose range passes the target; u < 1 keeps the target below S
-  if (own && (double)before <= t && (double)(before + own) > t) {
-    for (int i0 = w0; i0 < w1; i0 += 32) {
-      const int i = i0 + lane;
-      const unsigned long long W = i < w1 ? kept_mass(i) : 0ull;
-      const unsigned long long inc = before + warp_scan64(W, lane);
-      const uint32_t past = __ballot_sync(0xffffffffu, (double)inc > t);
-      if (past) {
-        if (lane == __ffs(past) - 1) {
-          a.token[row] = lo + i;
-          a.logprob[row] = -log1pf((float)(S - W) / (float)W);
-        }
-        break;
-      }
-      before = __shfl_sync(0xffffffffu, inc, 31);
+  if (last == ~0ull && tame) {
+    Halves sum;
+#pragma unroll 4
+    for (int i = w0 + lane; i < w1; i += 32) {
+      const float v = to_f32(buf[i]);
+      if (!(top - v <= R.range)) continue;
+      const float x = R.expo(v);
+      if (x >= log_min_p) sum.add(expf(x));
     }
+    own = sum.total();
+  } else {
+    for (int i = w0 + lane; i < w1; i += 32) own += R.kept_mass(i, last);
   }
-  cluster_sync();
+  R.draw(w0, w1, warp_sum64(own), last, u, a.token + row, a.logprob + row);
 }
 
 template <typename T>

@@ -28,41 +28,15 @@ from typing import Optional, Tuple
 
 import torch
 
-from .pard import _check, lib
+from . import pard
 
-PAGE = 16
-_CODE = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
-_I32, _I64, _F32 = torch.int32, torch.int64, torch.float32
-
-
-def _stream(t) -> int:
-    """The raw current stream; t must lie on the current device."""
-    dev = torch._C._cuda_getDevice() if t.is_cuda else -1
-    if t.get_device() != dev:
-        raise ValueError("tensors must lie on the current CUDA device")
-    return torch._C._cuda_getCurrentRawStream(dev)
-
-
-def _bad(name, t, dtype, shape):
-    what = f"{t.dtype} {tuple(t.shape)} on {t.device}" if isinstance(t, torch.Tensor) else type(t).__name__
-    raise ValueError(f"{name}: want a contiguous {dtype} tensor of shape {tuple(shape)} on the same device, got {what}")
-
-
-def _want(name, t, dtype, shape, dev):
-    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
-        _bad(name, t, dtype, shape)
-    return t.data_ptr()
-
-
-def _cache(name, t, dtype, dev):
-    """Pointer and page stride of a [pages, kv_heads, 16, head_dim] cache whose pages may lie apart."""
-    if t.dim() != 4 or t.dtype is not dtype or t.get_device() != dev or t.shape[2] != PAGE:
-        _bad(name, t, dtype, ("pages", "kv_heads", PAGE, "head_dim"))
-    n, h, _, d = t.shape
-    s = t.stride()
-    if s[3] != 1 or s[2] != d or (h > 1 and s[1] != PAGE * d):
-        raise ValueError(f"{name}: each page must be a contiguous [kv_heads, {PAGE}, head_dim] block")
-    return t.data_ptr(), s[0] if n > 1 else max(s[0], h * PAGE * d)
+pard.lib()  # raises if the library has not been built
+try:
+    from . import _tree_ops as _ops
+except ImportError as e:
+    raise RuntimeError("the torch binding of the tree operators is missing: build it with __graft_entry__.build() "
+                       "(there is no fallback)") from e
+_ops.set_error(pard.PardError)
 
 
 def tree_plan(parents, n_nodes, ctx_len, page_table, n_pages: int):
@@ -71,20 +45,7 @@ def tree_plan(parents, n_nodes, ctx_len, page_table, n_pages: int):
     parents [B, N] int32 (-1: follows the committed tokens), n_nodes [B],
     ctx_len [B], page_table [B, P] int32 over a cache of n_pages pages.
     Returns mask [B, N, ceil(N / 64)] int64, pos [B, N] int32, slots [B, N] int64."""
-    st = _stream(parents)
-    B, N = parents.shape
-    dev = parents.get_device()
-    P = page_table.shape[-1]
-    mask = torch.empty((B, N, (N + 63) // 64), dtype=_I64, device=parents.device)
-    pos = torch.empty((B, N), dtype=_I32, device=parents.device)
-    slots = torch.empty((B, N), dtype=_I64, device=parents.device)
-    code = lib().pard_tree_plan(
-        _want("parents", parents, _I32, (B, N), dev), _want("n_nodes", n_nodes, _I32, (B,), dev),
-        _want("ctx_len", ctx_len, _I32, (B,), dev), _want("page_table", page_table, _I32, (B, P), dev), B, N, P,
-        n_pages, mask.data_ptr(), pos.data_ptr(), slots.data_ptr(), st)
-    if code:
-        _check(code, "pard_tree_plan")
-    return mask, pos, slots
+    return _ops.tree_plan(parents, n_nodes, ctx_len, page_table, n_pages)
 
 
 def rope_frequencies(rot_dim: int, theta: float = 10000.0, scaling: Optional[str] = None, factor: float = 1.0,
@@ -131,7 +92,7 @@ def rope_frequencies(rot_dim: int, theta: float = 10000.0, scaling: Optional[str
         freq = freq * keep + freq / factor * (1.0 - keep)
     elif scaling is not None:
         raise ValueError(f"unknown scaling {scaling!r}")
-    return freq.to(_F32).to(device), amplitude
+    return freq.to(torch.float32).to(device), amplitude
 
 
 def qk_norm_rope(qkv, n_q_heads: int, n_kv_heads: int, pos, slots, k_cache, v_cache, inv_freq, q_gain=None,
@@ -143,49 +104,16 @@ def qk_norm_rope(qkv, n_q_heads: int, n_kv_heads: int, pos, slots, k_cache, v_ca
     slots [T] int64; caches [pages, Hkv, 16, hd]; inv_freq [rot / 2] fp32
     (rot_dim = 2 * its length; None: no rotation); gains [hd] or None.  Returns
     the queries [T, Hq, hd]."""
-    st = _stream(qkv)
-    dtype, dev = qkv.dtype, qkv.get_device()
-    if qkv.dim() != 2 or qkv.stride(1) != 1 or dtype not in _CODE:
-        raise ValueError("qkv: want [tokens, (Hq + 2 Hkv) * hd] rows of bf16 or fp16 with contiguous entries")
-    T, width = qkv.shape
-    kp, stride = _cache("k_cache", k_cache, dtype, dev)
-    vp, v_stride = _cache("v_cache", v_cache, dtype, dev)
-    n_pages, heads, _, hd = k_cache.shape
-    if stride != v_stride or v_cache.shape != k_cache.shape or heads != n_kv_heads or \
-            width != (n_q_heads + 2 * n_kv_heads) * hd:
-        raise ValueError("qkv and caches disagree on heads, head_dim, pages or page stride")
-    half = 0 if inv_freq is None else inv_freq.shape[0]
-    q = torch.empty((T, n_q_heads, hd), dtype=dtype, device=qkv.device)
-    code = lib().pard_qk_norm_rope(
-        qkv.data_ptr(), qkv.stride(0) if T > 1 else max(width, qkv.stride(0)), _CODE[dtype], T, n_q_heads, n_kv_heads,
-        hd, None if q_gain is None else _want("q_gain", q_gain, dtype, (hd,), dev),
-        None if k_gain is None else _want("k_gain", k_gain, dtype, (hd,), dev), eps,
-        _want("pos", pos, _I32, (T,), dev), _want("slots", slots, _I64, (T,), dev),
-        None if not half else _want("inv_freq", inv_freq, _F32, (half,), dev), 2 * half, interleaved, amplitude,
-        q.data_ptr(), n_q_heads * hd, kp, vp, stride, n_pages, st)
-    if code:
-        _check(code, "pard_qk_norm_rope")
-    return q
+    return _ops.qk_norm_rope(qkv, n_q_heads, n_kv_heads, pos, slots, k_cache, v_cache, inv_freq, q_gain, k_gain, eps,
+                             interleaved, amplitude)
 
 
 def tree_attention_workspace(batch: int, width: int, n_q_heads: int, n_kv_heads: int, head_dim: int, device="cuda"):
     """A workspace for tree_attention calls of these sizes (or smaller), one at a time."""
-    n = lib().pard_tree_attention_workspace_bytes(batch, width, n_q_heads, n_kv_heads, head_dim)
+    n = pard.lib().pard_tree_attention_workspace_bytes(batch, width, n_q_heads, n_kv_heads, head_dim)
     if n == 0:
         raise ValueError("tree_attention does not support these sizes")
     return torch.zeros(n, dtype=torch.uint8, device=device)
-
-
-_workspaces = {}  # (device, stream): what calls without a workspace of their own use, one after the other
-
-
-def _workspace(dev: int, st: int, n: int):
-    if torch.cuda.is_current_stream_capturing():  # a graph may run beside later calls: its calls have their own
-        return torch.zeros(n, dtype=torch.uint8, device=dev)
-    ws = _workspaces.get((dev, st))
-    if ws is None or ws.numel() < n:
-        ws = _workspaces[dev, st] = torch.zeros(n, dtype=torch.uint8, device=dev)
-    return ws
 
 
 def tree_attention(q, k_cache, v_cache, page_table, ctx_len, n_nodes, mask, scale: Optional[float] = None, out=None,
@@ -198,35 +126,8 @@ def tree_attention(q, k_cache, v_cache, page_table, ctx_len, n_nodes, mask, scal
     n_nodes [B] int32; mask [B, N, ceil(N / 64)] int64 of tree_plan; scale:
     1 / sqrt(hd) unless given; workspace: of tree_attention_workspace (without
     one, calls share one a stream).  Returns [B, N, Hq, hd]."""
-    st = _stream(q)
-    dtype, dev = q.dtype, q.get_device()
-    if q.dim() != 4 or dtype not in _CODE:
-        raise ValueError("q: want [batch, width, query heads, head_dim] of bf16 or fp16")
-    B, N, Hq, hd = q.shape
-    s = q.stride()
-    node = s[1] if N > 1 else (s[0] if B > 1 else Hq * hd)
-    if s[3] != 1 or (Hq > 1 and s[2] != hd) or (B > 1 and s[0] != N * node):
-        raise ValueError("q: a node's heads must be contiguous and nodes evenly spaced")
-    kp, stride = _cache("k_cache", k_cache, dtype, dev)
-    vp, v_stride = _cache("v_cache", v_cache, dtype, dev)
-    n_pages, Hkv, _, d = k_cache.shape
-    if stride != v_stride or v_cache.shape != k_cache.shape or d != hd:
-        raise ValueError("q and caches disagree on head_dim, pages or page stride")
-    P = page_table.shape[-1]
-    L = lib()
-    if workspace is None:
-        workspace = _workspace(dev, st, L.pard_tree_attention_workspace_bytes(B, N, Hq, Hkv, hd))
-    if out is None:
-        out = torch.empty((B, N, Hq, hd), dtype=dtype, device=q.device)
-    code = L.pard_tree_attention(
-        q.data_ptr(), node, _CODE[dtype], B, N, Hq, Hkv, hd, kp, vp, stride, n_pages,
-        _want("page_table", page_table, _I32, (B, P), dev), P, _want("ctx_len", ctx_len, _I32, (B,), dev),
-        _want("n_nodes", n_nodes, _I32, (B,), dev), _want("mask", mask, _I64, (B, N, (N + 63) // 64), dev),
-        hd ** -0.5 if scale is None else scale, _want("out", out, dtype, (B, N, Hq, hd), dev), workspace.data_ptr(),
-        workspace.numel(), st)
-    if code:
-        _check(code, "pard_tree_attention")
-    return out
+    return _ops.tree_attention(q, k_cache, v_cache, page_table, ctx_len, n_nodes, mask, scale, out, workspace,
+                               workspace is None and torch.cuda.is_current_stream_capturing())
 
 
 def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None):
@@ -237,24 +138,7 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None):
     [0, 1); temperature, top_p, min_p [R] fp32, top_k [R] int32, each or None.
     Returns token [R] int32 (-1: a row with no entry above -inf) and its
     log-probability among the entries kept [R] fp32."""
-    st = _stream(logits)
-    dtype, dev = logits.dtype, logits.get_device()
-    if logits.dim() != 2 or logits.stride(1) != 1 or dtype not in _CODE:
-        raise ValueError("logits: want [rows, vocab] of fp32, bf16 or fp16 with contiguous rows")
-    R, V = logits.shape
-    row = (R,)
-    token = torch.empty(R, dtype=_I32, device=logits.device)
-    logprob = torch.empty(R, dtype=_F32, device=logits.device)
-    code = lib().pard_sample(
-        logits.data_ptr(), logits.stride(0) if R > 1 else max(V, logits.stride(0)), _CODE[dtype], R, V,
-        _want("u", u, _F32, row, dev),
-        None if temperature is None else _want("temperature", temperature, _F32, row, dev),
-        None if top_k is None else _want("top_k", top_k, _I32, row, dev),
-        None if top_p is None else _want("top_p", top_p, _F32, row, dev),
-        None if min_p is None else _want("min_p", min_p, _F32, row, dev), token.data_ptr(), logprob.data_ptr(), st)
-    if code:
-        _check(code, "pard_sample")
-    return token, logprob
+    return _ops.sample(logits, u, temperature, top_k, top_p, min_p)
 
 
 def tree_commit(sampled, tokens, parents, n_nodes, ctx_len, page_table, pool):
@@ -265,26 +149,4 @@ def tree_commit(sampled, tokens, parents, n_nodes, ctx_len, page_table, pool):
     int32; pool [layers, 2, pages, Hkv, 16, hd] bf16 or fp16.  Returns
     accept_len [B], emitted [B, N] (-1 after the emitted tokens) and the new
     context lengths [B]."""
-    st = _stream(sampled)
-    dev = sampled.get_device()
-    B, N = sampled.shape
-    P = page_table.shape[-1]
-    if pool.dim() != 6 or pool.shape[1] != 2 or pool.shape[4] != PAGE or pool.get_device() != dev or \
-            pool.dtype not in (torch.bfloat16, torch.float16):
-        raise ValueError("pool: want [layers, 2, pages, kv_heads, 16, head_dim] of bf16 or fp16 on the same device")
-    L, _, n_pages, Hkv, _, hd = pool.shape
-    s = pool.stride()
-    if s[5] != 1 or s[4] != hd or (Hkv > 1 and s[3] != PAGE * hd):
-        raise ValueError("pool: each page must be a contiguous [kv_heads, 16, head_dim] block")
-    accept = torch.empty(B, dtype=_I32, device=sampled.device)
-    emitted = torch.empty((B, N), dtype=_I32, device=sampled.device)
-    length = torch.empty(B, dtype=_I32, device=sampled.device)
-    code = lib().pard_tree_commit(
-        _want("sampled", sampled, _I32, (B, N), dev), _want("tokens", tokens, _I32, (B, N), dev),
-        _want("parents", parents, _I32, (B, N), dev), _want("n_nodes", n_nodes, _I32, (B,), dev),
-        _want("ctx_len", ctx_len, _I32, (B,), dev), _want("page_table", page_table, _I32, (B, P), dev), B, N, P,
-        pool.data_ptr(), s[0], s[1], s[2] if n_pages > 1 else Hkv * PAGE * hd, L, Hkv, hd, n_pages,
-        accept.data_ptr(), emitted.data_ptr(), length.data_ptr(), st)
-    if code:
-        _check(code, "pard_tree_commit")
-    return accept, emitted, length
+    return _ops.tree_commit(sampled, tokens, parents, n_nodes, ctx_len, page_table, pool)
