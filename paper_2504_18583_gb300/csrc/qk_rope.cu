@@ -7,12 +7,16 @@
 // on the pairs (i, i + rot/2) or (2i, 2i + 1) of a head's first rot entries.
 // All arithmetic is in 32 bits, rounded once to the output's type.
 //
-// What bounds it: HBM (each entry is read and written once).  A lane holds
-// eight entries (16 bytes), a head is 8 or 16 lanes, so the norm is three or
-// four shuffles and a half-split pair's other entries are rot/16 lanes away:
-// they are exchanged as the packed input, four shuffles for eight entries.
-// One CTA takes one token (or, where tokens are few, part of its heads); the
-// loads go out before the angles are computed.
+// What bounds it: HBM (each entry is read and written once) and, next to it, the
+// instructions, about 150 for a warp's 256 entries.  A lane holds eight entries
+// (16 bytes), a head is 8 or 16 lanes, so the norm is three or four shuffles and
+// a half-split pair's other entries are rot/16 lanes away: they are exchanged as
+// the packed input, four shuffles for eight entries.  Gains and rotation are
+// multiplied together once a token, by all threads, into two factors an entry.
+// The loads of the next token's heads are out while a CTA works on one's.
+// Measured, 8191 tokens of 48 heads of 128: 42 us, 4.8 TB/s (67 us with a CTA a
+// token and the gains applied to every head; 48 with 64-bit divisions for the
+// place of an item).
 //
 // Angles.  position * inv_freq in 32 bits is off by 2^-24 of itself: 4e-3 at
 // position 65536.  Here each frequency becomes a whole number of 2^-64 turns,
@@ -28,6 +32,7 @@ namespace pard {
 namespace {
 
 constexpr int kRopeThreads = 256;
+static_assert(kPageTok == 16, "slots are taken apart by shifts");
 constexpr int kRopeHeads = 3;  // heads a lane group has in flight
 
 template <typename T> struct Pack;
@@ -70,124 +75,161 @@ __device__ __forceinline__ uint64_t turns_per_position(float f) {
   return f < 0.f ? 0 - t : t;
 }
 
+__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
+
 }  // namespace
 
-template <typename T, int HD>
-__global__ void __launch_bounds__(kRopeThreads) qk_rope_kernel(const QkRopeArgs a, int heads_per_cta) {
+// A CTA has U heads of every lane group, those of its blockIdx.y, and walks over
+// tokens: the next one's loads are out while it works on one.
+template <typename T, int HD, int U>
+__global__ void __launch_bounds__(kRopeThreads, U == 1 ? 5 : 4) qk_rope_kernel(const __grid_constant__ QkRopeArgs a) {
   constexpr int kGroup = HD / 8;                      // lanes of one head
   constexpr int kGroups = kRopeThreads / kGroup;      // heads a CTA takes at once
-  __shared__ float2 s_turn[HD / 2];                   // amplitude * (cos, sin) of this token's pairs
-  const int tok = blockIdx.x, tid = threadIdx.x;
-  const int g = tid / kGroup, l = tid % kGroup, lane = tid & 31;
-  const int heads = a.n_q_heads + 2 * a.n_kv_heads;
-  const int h0 = blockIdx.y * heads_per_cta, h1 = min(heads, h0 + heads_per_cta);
-  const T* row = reinterpret_cast<const T*>(a.qkv) + (int64_t)tok * a.qkv_stride + l * 8;
-  uint4 x[kRopeHeads];
-#pragma unroll
-  for (int e = 0; e < kRopeHeads; ++e) {
-    const int h = h0 + e * kGroups + g;
-    if (h < h1) x[e] = *reinterpret_cast<const uint4*>(row + (int64_t)h * HD);
-  }
-  const int half = a.rot_dim / 2;
-  if (tid < half) {
-    const uint64_t f = turns_per_position(a.inv_freq[tid]);
-    const uint64_t phase = f * (uint64_t)(int64_t)a.pos[tok];
-    float sn, cs;
-    sincospif((float)(int32_t)(phase >> 32) * 4.656612873077393e-10f, &sn, &cs);  // 2^-31: half turns
-    s_turn[tid] = make_float2(a.amplitude * cs, a.amplitude * sn);
-  }
-  const int64_t slot = a.slots[tok];
-  const int64_t page = slot >= 0 ? slot / kPageTok : -1;
-  const bool write = page >= 0 && page < a.n_pages;
-  const int64_t cache_at = page * a.page_stride + (slot % kPageTok) * HD + l * 8;
-  __syncthreads();
-  // this lane's factors: out = own * cos + other * sin', with the half-split
+  // Each entry's factors of a token, queries' and keys': gain and rotation in
+  // one, out = norm * (own * x + other * y), pair i of all lanes side by side (in
+  // entry order a lane's were 64 bytes from the next lane's: four-way bank
+  // conflicts, 61 us against 48 for 8191 tokens).  Two tokens in turn.
+  __shared__ float4 s_turn[2][2][HD / 2];
+  const int tid = threadIdx.x, g = tid / kGroup, l = tid % kGroup, lane = tid & 31;
+  const int heads = a.n_q_heads + 2 * a.n_kv_heads, half = a.rot_dim / 2, e0 = l * 8;
+  const int h0 = blockIdx.y * U * kGroups + g;
+  // this lane's entries: out = own * cos + other * sin', with the half-split
   // layout's other entries `away` lanes off
-  const int e0 = l * 8;
   const bool rotates = e0 < a.rot_dim, upper = !a.interleaved && e0 >= half;
   const int away = a.interleaved || !rotates ? 0 : (upper ? -(half / 8) : half / 8);
-  float cs[8], sn[8];
-  if (rotates) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int i = a.interleaved ? (e0 + e) / 2 : (upper ? e0 + e - half : e0 + e);
-      const float2 t = s_turn[i];
-      cs[e] = t.x;
-      sn[e] = (a.interleaved ? (e & 1) != 0 : upper) ? t.y : -t.y;
+  const int far_lane = lane + away;
+  // the entry whose factors this thread computes
+  const int te = tid % HD, tk = tid / HD;  // tk 0: queries, 1: keys, else none
+  const bool t_turns = te < a.rot_dim, t_odd = a.interleaved ? te & 1 : te >= half;
+  uint64_t per_pos = 0;
+  float t_own = 1.f, t_far = 1.f;
+  if (tk < 2) {
+    const T* gain = reinterpret_cast<const T*>(tk ? a.k_gain : a.q_gain);
+    if (t_turns) per_pos = turns_per_position(a.inv_freq[a.interleaved ? te / 2 : (t_odd ? te - half : te)]);
+    if (gain) {
+      t_own = to_float(gain[te]);
+      if (t_turns) t_far = to_float(gain[a.interleaved ? te ^ 1 : (t_odd ? te - half : te + half)]);
     }
   }
-  for (int base = h0; base < h1; base += kRopeHeads * kGroups) {
-    if (base > h0) {
+  const bool q_norm = a.q_gain != nullptr, k_norm = a.k_gain != nullptr;
+  const T* qkv = reinterpret_cast<const T*>(a.qkv) + (int64_t)h0 * HD + e0;
+  T* q = reinterpret_cast<T*>(a.q) + (int64_t)h0 * HD + e0;
+  auto load = [&](int tok, uint4 (&x)[U]) {
+    const T* row = qkv + (int64_t)tok * a.qkv_stride;
 #pragma unroll
-      for (int e = 0; e < kRopeHeads; ++e) {
-        const int h = base + e * kGroups + g;
-        if (h < h1) x[e] = *reinterpret_cast<const uint4*>(row + (int64_t)h * HD);
-      }
+    for (int e = 0; e < U; ++e) {
+      x[e] = make_uint4(0, 0, 0, 0);
+      if (h0 + e * kGroups < heads) x[e] = __ldcs(reinterpret_cast<const uint4*>(row + e * kGroups * HD));
     }
+  };
+  int tok = blockIdx.x;
+  uint4 x[U];
+  load(tok, x);
+  int pos = a.pos[tok];
+  int64_t slot = a.slots[tok];
+  for (int buf = 0; tok < a.n_tokens; buf ^= 1) {
+    if (tk < 2) {
+      const uint64_t phase = per_pos * (uint64_t)(int64_t)pos;
+      float sn, cs;
+      sincospif((float)(int32_t)(phase >> 32) * 4.656612873077393e-10f, &sn, &cs);  // 2^-31: half turns
+      reinterpret_cast<float2*>(s_turn[buf][tk])[((te % 8 / 2) * kGroup + te / 8) * 2 + (te & 1)] =
+          t_turns ? make_float2(t_own * (a.amplitude * cs), (t_odd ? t_far : -t_far) * (a.amplitude * sn)) : make_float2(t_own, 0.f);
+    }
+    const bool write = slot >= 0 && slot < (int64_t)a.n_pages * kPageTok;
+    const int64_t cache_at = (int64_t)(uint32_t)(slot >> 4) * a.page_stride + (int)(slot & (kPageTok - 1)) * HD + e0;
+    __syncthreads();  // (the other buffer's readers are past it: they arrived here)
+    uint4 ahead[U];
+    const int after = tok + gridDim.x;
+    if (after < a.n_tokens) {
+      load(after, ahead);
+      pos = a.pos[after];
+      slot = a.slots[after];
+    }
+    T* q_row = q + (int64_t)tok * a.q_stride;
 #pragma unroll
-    for (int e = 0; e < kRopeHeads; ++e) {
-      const int h = base + e * kGroups + g;
-      // shuffles below: a warp's groups leave the loop together or sit out
-      const bool on = h < h1;
-      if (!__any_sync(0xffffffffu, on)) continue;
+    for (int e = 0; e < U; ++e) {
+      const int h = h0 + e * kGroups;
+      const bool on = h < heads;
       const bool is_q = h < a.n_q_heads, is_v = h >= a.n_q_heads + a.n_kv_heads;
-      const uint4 raw = on ? x[e] : make_uint4(0, 0, 0, 0);
+      const uint4 raw = x[e];
       uint4 out = raw;
       if (__any_sync(0xffffffffu, on && !is_v)) {
-        uint4 far;
-        const int from = lane + away;
-        far.x = __shfl_sync(0xffffffffu, raw.x, from);
-        far.y = __shfl_sync(0xffffffffu, raw.y, from);
-        far.z = __shfl_sync(0xffffffffu, raw.z, from);
-        far.w = __shfl_sync(0xffffffffu, raw.w, from);
-        float v[8], o[8];
+        float v[8], t[8];
         unpack<T>(raw, v);
-        unpack<T>(far, o);
-        const T* gain = reinterpret_cast<const T*>(is_q ? a.q_gain : a.k_gain);
-        float ss = 0.f;
+        float r = 1.f;
+        if (__any_sync(0xffffffffu, is_q ? q_norm : k_norm)) {
+          float ss = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) ss = fmaf(v[i], v[i], ss);
+          for (int i = 0; i < 8; ++i) ss = fmaf(v[i], v[i], ss);
 #pragma unroll
-        for (int d = kGroup / 2; d > 0; d >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
-        if (gain && !is_v) {
-          const float r = rsqrtf(ss * (1.0f / HD) + a.eps);
-          float gn[8], gf[8];
-          unpack<T>(*reinterpret_cast<const uint4*>(gain + e0), gn);
-          unpack<T>(*reinterpret_cast<const uint4*>(gain + e0 + away * 8), gf);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) { v[i] *= r * gn[i]; o[i] *= r * gf[i]; }
+          for (int d = kGroup / 2; d > 0; d >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
+          if (is_q ? q_norm : k_norm) r = rsqrtf(ss * (1.0f / HD) + a.eps);
         }
-        if (rotates) {
-          float t[8];
+        const float4* turn = &s_turn[buf][is_q ? 0 : 1][l];
+        if (a.interleaved) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) t[i] = fmaf(a.interleaved ? v[i ^ 1] : o[i], sn[i], v[i] * cs[i]);
+          for (int i = 0; i < 4; ++i) {
+            const float4 c = turn[i * kGroup];
+            t[2 * i] = v[2 * i] * c.x;
+            t[2 * i + 1] = v[2 * i + 1] * c.z;
+            if (rotates) {
+              t[2 * i] = fmaf(v[2 * i + 1], c.y, t[2 * i]);
+              t[2 * i + 1] = fmaf(v[2 * i], c.w, t[2 * i + 1]);
+            }
+          }
+        } else {
+          uint4 far;
+          far.x = __shfl_sync(0xffffffffu, raw.x, far_lane);
+          far.y = __shfl_sync(0xffffffffu, raw.y, far_lane);
+          far.z = __shfl_sync(0xffffffffu, raw.z, far_lane);
+          far.w = __shfl_sync(0xffffffffu, raw.w, far_lane);
+          float o[8];
+          unpack<T>(far, o);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] = t[i];
+          for (int i = 0; i < 4; ++i) {
+            const float4 c = turn[i * kGroup];
+            t[2 * i] = v[2 * i] * c.x;
+            t[2 * i + 1] = v[2 * i + 1] * c.z;
+            if (rotates) {
+              t[2 * i] = fmaf(o[2 * i], c.y, t[2 * i]);
+              t[2 * i + 1] = fmaf(o[2 * i + 1], c.w, t[2 * i + 1]);
+            }
+          }
         }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = t[i] * r;
         if (!is_v)
           out = make_uint4(Pack<T>::from(v[0], v[1]), Pack<T>::from(v[2], v[3]), Pack<T>::from(v[4], v[5]),
                            Pack<T>::from(v[6], v[7]));
       }
-      if (!on) continue;
-      if (is_q) {
-        *reinterpret_cast<uint4*>(reinterpret_cast<T*>(a.q) + (int64_t)tok * a.q_stride + (int64_t)h * HD + e0) = out;
-      } else if (write) {
+      if (on && is_q) {
+        *reinterpret_cast<uint4*>(q_row + e * kGroups * HD) = out;
+      } else if (on && write) {
         const int kh = h - a.n_q_heads - (is_v ? a.n_kv_heads : 0);
         T* cache = reinterpret_cast<T*>(is_v ? a.v_cache : a.k_cache);
-        *reinterpret_cast<uint4*>(cache + cache_at + (int64_t)kh * kPageTok * HD) = out;
+        *reinterpret_cast<uint4*>(cache + cache_at + kh * (kPageTok * HD)) = out;
       }
     }
+#pragma unroll
+    for (int e = 0; e < U; ++e) x[e] = ahead[e];
+    tok = after;
   }
+}
+
+template <typename T, int HD, int U>
+static void launch_items(const QkRopeArgs& a, int most, cudaStream_t s) {
+  constexpr int kTake = U * kRopeThreads / (HD / 8);
+  const int chunks = (a.n_q_heads + 2 * a.n_kv_heads + kTake - 1) / kTake;
+  const int across = most / chunks < 1 ? 1 : most / chunks;
+  qk_rope_kernel<T, HD, U><<<dim3(a.n_tokens < across ? a.n_tokens : across, chunks), kRopeThreads, 0, s>>>(a);
 }
 
 template <typename T, int HD>
 static void run_rope(const QkRopeArgs& a, cudaStream_t s) {
-  constexpr int kGroups = kRopeThreads / (HD / 8);
-  const int heads = a.n_q_heads + 2 * a.n_kv_heads;
-  const int rounds = (heads + kGroups - 1) / kGroups;
-  // few tokens: one round of heads a CTA, so that no thread works in turns
-  const int per_cta = a.n_tokens <= 304 ? kGroups : rounds * kGroups;
-  qk_rope_kernel<T, HD><<<dim3(a.n_tokens, (heads + per_cta - 1) / per_cta), kRopeThreads, 0, s>>>(a, per_cta);
+  // few tokens: a head a lane group, so that no thread works in turns; many: as
+  // many as a lane can have in flight
+  if (a.n_tokens <= 304) launch_items<T, HD, 1>(a, 152 * 5, s); else launch_items<T, HD, kRopeHeads>(a, 152 * 4, s);
 }
 
 void launch_qk_rope(const QkRopeArgs& a, cudaStream_t s) {
