@@ -591,3 +591,75 @@ def test_refusals(tree):
         tree.qk_norm_rope(bf(3, 8 * 64 + 8)[:, 1:513], 4, 2, i32(3), i32(3).long(), bf(3, 2, 16, 64), bf(3, 2, 16, 64), None)
     with pytest.raises(ValueError):
         tree.tree_commit(i32(1, 4), i32(1, 4), i32(1, 4), i32(1), i32(1), i32(1, 2), bf(2, 1, 3, 2, 16, 64))
+
+
+# ---- the operators together -----------------------------------------------------------------
+def test_tree_decoding_emits_what_autoregressive_decoding_would():
+    """The example's model: every token that tree decoding emits is, within
+    2^-4 of the logits (bf16 cache and attention; logits of about +-10), the one
+    that a pass over the emitted sequence itself, as a chain, has largest, and
+    trees need fewer passes than tokens."""
+    import os
+    import sys
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import tree_decode as E
+    from paper_2504_18583_gb300 import tree
+    model = E.Model()
+    g = torch.Generator().manual_seed(5)
+    prompts = [torch.randint(0, model.vocab, (n,), generator=g).tolist() for n in (40, 7, 100)]
+    n_new = 64
+    out, passes = E.generate(model, prompts, n_new)
+    assert passes < n_new
+    B, pages = len(out), 16
+    table = torch.arange(B * pages, dtype=torch.int32, device="cuda").view(B, pages)
+    pool = torch.zeros((model.layers, 2, B * pages, model.Hkv, PAGE, model.hd), dtype=torch.bfloat16, device="cuda")
+    N = max(len(o) for o in out)
+    assert [len(o) - len(p) for o, p in zip(out, prompts)] == [n_new] * B
+    chain, nodes, ctx = dev([[i - 1 for i in range(N)]] * B), dev([len(o) for o in out]), dev([0] * B)
+    tokens = dev([o + [0] * (N - len(o)) for o in out])
+    plan = tree.tree_plan(chain, nodes, ctx, table, B * pages)
+    logits = model.forward(tokens, plan, pool, table, ctx, nodes).cpu()
+    for b, (o, p) in enumerate(zip(out, prompts)):
+        for i in range(len(p) - 1, len(o) - 1):
+            assert logits[b, i, o[i + 1]] >= logits[b, i].max() - 2.0 ** -4, (b, i)
+
+
+def test_calls_in_a_cuda_graph(tree):
+    """The whole step captured once and replayed on other inputs."""
+    rs = np.random.RandomState(3)
+    B, N, Hq, Hkv, hd, n_pages = 3, 9, 8, 2, 64, 40
+    g = torch.Generator(device="cuda").manual_seed(6)
+    pool = torch.randn((1, 2, n_pages, Hkv, PAGE, hd), generator=g, device="cuda").bfloat16()
+    lens, nodes = dev([100, 30, 7]), dev([9, 4, 6])
+    table = dev(np.arange(36).reshape(3, 12))
+    parents = dev([random_tree(rs, N) for _ in range(B)])
+    qkv = torch.randn((B * N, (Hq + 2 * Hkv) * hd), generator=g, device="cuda").bfloat16()
+    logits, u = torch.randn((B * N, 500), generator=g, device="cuda"), torch.rand(B * N, generator=g, device="cuda")
+    tokens = dev(rs.randint(0, 500, (B, N)))
+    freq, _ = tree.rope_frequencies(hd)
+
+    def step():
+        mask, pos, slots = tree.tree_plan(parents, nodes, lens, table, n_pages)
+        q = tree.qk_norm_rope(qkv, Hq, Hkv, pos.view(-1), slots.view(-1), pool[0, 0], pool[0, 1], freq)
+        o = tree.tree_attention(q.view(B, N, Hq, hd), pool[0, 0], pool[0, 1], table, lens, nodes, mask)
+        token, logp = tree.sample(logits, u)
+        return (o, token, logp) + tuple(tree.tree_commit(token.view(B, N), tokens, parents, nodes, lens, table, pool))
+
+    kept = pool.clone()
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    pool.copy_(kept)
+    with torch.cuda.graph(graph):
+        outs = step()
+    for seed in range(3):
+        g.manual_seed(100 + seed)
+        qkv.copy_(torch.randn(qkv.shape, generator=g, device="cuda"))
+        logits.copy_(torch.randn(logits.shape, generator=g, device="cuda"))
+        u.copy_(torch.rand(u.shape, generator=g, device="cuda"))
+        pool.copy_(kept)
+        want = [x.clone() for x in step()] + [pool.clone()]
+        pool.copy_(kept)
+        graph.replay()
+        for x, y in zip(want, list(outs) + [pool]):
+            assert torch.equal(x, y)
