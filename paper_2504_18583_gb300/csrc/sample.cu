@@ -42,15 +42,18 @@ namespace {
 constexpr int kSmpThreads = 512;
 constexpr int kSmpWarps = kSmpThreads / 32;
 constexpr int kBins = 1024;
+constexpr int kFine = 256;             // bins of the entries that a cut may fall among
 constexpr int kList = 2048;            // entries one CTA sorts
+constexpr int kFew = 256;              // up to here, each is compared with all others instead
 constexpr int kSmpMaxCluster = 8;
 constexpr int kSliceBytes = 64 * 1024; // a CTA's share of a row: two CTAs an SM
 constexpr float kRange = 28.5f;        // e^-28.5 * 2^40 rounds to 0
 constexpr float kWeightOne = 1099511627776.0f;  // 2^40
-static_assert(kBins == 2 * kSmpThreads && kList == 4 * kSmpThreads, "bins and entries a thread");
+static_assert(kBins == 2 * kSmpThreads && kList == 4 * kSmpThreads && 2 * kFine == kSmpThreads && 2 * kFew == kSmpThreads,
+              "bins and entries a thread");
 
 struct Exchange {  // what a CTA tells its cluster; two, used in turn
-  float top, low;
+  float top, low, var;
   int n;
   unsigned long long a, b, c;
 };
@@ -72,10 +75,10 @@ struct Halves {
 
 struct SmpShared {
   uint64_t list[kList];
-  union {
-    struct { uint32_t count[kBins], place[kBins], extra[kBins]; };
-    unsigned long long mass[kBins];
-  };
+  uint32_t count[kBins], place[kBins], extra[kBins];
+  unsigned long long mass[kFine];
+  uint64_t cut[kFew];
+  struct alignas(16) Pair { unsigned long long key, mass; } few[kFew];
   Exchange ex[2];
   unsigned long long warp64[kSmpWarps], above[kSmpWarps], part[3][kSmpWarps];
   int first[kSmpMaxCluster + 1];
@@ -87,7 +90,8 @@ struct SmpShared {
   uint32_t before_k;
   float mass_k, warp_var[kSmpWarps];
   unsigned long long reply;  // the leader's answer to its cluster
-  int again;
+  unsigned long long cut_key;
+  int n_cut;
 };
 
 __device__ __forceinline__ uint32_t ld_cluster32(uint32_t a) {
@@ -342,6 +346,89 @@ struct Row {
     }
     return (uint64_t)zl << 32 | il;
   }
+  // Of the up to kFew entries in sh.few and this thread's, entry `e`: how many
+  // come before it, and their mass.  Threads of one entry are neighbours, `parts`
+  // of them, and each looks at every parts-th.
+  template <typename Before>
+  __device__ void few_before(int m, int e, int parts, Before&& is_before, int* rank_of, unsigned long long* mass_of) {
+    int r = 0;
+    unsigned long long b = 0;
+    if (e - (lane / parts) < m) {
+#pragma unroll 4
+      for (int j = tid % parts; j < m; j += parts) {
+        const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(&sh.few[j]);
+        if (is_before(o.x)) { ++r; b += o.y; }
+      }
+      for (int o = parts / 2; o > 0; o >>= 1) {
+        r += __shfl_xor_sync(0xffffffffu, r, o);
+        b += __shfl_xor_sync(0xffffffffu, b, o);
+      }
+    }
+    *rank_of = r;
+    *mass_of = b;
+  }
+  // sum of one value a thread over the CTA
+  __device__ unsigned long long block_sum64(unsigned long long v) {
+    v = warp_sum64(v);
+    if (lane == 0) sh.warp64[warp] = v;
+    __syncthreads();
+    return warp_sum64(lane < kSmpWarps ? sh.warp64[lane] : 0ull);
+  }
+  // finish_list for up to kFew entries: each thread (or two, or four) compares its
+  // entry with all others, which takes fewer dependent steps than sorting.
+  __device__ void finish_few(int m, int k, bool need_p, float p, double u, int32_t* token, float* logprob) {
+    const int parts = m <= kFew / 2 ? 4 : 2, e = tid / parts;
+    const bool own = e < m && tid % parts == 0;
+    const uint64_t key = e < m ? sh.list[e] : ~0ull;
+    const float v = key_z(key);
+    const unsigned long long W = e < m ? whole(weight(v)) : 0ull;
+    if (own) sh.few[e] = {key, W};
+    __syncthreads();
+    int r;
+    unsigned long long before;
+    few_before(m, e, parts, [&](unsigned long long o) { return o < key; }, &r, &before);
+    const unsigned long long all = block_sum64(own && r < k ? W : 0ull);  // the top-k's mass
+    const double bar = (double)p * (double)all;
+    const bool kept = own && r < k && (r == 0 || (likely(v) && (!need_p || (double)before < bar)));
+    // then in index order
+    if (own) sh.few[e] = {key << 32 | key >> 32, kept ? W : 0ull};
+    __syncthreads();
+    const uint32_t index = (uint32_t)key;
+    unsigned long long upto;
+    few_before(m, e, parts, [&](unsigned long long o) { return (uint32_t)(o >> 32) < index; }, &r, &upto);
+    const unsigned long long S = block_sum64(kept ? W : 0ull);
+    const double t = u * (double)S;
+    if (kept && (double)upto <= t && (double)(upto + W) > t) {
+      *token = (int)index;
+      *logprob = -log1pf((float)(S - W) / (float)W);
+    }
+  }
+  // The cut among up to kFew entries of all CTAs (their n_cut and cut; a
+  // cluster_sync lies before this): the last whose mass before it is below the
+  // bar.  Every CTA finds it for itself.
+  __device__ uint64_t cut_few(int m, unsigned long long from, double bar) {
+    const int c = lane < size ? (int)ld_cluster32(mapa_shared(&sh.n_cut, lane)) : 0;
+    int inc = c;
+#pragma unroll
+    for (int o = 1; o < kSmpMaxCluster; o <<= 1) {
+      const int t = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += t;
+    }
+    const int exc = inc - c;
+    const int e = tid / 2;
+    int r = 0;
+#pragma unroll
+    for (int o = 0; o < kSmpMaxCluster - 1; ++o) r += e >= __shfl_sync(0xffffffffu, inc, o);
+    const int at = e - __shfl_sync(0xffffffffu, exc, r);
+    const uint64_t key = e < m ? ld_cluster64(mapa_shared(&sh.cut[at], r)) : ~0ull;
+    if (e < m && (tid & 1) == 0) sh.few[e] = {key, mass(key_z(key))};
+    __syncthreads();
+    unsigned long long before;
+    few_before(m, e, 2, [&](unsigned long long o) { return o < key; }, &r, &before);
+    if (e < m && (tid & 1) == 0 && (double)(from + before) < bar) atomicMax(&sh.cut_key, (unsigned long long)key);
+    __syncthreads();
+    return sh.cut_key;
+  }
   // Sorts the list's m entries and returns the last that a nucleus keeps, of
   // which `before` lies before the list: the last whose mass before it is below
   // the bar, or the first.
@@ -433,47 +520,48 @@ struct Row {
     __syncthreads();
     if (lane == 0) sh.warp64[warp] = own;
     __syncthreads();
-    unsigned long long before;
-    const unsigned long long mine = warps_total(sh.warp64, &before);
+    unsigned long long own_before;
+    const unsigned long long mine = warps_total(sh.warp64, &own_before);
     Exchange* e = &sh.ex[turn];
     if (tid == 0) e->a = mine;
     cluster_sync();
     const unsigned long long of = lane < size ? ld_cluster64(mapa_shared(&e->a, lane)) : 0ull;
     const unsigned long long S = warp_sum64(of);
-    before += warp_sum64(lane < rank ? of : 0ull);
+    unsigned long long before = own_before + warp_sum64(lane < rank ? of : 0ull);
     const double t = u * (double)S;
-    // the warp whose range passes the target (u < 1 keeps it below S)
-    if (own && (double)before <= t && (double)(before + own) > t) {
-#pragma unroll 1
-      for (int i0 = w0; i0 < w1; i0 += 128) {
-        unsigned long long W[4];
+    // this CTA reads no other's shared memory from here on
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    // the CTA, and in it the warp, whose range passes the target (u < 1 keeps it below S)
+    if (mine && (double)(before - own_before) <= t && (double)(before - own_before + mine) > t) {
+      if (lane == 0 && own && (double)before <= t && (double)(before + own) > t) {
+        sh.first[0] = w0;
+        sh.first[1] = w1;
+        sh.reply = before;
+      }
+      __syncthreads();
+      const int r0 = sh.first[0], r1 = sh.first[1];
+      before = sh.reply;
+      for (int i0 = r0; i0 < r1; i0 += 4 * kSmpThreads) {
+        unsigned long long W[4], all;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const int i = i0 + 32 * q + lane;
-          W[q] = i < w1 ? kept_mass(i, last) : 0ull;
+          const int i = i0 + 4 * tid + q;
+          W[q] = i < r1 ? kept_mass(i, last) : 0ull;
         }
-        const unsigned long long four = warp_sum64(W[0] + W[1] + W[2] + W[3]);
-        if ((double)(before + four) <= t) {
-          before += four;
-          continue;
-        }
+        unsigned long long upto = before + scan_before(W, &all);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const unsigned long long inc = before + warp_scan64(W[q], lane);
-          const uint32_t past = __ballot_sync(0xffffffffu, (double)inc > t);
-          if (past) {
-            if (lane == __ffs(past) - 1) {
-              *token = lo + i0 + 32 * q + lane;
-              *logprob = -log1pf((float)(S - W[q]) / (float)W[q]);
-            }
-            break;
+          const double was = (double)upto;
+          upto += W[q];
+          if (W[q] && was <= t && (double)upto > t) {
+            *token = lo + i0 + 4 * tid + q;
+            *logprob = -log1pf((float)(S - W[q]) / (float)W[q]);
           }
-          before = __shfl_sync(0xffffffffu, inc, 31);
         }
-        break;
+        before += all;
       }
     }
-    cluster_sync();  // no CTA leaves while another reads its shared memory
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   }
   __device__ bool reaches(uint64_t key, bool by_mass, double bar, uint64_t most) {
     key = key < most ? key : most;
@@ -507,6 +595,12 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
   constexpr int kPer = 16 / (int)sizeof(T);
   const int pieces = (n - head) / kPer;
 
+  const float temp = a.temperature ? a.temperature[row] : 1.0f;
+  const float p = a.top_p ? a.top_p[row] : 1.0f;
+  const float min_p = a.min_p ? fminf(a.min_p[row], 1.0f) : 0.f;
+  const float log_min_p = min_p > 0.f ? logf(min_p) : -INFINITY;
+  const double u = (double)fminf(fmaxf(a.u[row], 0.f), 0.99999994f);
+  const int k = a.top_k ? a.top_k[row] : 0;
   float top = -INFINITY;  // a NaN is no maximum
   {
     const uint4* s4 = reinterpret_cast<const uint4*>(src + head);
@@ -549,7 +643,6 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
     const float t = lane < size ? __uint_as_float(ld_cluster32(mapa_shared(&sh.ex[0].top, lane))) : -INFINITY;
     top = warp_max(t);
   }
-  const float temp = a.temperature ? a.temperature[row] : 1.0f;
   // whatever follows, the row gets an answer
   if (rank == 0 && tid == 0) {
     a.token[row] = -1;
@@ -578,11 +671,6 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
     cluster_sync();
     return;
   }
-  const float p = a.top_p ? a.top_p[row] : 1.0f;
-  const float min_p = a.min_p ? fminf(a.min_p[row], 1.0f) : 0.f;
-  const float log_min_p = min_p > 0.f ? logf(min_p) : -INFINITY;
-  const double u = (double)fminf(fmaxf(a.u[row], 0.f), 0.99999994f);
-  const int k = a.top_k ? a.top_k[row] : 0;
   bool need_k = k > 0 && k < a.vocab, need_p = p < 1.0f;
   const float inv_temp = 1.0f / temp;
   const bool tame = top < INFINITY && temp > 1e-12f && temp < 1e12f;
@@ -596,24 +684,34 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
   if (general && tame) {
     // ---- A, B: few entries can matter; a guess finds them ------------------------
     // Counted: each thread's largest entry.  Any k of them bound the k-th entry
-    // of the row from below; of the rest, entries as large as the 256th of them
-    // are few, and are counted too where top-p asks for masses, with one in eight
+    // of the row from below.  Where top-p asks for masses, each CTA also counts
+    // all its entries as large as the 32nd of its threads' (few), and one in eight
     // of the others.
-    float var = 0.f;
     const float own_place = R.place(thread_top);
     if (own_place < (float)kBins) atomicAdd(&sh.count[(int)own_place], 1u);
-    if (tid == 0) { sh.bin_k = kBins; sh.bin_p = kBins; sh.over = 0; sh.n_list = 0; }
-    cluster_sync();
-    uint32_t cnt[2] = {0, 0};
+    if (tid == 0) {
+      sh.bin_k = sh.bin_p = kBins;
+      sh.over = sh.n_list = sh.n_cut = 0;
+      sh.cut_key = 0;
+    }
+    if (tid < kFine) sh.mass[tid] = 0;
+    if (need_k) cluster_sync(); else __syncthreads();
     // this thread's two bins of all CTAs, their loads together
-    auto gather = [&](const uint32_t* of, uint32_t (&to)[2]) {
-      uint2 c[kSmpMaxCluster];
+    uint2 bins[kSmpMaxCluster];
+    auto gather = [&]() {
 #pragma unroll
-      for (int r = 0; r < kSmpMaxCluster; ++r) c[r] = r < size ? ld_cluster32x2(mapa_shared(of + 2 * tid, r)) : make_uint2(0, 0);
-#pragma unroll
-      for (int r = 0; r < kSmpMaxCluster; ++r) { to[0] += c[r].x; to[1] += c[r].y; }
+      for (int r = 0; r < kSmpMaxCluster; ++r)
+        bins[r] = r < size ? ld_cluster32x2(mapa_shared(sh.count + 2 * tid, r)) : make_uint2(0, 0);
     };
-    gather(sh.count, cnt);
+    uint32_t cnt[2] = {0, 0};
+    if (need_k) {
+      gather();
+#pragma unroll
+      for (int r = 0; r < kSmpMaxCluster; ++r) { cnt[0] += bins[r].x; cnt[1] += bins[r].y; }
+    } else {
+      cnt[0] = sh.count[2 * tid];
+      cnt[1] = sh.count[2 * tid + 1];
+    }
     // first bins up to which the counts, or the masses, reach a bar
     auto first_bin = [&](bool lo_reaches, bool hi_reaches, int* where) {
       const int at = lo_reaches ? 2 * tid : hi_reaches ? 2 * tid + 1 : kBins;
@@ -630,11 +728,10 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
       if (lane == 31) sh.warp_cnt[warp] = ci;
       __syncthreads();
       ci += __reduce_add_sync(0xffffffffu, lane < warp ? sh.warp_cnt[lane] : 0);
-      const uint32_t want = need_k ? (uint32_t)k : 256u;
+      const uint32_t want = need_k ? (uint32_t)k : (uint32_t)kSmpThreads / 16;
       first_bin(ci - cnt[1] >= want, ci >= want, &sh.bin_k);
       __syncthreads();
     }
-    float m_all = 0.f, mi = 0.f, m_last = 0.f;
     if (!need_k) {
       const float heavy = (float)min(sh.bin_k + 1, kBins);
 #pragma unroll 4
@@ -643,38 +740,48 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
         if (t >= heavy && (j & 7)) continue;
         if (t < (float)kBins) atomicAdd(t < heavy ? &sh.place[(int)t] : &sh.extra[(int)t], 1u);
       }
-      cluster_sync();
-      if (tid == 0) sh.bin_k = kBins;
-      uint32_t ex[2] = {0, 0}, smp[2] = {0, 0};
-      gather(sh.place, ex);
-      gather(sh.extra, smp);
+      __syncthreads();
       // (of each run of 8 x 512 entries the first 512 were looked at)
-      const int runs = per_cta / (8 * kSmpThreads), seen = runs * kSmpThreads + min(kSmpThreads, per_cta - runs * 8 * kSmpThreads);
-      const float step = range / (kBins * temp), each = (float)per_cta / (float)seen;
-      float ms[2];
+      const int runs = n / (8 * kSmpThreads), seen = runs * kSmpThreads + min(kSmpThreads, n - runs * 8 * kSmpThreads);
+      const float step = range / (kBins * temp), each = seen > 0 ? (float)n / (float)seen : 0.f;
+      float w[2], var = 0.f;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const float w = __expf(-(2 * tid + e + 0.5f) * step);
-        ms[e] = (ex[e] + each * smp[e]) * w;
-        var += each * each * smp[e] * w * w;
+        const int b = 2 * tid + e;
+        const float seldom = each * sh.extra[b];
+        w[e] = __expf(-(b + 0.5f) * step);
+        var += each * seldom * w[e] * w[e];
+        sh.count[b] = __float_as_uint(sh.place[b] + seldom);
       }
-      mi = ms[0] + ms[1];
-      m_last = ms[1];
+      var = warp_sum(var);
+      if (lane == 0) sh.warp_var[warp] = var;
+      __syncthreads();
+      if (warp == 0) {
+        var = warp_sum(lane < kSmpWarps ? sh.warp_var[lane] : 0.f);
+        if (lane == 0) { sh.ex[0].var = var; sh.bin_k = kBins; }
+      }
+      cluster_sync();
+      gather();
+      var = warp_sum(lane < size ? __uint_as_float(ld_cluster32(mapa_shared(&sh.ex[0].var, lane))) : 0.f);
+      float ms[2] = {0.f, 0.f};
+#pragma unroll
+      for (int r = 0; r < kSmpMaxCluster; ++r) { ms[0] += __uint_as_float(bins[r].x); ms[1] += __uint_as_float(bins[r].y); }
+      ms[0] *= w[0];
+      ms[1] *= w[1];
+      float mi = ms[0] + ms[1];
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const float tm = __shfl_up_sync(0xffffffffu, mi, o);
         if (lane >= o) mi += tm;
       }
-      var = warp_sum(var);
-      if (lane == 31) { sh.warp_mass[warp] = mi; sh.warp_var[warp] = var; }
+      if (lane == 31) sh.warp_mass[warp] = mi;
       __syncthreads();
       const float m = lane < kSmpWarps ? sh.warp_mass[lane] : 0.f;
       mi += warp_sum(lane < warp ? m : 0.f);
-      m_all = warp_sum(m);
-      var = warp_sum(lane < kSmpWarps ? sh.warp_var[lane] : 0.f);
+      const float m_all = warp_sum(m);
       const float slack = 5.f * sqrtf(var) + 0.004f * m_all, bar0 = p * m_all;
-      first_bin(mi - m_last >= bar0 - slack, mi >= bar0 - slack, &sh.bin_k);
-      first_bin(mi - m_last >= bar0 + slack, mi >= bar0 + slack, &sh.bin_p);
+      first_bin(mi - ms[1] >= bar0 - slack, mi >= bar0 - slack, &sh.bin_k);
+      first_bin(mi - ms[1] >= bar0 + slack, mi >= bar0 + slack, &sh.bin_p);
       __syncthreads();
     }
     // Top-k: places before `inner` are the candidates.  Top-p: places before
@@ -682,12 +789,9 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
     const float inner = need_k ? (float)min(sh.bin_k + 1, kBins) : (float)min(sh.bin_k, kBins - 1);
     const float outer = (float)min(sh.bin_p + 1, kBins);
     const bool guess = !need_k || sh.bin_k < kBins;
-    const float finer = kBins / (outer - inner);
-    auto fine_bin = [&](float t) { return min(kBins - 1, (int)((t - inner) * finer)); };
-    cluster_sync();  // the counts have been read: their place is taken again below
+    const float finer = kFine / (outer - inner);
+    auto fine_bin = [&](float t) { return min(kFine - 1, (int)((t - inner) * finer)); };
     if (guess && need_k) {
-      if (tid == 0) sh.n_list = 0;
-      __syncthreads();
 #pragma unroll 4
       for (int i = tid; i < n; i += kSmpThreads) {
         const float v = to_f32(buf[i]);
@@ -701,15 +805,15 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
       if (R.cluster_int(&sh.n_list) <= kList) {
         const int m = rank == 0 ? R.pull() : 0;
         cluster_sync();  // the others leave: only the leader goes on
-        if (rank == 0) R.finish_list(m, k, need_p, p, u, a.token + row, a.logprob + row);
+        if (rank == 0) {
+          if (m <= kFew) R.finish_few(m, k, need_p, p, u, a.token + row, a.logprob + row);
+          else R.finish_list(m, k, need_p, p, u, a.token + row, a.logprob + row);
+        }
         return;
       }
       cluster_sync();
     } else if (guess) {
       // the exact masses before `inner` and of all, and the entries between
-      if (tid == 0) sh.n_list = 0;
-      for (int i = tid; i < kBins; i += kSmpThreads) sh.mass[i] = 0;
-      __syncthreads();
       Halves all, sure;
       unsigned long long between = 0;
 #pragma unroll 4
@@ -738,53 +842,58 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
       bool fits = (double)v[1] < bar && (double)(v[1] + v[2]) >= bar;
       fits &= R.cluster_int(&sh.over) == 0;
       if (fits) {
-        // the fine bin that the cut falls into, exactly
-        unsigned long long f[2] = {0, 0};
+        // the fine bin that the cut falls into, exactly: two threads a bin, each for
+        // every other CTA
+        unsigned long long f = 0;
 #pragma unroll
-        for (int r = 0; r < kSmpMaxCluster; ++r)
-          if (r < size) {
-            f[0] += ld_cluster64(mapa_shared(&sh.mass[2 * tid], r));
-            f[1] += ld_cluster64(mapa_shared(&sh.mass[2 * tid + 1], r));
-          }
-        const unsigned long long inc = warp_scan64(f[0] + f[1], lane);
+        for (int r = 0; r < kSmpMaxCluster; r += 2)
+          if (r + (tid & 1) < size) f += ld_cluster64(mapa_shared(&sh.mass[tid / 2], r + (tid & 1)));
+        f += __shfl_xor_sync(0xffffffffu, f, 1);
+        const unsigned long long inc = warp_scan64((tid & 1) ? f : 0ull, lane);
         if (lane == 31) sh.warp64[warp] = inc;
         __syncthreads();
         unsigned long long before;
         R.warps_total(sh.warp64, &before);
-        before += v[1] + inc - f[0] - f[1];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          if ((double)before < bar && (double)(before + f[e]) >= bar) { sh.found = 2 * tid + e; sh.reply = before; }
-          before += f[e];
-        }
+        before += v[1] + inc - f;
+        if ((tid & 1) && (double)before < bar && (double)(before + f) >= bar) { sh.found = tid / 2; sh.reply = before; }
         __syncthreads();
         const int fine = sh.found, n_mine = sh.n_list;
         const unsigned long long m_before = sh.reply;
-        // its entries, in front of the list (each thread's own first: they move down)
         uint64_t keep[kList / kSmpThreads];
         bool in[kList / kSmpThreads];
 #pragma unroll
         for (int e = 0; e < kList / kSmpThreads; ++e) {
           const int i = e * kSmpThreads + tid;
           keep[e] = i < n_mine ? sh.list[i] : ~0ull;
-          const float t = R.place(key_z(keep[e]));
-          in[e] = i < n_mine && fine_bin(t) == fine;
-        }
-        cluster_sync();  // all have read n_list, mass and over
-        if (tid == 0) sh.n_list = 0;
-        __syncthreads();
-#pragma unroll
-        for (int e = 0; e < kList / kSmpThreads; ++e)
-          if (in[e]) sh.list[atomicAdd(&sh.n_list, 1)] = keep[e];
-        cluster_sync();
-        fits = R.cluster_int(&sh.n_list) <= kList;
-        if (fits) {
-          if (rank == 0) {
-            const uint64_t key = R.cut_list(R.pull(), m_before, bar);
-            if (tid == 0) sh.reply = key;
+          in[e] = i < n_mine && fine_bin(R.place(key_z(keep[e]))) == fine;
+          if (in[e]) {
+            const int at = atomicAdd(&sh.n_cut, 1);
+            if (at < kFew) sh.cut[at] = keep[e];
           }
+        }
+        cluster_sync();
+        const int n_cut = R.cluster_int(&sh.n_cut);
+        if (n_cut <= kFew) {
+          last = R.cut_few(n_cut, m_before, bar);
+        } else {
+          // many: in front of the list, for the leader to sort
+          if (tid == 0) sh.n_list = 0;
+          __syncthreads();
+#pragma unroll
+          for (int e = 0; e < kList / kSmpThreads; ++e)
+            if (in[e]) sh.list[atomicAdd(&sh.n_list, 1)] = keep[e];
           cluster_sync();
-          last = ld_cluster64(mapa_shared(&sh.reply, 0));
+          fits = n_cut <= kList;
+          if (fits) {
+            if (rank == 0) {
+              const uint64_t key = R.cut_list(R.pull(), m_before, bar);
+              if (tid == 0) sh.reply = key;
+            }
+            cluster_sync();
+            last = ld_cluster64(mapa_shared(&sh.reply, 0));
+          }
+        }
+        if (fits) {
           general = false;
           if (log_min_p == -INFINITY) {
             // kept: what was sure, and the entries between up to the cut
@@ -799,6 +908,8 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
         }
       }
       cluster_sync();
+    } else {
+      cluster_sync();  // the counts have been read: they are taken again below
     }
   }
   if (general) {
