@@ -64,11 +64,14 @@ struct Exchange {  // what a CTA tells its cluster; two, used in turn
 struct Halves {
   int hi = 0, lo = 0;
   static constexpr float kMagic = 12582912.0f;  // 1.5 * 2^23
-  __device__ __forceinline__ void add(float w) {
+  static __device__ __forceinline__ Halves of(float w) {
     const float a = fmaf(w, 1048576.0f, kMagic), h = a - kMagic;          // rint(w 2^20)
     const float b = fmaf(fmaf(w, 1048576.0f, -h), 1048576.0f, kMagic);    // the rest, in 2^-40
-    hi += __float_as_int(a) - 0x4B400000;
-    lo += __float_as_int(b) - 0x4B400000;
+    return {__float_as_int(a) - 0x4B400000, __float_as_int(b) - 0x4B400000};
+  }
+  __device__ __forceinline__ void add(Halves w, bool in = true) {
+    hi += in ? w.hi : 0;
+    lo += in ? w.lo : 0;
   }
   __device__ __forceinline__ unsigned long long total() const { return (unsigned long long)((long long)hi * 1048576 + lo); }
 };
@@ -85,7 +88,7 @@ struct SmpShared {
   float warp_top[kSmpWarps], warp_low[kSmpWarps];
   uint32_t warp_cnt[kSmpWarps];
   float warp_mass[kSmpWarps];
-  int n_list, found, over;
+  int n_list, found;
   int bin_k, bin_p;
   uint32_t before_k;
   float mass_k, warp_var[kSmpWarps];
@@ -678,6 +681,8 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
   Row<T> R{sh, buf, lo, n, rank, size, tid, lane, warp, 1, top, temp, inv_temp, kBins / range, range, log_min_p, tame};
 
   uint64_t last = ~0ull;  // the last entry that top-k and top-p keep
+  unsigned long long own = 0;  // the kept mass of this warp's range
+  bool summed = false;
   const int per_warp = (n + 32 * kSmpWarps - 1) / (32 * kSmpWarps) * 32;
   const int w0 = min(n, warp * per_warp), w1 = min(n, w0 + per_warp);
   bool general = need_k || need_p;
@@ -685,13 +690,13 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
     // ---- A, B: few entries can matter; a guess finds them ------------------------
     // Counted: each thread's largest entry.  Any k of them bound the k-th entry
     // of the row from below.  Where top-p asks for masses, each CTA also counts
-    // all its entries as large as the 32nd of its threads' (few), and one in eight
-    // of the others.
+    // all its entries as large as the 384th of its threads' (a few in a hundred), and
+    // one in eight of the others.
     const float own_place = R.place(thread_top);
     if (own_place < (float)kBins) atomicAdd(&sh.count[(int)own_place], 1u);
     if (tid == 0) {
       sh.bin_k = sh.bin_p = kBins;
-      sh.over = sh.n_list = sh.n_cut = 0;
+      sh.n_list = sh.n_cut = 0;
       sh.cut_key = 0;
     }
     if (tid < kFine) sh.mass[tid] = 0;
@@ -728,7 +733,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
       if (lane == 31) sh.warp_cnt[warp] = ci;
       __syncthreads();
       ci += __reduce_add_sync(0xffffffffu, lane < warp ? sh.warp_cnt[lane] : 0);
-      const uint32_t want = need_k ? (uint32_t)k : (uint32_t)kSmpThreads / 16;
+      const uint32_t want = need_k ? (uint32_t)k : (uint32_t)kSmpThreads * 3 / 4;
       first_bin(ci - cnt[1] >= want, ci >= want, &sh.bin_k);
       __syncthreads();
     }
@@ -750,7 +755,8 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
         const int b = 2 * tid + e;
         const float seldom = each * sh.extra[b];
         w[e] = __expf(-(b + 0.5f) * step);
-        var += each * seldom * w[e] * w[e];
+        // (an entry's place in its bin is unknown: a uniform one's variance is 1/12)
+        var += (each * seldom + sh.place[b] * (step * step / 12.f)) * w[e] * w[e];
         sh.count[b] = __float_as_uint(sh.place[b] + seldom);
       }
       var = warp_sum(var);
@@ -779,7 +785,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
       const float m = lane < kSmpWarps ? sh.warp_mass[lane] : 0.f;
       mi += warp_sum(lane < warp ? m : 0.f);
       const float m_all = warp_sum(m);
-      const float slack = 5.f * sqrtf(var) + 0.004f * m_all, bar0 = p * m_all;
+      const float slack = 5.f * sqrtf(var) + 0.0005f * m_all, bar0 = p * m_all;
       first_bin(mi - ms[1] >= bar0 - slack, mi >= bar0 - slack, &sh.bin_k);
       first_bin(mi - ms[1] >= bar0 + slack, mi >= bar0 + slack, &sh.bin_p);
       __syncthreads();
@@ -819,15 +825,13 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
 #pragma unroll 4
       for (int i = w0 + lane; i < w1; i += 32) {
         const float v = to_f32(buf[i]), t = R.place(v);
-        if (!(t <= (float)kBins)) continue;
-        const float w = R.weight(v);
+        const Halves w = Halves::of(t <= (float)kBins ? expf(R.expo(v)) : 0.f);
         all.add(w);
-        if (t < inner) {
-          sure.add(w);
-        } else if (t < outer) {
+        sure.add(w, t < inner);
+        if (t >= inner && t < outer) {
           const int at = atomicAdd(&sh.n_list, 1);
           if (at < kList) sh.list[at] = entry_key(v, lo + i);
-          const unsigned long long W = R.whole(w);
+          const unsigned long long W = w.total();
           between += W;
           atomicAdd(&sh.mass[fine_bin(t)], W);
         }
@@ -835,12 +839,9 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
       const unsigned long long mine = warp_sum64(sure.total());
       if (lane == 0) sh.above[warp] = mine;
       unsigned long long v[3] = {all.total(), sure.total(), between};
-      __syncthreads();
-      if (tid == 0) sh.over = sh.n_list > kList;
       R.cluster_total(v);
       const double bar = (double)p * (double)v[0];
       bool fits = (double)v[1] < bar && (double)(v[1] + v[2]) >= bar;
-      fits &= R.cluster_int(&sh.over) == 0;
       if (fits) {
         // the fine bin that the cut falls into, exactly: two threads a bin, each for
         // every other CTA
@@ -859,16 +860,26 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
         __syncthreads();
         const int fine = sh.found, n_mine = sh.n_list;
         const unsigned long long m_before = sh.reply;
+        // its entries: from the list, or, where that was too short, from all
+        const bool listed = n_mine <= kList;
         uint64_t keep[kList / kSmpThreads];
-        bool in[kList / kSmpThreads];
+        auto in_fine = [&](float t) { return t >= inner && t < outer && fine_bin(t) == fine; };
+        auto cut_add = [&](uint64_t key) {
+          const int at = atomicAdd(&sh.n_cut, 1);
+          if (at < kFew) sh.cut[at] = key;
+        };
+        if (listed) {
 #pragma unroll
-        for (int e = 0; e < kList / kSmpThreads; ++e) {
-          const int i = e * kSmpThreads + tid;
-          keep[e] = i < n_mine ? sh.list[i] : ~0ull;
-          in[e] = i < n_mine && fine_bin(R.place(key_z(keep[e]))) == fine;
-          if (in[e]) {
-            const int at = atomicAdd(&sh.n_cut, 1);
-            if (at < kFew) sh.cut[at] = keep[e];
+          for (int e = 0; e < kList / kSmpThreads; ++e) {
+            const int i = e * kSmpThreads + tid;
+            keep[e] = i < n_mine ? sh.list[i] : ~0ull;  // (no entry's key: its z is a NaN)
+            if (in_fine(R.place(key_z(keep[e])))) cut_add(keep[e]);
+          }
+        } else {
+#pragma unroll 4
+          for (int i = tid; i < n; i += kSmpThreads) {
+            const float v = to_f32(buf[i]);
+            if (in_fine(R.place(v))) cut_add(entry_key(v, lo + i));
           }
         }
         cluster_sync();
@@ -877,14 +888,21 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
           last = R.cut_few(n_cut, m_before, bar);
         } else {
           // many: in front of the list, for the leader to sort
-          if (tid == 0) sh.n_list = 0;
-          __syncthreads();
-#pragma unroll
-          for (int e = 0; e < kList / kSmpThreads; ++e)
-            if (in[e]) sh.list[atomicAdd(&sh.n_list, 1)] = keep[e];
-          cluster_sync();
           fits = n_cut <= kList;
           if (fits) {
+            if (tid == 0) sh.n_list = 0;
+            __syncthreads();
+            if (listed) {
+#pragma unroll
+              for (int e = 0; e < kList / kSmpThreads; ++e)
+                if (in_fine(R.place(key_z(keep[e])))) sh.list[atomicAdd(&sh.n_list, 1)] = keep[e];
+            } else {
+              for (int i = tid; i < n; i += kSmpThreads) {
+                const float v = to_f32(buf[i]);
+                if (in_fine(R.place(v))) sh.list[atomicAdd(&sh.n_list, 1)] = entry_key(v, lo + i);
+              }
+            }
+            cluster_sync();
             if (rank == 0) {
               const uint64_t key = R.cut_list(R.pull(), m_before, bar);
               if (tid == 0) sh.reply = key;
@@ -895,19 +913,19 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
         }
         if (fits) {
           general = false;
-          if (log_min_p == -INFINITY) {
+          if (listed && log_min_p == -INFINITY) {
             // kept: what was sure, and the entries between up to the cut
 #pragma unroll
             for (int e = 0; e < kList / kSmpThreads; ++e)
               if (e * kSmpThreads + tid < n_mine && keep[e] <= last)
                 atomicAdd(&sh.above[((int)(uint32_t)keep[e] - lo) / per_warp], R.mass(key_z(keep[e])));
             __syncthreads();
-            R.draw(w0, w1, sh.above[warp], last, u, a.token + row, a.logprob + row);
-            return;
+            own = sh.above[warp];
+            summed = true;
           }
         }
       }
-      cluster_sync();
+      if (general) cluster_sync();  // masses and counts are taken again below
     } else {
       cluster_sync();  // the counts have been read: they are taken again below
     }
@@ -1064,21 +1082,24 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
     }
   }
   // ---- the draw, in index order: warps own consecutive ranges ------------------
-  unsigned long long own = 0;
-  if (last == ~0ull && tame) {
-    Halves sum;
+  if (!summed) {
+    if (tame) {
+      const float z_last = last == ~0ull ? -INFINITY : key_z(last);
+      const int i_last = (int)(uint32_t)last - lo;
+      Halves sum;
 #pragma unroll 4
-    for (int i = w0 + lane; i < w1; i += 32) {
-      const float v = to_f32(buf[i]);
-      if (!(top - v <= R.range)) continue;
-      const float x = R.expo(v);
-      if (x >= log_min_p) sum.add(expf(x));
+      for (int i = w0 + lane; i < w1; i += 32) {
+        const float v = to_f32(buf[i]), x = R.expo(v);
+        const bool in = top - v <= R.range && x >= log_min_p && (v > z_last || (v == z_last && i <= i_last));
+        sum.add(Halves::of(in ? expf(x) : 0.f));
+      }
+      own = sum.total();
+    } else {
+      for (int i = w0 + lane; i < w1; i += 32) own += R.kept_mass(i, last);
     }
-    own = sum.total();
-  } else {
-    for (int i = w0 + lane; i < w1; i += 32) own += R.kept_mass(i, last);
+    own = warp_sum64(own);
   }
-  R.draw(w0, w1, warp_sum64(own), last, u, a.token + row, a.logprob + row);
+  R.draw(w0, w1, own, last, u, a.token + row, a.logprob + row);
 }
 
 template <typename T>
