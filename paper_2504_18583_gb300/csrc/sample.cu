@@ -46,7 +46,6 @@ constexpr int kFine = 256;             // bins of the entries that a cut may fal
 constexpr int kList = 2048;            // entries one CTA sorts
 constexpr int kFew = 256;              // up to here, each is compared with all others instead
 constexpr int kSmpMaxCluster = 8;
-constexpr int kSliceBytes = 64 * 1024; // a CTA's share of a row: two CTAs an SM
 constexpr float kRange = 28.5f;        // e^-28.5 * 2^40 rounds to 0
 constexpr float kWeightOne = 1099511627776.0f;  // 2^40
 static_assert(kBins == 2 * kSmpThreads && kList == 4 * kSmpThreads && 2 * kFine == kSmpThreads && 2 * kFew == kSmpThreads,
@@ -78,10 +77,14 @@ struct Halves {
 
 struct SmpShared {
   uint64_t list[kList];
-  uint32_t count[kBins], place[kBins], extra[kBins];
+  struct alignas(16) Pair { unsigned long long key, mass; };
+  // `few` follows after the counts' last use by any CTA
+  union {
+    struct { uint32_t count[kBins], place[kBins]; };
+    Pair few[kFew];
+  };
   unsigned long long mass[kFine];
   uint64_t cut[kFew];
-  struct alignas(16) Pair { unsigned long long key, mass; } few[kFew];
   Exchange ex[2];
   unsigned long long warp64[kSmpWarps], above[kSmpWarps], part[3][kSmpWarps];
   int first[kSmpMaxCluster + 1];
@@ -633,7 +636,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
       top = fmaxf(top, to_f32(v));
     }
   }
-  for (int i = tid; i < kBins; i += kSmpThreads) sh.count[i] = sh.place[i] = sh.extra[i] = 0;
+  for (int i = tid; i < kBins; i += kSmpThreads) sh.count[i] = sh.place[i] = 0;
   // the row's largest entry
   const float thread_top = top;
   top = warp_max(top);
@@ -743,7 +746,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
       for (int i = tid, j = 0; i < n; i += kSmpThreads, ++j) {
         const float v = to_f32(buf[i]), t = R.place(v);
         if (t >= heavy && (j & 7)) continue;
-        if (t < (float)kBins) atomicAdd(t < heavy ? &sh.place[(int)t] : &sh.extra[(int)t], 1u);
+        if (t < (float)kBins) atomicAdd(&sh.place[(int)t], t < heavy ? 1u : 0x10000u);
       }
       __syncthreads();
       // (of each run of 8 x 512 entries the first 512 were looked at)
@@ -753,11 +756,12 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int b = 2 * tid + e;
-        const float seldom = each * sh.extra[b];
+        const uint32_t both = sh.place[b];  // all counted, and one in eight: 16 bits each (a wrap spoils a guess only)
+        const float seldom = each * (both >> 16), every = both & 0xFFFF;
         w[e] = __expf(-(b + 0.5f) * step);
         // (an entry's place in its bin is unknown: a uniform one's variance is 1/12)
-        var += (each * seldom + sh.place[b] * (step * step / 12.f)) * w[e] * w[e];
-        sh.count[b] = __float_as_uint(sh.place[b] + seldom);
+        var += (each * seldom + every * (step * step / 12.f)) * w[e] * w[e];
+        sh.count[b] = __float_as_uint(every + seldom);
       }
       var = warp_sum(var);
       if (lane == 0) sh.warp_var[warp] = var;
@@ -1102,34 +1106,73 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
   R.draw(w0, w1, own, last, u, a.token + row, a.logprob + row);
 }
 
+// How many CTAs share a row.  Rows run in rounds of as many clusters as the GPU
+// holds (a cluster stays within one group of SMs, so sizes differ in what they
+// leave idle: of 128256 floats a row 36 clusters of 8 run at once, or 46 of 6), and
+// a round takes the time of a CTA's entries and of its dependent steps, which
+// cost as much as some 18000 entries.  464 such rows: 244 us with 6, 272 with 7,
+// 270 with 8; one row is fastest with 8.
+struct Shape {
+  int size, per_cta, smem;
+};
+template <typename T>
+static Shape shape_of(int rows, int vocab) {
+  constexpr int kMaxShared = 227 * 1024;
+  static const cudaError_t allowed =
+      cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxShared);
+  if (allowed != cudaSuccess) throw allowed;
+  thread_local int of_vocab = 0, active[kSmpMaxCluster + 1];  // clusters at once, of the last vocabulary
+  const bool known = of_vocab == vocab;
+  Shape best{};
+  int64_t best_cost = INT64_MAX;
+  for (int size = 1; size <= kSmpMaxCluster; ++size) {
+    if (size > 1 && vocab / size < 2048) break;  // (best holds a size: one CTA has room for 4096 entries)
+    const int per_cta = (vocab + 8 * size - 1) / (8 * size) * 8;
+    const int smem = (int)((sizeof(SmpShared) + 15) / 16 * 16 + 16 + ((size_t)per_cta * sizeof(T) + 15) / 16 * 16);
+    if (smem > kMaxShared) continue;
+    if (!known) {
+      cudaLaunchConfig_t cfg = {};
+      cfg.gridDim = dim3((unsigned)size);
+      cfg.blockDim = dim3(kSmpThreads);
+      cfg.dynamicSmemBytes = smem;
+      cudaLaunchAttribute attr[1];
+      attr[0].id = cudaLaunchAttributeClusterDimension;
+      attr[0].val.clusterDim.x = size;
+      attr[0].val.clusterDim.y = 1;
+      attr[0].val.clusterDim.z = 1;
+      cfg.attrs = attr;
+      cfg.numAttrs = 1;
+      const cudaError_t e = cudaOccupancyMaxActiveClusters(&active[size], sample_kernel<T>, &cfg);
+      if (e != cudaSuccess) throw e;
+    }
+    if (active[size] < 1) continue;
+    const int64_t cost = (int64_t)((rows + active[size] - 1) / active[size]) * (per_cta + 18000);
+    if (cost < best_cost) {
+      best_cost = cost;
+      best = {size, per_cta, smem};
+    }
+  }
+  of_vocab = vocab;
+  if (best.size == 0) throw cudaErrorInvalidConfiguration;
+  return best;
+}
+
 template <typename T>
 static void run_sample(const SampleArgs& a, cudaStream_t s) {
-  // as many CTAs a row as keep a slice within 64 KB; more where rows are few
-  const int64_t bytes = (int64_t)a.vocab * sizeof(T);
-  int size = (int)((bytes + kSliceBytes - 1) / kSliceBytes);
-  while (size < kSmpMaxCluster && a.rows * size < 152 && a.vocab / (size + 1) >= 2048) ++size;
-  if (size > kSmpMaxCluster) size = kSmpMaxCluster;
-  const int per_cta = (a.vocab + 8 * size - 1) / (8 * size) * 8;
-  const int smem = (int)((sizeof(SmpShared) + 15) / 16 * 16 + 16 + ((size_t)per_cta * sizeof(T) + 15) / 16 * 16);
-  static int configured = 0;
-  if (smem > configured) {
-    const cudaError_t e = cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e != cudaSuccess) throw e;
-    configured = smem;
-  }
+  const Shape shape = shape_of<T>(a.rows, a.vocab);
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)a.rows * size);
+  cfg.gridDim = dim3((unsigned)a.rows * shape.size);
   cfg.blockDim = dim3(kSmpThreads);
-  cfg.dynamicSmemBytes = smem;
+  cfg.dynamicSmemBytes = shape.smem;
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = size;
+  attr[0].val.clusterDim.x = shape.size;
   attr[0].val.clusterDim.y = 1;
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, sample_kernel<T>, a, per_cta);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, sample_kernel<T>, a, shape.per_cta);
   if (e != cudaSuccess) throw e;
 }
 
