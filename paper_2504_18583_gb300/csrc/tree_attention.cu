@@ -179,6 +179,18 @@ __device__ __forceinline__ void scale_row(uint32_t o_addr, float alpha) {
         : "memory");
   }
 }
+// 32 bytes of an output row: rows lie apart, so what a warp writes at once are
+// pieces of 32 rows, and whole 32-byte sectors take half the passes of 16 bytes.
+__device__ __forceinline__ void store32(void* to, const uint32_t* v, bool wide) {
+  if (wide) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(to), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
+                 "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
+  } else {
+    reinterpret_cast<uint4*>(to)[0] = make_uint4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<uint4*>(to)[1] = make_uint4(v[4], v[5], v[6], v[7]);
+  }
+}
 // Two 16-bit values with infinities and NaN replaced by zero.
 template <typename T>
 __device__ __forceinline__ uint32_t finite_of(uint32_t v) {
@@ -441,6 +453,71 @@ __device__ __noinline__ void join(const TreeAttnArgs& a, const uint16_t* slots, 
       p.x = Num<T>::pack(acc[e].x * inv, acc[e].y * inv);
       p.y = Num<T>::pack(acc[e].z * inv, acc[e].w * inv);
       if (c + e * step < n_c4) *reinterpret_cast<uint2*>(out + (c + e * step) * 4) = p;
+    }
+  }
+}
+
+// 32 columns of this row's sum, unnormalised: a group's own accumulator, or both
+// groups' (the second's only if it had a tile: it has written nothing else there).
+template <int HD, int BLOCKS>
+__device__ __forceinline__ void own_columns(uint32_t (&o)[32], uint32_t addr, float w0, float w1, bool second) {
+  tm_ld32(addr, o);
+  if (BLOCKS == 1) {
+    uint32_t o1[32];
+    tm_ld32(addr + HD, o1);
+    tm_landed<32>(o1);
+    tm_landed<32>(o);
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      o[i] = __float_as_uint((second ? __uint_as_float(o1[i]) * w1 : 0.f) + __uint_as_float(o[i]) * w0);
+  } else {
+    tm_landed<32>(o);
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store_columns(T* out, const uint32_t (&o)[32], float inv, bool wide) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    uint32_t y[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      y[e] = Num<T>::pack(__uint_as_float(o[16 * i + 2 * e]) * inv, __uint_as_float(o[16 * i + 2 * e + 1]) * inv);
+    store32(out + 16 * i, y, wide);
+  }
+}
+// Joins the other part's partial with this CTA's own, still in tensor memory,
+// with join()'s arithmetic: the first part's product, then the second's.  All
+// threads of a warp take part; 64 columns' loads go out together.
+template <typename T, int HD, int BLOCKS>
+__device__ __noinline__ void join_two(const Partial other, uint32_t addr, int g, int row, bool first, float m, float sum,
+                                      float w0, float w1, bool second, int col0, bool on, T* out, bool wide) {
+  constexpr int kCols = BLOCKS == 2 ? HD : HD / 2, kPieces = kCols < 64 ? 8 : 16;
+  fence_gpu();
+  const float2 st = *other.stats(HD, g, row);
+  float x_mine = 0.f, x_other = 0.f, inv = 0.f;
+#pragma unroll 1
+  for (int c0 = col0; c0 < col0 + kCols; c0 += 4 * kPieces) {
+    float4 v[kPieces];
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) v[i] = *other.o(c0 / 4 + i, row);
+    if (c0 == col0) {
+      const float top = fmaxf(m, st.x), base = top == -INFINITY ? 0.f : top;
+      x_mine = ex2(m - base);
+      x_other = ex2(st.x - base);
+      const float l = first ? fmaf(st.y, x_other, sum * x_mine) : fmaf(sum, x_mine, st.y * x_other);
+      inv = l > 0.f ? 1.0f / l : 0.f;
+    }
+#pragma unroll
+    for (int h = 0; h < kPieces / 8; ++h) {
+      uint32_t o[32];
+      own_columns<HD, BLOCKS>(o, addr + c0 + 32 * h, w0, w1, second);
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        const float4 q = v[8 * h + i / 4];
+        const float x = __uint_as_float(o[i]), y = i % 4 == 0 ? q.x : i % 4 == 1 ? q.y : i % 4 == 2 ? q.z : q.w;
+        o[i] = __float_as_uint(first ? fmaf(y, x_other, x * x_mine) : fmaf(x, x_mine, y * x_other));
+      }
+      if (on) store_columns(out + c0 + 32 * h, o, inv, wide);
     }
   }
 }
@@ -820,6 +897,7 @@ __global__ void __launch_bounds__(kTaThreads, 1)
     const uint32_t my = tmem + ((uint32_t)((warp & 3) * 32) << 16);
     const uint32_t s_addr = my + g * kTile, o_addr = my + 2 * kTile + g * HD;
     const float sl2 = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1e-30f);  // a masked score stays -inf at scale 0
+    const bool wide_out = (reinterpret_cast<uintptr_t>(a.out) & 31) == 0;
     uint32_t ph_s = 0, ph_o = 0, ph_pair = 0, ph_met = 0;
     auto meet = [&] {  // both groups, 256 threads
       __syncwarp();
@@ -979,75 +1057,32 @@ __global__ void __launch_bounds__(kTaThreads, 1)
       const bool whole = w.t0 == 0 && w.t1 == w.s.tiles, on = row < rows;
       // A unit's contributors are consecutive CTAs.  All but the last to arrive
       // leave their partial; that one joins them, in tile order.  Where two share
-      // a unit, the owner of its first tile looks before it leaves its own: in
-      // ranges it came to the unit last of all its work, the other has arrived as
-      // a rule, and the two are joined straight from tensor memory.
+      // a unit, the last joins the other's partial with what it still has in
+      // tensor memory; one that finds the other there already, as the owner of a
+      // unit's first tile does as a rule (in ranges it came to it last of all its
+      // work), leaves no partial of its own.
       const int count = whole ? 1 : w.count, me = w.me, c0 = w.c0;
       uint32_t* arrived = reinterpret_cast<uint32_t*>(a.workspace) + 2 * c0 + g;
       const Partial mine = slot_of(a, 2 * blockIdx.x + (w.t0 > 0 ? 0 : 1), HD, BLOCKS);
       bool two = false;
-      if (count == 2 && me == 0) {
+      if (count == 2) {
         if (t == 0) sh.last_in[g] = ld_acquire(arrived) == 1;
         group_meet();
         if (!ok) break;
         two = sh.last_in[g];
       }
-      const Partial other = slot_of(a, 2 * (c0 + 1), HD, BLOCKS);
-      float x_mine = 1.f, x_other = 0.f, inv = sum > 0.f ? 1.0f / sum : 0.f;
-      if (two) {
-        fence_gpu();
-        const float2 st = *other.stats(HD, g, in_block);
-        const float top = fmaxf(m_ref, st.x), base = top == -INFINITY ? 0.f : top;
-        x_mine = ex2(m_ref - base);
-        x_other = ex2(st.x - base);
-        const float l = fmaf(st.y, x_other, sum * x_mine);  // all as join() would
-        inv = l > 0.f ? 1.0f / l : 0.f;
-      }
-      {
-        T* out = reinterpret_cast<T*>(a.out) +
-                 (((int64_t)w.b * a.width + node) * a.n_q_heads + (int64_t)w.head * group + (row - node * group)) * HD;
+      T* out = reinterpret_cast<T*>(a.out) +
+               (((int64_t)w.b * a.width + node) * a.n_q_heads + (int64_t)w.head * group + (row - node * group)) * HD;
+      if (!two) {
+        const float inv = sum > 0.f ? 1.0f / sum : 0.f;
 #pragma unroll 1
         for (int c = col0; c < col0 + kCols; c += 32) {
-          float4 v[8];
-          if (two && on) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = *other.o(c / 4 + i, in_block);
-          }
           uint32_t o[32];
-          if (BLOCKS == 2) {
-            tm_ld32(o_addr + c, o);
-            tm_landed<32>(o);
+          own_columns<HD, BLOCKS>(o, my + 2 * kTile + (BLOCKS == 2 ? g * HD : 0) + c, w0, n > 1 ? w1 : 0.f, n > 1);
+          if (!on) continue;
+          if (whole) {
+            store_columns<T>(out + c, o, inv, wide_out);
           } else {
-            uint32_t o1[32];
-            tm_ld32(my + 2 * kTile + c, o);
-            tm_ld32(my + 2 * kTile + HD + c, o1);
-            tm_landed<32>(o);
-            tm_landed<32>(o1);
-            // a group without a tile has written nothing there
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              o[i] = __float_as_uint((n > 1 ? __uint_as_float(o1[i]) * w1 : 0.f) + __uint_as_float(o[i]) * w0);
-          }
-          if (two) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              o[4 * i] = __float_as_uint(fmaf(v[i].x, x_other, __uint_as_float(o[4 * i]) * x_mine));
-              o[4 * i + 1] = __float_as_uint(fmaf(v[i].y, x_other, __uint_as_float(o[4 * i + 1]) * x_mine));
-              o[4 * i + 2] = __float_as_uint(fmaf(v[i].z, x_other, __uint_as_float(o[4 * i + 2]) * x_mine));
-              o[4 * i + 3] = __float_as_uint(fmaf(v[i].w, x_other, __uint_as_float(o[4 * i + 3]) * x_mine));
-            }
-          }
-          if (on && (whole || two)) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              uint4 p;
-              p.x = Num<T>::pack(__uint_as_float(o[8 * i]) * inv, __uint_as_float(o[8 * i + 1]) * inv);
-              p.y = Num<T>::pack(__uint_as_float(o[8 * i + 2]) * inv, __uint_as_float(o[8 * i + 3]) * inv);
-              p.z = Num<T>::pack(__uint_as_float(o[8 * i + 4]) * inv, __uint_as_float(o[8 * i + 5]) * inv);
-              p.w = Num<T>::pack(__uint_as_float(o[8 * i + 6]) * inv, __uint_as_float(o[8 * i + 7]) * inv);
-              *reinterpret_cast<uint4*>(out + c + 8 * i) = p;
-            }
-          } else if (on) {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
               *mine.o(c / 4 + i, in_block) = make_float4(__uint_as_float(o[4 * i]), __uint_as_float(o[4 * i + 1]),
@@ -1056,30 +1091,41 @@ __global__ void __launch_bounds__(kTaThreads, 1)
         }
         if (patch && on)
           patch_row<T, HD>(a, w.b, w.head, w.s, max(w.t0 * kTile, w.s.ctx), min(w.t1 * kTile, w.s.keys), mrow, col0, kCols,
-                           whole || two ? out : nullptr, mine, in_block);
+                           whole ? out : nullptr, mine, in_block);
+        if (!whole) {
+          *mine.stats(HD, g, in_block) = make_float2(m_ref, sum);
+          // written before the group meets, read after, and written again only when
+          // all of it has been through another tile
+#pragma unroll 1
+          for (int i = t; i < count; i += kTile)
+            sh.slots[g][i] = (uint16_t)(2 * (c0 + i) + (i == 0 ? 1 : 0));
+          fence_gpu();
+          group_meet();
+          if (!ok) break;
+          if (t == 0) sh.last_in[g] = arrive_acq_rel(arrived) == (uint32_t)count - 1;
+          group_meet();
+          if (!ok) break;
+          if (sh.last_in[g]) {
+            if (count == 2) {
+              two = true;
+            } else {
+              fence_gpu();
+              T* unit = reinterpret_cast<T*>(a.out) + ((int64_t)w.b * a.width * a.n_q_heads + (int64_t)w.head * group) * HD;
+              const int live = min(kTile, rows - row_base);
+              join<T, HD, BLOCKS>(a, sh.slots[g], count, g, t, in_block - t, live, col0 / 4, kCols / 4, unit, row_base);
+              if (t == 0) *arrived = 0;  // as the next call wants it
+            }
+          }
+        }
       }
       if (two) {
-        if (t == 0) *arrived = 0;  // both have arrived: as the next call wants it
-      } else if (!whole) {
-        *mine.stats(HD, g, in_block) = make_float2(m_ref, sum);
-        // written before the group meets, read after, and written again only when
-        // all of it has been through another tile
-#pragma unroll 1
-        for (int i = t; i < count; i += kTile)
-          sh.slots[g][i] = (uint16_t)(2 * (c0 + i) + (i == 0 ? 1 : 0));
-        fence_gpu();
-        group_meet();
-        if (!ok) break;
-        if (t == 0) sh.last_in[g] = arrive_acq_rel(arrived) == (uint32_t)count - 1;
-        group_meet();
-        if (!ok) break;
-        if (sh.last_in[g]) {
-          fence_gpu();
-          if (t == 0) *arrived = 0;
-          T* unit = reinterpret_cast<T*>(a.out) + ((int64_t)w.b * a.width * a.n_q_heads + (int64_t)w.head * group) * HD;
-          const int live = min(kTile, rows - row_base);
-          join<T, HD, BLOCKS>(a, sh.slots[g], count, g, t, in_block - t, live, col0 / 4, kCols / 4, unit, row_base);
-        }
+        const Partial other = slot_of(a, 2 * (c0 + 1 - me) + me, HD, BLOCKS);
+        join_two<T, HD, BLOCKS>(other, my + 2 * kTile + (BLOCKS == 2 ? g * HD : 0), g, in_block, me == 0, m_ref, sum, w0,
+                                n > 1 ? w1 : 0.f, n > 1, col0, on, out, wide_out);
+        if (patch && on)
+          patch_row<T, HD>(a, w.b, w.head, w.s, max(w.t0 * kTile, w.s.ctx), min(w.t1 * kTile, w.s.keys), mrow, col0, kCols,
+                           out, mine, in_block);
+        if (t == 0) *arrived = 0;
       }
       if (BLOCKS == 1) {  // the queries' place holds the sums, and each group reads both accumulators
         meet();
