@@ -806,11 +806,13 @@ __global__ void __launch_bounds__(kTaThreads, 1)
           const int i = tile0 + j;
           const bool more = j + 1 < n;
           if (j >= 0) wait_v(i);
-          if (more) wait_k(i + 1);
           if (!ok) break;
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
             if (j >= 0) outputs(g, i, j == 0, keys0 - j * kTile);
+            // (asked for here, since the load of a stage that has just come free is
+            // what a step would wait for)
+            if (more && g == 0) wait_k(i + 1);
             if (!ok) break;
             if (more) scores(g, i + 1); else commit(sh.o_full + g);
           }
