@@ -52,7 +52,7 @@ static_assert(kBins == 2 * kSmpThreads && kList == 4 * kSmpThreads && 2 * kFine 
               "bins and entries a thread");
 
 struct Exchange {  // what a CTA tells its cluster; two, used in turn
-  float top, low, var;
+  float top, low;
   int n;
   unsigned long long a, b, c;
 };
@@ -178,6 +178,9 @@ struct Row {
   __device__ unsigned long long mass(float v) const { return dist(v) > range ? 0ull : whole(weight(v)); }
   // place among the bins, as a real number; more than kBins: no weight
   __device__ float place(float v) const { return (top - v) * scale; }
+
+  // what an entry of a place before p has at least, and some others have too
+  __device__ float at_least(float p) const { return __fsub_rd(top, (p + 1.f) / scale); }
 
   // a word of every CTA of the cluster, summed: a lane reads one
   __device__ int cluster_int(const int* mine) {
@@ -599,7 +602,13 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
   T* buf = reinterpret_cast<T*>(raw + shift);
   const int head = min(n, shift ? (16 - shift) / (int)sizeof(T) : 0);
   constexpr int kPer = 16 / (int)sizeof(T);
-  const int pieces = (n - head) / kPer;
+  const int pieces = (n - head) / kPer, tail = n - head - pieces * kPer;
+  auto largest = [](const T* x) {
+    float m = to_f32(x[0]);
+#pragma unroll
+    for (int e = 1; e < kPer; ++e) m = fmaxf(m, to_f32(x[e]));
+    return m;
+  };
 
   const float temp = a.temperature ? a.temperature[row] : 1.0f;
   const float p = a.top_p ? a.top_p[row] : 1.0f;
@@ -628,7 +637,6 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
         for (int j = 0; j < kPer; ++j) top = fmaxf(top, to_f32(q[j]));
       }
     }
-    const int tail = n - head - pieces * kPer;
     if (tid < head + tail) {
       const int i = tid < head ? tid : n - tail + (tid - head);
       const T v = src[i];
@@ -693,7 +701,7 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
     // ---- A, B: few entries can matter; a guess finds them ------------------------
     // Counted: each thread's largest entry.  Any k of them bound the k-th entry
     // of the row from below.  Where top-p asks for masses, each CTA also counts
-    // all its entries as large as the 384th of its threads' (a few in a hundred), and
+    // all its entries as large as the 128th of its threads' (one in a hundred or so), and
     // one in eight of the others.
     const float own_place = R.place(thread_top);
     if (own_place < (float)kBins) atomicAdd(&sh.count[(int)own_place], 1u);
@@ -736,62 +744,86 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
       if (lane == 31) sh.warp_cnt[warp] = ci;
       __syncthreads();
       ci += __reduce_add_sync(0xffffffffu, lane < warp ? sh.warp_cnt[lane] : 0);
-      const uint32_t want = need_k ? (uint32_t)k : (uint32_t)kSmpThreads * 3 / 4;
+      const uint32_t want = need_k ? (uint32_t)k : (uint32_t)kSmpThreads / 4;
       first_bin(ci - cnt[1] >= want, ci >= want, &sh.bin_k);
       __syncthreads();
     }
     if (!need_k) {
       const float heavy = (float)min(sh.bin_k + 1, kBins);
-#pragma unroll 4
-      for (int i = tid, j = 0; i < n; i += kSmpThreads, ++j) {
-        const float v = to_f32(buf[i]), t = R.place(v);
-        if (t >= heavy && (j & 7)) continue;
-        if (t < (float)kBins) atomicAdd(&sh.place[(int)t], t < heavy ? 1u : 0x10000u);
+      // (16 bytes of 512 threads a turn; a warp looks closely at every eighth of its
+      // pieces, so that what is looked at is spread over the slice, and else only at
+      // those that hold a heavy entry)
+      const int spread = pieces > 4 * kSmpThreads ? 7 : 0;
+      const float maybe = R.at_least(heavy);
+      auto counted = [&](T x, bool look) {
+        const float t = R.place(to_f32(x));
+        if (t < heavy) atomicAdd(&sh.place[(int)t], 1u);
+        else if (look && t < (float)kBins) atomicAdd(&sh.place[(int)t], 0x10000u);
+      };
+#pragma unroll 2
+      for (int at = tid, turn = warp; at < pieces; at += kSmpThreads, ++turn) {
+        const uint4 raw = reinterpret_cast<const uint4*>(buf + head)[at];
+        const T* x = reinterpret_cast<const T*>(&raw);
+        const bool look = (turn & spread) == 0;
+        if (!look && !(largest(x) >= maybe)) continue;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) counted(x[e], look);
       }
+      if (tid < head + tail) counted(buf[tid < head ? tid : n - tail + (tid - head)], true);
       __syncthreads();
-      // (of each run of 8 x 512 entries the first 512 were looked at)
-      const int runs = n / (8 * kSmpThreads), seen = runs * kSmpThreads + min(kSmpThreads, n - runs * 8 * kSmpThreads);
-      const float step = range / (kBins * temp), each = seen > 0 ? (float)n / (float)seen : 0.f;
-      float w[2], var = 0.f;
+      // (how many pieces were looked at closely, of all)
+      const int turns = pieces / kSmpThreads, rest = pieces - turns * kSmpThreads, first = 32 * (-turns & 7);
+      auto of_warp = [](int k) { return min(32, max(0, k)); };
+      const int seen = spread ? 64 * turns + of_warp(rest - first) + of_warp(rest - first - 256) : pieces;
+      const float step = range / (kBins * temp), each = seen > 0 ? (float)pieces / (float)seen : 1.f;
+      // a bin's entries as they are reckoned, and the variance of that number in
+      // units of the bin's weight (of an entry that is counted, only its place in
+      // the bin is unknown: a uniform one's variance is 1/12): 16 bits each
+      float w[2];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int b = 2 * tid + e;
         const uint32_t both = sh.place[b];  // all counted, and one in eight: 16 bits each (a wrap spoils a guess only)
         const float seldom = each * (both >> 16), every = both & 0xFFFF;
         w[e] = __expf(-(b + 0.5f) * step);
-        // (an entry's place in its bin is unknown: a uniform one's variance is 1/12)
-        var += (each * seldom + every * (step * step / 12.f)) * w[e] * w[e];
-        sh.count[b] = __float_as_uint(every + seldom);
+        sh.count[b] = __half_as_ushort(__float2half_rn(fminf(every + seldom, 65000.f))) |
+                      (__float_as_uint(each * seldom + every * (step * step / 12.f)) & 0xFFFF0000u);
       }
-      var = warp_sum(var);
-      if (lane == 0) sh.warp_var[warp] = var;
-      __syncthreads();
-      if (warp == 0) {
-        var = warp_sum(lane < kSmpWarps ? sh.warp_var[lane] : 0.f);
-        if (lane == 0) { sh.ex[0].var = var; sh.bin_k = kBins; }
-      }
+      if (tid == 0) sh.bin_k = kBins;
       cluster_sync();
       gather();
-      var = warp_sum(lane < size ? __uint_as_float(ld_cluster32(mapa_shared(&sh.ex[0].var, lane))) : 0.f);
-      float ms[2] = {0.f, 0.f};
+      float ms[2] = {0.f, 0.f}, vs[2] = {0.f, 0.f};
 #pragma unroll
-      for (int r = 0; r < kSmpMaxCluster; ++r) { ms[0] += __uint_as_float(bins[r].x); ms[1] += __uint_as_float(bins[r].y); }
-      ms[0] *= w[0];
-      ms[1] *= w[1];
-      float mi = ms[0] + ms[1];
+      for (int r = 0; r < kSmpMaxCluster; ++r) {
+        const uint32_t c[2] = {bins[r].x, bins[r].y};
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          ms[e] += __half2float(__ushort_as_half((unsigned short)(c[e] & 0xFFFF))) * w[e];
+          vs[e] += __uint_as_float(c[e] & 0xFFFF0000u) * w[e] * w[e];
+        }
+      }
+      float mi = ms[0] + ms[1], vi = vs[0] + vs[1];
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
-        const float tm = __shfl_up_sync(0xffffffffu, mi, o);
-        if (lane >= o) mi += tm;
+        const float tm = __shfl_up_sync(0xffffffffu, mi, o), tv = __shfl_up_sync(0xffffffffu, vi, o);
+        if (lane >= o) { mi += tm; vi += tv; }
       }
-      if (lane == 31) sh.warp_mass[warp] = mi;
+      if (lane == 31) { sh.warp_mass[warp] = mi; sh.warp_var[warp] = vi; }
       __syncthreads();
-      const float m = lane < kSmpWarps ? sh.warp_mass[lane] : 0.f;
+      const float m = lane < kSmpWarps ? sh.warp_mass[lane] : 0.f, v = lane < kSmpWarps ? sh.warp_var[lane] : 0.f;
       mi += warp_sum(lane < warp ? m : 0.f);
-      const float m_all = warp_sum(m);
-      const float slack = 5.f * sqrtf(var) + 0.0005f * m_all, bar0 = p * m_all;
-      first_bin(mi - ms[1] >= bar0 - slack, mi >= bar0 - slack, &sh.bin_k);
-      first_bin(mi - ms[1] >= bar0 + slack, mi >= bar0 + slack, &sh.bin_p);
+      vi += warp_sum(lane < warp ? v : 0.f);
+      const float m_all = warp_sum(m), v_all = warp_sum(v);
+      // The cut lies where what is before, less p of all, turns positive: that is
+      // (1 - p) of what is before less p of what is after, and its error is small
+      // where p is near 1, as what is after is.
+      auto past = [&](float before, float var, float sign) {
+        const float after = fmaxf(m_all - before, 0.f);
+        const float err = sqrtf((1.f - p) * (1.f - p) * var + p * p * fmaxf(v_all - var, 0.f));
+        return (1.f - p) * before - p * after >= sign * (5.f * err + 0.001f * fminf(before, after));
+      };
+      first_bin(past(mi - ms[1], vi - vs[1], -1.f), past(mi, vi, -1.f), &sh.bin_k);
+      first_bin(past(mi - ms[1], vi - vs[1], 1.f), past(mi, vi, 1.f), &sh.bin_p);
       __syncthreads();
     }
     // Top-k: places before `inner` are the candidates.  Top-p: places before
@@ -802,13 +834,25 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
     const float finer = kFine / (outer - inner);
     auto fine_bin = [&](float t) { return min(kFine - 1, (int)((t - inner) * finer)); };
     if (guess && need_k) {
-#pragma unroll 4
-      for (int i = tid; i < n; i += kSmpThreads) {
-        const float v = to_f32(buf[i]);
+      const float maybe = R.at_least(inner);
+      auto listed = [&](T x, int i) {
+        const float v = to_f32(x);
         if (R.place(v) < inner) {
           const int at = atomicAdd(&sh.n_list, 1);
           if (at < kList) sh.list[at] = entry_key(v, lo + i);
         }
+      };
+#pragma unroll 4
+      for (int at = tid; at < pieces; at += kSmpThreads) {
+        const uint4 raw = reinterpret_cast<const uint4*>(buf + head)[at];
+        const T* x = reinterpret_cast<const T*>(&raw);
+        if (!(largest(x) >= maybe)) continue;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) listed(x[e], head + at * kPer + e);
+      }
+      if (tid < head + tail) {
+        const int i = tid < head ? tid : n - tail + (tid - head);
+        listed(buf[i], i);
       }
       __syncthreads();
       cluster_sync();
