@@ -11,25 +11,33 @@
 // result, and a cut or a draw is exact for those weights (32-bit floating sums
 // over 1e5 entries move a draw's boundaries by 1e-7 each).
 //
-// What bounds it: HBM for many rows (each logit is read once and stays in
-// shared memory) and, next to it, instructions: a row of 128256 entries is 200
-// of them a lane, so a pass over all entries is kept to what it must do.  For
-// few rows, dependent steps.  A cluster of up to eight CTAs holds a row, an
-// index range each.  Nothing is sorted but the entries that a cut can depend on:
+// A cluster of up to eight CTAs holds a row, an index range each, in shared
+// memory, so each logit is read once.  Nothing is sorted or compared but the
+// entries that a cut can depend on:
 //   A  top-k: any k entries bound the k-th from below; the threads' largest
 //      entries (4096 a row) are counted into 1024 bins over max z - z, and the
 //      entries up to the k-th one's bin, a few more than k, go to one CTA, which
-//      sorts them and does the rest;
-//   B  top-p alone: the same counts, and one in eight of the other entries,
-//      guess the masses; one pass then has the exact mass of what is kept for
-//      sure and of all, and the entries between the guess's bounds by finer bins;
-//      the entries of the bin that the cut falls into are sorted;
-//   C  whatever these do not cover (more than 2048 entries to sort, ties, extreme
-//      temperatures, a guess that failed): a histogram of all entries, exact
-//      masses around the cut's bin, and, in a bin of more than 2048 entries,
-//      bisection over (z, i).
+//      does the rest: up to 256 are compared each with all others, which gives
+//      every one its place and the mass before it in one step where a sort is a
+//      chain of them; more are sorted;
+//   B  top-p alone: counts of the largest entries, and of one in eight of the
+//      others, give each bin's mass and its error; between the bins where the cut
+//      may lie by five of these errors, one pass has all entries by finer bins, and
+//      the exact masses of what is kept for sure and of all; every CTA compares the
+//      entries of the fine bin that the cut falls into;
+//   C  whatever these do not cover (ties by the thousand, extreme temperatures, a
+//      guess that failed): a histogram of all entries, exact masses around the
+//      cut's bin, and, in a bin of more than 2048 entries, bisection over (z, i).
 // The draw is a scan in index order: masses of CTAs, then of warps' ranges, then
-// of the one range that the target falls into.
+// of the entries of the one range that the target falls into.
+//
+// What bounds it.  Many rows: the latency of the steps.  464 rows of 128256
+// floats take 207 us, a sixth of HBM's rate (35 us): a top-p row 55000 clocks,
+// of which the exact pass is 10000 (40 instructions an entry), reading 6000,
+// and the rest some fifteen meetings of a CTA or the cluster; a top-k row 20000
+// and its leader 10000 more.  Two CTAs an SM overlap (issue slots 41% busy); 16
+// warps each, two slices, are what shared memory holds, and reading the row from
+// L2 in every pass instead, with four CTAs an SM, took 1081 us.  One row: 12 us.
 #include <cuda_fp16.h>
 
 #include "common.cuh"
@@ -59,7 +67,7 @@ struct Exchange {  // what a CTA tells its cluster; two, used in turn
 
 // Whole weights rint(w 2^40) summed in 32-bit halves at full rate: a sum with
 // 1.5 * 2^23 leaves a whole number in the low bits, which add as integers (a
-// lane has at most 64 weights of a row: the halves stay within 32 bits).
+// lane has at most 256 weights of a row: the halves stay within 32 bits).
 struct Halves {
   int hi = 0, lo = 0;
   static constexpr float kMagic = 12582912.0f;  // 1.5 * 2^23
