@@ -60,14 +60,18 @@ def peaks():
     return 6800.0, "fallback"
 
 
+TREE_SOURCES = {"tree.cu", "tree.h", "tree_api.cu", "tree_attention.cu", "qk_rope.cu", "sample.cu"}
+
+
 def kernel_source_hash() -> str:
-    """Hash of the CUDA sources and the C header (ties a measured traffic figure to the code it was taken on)."""
+    """Hash of the decode step's CUDA sources (ties a measured traffic figure to the code it was taken on); the tree
+    operators' own are not part of it."""
     import glob
     import hashlib
     h = hashlib.sha256()
     csrc = os.path.join(ROOT, "paper_2504_18583_gb300", "csrc")
-    files = sorted(glob.glob(os.path.join(csrc, "*.cu")) + glob.glob(os.path.join(csrc, "*.cuh")) +
-                   glob.glob(os.path.join(csrc, "*.h")) + [os.path.join(ROOT, "include", "pard.h")])
+    files = sorted(f for p in ("*.cu", "*.cuh", "*.h") for f in glob.glob(os.path.join(csrc, p))
+                   if os.path.basename(f) not in TREE_SOURCES)
     for f in files:
         h.update(os.path.basename(f).encode())
         h.update(open(f, "rb").read())
