@@ -369,6 +369,47 @@ def test_attention_cache_past_32_bit_offsets(tree):
     assert ((out[0].double() - want).abs() <= 2.0 ** -8 * (want.abs() + 2 * mag)).all()
 
 
+@pytest.mark.parametrize("dtype,hd,width", [(torch.bfloat16, 128, 5), (torch.float16, 64, 200), (torch.float16, 128, 140)])
+def test_attention_units_of_two_parts(tree, dtype, hd, width):
+    """As many units as half of the CTAs and contexts to match: two CTAs share each, and whichever is last joins them.
+    One node's values hold infinities: they reach those who see it whoever joins."""
+    edit_at = 2400 + 1
+
+    def edit(pool, table, q):
+        pool[table[0, edit_at // PAGE], 1, :, edit_at % PAGE, 7] = float("inf")
+
+    check_attention(tree, dtype, 70, 70, hd, [2400], [width], width, seed=width)
+    for _, got, want, tol, sees, v in run_attention(tree, dtype, 70, 70, hd, [2400], [width], width, seed=width, edit=edit):
+        sight = sees[:, edit_at]
+        assert torch.isposinf(got[sight][:, :, 7]).all() and torch.isfinite(got[~sight]).all()
+        cols = [c for c in range(hd) if c != 7]
+        assert ((got.double() - want).abs() <= tol)[:, :, cols].all()
+
+
+def test_attention_output_off_32_bytes(tree):
+    """An output that is 16-byte aligned and no more, through the C call; bytes around it stay as they were."""
+    from paper_2504_18583_gb300 import pard
+    lib = pard.lib()
+    B, N, Hq, Hkv, hd = 2, 6, 8, 2, 128
+    g = torch.Generator(device="cuda").manual_seed(3)
+    pool = torch.randn((12, 2, Hkv, PAGE, hd), generator=g, device="cuda").to(torch.bfloat16)
+    q = torch.randn((B, N, Hq, hd), generator=g, device="cuda").to(torch.bfloat16)
+    table, lens, nodes = dev([[0, 3, 5, 7, 9], [1, 2, 4, 6, 8]]), dev([60, 31]), dev([6, 4])
+    mask = torch.ones((B, N, 1), dtype=torch.int64, device="cuda")
+    want = tree.tree_attention(q, pool[:, 0], pool[:, 1], table, lens, nodes, mask)
+    buf = torch.full((want.numel() + 32,), 7.0, dtype=torch.bfloat16, device="cuda")
+    assert buf.data_ptr() % 32 == 0
+    size = lib.pard_tree_attention_workspace_bytes(B, N, Hq, Hkv, hd)
+    work = torch.zeros(size, dtype=torch.uint8, device="cuda")
+    ptr = lambda t: t.data_ptr()  # noqa: E731
+    status = lib.pard_tree_attention(ptr(q), Hq * hd, 0, B, N, Hq, Hkv, hd, ptr(pool), ptr(pool[:, 1]), pool.stride(0), 12,
+                                     ptr(table), 5, ptr(lens), ptr(nodes), ptr(mask), hd ** -0.5, ptr(buf) + 16, ptr(work),
+                                     size, torch.cuda.current_stream().cuda_stream)
+    assert status == 0
+    assert torch.equal(buf[8:-24].view_as(want), want)
+    assert (buf[:8] == 7).all() and (buf[-24:] == 7).all()
+
+
 def test_attention_on_another_stream(tree):
     st = torch.cuda.Stream()
     with torch.cuda.stream(st):
@@ -461,6 +502,30 @@ def test_sample_flat_and_tied_rows(tree, V):
         for k, p, m in ((0, 0.5, 0.0), (V // 3, 1.0, 0.0), (3000, 0.9, 0.0), (4000, 0.37, 0.2), (1, 0.9, 0.0), (0, 1.0, 1.0)):
             R = len(z)
             check_sample(tree, dev(z, torch.float32), rs.rand(R), np.full(R, T), np.full(R, k), np.full(R, p), np.full(R, m))
+
+
+@pytest.mark.parametrize("dtype,V", [(torch.float32, 128256), (torch.float32, 20011), (torch.bfloat16, 50257), (torch.float16, 130001)])
+def test_sample_wide_cuts_and_many_rows(tree, dtype, V):
+    """Cuts in flat, rounded, heavy-tailed and peaked rows, where thousands of entries lie near them; a row's draw
+    does not depend on how many rows there are (and with them how many CTAs share one)."""
+    rs = np.random.RandomState(V % 997)
+    g = torch.Generator().manual_seed(V)
+    rows, k, p, m, T = [], [], [], [], []
+    for kind in range(8):
+        x = torch.randn(V, generator=g)
+        z = [x * 0.05, x * 0.8, x * 3, torch.round(x * 8) / 8, torch.round(x * 2) / 64, -x.abs().pow(3), x.abs().sqrt() * 6,
+             torch.where(torch.rand(V, generator=g) < 0.001, x + 9, x)][kind]
+        for kk, pp, mm in ((0, 0.9, 0.0), (0, 0.999, 0.0), (0, 0.03, 0.0), (0, 0.97, 0.02), (257, 1.0, 0.0), (1500, 0.98, 0.0)):
+            rows.append(z)
+            k.append(kk), p.append(pp), m.append(mm), T.append(rs.uniform(0.5, 1.4))
+    z = torch.stack(rows).to(dtype).cuda()
+    u, k, p, m, T = rs.rand(len(rows)), np.array(k), np.array(p), np.array(m), np.array(T)
+    assert check_sample(tree, z, u, T, k, p, m) >= len(rows) - 4
+    f = lambda a: dev(a, torch.float32)  # noqa: E731
+    few = [tree.sample(z[i:i + 6], f(u[i:i + 6]), f(T[i:i + 6]), dev(k[i:i + 6]), f(p[i:i + 6]), f(m[i:i + 6])) for i in range(0, 48, 6)]
+    many = tree.sample(z.repeat(8, 1), f(np.tile(u, 8)), f(np.tile(T, 8)), dev(np.tile(k, 8)), f(np.tile(p, 8)), f(np.tile(m, 8)))
+    for i in range(2):
+        assert torch.equal(many[i], torch.cat([x[i] for x in few]).repeat(8))
 
 
 def test_sample_masked_and_nonfinite_rows(tree):
