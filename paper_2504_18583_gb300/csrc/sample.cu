@@ -32,12 +32,12 @@
 // of the entries of the one range that the target falls into.
 //
 // What bounds it.  Many rows: the latency of the steps.  464 rows of 128256
-// floats take 207 us, a sixth of HBM's rate (35 us): a top-p row 55000 clocks,
+// floats take 201 us, a sixth of HBM's rate (35 us): a top-p row 55000 clocks,
 // of which the exact pass is 10000 (40 instructions an entry), reading 6000,
 // and the rest some fifteen meetings of a CTA or the cluster; a top-k row 20000
 // and its leader 10000 more.  Two CTAs an SM overlap (issue slots 41% busy); 16
 // warps each, two slices, are what shared memory holds, and reading the row from
-// L2 in every pass instead, with four CTAs an SM, took 1081 us.  One row: 12 us.
+// L2 in every pass instead, with four CTAs an SM, took 1081 us.  One row: 10 us.
 #include <cuda_fp16.h>
 
 #include "common.cuh"
@@ -618,6 +618,8 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
     return m;
   };
 
+  pdl_trigger();
+  pdl_wait();
   const float temp = a.temperature ? a.temperature[row] : 1.0f;
   const float p = a.top_p ? a.top_p[row] : 1.0f;
   const float min_p = a.min_p ? fminf(a.min_p[row], 1.0f) : 0.f;
@@ -1162,8 +1164,8 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
 // holds (a cluster stays within one group of SMs, so sizes differ in what they
 // leave idle: of 128256 floats a row 36 clusters of 8 run at once, or 46 of 6), and
 // a round takes the time of a CTA's entries and of its dependent steps, which
-// cost as much as some 18000 entries.  464 such rows: 244 us with 6, 272 with 7,
-// 270 with 8; one row is fastest with 8.
+// cost as much as some 18000 entries.  464 such rows took 244 us with 6,
+// 272 with 7, 270 with 8; one row is fastest with 8.
 struct Shape {
   int size, per_cta, smem;
 };
@@ -1212,20 +1214,7 @@ static Shape shape_of(int rows, int vocab) {
 template <typename T>
 static void run_sample(const SampleArgs& a, cudaStream_t s) {
   const Shape shape = shape_of<T>(a.rows, a.vocab);
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)a.rows * shape.size);
-  cfg.blockDim = dim3(kSmpThreads);
-  cfg.dynamicSmemBytes = shape.smem;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = shape.size;
-  attr[0].val.clusterDim.y = 1;
-  attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, sample_kernel<T>, a, shape.per_cta);
-  if (e != cudaSuccess) throw e;
+  launch_in_turn(sample_kernel<T>, dim3((unsigned)a.rows * shape.size), kSmpThreads, shape.smem, shape.size, s, a, shape.per_cta);
 }
 
 void launch_sample(const SampleArgs& a, cudaStream_t s) {

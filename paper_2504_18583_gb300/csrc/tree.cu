@@ -19,6 +19,8 @@ __global__ void __launch_bounds__(kTreeMaxNodes) tree_plan_kernel(const TreePlan
   __shared__ uint64_t s_set[kTreeMaxWords][kTreeMaxNodes];
   __shared__ int s_link[kTreeMaxNodes];
   const int b = blockIdx.x, i = threadIdx.x;
+  pdl_trigger();
+  pdl_wait();
   const int n = min(max(a.n_nodes[b], 0), a.width);
   const int ctx = max(a.ctx_len[b], 0);
   const size_t at = (size_t)b * a.width + i;
@@ -61,9 +63,7 @@ __global__ void __launch_bounds__(kTreeMaxNodes) tree_plan_kernel(const TreePlan
 
 void launch_tree_plan(const TreePlanArgs& a, cudaStream_t s) {
   const int threads = (a.width + 31) / 32 * 32;
-  tree_plan_kernel<<<a.batch, threads, 0, s>>>(a);
-  const cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess) throw e;
+  launch_in_turn(tree_plan_kernel, dim3(a.batch), threads, 0, 0, s, a);
 }
 
 // Commit.  Every CTA walks its sequence's tree for itself (cheaper than a
@@ -81,6 +81,8 @@ __global__ void __launch_bounds__(kCommitThreads) tree_commit_kernel(const TreeC
   __shared__ int64_t s_src[kTreeMaxNodes], s_dst[kTreeMaxNodes];
   __shared__ int s_moves, s_count;
   const int b = blockIdx.y, tid = threadIdx.x;
+  pdl_trigger();
+  pdl_wait();
   const int n = min(max(a.n_nodes[b], 0), a.width);
   const int ctx = max(a.ctx_len[b], 0);
   const size_t at = (size_t)b * a.width;
@@ -145,9 +147,7 @@ __global__ void __launch_bounds__(kCommitThreads) tree_commit_kernel(const TreeC
 }
 
 void launch_tree_commit(const TreeCommitArgs& a, cudaStream_t s) {
-  tree_commit_kernel<<<dim3(2 * a.n_layers, a.batch), kCommitThreads, 0, s>>>(a);
-  const cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess) throw e;
+  launch_in_turn(tree_commit_kernel, dim3(2 * a.n_layers, a.batch), kCommitThreads, 0, 0, s, a);
 }
 
 }  // namespace pard

@@ -37,16 +37,16 @@
 // would reach every row otherwise).
 //
 // What bounds it, measured:
-//   8 sequences x 64 nodes at 4096, 64/8 heads of 128: 71 us; 35.7 us of products
+//   8 sequences x 64 nodes at 4096, 64/8 heads of 128: 68 us; 36 us of products
 //     at the peak.  A pair of tiles takes 3300 clocks: 2100 of products, and the
 //     chain softmax (1310) -> P V -> scores of one group, of which the issuing
 //     warp's waits and commits are 600; the tensor pipe is busy half the time.
-//   16 ragged sequences x 29 nodes, 32/8 heads of 128: 30 us; 11 us of K and V.
+//   16 ragged sequences x 29 nodes, 32/8 heads of 128: 28 us; 11 us of K and V.
 //     7000 clocks to the first instruction of a role (lengths, shares, barriers),
 //     7000 more to the first scores, then 28000 near HBM's rate, 4000 at the end.
-//   2 x 13 nodes at 65000, 32/8 heads of 64: 63 us; 35 us of K and V.  75000 of
+//   2 x 13 nodes at 65000, 32/8 heads of 64: 60 us; 35 us of K and V.  75000 of
 //     115000 clocks near HBM's rate, 14000 before, 20000 for joining ten parts.
-//   1 node at 512: 15 us, all of it dependent steps.
+//   1 node at 512: 13 us, all of it dependent steps.
 #include <cuda_fp16.h>
 
 #include <cstring>
@@ -583,6 +583,8 @@ __global__ void __launch_bounds__(kTaThreads, 1)
     fence_barrier_init();
     *abort_flag = 0;
   }
+  pdl_trigger();
+  pdl_wait();
   const uint32_t stalled = reinterpret_cast<const volatile uint32_t*>(a.workspace)[kStalledWord];
   // The share's form and, in ranges, this CTA's first place: two rounds over the
   // sequences, their sum and then the place in it; both are one round of a
@@ -1235,9 +1237,7 @@ void run_attention(const TreeAttnArgs& a, cudaStream_t s) {
   }();
   const int grid = sms < kMaxGrid ? sms : kMaxGrid;
   const CUtensorMap km = cache_map(a, a.k_cache), vm = cache_map(a, a.v_cache);
-  kernel<<<grid, kTaThreads, smem, s>>>(a, km, vm);
-  const cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess) throw e;
+  launch_in_turn(kernel, dim3(grid), kTaThreads, smem, 0, s, a, km, vm);
 }
 
 template <typename T>
