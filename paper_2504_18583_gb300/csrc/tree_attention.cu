@@ -37,16 +37,16 @@
 // would reach every row otherwise).
 //
 // What bounds it, measured:
-//   8 sequences x 64 nodes at 4096, 64/8 heads of 128: 68 us; 36 us of products
+//   8 sequences x 64 nodes at 4096, 64/8 heads of 128: 69 us; 36 us of products
 //     at the peak.  A pair of tiles takes 3300 clocks: 2100 of products, and the
 //     chain softmax (1310) -> P V -> scores of one group, of which the issuing
 //     warp's waits and commits are 600; the tensor pipe is busy half the time.
 //   16 ragged sequences x 29 nodes, 32/8 heads of 128: 28 us; 11 us of K and V.
 //     7000 clocks to the first instruction of a role (lengths, shares, barriers),
 //     7000 more to the first scores, then 28000 near HBM's rate, 4000 at the end.
-//   2 x 13 nodes at 65000, 32/8 heads of 64: 60 us; 35 us of K and V.  75000 of
-//     115000 clocks near HBM's rate, 14000 before, 20000 for joining ten parts.
-//   1 node at 512: 13 us, all of it dependent steps.
+//   2 x 13 nodes at 65000, 32/8 heads of 64: 57 us; 35 us of K and V.  70000 of
+//     110000 clocks near HBM's rate, 14000 before, 20000 for joining ten parts.
+//   1 node at 512: 12 us, all of it dependent steps.
 #include <cuda_fp16.h>
 
 #include <cstring>
@@ -612,15 +612,11 @@ __global__ void __launch_bounds__(kTaThreads, 1)
       const int most = __reduce_max_sync(0xffffffffu, cost ? s.tiles : 0);
       if (lane == 31) { sh.sum[warp] = inc; sh.units[warp] = u; sh.most[warp] = most; }
       __syncthreads();
-      int step = 0;
-#pragma unroll 1
-      for (int i = 0; i < kTaThreads / 32; ++i) {
-        if (i < warp) inc += sh.sum[i];
-        step += sh.sum[i];
-        units += sh.units[i];
-        longest = max(longest, sh.most[i]);
-      }
-      inc += run;
+      const bool is = lane < kTaThreads / 32;
+      const int of = is ? sh.sum[lane] : 0, step = __reduce_add_sync(0xffffffffu, of);
+      inc += run + __reduce_add_sync(0xffffffffu, lane < warp ? of : 0);
+      units += __reduce_add_sync(0xffffffffu, is ? sh.units[lane] : 0);
+      longest = max(longest, __reduce_max_sync(0xffffffffu, is ? sh.most[lane] : 0));
       run += step;
       if (a.batch <= kTaThreads) {
         ranges.set(run, grid);
