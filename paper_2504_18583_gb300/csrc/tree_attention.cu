@@ -254,7 +254,9 @@ __device__ __forceinline__ int parts_of(int tiles, int most) {
   // (the quotient in floating point is exact: half a unit off any whole number)
   return tiles <= most + kSplit ? 1 : (int)__fdividef((float)(tiles + most) - 0.5f, (float)most);
 }
-// Where CTA c's range begins: floor(total c / grid).
+// Where CTA c's range begins: floor(total c / grid).  With fewer places than
+// CTAs a range is one place or none, and its beginning is then also the number
+// of CTAs before c that have one.
 struct Ranges {
   int total, grid, each, rest;
   __device__ __forceinline__ void set(int n, int g) {
@@ -279,7 +281,7 @@ struct Walk {
   int at;              // place of the whole pass that off counts from
   Seq s;
   int head, block, t0, t1;
-  int count, me, c0;   // the unit's contributors, this CTA's place among them, the first of them
+  int count, me, c0;   // the unit's contributors, this CTA's place among them, the first of them (among CTAs with a place)
   __device__ __forceinline__ void load(const TreeAttnArgs& a, const int2* cache, int rows_per_block) {
     const int2 v = b < kSeqCache ? cache[b] : make_int2(a.ctx_len[b], a.n_nodes[b]);
     s = seq_of(a, v.x, v.y, rows_per_block);
@@ -312,8 +314,14 @@ struct Walk {
         while (c0 > 0 && ranges.at(c0) > u0 && Ranges::cut(ranges.at(c0) - u0, len) > 0) --c0;
         int c1 = blockIdx.x;
         while (c1 + 1 < ranges.grid && ranges.at(c1 + 1) < u0 + len && Ranges::cut(ranges.at(c1 + 1) - u0, len) < len) ++c1;
+        me = blockIdx.x;
+        if (ranges.each == 0) {  // those between them whose range is empty never arrive
+          c0 = ranges.at(c0);
+          c1 = ranges.at(c1);
+          me = ranges.at(me);
+        }
         count = c1 - c0 + 1;
-        me = (int)blockIdx.x - c0;
+        me -= c0;
       }
       return true;
     }
@@ -1079,7 +1087,7 @@ __global__ void __launch_bounds__(kTaThreads, 1)
       // work), leaves no partial of its own.
       const int count = whole ? 1 : w.count, me = w.me, c0 = w.c0;
       uint32_t* arrived = reinterpret_cast<uint32_t*>(a.workspace) + 2 * c0 + g;
-      const Partial mine = slot_of(a, 2 * blockIdx.x + (w.t0 > 0 ? 0 : 1), HD, BLOCKS);
+      const Partial mine = slot_of(a, 2 * (c0 + me) + (w.t0 > 0 ? 0 : 1), HD, BLOCKS);
       bool two = false;
       if (count == 2) {
         if (t == 0) sh.last_in[g] = ld_acquire(arrived) == 1;
