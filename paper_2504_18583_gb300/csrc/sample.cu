@@ -1117,7 +1117,8 @@ __global__ void __launch_bounds__(kSmpThreads, 2) sample_kernel(const SampleArgs
           if (b == bin_p) v[2] += W;
         }
         R.cluster_total(v);
-        bar = (double)p * (double)v[0];
+        // (a bar of 0 is reached before any entry; the largest is kept all the same)
+        bar = fmax((double)p * (double)v[0], 1.0);
         if (bin_p > 0 && (double)v[1] >= bar) --bin_p;
         else if (bin_p < kBins - 1 && (double)(v[1] + v[2]) < bar) ++bin_p;
         else break;

@@ -1,10 +1,11 @@
 """Edges of the tree operators that a wrong share, cut or rounding would show at:
 against the 64-bit forms of test_gpu_tree.py, with its tolerances where no other
 is derived here."""
+import numpy as np
 import pytest
 import torch
 
-from test_gpu_tree import check_attention, tree  # noqa: F401  (tree: the module's fixture)
+from test_gpu_tree import check_attention, check_sample, tree  # noqa: F401  (tree: the module's fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -35,3 +36,22 @@ def test_attention_large_batch_mostly_idle(tree, batch, Hkv, active):  # noqa: F
     for seed in (1, 2):
         check_attention(given, torch.bfloat16, 4 * Hkv, Hkv, 64, lens, nodes, 5, seed=seed)
         check_attention(given, torch.bfloat16, 4 * Hkv, Hkv, 64, [3000, 40], [5, 4], 5, seed=seed)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("k,m", [(0, 0.0), (3500, 0.0), (0, 1.0)])
+def test_sample_empty_nucleus_among_ties(tree, dtype, k, m):  # noqa: F811
+    """top_p = 0 (or below) where thousands of entries tie at the maximum and the lowest indices are not among
+    them: the first of the tied is kept, alone."""
+    V = 5003
+    z = torch.zeros((5, V))
+    z[0, 0] = float("-inf")
+    z[1, :700] = -4.0
+    z[2, :1500] = float("nan")
+    z[3, :2000], z[3, 4000:] = -1e30, 3.0
+    z[4, 1:3000] = 7.5
+    R = len(z)
+    for p in (0.0, -1.0, 1e-30):
+        for T in (1.0, 1e-20):
+            full = lambda v: np.full(R, v)  # noqa: E731
+            assert check_sample(tree, z.to(dtype).cuda(), np.linspace(0, 0.99, R), full(T), full(k), full(p), full(m)) == R
