@@ -28,7 +28,11 @@
 // by more than 2^8 since the last time.  Probabilities are rounded to the
 // cache's 16-bit type for the second product, which takes 16-bit operands; their
 // sum is taken before that, in 32 bits.  (Against 64 bits the output's error is
-// 1.2 to 1.45 times that of 32-bit probabilities rounded once at the end.)
+// 1.2 to 1.45 times that of 32-bit probabilities rounded once at the end.)  fp16
+// has few exponents: its probabilities are held times 2^7, sums and outputs with
+// them, so that one is rounded to its 11 bits down to 2^-21 of the largest and
+// to a multiple of 2^-31 below that.  (Times 1 a long context's many small ones
+// lost up to all of their part: those 18 nats below a single key vanished.)
 //
 // Masks touch only tiles that reach past the context: a row's 256 mask bits
 // select among its scores.  Values there may hold anything: what lies past the
@@ -78,6 +82,7 @@ template <typename T> struct Num;
 template <> struct Num<__nv_bfloat16> {
   static constexpr uint32_t kFormat = 1;        // of the instruction descriptor
   static constexpr uint32_t kExponent = 0x7F80; // all ones: infinity or NaN
+  static constexpr float kRaise = 0.f;          // probabilities are held times 2^kRaise
   static __device__ __forceinline__ uint32_t pack(float x, float y) {
     __nv_bfloat162 p = __floats2bfloat162_rn(x, y);
     return *reinterpret_cast<uint32_t*>(&p);
@@ -87,6 +92,7 @@ template <> struct Num<__nv_bfloat16> {
 template <> struct Num<__half> {
   static constexpr uint32_t kFormat = 0;
   static constexpr uint32_t kExponent = 0x7C00;
+  static constexpr float kRaise = 7.f;          // times 2^kLazy still below 65504
   static __device__ __forceinline__ uint32_t pack(float x, float y) {
     __half2 p = __floats2half2_rn(x, y);
     return *reinterpret_cast<uint32_t*>(&p);
@@ -1018,7 +1024,8 @@ __global__ void __launch_bounds__(kTaThreads, 1)
 #pragma unroll
         for (int i = 0; i < kTile; i += 2)
           mx[i >> 1 & 3] = fmaxf(fmaxf(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), mx[i >> 1 & 3]);
-        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * sl2;
+        // what probabilities are taken against: 2^kRaise below the largest
+        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * sl2 - Num<T>::kRaise;
         if (j == j0) {
           m_ref = top;
         } else if (__any_sync(0xffffffffu, top > m_ref + kLazy)) {

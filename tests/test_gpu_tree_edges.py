@@ -5,7 +5,8 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_tree import check_attention, check_sample, tree  # noqa: F401  (tree: the module's fixture)
+from test_gpu_tree import (PAGE, ROUND, attention_reference, check_attention, check_sample, dev, mask_of,  # noqa: F401
+                           tree)
 
 pytestmark = pytest.mark.gpu
 
@@ -55,3 +56,41 @@ def test_sample_empty_nucleus_among_ties(tree, dtype, k, m):  # noqa: F811
         for T in (1.0, 1e-20):
             full = lambda v: np.full(R, v)  # noqa: E731
             assert check_sample(tree, z.to(dtype).cuda(), np.linspace(0, 0.99, R), full(T), full(k), full(p), full(m)) == R
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("Hq,Hkv,hd,nodes", [(8, 8, 128, 3), (8, 8, 64, 140)])
+@pytest.mark.parametrize("hot", [0, 200, 639])
+def test_attention_small_weights_add_up(tree, dtype, Hq, Hkv, hd, nodes, hot):  # noqa: F811
+    """One key stands 5 to 20 nats above hundreds of others, and only the others' values are not zero: they share
+    a mean, so that what is lost of each weight adds up.
+
+    A weight is rounded to the type as 2^7 times its ratio to the largest so far: u of itself, or, among fp16's
+    subnormals, 2^-25, which is 2^-32 of the largest's.  On top of u |o| + 2 u sum w |v| (test_gpu_tree.py) the
+    output may then be off by 2^-32 sum |v|; bf16 has no subnormals there.  Scores of up to 20 are 32-bit sums of
+    exact products: a weight's relative error of 20 * 2^-22 is far below u."""
+    g = torch.Generator().manual_seed(hot + nodes)
+    L = 640
+    pages = -(-(L + nodes) // PAGE)
+    k = torch.zeros((pages * PAGE, Hkv, hd))
+    k[hot, :, 0] = 1.0
+    v = 1024.0 * (1.0 + 0.25 * torch.rand((pages * PAGE, Hkv, hd), generator=g))
+    v[hot] = 0.0
+    q = torch.zeros((1, nodes, Hq, hd))
+    nats = torch.tensor([5.0, 5.5, 10.0, 14.0, 17.0, 18.0, 19.0, 20.0])
+    q[0, :, :, 0] = nats[:Hq] * hd ** 0.5
+    q, k, v = q.to(dtype), k.to(dtype), v.to(dtype)
+    paged = lambda x: x.view(pages, PAGE, Hkv, hd).transpose(1, 2).contiguous().cuda()  # noqa: E731
+    mask = mask_of([[-1] + [0] * (nodes - 1)], [nodes], nodes)
+    got = tree.tree_attention(q.cuda(), paged(k), paged(v), dev([list(range(pages))]), dev([L]), dev([nodes]),
+                              torch.from_numpy(mask.view(np.int64)).cuda()).cpu()[0]
+    sees = torch.ones((nodes, L + nodes), dtype=torch.bool)
+    for i in range(nodes):
+        for j in range(nodes):
+            sees[i, L + j] = bool(int(mask[0, i, j // 64]) >> (j % 64) & 1)
+    want, mag = attention_reference(q[0], k[:L + nodes], v[:L + nodes], sees, hd ** -0.5)
+    tol = ROUND[dtype] * (want.abs() + 2 * mag)
+    if dtype == torch.float16:
+        tol = tol + 2.0 ** -32 * v[:L + nodes].double().abs().sum(0).amax() + 2.0 ** -24
+    err = (got.double() - want).abs()
+    assert (err <= tol).all(), float((err / tol).max())
