@@ -60,6 +60,7 @@
 
 #include "common.cuh"
 #include "tree.h"
+#include "warp_wait.cuh"
 
 namespace pard {
 
@@ -221,18 +222,6 @@ __device__ __forceinline__ uint32_t finite_of(uint32_t v) {
   if ((v >> 16 & e) == e) v &= 0x0000FFFFu;
   return v;
 }
-// A bounded wait that all lanes of a warp leave with the same answer.  (Counted
-// and not timed: the loop is inlined some twenty times, and what a CTA runs once
-// it waits for, instruction by instruction.  Each try suspends the warp for a
-// while by itself.)
-constexpr int kTries = 1 << 22;
-__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort) {
-  bool done = mbar_try_wait(bar, parity);
-#pragma unroll 1
-  for (int i = 0; !done && i < kTries && !*abort; ++i) done = mbar_try_wait(bar, parity);
-  return __all_sync(0xffffffffu, done);
-}
-
 // Keys, tiles and row blocks of a sequence.
 struct Seq {
   int ctx, nodes, keys, plain, tiles, blocks;  // plain: keys that every node sees
