@@ -186,11 +186,16 @@ PyObject* qk_norm_rope(PyObject* const* a, Py_ssize_t n) {
 }
 
 // what attention calls without a workspace of their own use, one after the other on a stream
-at::Tensor& shared_workspace(const Where& w, int64_t bytes) {
+at::Tensor& workspace_of(int dev, void* stream) {
   static auto* all = new std::map<std::pair<int, void*>, at::Tensor>;  // never torn down: CUDA may be gone before it
-  at::Tensor& t = (*all)[{w.dev, w.stream}];
-  if (!t.defined() || t.numel() < bytes) t = at::zeros({bytes}, w.options(at::kByte));
-  return t;
+  return (*all)[{dev, stream}];
+}
+PyObject* shared_workspace(PyObject* const*, Py_ssize_t n) {
+  count_is(n, 0);
+  const auto dev = c10::cuda::current_device();
+  const at::Tensor& t = workspace_of(dev, c10::cuda::getCurrentCUDAStream(dev).stream());
+  if (!t.defined()) Py_RETURN_NONE;
+  return wrap(t);
 }
 
 PyObject* tree_attention(PyObject* const* a, Py_ssize_t n) {
@@ -226,7 +231,9 @@ PyObject* tree_attention(PyObject* const* a, Py_ssize_t n) {
   } else if (capturing) {  // a graph may run beside later calls: its calls have their own
     workspace = at::zeros({std::max<int64_t>(need, 16)}, w.options(at::kByte));
   } else {
-    workspace = shared_workspace(w, std::max<int64_t>(need, 16));
+    at::Tensor& shared = workspace_of(w.dev, w.stream);
+    if (!shared.defined() || shared.numel() < need) shared = at::zeros({std::max<int64_t>(need, 16)}, w.options(at::kByte));
+    workspace = shared;
   }
   done(pard_tree_attention(q.data_ptr(), node, code, B, N, Hq, Hkv, hd, kc.data_ptr(), vc.data_ptr(), stride, kc.size(0),
                            d_table, P, d_ctx, d_nodes, reinterpret_cast<const uint64_t*>(d_mask), (float)scale,
@@ -297,6 +304,7 @@ PyMethodDef method(const char* name) {
 PyMethodDef g_methods[] = {method<tree_plan>("tree_plan"),
                            method<qk_norm_rope>("qk_norm_rope"),
                            method<tree_attention>("tree_attention"),
+                           method<shared_workspace>("shared_workspace"),
                            method<sample>("sample"),
                            method<tree_commit>("tree_commit"),
                            {"set_error", set_error, METH_O, nullptr},

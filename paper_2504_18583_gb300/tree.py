@@ -116,6 +116,15 @@ def tree_attention_workspace(batch: int, width: int, n_q_heads: int, n_kv_heads:
     return torch.zeros(n, dtype=torch.uint8, device=device)
 
 
+def shared_workspace():
+    """The workspace that tree_attention calls without one use on the current stream; None before the first.
+
+    Should a wait inside the kernel ever run out (2 s), that call's output is NaN, and so is that of every later call
+    with the same workspace.  Once the cause is gone, ``shared_workspace().zero_()`` makes it fit for use again (a
+    call that a CUDA graph captured has a workspace of its own, which each replay zeroes)."""
+    return _ops.shared_workspace()
+
+
 def tree_attention(q, k_cache, v_cache, page_table, ctx_len, n_nodes, mask, scale: Optional[float] = None, out=None,
                    workspace=None):
     """Attention of tree nodes over the paged cache and their ancestors
@@ -125,7 +134,7 @@ def tree_attention(q, k_cache, v_cache, page_table, ctx_len, n_nodes, mask, scal
     projection do); caches [pages, Hkv, 16, hd]; page_table [B, P], ctx_len [B],
     n_nodes [B] int32; mask [B, N, ceil(N / 64)] int64 of tree_plan; scale:
     1 / sqrt(hd) unless given; workspace: of tree_attention_workspace (without
-    one, calls share one a stream).  Returns [B, N, Hq, hd]."""
+    one, calls share one a stream: shared_workspace).  Returns [B, N, Hq, hd]."""
     return _ops.tree_attention(q, k_cache, v_cache, page_table, ctx_len, n_nodes, mask, scale, out, workspace,
                                workspace is None and torch.cuda.is_current_stream_capturing())
 

@@ -5,8 +5,8 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_tree import (PAGE, ROUND, attention_reference, check_attention, check_sample, dev, mask_of,  # noqa: F401
-                           tree)
+from test_gpu_tree import (PAGE, ROUND, attention_reference, build_case, check_attention,  # noqa: F401
+                           check_sample, dev, mask_of, tree)
 
 pytestmark = pytest.mark.gpu
 
@@ -94,3 +94,32 @@ def test_attention_small_weights_add_up(tree, dtype, Hq, Hkv, hd, nodes, hot):  
         tol = tol + 2.0 ** -32 * v[:L + nodes].double().abs().sum(0).amax() + 2.0 ** -24
     err = (got.double() - want).abs()
     assert (err <= tol).all(), float((err / tol).max())
+
+
+@pytest.mark.parametrize("shared", [True, False])
+@pytest.mark.parametrize("dtype,hd,lens,nodes,width", [
+    (torch.bfloat16, 128, [2000, 77], [4, 5], 5),       # parts of units
+    (torch.float16, 64, [300, 0, 9], [70, 64, 1], 70),  # two blocks of query vectors
+    (torch.bfloat16, 64, [3000] + [7] * 69, [3] * 70, 4),  # ranges over many sequences
+])
+def test_attention_after_a_wait_ran_out(tree, shared, dtype, hd, lens, nodes, width):  # noqa: F811
+    """The mark that a wait leaves in the workspace when it runs out, set by hand: every used node is NaN, call after
+    call, and right again once the workspace has been zeroed."""
+    B, Hq, Hkv = len(lens), 8, 4
+    rs, g = np.random.RandomState(B), torch.Generator(device="cuda").manual_seed(B)
+    parents, table, n_pages = build_case(rs, lens, nodes, width)
+    mask = torch.from_numpy(mask_of(parents, nodes, width).view(np.int64)).cuda()
+    kv = torch.randn((2, n_pages, Hkv, PAGE, hd), generator=g, device="cuda").to(dtype)
+    q = torch.randn((B, width, Hq, hd), generator=g, device="cuda").to(dtype)
+    workspace = None if shared else tree.tree_attention_workspace(B, width, Hq, Hkv, hd)
+    call = lambda: tree.tree_attention(q, kv[0], kv[1], dev(table), dev(lens), dev(nodes), mask, workspace=workspace)  # noqa: E731
+    want = call()
+    used = torch.arange(width, device="cuda")[None] < dev(nodes)[:, None]
+    assert torch.isfinite(want).all() and (want[used] != 0).any(-1).all()
+    area = tree.shared_workspace() if shared else workspace
+    area.view(torch.int32)[320] = 1  # behind two counts for each of up to 160 CTAs
+    for _ in range(2):
+        got = call()
+        assert torch.isnan(got[used]).all() and (got[~used] == 0).all()
+    area.zero_()
+    assert torch.equal(call(), want)
