@@ -60,7 +60,8 @@ def peaks():
     return 6800.0, "fallback"
 
 
-TREE_SOURCES = {"tree.cu", "tree.h", "tree_api.cu", "tree_attention.cu", "qk_rope.cu", "sample.cu", "warp_wait.cuh"}
+TREE_SOURCES = {"tree.cu", "tree.h", "tree_api.cu", "tree_attention.cu", "qk_rope.cu", "sample.cu", "warp_wait.cuh",
+                "per_device.h"}
 
 
 def kernel_source_hash() -> str:

@@ -41,6 +41,7 @@
 #include <cuda_fp16.h>
 
 #include "common.cuh"
+#include "per_device.h"
 #include "tree.h"
 
 namespace pard {
@@ -1173,11 +1174,13 @@ struct Shape {
 template <typename T>
 static Shape shape_of(int rows, int vocab) {
   constexpr int kMaxShared = 227 * 1024;
-  static const cudaError_t allowed =
-      cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxShared);
-  if (allowed != cudaSuccess) throw allowed;
-  thread_local int of_vocab = 0, active[kSmpMaxCluster + 1];  // clusters at once, of the last vocabulary
-  const bool known = of_vocab == vocab;
+  static OncePerDevice allowed;
+  const int dev = current_device();
+  allowed.get(dev, [] { return allow_shared(sample_kernel<T>, kMaxShared); });
+  // clusters at once, of the last device and vocabulary
+  thread_local int of_dev = -1, of_vocab = 0, active[kSmpMaxCluster + 1];
+  const bool known = of_dev == dev && of_vocab == vocab;
+  if (!known) of_vocab = 0;  // until all of them are
   Shape best{};
   int64_t best_cost = INT64_MAX;
   for (int size = 1; size <= kSmpMaxCluster; ++size) {
@@ -1207,6 +1210,7 @@ static Shape shape_of(int rows, int vocab) {
       best = {size, per_cta, smem};
     }
   }
+  of_dev = dev;
   of_vocab = vocab;
   if (best.size == 0) throw cudaErrorInvalidConfiguration;
   return best;

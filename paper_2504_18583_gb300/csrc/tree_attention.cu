@@ -59,6 +59,7 @@
 #include <cudaTypedefs.h>
 
 #include "common.cuh"
+#include "per_device.h"
 #include "tree.h"
 #include "warp_wait.cuh"
 
@@ -1228,13 +1229,14 @@ template <typename T, int HD, int BLOCKS>
 void run_attention(const TreeAttnArgs& a, cudaStream_t s) {
   constexpr int smem = smem_bytes<HD, BLOCKS>();
   auto* kernel = tree_attention_kernel<T, HD, BLOCKS>;
-  static const cudaError_t configured = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-  if (configured != cudaSuccess) throw configured;
-  static const int sms = [] {
-    int dev = 0, n = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) n = 1;
+  static OncePerDevice ctas;
+  const int dev = current_device(), sms = ctas.get(dev, [&] {
+    allow_shared(kernel, smem);
+    int n = 0;
+    const cudaError_t e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess) throw e;
     return n;
-  }();
+  });
   const int grid = sms < kMaxGrid ? sms : kMaxGrid;
   const CUtensorMap km = cache_map(a, a.k_cache), vm = cache_map(a, a.v_cache);
   launch_in_turn(kernel, dim3(grid), kTaThreads, smem, 0, s, a, km, vm);
