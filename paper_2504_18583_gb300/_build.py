@@ -3,14 +3,17 @@ that calls its tree operators on torch tensors.
 
 Translation units are compiled in parallel and linked into
 ``paper_2504_18583_gb300/libpard.so``; ``csrc/torch_binding.cpp`` becomes
-``_tree_ops*.so`` beside it, compiled by the host compiler against the running
-torch.  A rebuild happens only when a source or header is newer than they are.
+``_tree_ops*.so`` beside it, compiled by the host compiler against the installed
+torch; without torch only the library is built, which needs none.  A rebuild
+happens when a source or header is newer than they are, or torch is another one.
 """
 from __future__ import annotations
 
 import concurrent.futures as cf
 import fcntl
 import glob
+import importlib.metadata
+import importlib.util
 import os
 import shutil
 import subprocess
@@ -23,6 +26,7 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libpard.so")
 BINDING_SRC = os.path.join(CSRC, "torch_binding.cpp")
 BINDING = os.path.join(PKG, "_tree_ops" + sysconfig.get_config_var("EXT_SUFFIX"))
+BINDING_TORCH = os.path.join(BUILD, "torch_binding.torch")  # which torch it was compiled against
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr",
@@ -49,10 +53,28 @@ def _deps():
         glob.glob(os.path.join(ROOT, "include", "*.h")) + [BINDING_SRC, os.path.abspath(__file__)]
 
 
+def installed_torch():
+    """Version and place of the torch that this Python would import, or None; torch is not imported for it."""
+    spec = importlib.util.find_spec("torch")
+    if spec is None:
+        return None
+    try:
+        version = importlib.metadata.version("torch")
+    except importlib.metadata.PackageNotFoundError:
+        version = "unknown"
+    return f"{version} {spec.origin}"
+
+
 def up_to_date() -> bool:
-    if not (os.path.exists(LIB) and os.path.exists(BINDING)):
+    made = [LIB]
+    torch = installed_torch()
+    if torch is not None:
+        made.append(BINDING)
+        if not os.path.exists(BINDING_TORCH) or open(BINDING_TORCH).read() != torch:
+            return False
+    if not all(os.path.exists(p) for p in made):
         return False
-    t = min(os.path.getmtime(LIB), os.path.getmtime(BINDING))
+    t = min(os.path.getmtime(p) for p in made)
     return all(os.path.getmtime(p) <= t for p in _deps())
 
 
@@ -86,10 +108,10 @@ def _compile_and_link(verbose: bool, extra_flags) -> str:
             print(r.stdout, r.stderr)
         return obj
 
+    torch = installed_torch()
     with cf.ThreadPoolExecutor(max_workers=min(12, os.cpu_count() or 4)) as ex:
-        binding = ex.submit(_compile_binding)
+        binding = ex.submit(_compile_binding) if torch is not None else None
         objs = list(ex.map(compile_one, _sources()))
-        binding_obj = binding.result()
     tmp = LIB + ".tmp"
     r = subprocess.run([cc, *ARCH, "-shared", "-o", tmp, *objs, "-lcuda"], capture_output=True, text=True)
     if r.returncode != 0:
@@ -100,7 +122,10 @@ def _compile_and_link(verbose: bool, extra_flags) -> str:
         if r.returncode != 0:
             raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
     os.replace(tmp, LIB)
-    _link_binding(binding_obj)
+    if binding is not None:  # (the library is there whatever becomes of it)
+        _link_binding(binding.result())
+        with open(BINDING_TORCH, "w") as f:
+            f.write(torch)
     return LIB
 
 
