@@ -49,7 +49,7 @@ def tree_plan(parents, n_nodes, ctx_len, page_table, n_pages: int):
 
 
 def rope_frequencies(rot_dim: int, theta: float = 10000.0, scaling: Optional[str] = None, factor: float = 1.0,
-                     original_len: int = 8192, low: float = 1.0, high: float = 4.0,
+                     original_len: int = 8192, low: float = 1.0, high: Optional[float] = None,
                      device="cuda") -> Tuple[torch.Tensor, float]:
     """inv_freq [rot_dim / 2] (fp32, radians a position) and the amplitude of
     qk_norm_rope, for positions stretched by ``factor`` past ``original_len``:
@@ -60,11 +60,13 @@ def rope_frequencies(rot_dim: int, theta: float = 10000.0, scaling: Optional[str
                 frequency is divided by the factor, the highest kept
     "parts"     frequencies that turn fewer than ``low`` times over
                 original_len divided by the factor, more than ``high`` times
-                kept, linear in the turns between
+                (4 unless given) kept, linear in the turns between
     "yarn"      the same with the ramp linear in the pair's index between
-                those of ``high`` and ``low`` turns (32 and 1 as a rule), and the
+                those of ``high`` (32 unless given) and ``low`` turns, and the
                 amplitude 0.1 ln(factor) + 1
     """
+    if high is None:
+        high = 32.0 if scaling == "yarn" else 4.0
     if rot_dim < 2 or rot_dim % 2:
         raise ValueError("rot_dim must be even and positive")
     if not (factor >= 1.0 and theta > 1.0 and original_len > 0):
