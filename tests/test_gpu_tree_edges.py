@@ -1,12 +1,16 @@
 """Edges of the tree operators that a wrong share, cut or rounding would show at:
 against the 64-bit forms of test_gpu_tree.py, with its tolerances where no other
 is derived here."""
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
 
+from conftest import ROOT
 from test_gpu_tree import (PAGE, ROUND, attention_reference, build_case, check_attention,  # noqa: F401
-                           check_sample, dev, mask_of, tree)
+                           check_sample, dev, mask_of, rope_reference, tree)
 
 pytestmark = pytest.mark.gpu
 
@@ -123,3 +127,79 @@ def test_attention_after_a_wait_ran_out(tree, shared, dtype, hd, lens, nodes, wi
         assert torch.isnan(got[used]).all() and (got[~used] == 0).all()
     area.zero_()
     assert torch.equal(call(), want)
+
+
+@pytest.mark.parametrize("batch,most", [(385, 90), (1000, 20)])
+def test_attention_more_sequences_than_threads(tree, batch, most):  # noqa: F811
+    """The shares of more sequences than a CTA has threads are worked out in several steps, two rounds of them."""
+    rs = np.random.RandomState(batch)
+    lens, nodes = [int(x) for x in rs.randint(0, most, batch)], [int(x) for x in rs.randint(0, 5, batch)]
+    lens[batch - 1], nodes[batch - 1] = 2000, 4
+    check_attention(tree, torch.bfloat16, 4, 2, 64, lens, nodes, 4, seed=batch)
+
+
+FIRST_CALLS = """
+import sys
+import torch
+sys.path.insert(0, sys.argv[1])
+from paper_2504_18583_gb300 import tree
+g = torch.Generator(device="cuda").manual_seed(1)
+z, u = torch.randn((3, 50000), generator=g, device="cuda"), torch.rand(3, generator=g, device="cuda")
+q = torch.randn((1, 5, 8, 64), generator=g, device="cuda").bfloat16()
+kv = torch.randn((2, 4, 2, 16, 64), generator=g, device="cuda").bfloat16()
+i32 = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")
+table, ctx, nodes, mask = i32([[2, 0, 1, 3]]), i32([40]), i32([5]), torch.full((1, 5, 1), 31, device="cuda")
+top_p = torch.full((3,), 0.9, device="cuda")
+step = lambda: tree.sample(z, u, top_p=top_p) + (tree.tree_attention(q, kv[0], kv[1], table, ctx, nodes, mask),)
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    outs = step()
+for _ in range(2):
+    for x in outs:
+        x.zero_()
+    graph.replay()
+    assert all(torch.equal(x, y) for x, y in zip(outs, step()))
+print("same")
+"""
+
+
+def test_first_calls_of_a_process_inside_a_capture():
+    """What a launch sets and asks once a device, it may do while a stream is being captured."""
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS, ROOT], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.strip() == "same", r.stdout + r.stderr
+
+
+def test_rotation_and_commit_past_32_bit_offsets(tree):  # noqa: F811
+    """Pages that lie 1.5 GB apart: entry offsets pass 2^31 at the fourth page."""
+    Hq, Hkv, hd, stride = 4, 2, 64, 768 * 1024 * 1024
+    page = Hkv * PAGE * hd
+    buf = torch.empty(3 * stride + 2 * page, dtype=torch.bfloat16, device="cuda")
+    pool = buf.as_strided((1, 2, 4, Hkv, PAGE, hd), (8 * stride, page, stride, PAGE * hd, hd, 1))
+    g = torch.Generator().manual_seed(4)
+    start = torch.randn((1, 2, 4, Hkv, PAGE, hd), generator=g).to(torch.bfloat16)
+    pool.copy_(start)
+    # rows for every slot of the last page, and a few elsewhere
+    slots = torch.tensor([3 * PAGE + i for i in range(PAGE)] + [5, 2 * PAGE + 1])
+    T = len(slots)
+    qkv = torch.randn((T, (Hq + 2 * Hkv) * hd), generator=g).to(torch.bfloat16)
+    pos = torch.arange(T) + 7
+    freq, _ = tree.rope_frequencies(hd)
+    tree.qk_norm_rope(qkv.cuda(), Hq, Hkv, pos.to(torch.int32).cuda(), slots.cuda(), pool[0, 0], pool[0, 1], freq)
+    x = qkv.view(T, -1, hd)
+    keys = rope_reference(x[:, Hq:Hq + Hkv], None, 0.0, pos, freq.cpu(), hd, False, 1.0)
+    got, want = pool.cpu(), start.clone()
+    at = (slots // PAGE, slice(None), slots % PAGE)
+    assert ((got[0, 0][at].double() - keys).abs() <= ROUND[torch.bfloat16] * keys.abs() + 2.0 ** -18 * keys.abs().amax(-1, keepdim=True)).all()
+    want[0, 0][at], want[0, 1][at] = got[0, 0][at], x[:, Hq + Hkv:]
+    assert torch.equal(got, want)
+    # a path over the boundary between the second page of the table and the far one
+    parents, tokens, sampled = [[-1, 0, 0, 2, 3, 3, 5]], [[0, 9, 1, 2, 9, 3, 4]], [[1, 0, 2, 3, 0, 4, 8]]
+    table, ctx = [[1, 3, 0]], 14
+    acc, emitted, new = tree.tree_commit(dev(sampled), dev(tokens), dev(parents), dev([7]), dev([ctx]), dev(table), pool)
+    assert acc.tolist() == [4] and emitted.tolist() == [[1, 2, 3, 4, 8, -1, -1]] and new.tolist() == [ctx + 5]
+    where = lambda i: (table[0][(ctx + i) // PAGE], (ctx + i) % PAGE)  # noqa: E731
+    for j, i in enumerate([0, 2, 3, 5, 6]):
+        (p, o), (sp, so) = where(j), where(i)
+        want[:, :, p, :, o] = want[:, :, sp, :, so].clone()
+    assert torch.equal(pool.cpu(), want)
