@@ -65,14 +65,14 @@ TREE_SOURCES = {"tree.cu", "tree.h", "tree_api.cu", "tree_attention.cu", "qk_rop
 
 
 def kernel_source_hash() -> str:
-    """Hash of the decode step's CUDA sources (ties a measured traffic figure to the code it was taken on); the tree
-    operators' own are not part of it."""
+    """Hash of the decode step's CUDA sources and the C header that they include (ties a measured traffic figure to the
+    code it was taken on); the tree operators' own are not part of it."""
     import glob
     import hashlib
     h = hashlib.sha256()
     csrc = os.path.join(ROOT, "paper_2504_18583_gb300", "csrc")
     files = sorted(f for p in ("*.cu", "*.cuh", "*.h") for f in glob.glob(os.path.join(csrc, p))
-                   if os.path.basename(f) not in TREE_SOURCES)
+                   if os.path.basename(f) not in TREE_SOURCES) + [os.path.join(ROOT, "include", "pard.h")]
     for f in files:
         h.update(os.path.basename(f).encode())
         h.update(open(f, "rb").read())
