@@ -32,7 +32,7 @@
 // of the entries of the one range that the target falls into.
 //
 // What bounds it.  Many rows: the latency of the steps.  464 rows of 128256
-// floats take 201 us, a sixth of HBM's rate (35 us): a top-p row 55000 clocks,
+// floats take 201 to 210 us, a sixth of HBM's rate (35 us): a top-p row 55000 clocks,
 // of which the exact pass is 10000 (40 instructions an entry), reading 6000,
 // and the rest some fifteen meetings of a CTA or the cluster; a top-k row 20000
 // and its leader 10000 more.  Two CTAs an SM overlap (issue slots 41% busy); 16

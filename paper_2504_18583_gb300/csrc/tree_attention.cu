@@ -42,14 +42,17 @@
 //
 // What bounds it, measured:
 //   8 sequences x 64 nodes at 4096, 64/8 heads of 128: 69 us; 36 us of products
-//     at the peak.  A pair of tiles takes 3300 clocks: 2100 of products, and the
-//     chain softmax (1310) -> P V -> scores of one group, of which the issuing
-//     warp's waits and commits are 600; the tensor pipe is busy half the time.
+//     at the peak.  Its 128 units stay whole, so 24 of 152 CTAs have no part.  A
+//     pair of tiles takes 3300 clocks: 2100 of products, and the chain softmax
+//     (1310) -> P V -> scores of one group, of which the issuing warp's waits and
+//     commits are 600; the tensor pipe is busy half the time of the other 128.
 //   16 ragged sequences x 29 nodes, 32/8 heads of 128: 28 us; 11 us of K and V.
 //     7000 clocks to the first instruction of a role (lengths, shares, barriers),
-//     7000 more to the first scores, then 28000 near HBM's rate, 4000 at the end.
-//   2 x 13 nodes at 65000, 32/8 heads of 64: 57 us; 35 us of K and V.  70000 of
-//     110000 clocks near HBM's rate, 14000 before, 20000 for joining ten parts.
+//     7000 more to the first scores, then up to 28000 of tiles (144 parts, the
+//     longest of 14 tiles where the mean is 7), 5000 at the end.
+//   2 x 13 nodes at 65000, 32/8 heads of 64: 57 us; 35 us of K and V.  72000 of
+//     110000 clocks near HBM's rate, 15000 before, 6500 to write a part and 9000
+//     to 12000 for the last to join ten or eleven.
 //   1 node at 512: 12 us, all of it dependent steps.
 #include <cuda_fp16.h>
 

@@ -18,10 +18,10 @@ __device__ __forceinline__ bool mbar_try_wait_at(uint32_t bar, uint32_t parity) 
 }
 
 // What a wait does once its first try has failed: tries until kWaitLimitNs have
-// passed or *abort is raised.  One copy for all places that wait: inlined into
-// the twenty of the tree attention, the timed loop took registers from the
-// softmax (65000-token contexts 56.8 -> 60.2 us), and what a CTA runs once comes
-// from L2 instruction by instruction.
+// passed or *abort is raised.  One copy for all places that wait, since what a CTA
+// runs once comes from L2 instruction by instruction: with the timed loop inlined
+// into its twenty, the tree attention of 65000-token contexts took 60.2 us instead
+// of 56.8.
 static __device__ __noinline__ bool keep_waiting(uint32_t bar, uint32_t parity, volatile int* abort) {
   const unsigned long long t0 = globaltimer();
   bool done;

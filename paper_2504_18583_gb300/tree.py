@@ -136,7 +136,9 @@ def tree_attention(q, k_cache, v_cache, page_table, ctx_len, n_nodes, mask, scal
     projection do); caches [pages, Hkv, 16, hd]; page_table [B, P], ctx_len [B],
     n_nodes [B] int32; mask [B, N, ceil(N / 64)] int64 of tree_plan; scale:
     1 / sqrt(hd) unless given; workspace: of tree_attention_workspace (without
-    one, calls share one a stream: shared_workspace).  Returns [B, N, Hq, hd]."""
+    one, calls share one a stream: shared_workspace; a call that a CUDA graph
+    captures gets its own, which each replay zeroes, 11 to 43 MB: one that is
+    given saves that).  Returns [B, N, Hq, hd]."""
     return _ops.tree_attention(q, k_cache, v_cache, page_table, ctx_len, n_nodes, mask, scale, out, workspace,
                                workspace is None and torch.cuda.is_current_stream_capturing())
 
