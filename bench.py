@@ -61,7 +61,9 @@ def peaks():
 
 
 TREE_SOURCES = {"tree.cu", "tree.h", "tree_api.cu", "tree_attention.cu", "qk_rope.cu", "sample.cu", "warp_wait.cuh",
-                "per_device.h"}
+                "per_device.h", "attn_tc.cuh", "chunk_attention.cu", "chunk_attention.cuh",
+                "chunk_attention_8bit.cu", "adjust_logits.cu", "serve.h", "serve_api.cu",
+                "api_checks.h"}
 
 
 def kernel_source_hash() -> str:

@@ -1,0 +1,1158 @@
+// Attention of a chunk of new tokens a sequence over the paged cache:
+//   o_i = sum_j softmax_j(s q_i . k_j) v_j    over j <= p_i, and, with a window w,
+//                                             p_i - j < w or j < sinks
+// p_i = ctx + i the token's position; its own keys are in the cache already.
+// Both products on tcgen05 with the accumulators in tensor memory, one pass over
+// the keys with a running maximum and sum.
+//
+// A unit is a block of up to 128 or 256 consecutive query vectors (tokens x the
+// query heads that share a key/value head) of one sequence and the tiles of 128
+// keys that any of its rows sees: those of the first tokens that stay visible,
+// then those from the first row's window to the last row's position.  All units'
+// tiles in order (sequence, head, block) are cut into one even range a CTA, or,
+// where there are no more units than CTAs and a block a sequence, each CTA takes
+// one equal part of one unit.  CTAs work that out from the sequences' lengths,
+// which the host need not know.  How units are cut, parts joined and workspaces
+// kept is as in tree_attention.cu.
+//
+// Roles: warp 0 loads keys, warp 2 values, warp 1 issues the products, warp 3
+// looks after values that not every row sees; two warpgroups take the softmax, a
+// thread a row.  Work goes in steps of 64 keys, half a tile: each group has two
+// score buffers of 64 columns beside its accumulator, and the scores of its step
+// after the next are asked for as soon as a buffer's probabilities have been
+// multiplied.  So a group always has a step to work on while the products of the
+// one before run, and the tensor cores one to multiply.  With more than 128 query
+// vectors each group has its own 128 of them and takes both halves of a tile,
+// else both have the same rows and a half each (their sums are joined at the end).
+//
+// Masks touch only tiles that some row does not see whole: a row sees a run of
+// columns up to its own position, less those between the first tokens and its
+// window.  There values may hold anything: what lies past the block's last
+// position is zeroed in shared memory, and so are infinities and NaN of keys that
+// not every row sees, which the epilogue adds back for the rows that do.
+//
+// An 8-bit cache (e4m3 codes, a power of two a token and head) is loaded as it
+// lies, half of a stage, and four more warps turn it into the 16-bit operand in
+// place, a page at a time: codes and powers of two make 16-bit entries without a
+// rounding (fp16: down to 2^-24, and up to 65504), so everything behind them is
+// as for a 16-bit cache.
+// (A header, since 16-bit and 8-bit caches are compiled apart: a function that is
+// not inlined is given the registers of the kernels that call it, and those have 168
+// and 128.)
+#pragma once
+
+#include "attn_tc.cuh"
+#include "serve.h"
+
+namespace pard {
+
+namespace {
+
+constexpr int kSeqHeld = 64;                    // sequences whose lengths a CTA keeps at hand
+constexpr int kStep = kTile / 2;                // keys of a step
+constexpr int kConvWarps = 4;                   // warps that convert an 8-bit cache's tiles
+
+__host__ __device__ constexpr int chunk_threads(bool q8) { return q8 ? 384 + 32 * kConvWarps : 384; }
+// tiles of keys, and of values, in flight: what shared memory holds beside the queries
+__host__ __device__ constexpr int ck_stages(int hd, int blocks, bool q8) {
+  return hd == 128 ? (blocks == 1 ? 3 : 2) : (blocks == 1 ? 6 : 5);
+}
+__host__ __device__ constexpr int cv_stages(int hd, int blocks, bool q8) {
+  return hd == 128 ? (q8 ? 2 : 3) : (blocks == 1 ? 6 : 5);
+}
+
+// A sequence of the batch.
+struct Chunk {
+  int ctx, n, row0, keys, rows, blocks;  // keys: that the page table has room for; rows: query vectors a key/value head
+};
+__device__ __forceinline__ Chunk chunk_of(const ChunkAttnArgs& a, int ctx, int from, int to, int rows_per_block) {
+  Chunk s;
+  s.row0 = min(max(from, 0), a.n_tokens);
+  s.n = max(min(max(to, 0), a.n_tokens) - s.row0, 0);
+  s.ctx = min(max(ctx, 0), 1 << 30);
+  const int64_t end = (int64_t)s.ctx + s.n, most = (int64_t)a.max_pages * kPageTok;
+  s.keys = (int)(end < most ? end : most);
+  s.rows = s.n * (a.n_q_heads / a.n_kv_heads);
+  s.blocks = (s.rows + rows_per_block - 1) / rows_per_block;
+  return s;
+}
+// One block's positions and tiles: tiles [0, sink) then [sink + skip, sink + skip + tiles - sink).
+struct Span {
+  int p_lo, p_hi, end;    // first and last row's positions; keys that the last row may see
+  int sink, skip, tiles;
+  __device__ __forceinline__ int tile(int k) const { return k < sink ? k : k + skip; }
+};
+__device__ __forceinline__ int window_from(const ChunkAttnArgs& a, int p) { return a.window ? max(0, p - a.window + 1) : 0; }
+__device__ __forceinline__ Span span_of(const ChunkAttnArgs& a, const Chunk& s, int block, int rows_per_block) {
+  Span g;
+  const int group = a.n_q_heads / a.n_kv_heads, r0 = block * rows_per_block;
+  g.p_lo = s.ctx + r0 / group;
+  g.p_hi = s.ctx + (min(r0 + rows_per_block, s.rows) - 1) / group;
+  g.end = min(g.p_hi + 1, s.keys);
+  const int last = (g.end + kTile - 1) / kTile;  // tiles up to the end (one at least: a table has a page)
+  const int first = min(window_from(a, g.p_lo) / kTile, last - 1);
+  g.sink = min((min(a.sinks, g.end) + kTile - 1) / kTile, first);
+  g.skip = first - g.sink;
+  g.tiles = last - g.skip;
+  if (g.skip == 0) g.sink = 0;
+  return g;
+}
+// every row of the positions [lo, hi] sees these keys
+__device__ __forceinline__ bool all_see(const ChunkAttnArgs& a, const Chunk& s, int lo, int hi, int key0, int key1) {
+  return key1 <= min(lo + 1, s.keys) && (window_from(a, hi) <= key0 || key1 <= a.sinks);
+}
+
+// A warp's walk over its CTA's share: one segment (part of a unit) after the
+// other, in shared memory.
+struct ChunkWalk {
+  int left;            // places to go; in the one-part form 1, then 0
+  int b, off;          // sequence, and place within the unit
+  int at;              // place of the whole pass where the unit begins
+  Chunk s;
+  Span g;
+  int head, block, t0, t1;
+  int count, me, c0;   // the unit's contributors, this CTA's place among them, the first of them (among CTAs with a place)
+  __device__ __forceinline__ void load(const ChunkAttnArgs& a, const int2* held, int rows_per_block) {
+    if (b < kSeqHeld) s = chunk_of(a, held[b].x, held[b].y, held[b + 1].y, rows_per_block);
+    else s = chunk_of(a, a.ctx_len[b], a.starts[b], a.starts[b + 1], rows_per_block);
+  }
+  __device__ __noinline__ bool next(const ChunkAttnArgs& a, const int2* held, int rows_per_block, const Ranges& ranges,
+                                    bool one_part) {
+    if (one_part) return left-- > 0;
+    while (left > 0) {
+      const int len = g.tiles + kStart;
+      if (off >= len) {  // the next unit
+        at += len;
+        off = 0;
+        if (++block >= s.blocks) {
+          block = 0;
+          if (++head >= a.n_kv_heads) {
+            head = 0;
+            do {
+              if (++b >= a.batch) return false;
+              load(a, held, rows_per_block);
+            } while (s.blocks == 0);
+          }
+        }
+        g = span_of(a, s, block, rows_per_block);
+        continue;
+      }
+      const int x0 = Ranges::cut(off, len), x1 = off + left < len ? Ranges::cut(off + left, len) : len;
+      const int step = min(len - off, left);
+      off += step;
+      left -= step;
+      t0 = max(0, x0 - kStart);
+      t1 = x1 - kStart;
+      if (t1 <= t0) continue;
+      count = 1;
+      me = 0;
+      c0 = blockIdx.x;
+      if (t0 > 0 || t1 < g.tiles) {  // who else has a part of it
+        while (c0 > 0 && ranges.at(c0) > at && Ranges::cut(ranges.at(c0) - at, len) > 0) --c0;
+        int c1 = blockIdx.x;
+        while (c1 + 1 < ranges.grid && ranges.at(c1 + 1) < at + len && Ranges::cut(ranges.at(c1 + 1) - at, len) < len) ++c1;
+        me = blockIdx.x;
+        if (ranges.each == 0) {  // those between them whose range is empty never arrive
+          c0 = ranges.at(c0);
+          c1 = ranges.at(c1);
+          me = ranges.at(me);
+        }
+        count = c1 - c0 + 1;
+        me -= c0;
+      }
+      return true;
+    }
+    return false;
+  }
+};
+
+// The lowest n of 32 bits.
+__device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1u; }
+// 32 columns, the first of them key `key`, that a row sees: up to `end`, from `from` on or before `sinks`.
+__device__ __forceinline__ uint32_t seen32(int key, int end, int from, int sinks) {
+  return low_bits(end - key) & (~low_bits(from - key) | low_bits(sinks - key));
+}
+
+// A value's entry, of a 16-bit cache or an 8-bit one.
+template <typename T, int HD, bool Q8>
+__device__ __forceinline__ float value_at(const ChunkAttnArgs& a, int64_t page, int head, int tok, int c) {
+  if (!Q8)
+    return Num<T>::get(reinterpret_cast<const T*>(a.v_cache) + page * a.page_stride + ((int64_t)head * kPageTok + tok) * HD + c);
+  const uint32_t code = reinterpret_cast<const uint8_t*>(a.v_cache)[page * a.page_stride + ((int64_t)head * kPageTok + tok) * HD + c];
+  const uint32_t e = a.v_scale[page * a.scale_stride + (int64_t)head * kPageTok + tok];
+  if ((code & 0x7F) == 0x7F || e == 255u) return __int_as_float(0x7FFFFFFF);
+  const int ex = code >> 3 & 15, m = code & 7;
+  float x = ldexpf(ex ? (float)(8 + m) : (float)m, max(ex, 1) - 10 + (int)e - 127);
+  if (Num<T>::kFormat == 0) x = fminf(x, 65504.f);  // fp16: held there, as the product's operand is
+  const uint32_t y = Num<T>::pack(code & 0x80 ? -x : x, 0.f);
+  const uint16_t z = (uint16_t)y;
+  return Num<T>::get(&z);
+}
+
+// Adds the infinities and NaN of the values of a part's tiles that not every row
+// of the block sees back to a row that sees them: to the output, or to a partial.
+template <typename T, int HD, bool Q8>
+__device__ __noinline__ void patch_chunk(const ChunkAttnArgs& a, const ChunkWalk& w, int p, int col0, int cols, T* out,
+                                         Partial part, int row) {
+  const int end = min(p + 1, w.s.keys), from = window_from(a, p);
+  for (int k = w.t0; k < w.t1; ++k) {
+    const int k0 = w.g.tile(k) * kTile;
+    if (all_see(a, w.s, w.g.p_lo, w.g.p_hi, k0, k0 + kTile)) continue;
+    for (int pos = k0; pos < min(k0 + kTile, end); ++pos) {
+      if ((pos < from && pos >= a.sinks) || all_see(a, w.s, w.g.p_lo, w.g.p_hi, pos, pos + 1)) continue;
+      const int page = page_of(a.page_table + (size_t)w.b * a.max_pages, pos, a.max_pages, a.n_pages);
+      if (page < 0) continue;
+#pragma unroll 1
+      for (int c = col0; c < col0 + cols; ++c) {
+        const float x = value_at<T, HD, Q8>(a, page, w.head, pos % kPageTok, c);
+        if (fabsf(x) < INFINITY) continue;
+        if (out) {
+          const uint32_t y = Num<T>::pack(Num<T>::get(out + c) + x, 0.f);
+          *reinterpret_cast<uint16_t*>(out + c) = (uint16_t)y;
+        } else {
+          reinterpret_cast<float*>(part.o(c / 4, row))[c % 4] += x;
+        }
+      }
+    }
+  }
+}
+
+// ---- 8-bit entries into 16-bit ones -------------------------------------------
+// What multiplies a row's codes: a power of two in steps that stay in range.
+template <typename T> struct Widen;
+template <> struct Widen<__nv_bfloat16> {
+  // A code's bits moved into a bf16's are the value times 2^-120, subnormal codes
+  // too; two factors bring it back, the second 1 but for rows above 448 * 2^7.
+  uint32_t m1, m2;
+  bool far;
+  __device__ __forceinline__ void set(uint32_t e) {
+    const uint32_t x = e == 255u ? 0x7FFFu : (min(e, 134u) + 120u) << 7, y = e > 134u && e != 255u ? (e - 7u) << 7 : 0x3F80u;
+    m1 = x | x << 16;
+    m2 = y | y << 16;
+    far = e > 134u;
+  }
+  static __device__ __forceinline__ uint32_t mul(uint32_t x, uint32_t y) {
+    const __nv_bfloat162 p = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&x), *reinterpret_cast<const __nv_bfloat162*>(&y));
+    return *reinterpret_cast<const uint32_t*>(&p);
+  }
+  static __device__ __forceinline__ uint32_t move(uint32_t x) { return (x & 0x80008000u) | (x >> 4 & 0x07F007F0u); }
+  // four codes
+  __device__ __forceinline__ void four(uint32_t w, uint32_t& lo, uint32_t& hi) const {
+    lo = mul(move(__byte_perm(w, 0, 0x1404)), m1);
+    hi = mul(move(__byte_perm(w, 0, 0x3424)), m1);
+  }
+  __device__ __forceinline__ void four_far(uint32_t w, uint32_t& lo, uint32_t& hi) const {
+    four(w, lo, hi);
+    lo = mul(lo, m2);
+    hi = mul(hi, m2);
+    // codes that are NaN
+    if ((w & 0x7Fu) == 0x7Fu) lo |= 0x7FFFu;
+    if ((w >> 8 & 0x7Fu) == 0x7Fu) lo |= 0x7FFF0000u;
+    if ((w >> 16 & 0x7Fu) == 0x7Fu) hi |= 0x7FFFu;
+    if ((w >> 24 & 0x7Fu) == 0x7Fu) hi |= 0x7FFF0000u;
+  }
+  static __device__ __forceinline__ uint32_t odd(uint32_t w) { return ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }
+};
+template <> struct Widen<__half> {
+  // Codes are fp16 values; the factor is one where no product leaves the normal
+  // range, else the product is taken in 32 bits and held to 65504.
+  uint32_t m1;
+  float s;
+  bool far;
+  __device__ __forceinline__ void set(uint32_t e) {
+    far = e < 113u || e > 134u;
+    const uint32_t x = (min(max(e, 113u), 134u) - 112u) << 10;
+    m1 = x | x << 16;
+    s = e == 255u ? __int_as_float(0x7FFFFFFF) : __uint_as_float(e ? e << 23 : 1u << 22);
+  }
+  static __device__ __forceinline__ uint32_t codes(uint32_t two) {
+    uint32_t v;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(v) : "h"((uint16_t)two));
+    return v;
+  }
+  static __device__ __forceinline__ uint32_t mul(uint32_t x, uint32_t y) {
+    const __half2 p = __hmul2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&y));
+    return *reinterpret_cast<const uint32_t*>(&p);
+  }
+  __device__ __forceinline__ void four(uint32_t w, uint32_t& lo, uint32_t& hi) const {
+    lo = mul(codes(w), m1);
+    hi = mul(codes(w >> 16), m1);
+  }
+  __device__ __forceinline__ uint32_t wide(uint32_t two) const {
+    const uint32_t h = codes(two);
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
+    auto held = [&](float x) { x *= s; return x > 65504.f ? 65504.f : x < -65504.f ? -65504.f : x; };  // (NaN stays)
+    return Num<__half>::pack(held(f.x), held(f.y));
+  }
+  __device__ __forceinline__ void four_far(uint32_t w, uint32_t& lo, uint32_t& hi) const {
+    lo = wide(w);
+    hi = wide(w >> 16);
+  }
+  static __device__ __forceinline__ uint32_t odd(uint32_t) { return 0u; }  // the conversion knows NaN
+};
+
+// What a CTA keeps in shared memory behind the operands.
+template <int NK, int NV, bool Q8>
+struct ChunkControl {
+  uint64_t k_full[NK], k_empty[NK], v_full[NV], v_empty[NV];
+  uint64_t k_fit[NK], fixed[NV];  // a stage's keys (8-bit caches), values are fit for the product
+  uint64_t s_full[2][2];   // scores of a group are in one of its buffers
+  uint64_t p_full[2][2];   // their probabilities are, and O is scaled
+  uint64_t o_full[2][2];   // the product with a buffer's probabilities is done
+  uint64_t ready[2];       // the group has read O and laid out its queries
+  uint64_t pair, met[2];   // the two groups meet, a group's warps do
+  uint64_t drain;          // every product is done
+  alignas(16) uint8_t k_scale[Q8 ? NK * kTile : 16], v_scale[Q8 ? NV * kTile : 16];
+  int2 seq[kSeqHeld + 1];  // sequences' context lengths and first rows
+  uint32_t tmem, last_in[2], odd[NV];  // odd: a stage's values that not all rows see held infinities or NaN (a byte a warp)
+  int abort_flag, start_b, start_head, start_block, start_off;
+  int sum[16], units[16], most[16];
+  ChunkWalk walk[Q8 ? 16 : 12];
+  uint16_t slots[2][kMaxGrid];
+};
+template <int HD, int BLOCKS, bool Q8>
+constexpr int chunk_smem() {
+  return (BLOCKS + ck_stages(HD, BLOCKS, Q8) + cv_stages(HD, BLOCKS, Q8)) * stage_bytes(HD) +
+         (int)sizeof(ChunkControl<ck_stages(HD, BLOCKS, Q8), cv_stages(HD, BLOCKS, Q8), Q8>);
+}
+static_assert(chunk_smem<128, 1, false>() <= 227 * 1024 && chunk_smem<128, 2, false>() <= 227 * 1024, "shared memory of one CTA");
+static_assert(chunk_smem<64, 1, false>() <= 227 * 1024 && chunk_smem<64, 2, false>() <= 227 * 1024, "shared memory of one CTA");
+static_assert(chunk_smem<128, 1, true>() <= 227 * 1024 && chunk_smem<128, 2, true>() <= 227 * 1024, "shared memory of one CTA");
+static_assert(chunk_smem<64, 1, true>() <= 227 * 1024 && chunk_smem<64, 2, true>() <= 227 * 1024, "shared memory of one CTA");
+
+}  // namespace
+
+template <typename T, int HD, int BLOCKS, bool Q8>
+__global__ void __launch_bounds__(chunk_threads(Q8), 1)
+    chunk_attention_kernel(const __grid_constant__ ChunkAttnArgs a, const __grid_constant__ CUtensorMap kmap,
+                           const __grid_constant__ CUtensorMap vmap) {
+  constexpr int NK = ck_stages(HD, BLOCKS, Q8), NV = cv_stages(HD, BLOCKS, Q8), kStage = stage_bytes(HD);
+  constexpr int kChunks = HD / 64, kChunkBytes = kTile * 128, kRows = kTile * BLOCKS, kThreads = chunk_threads(Q8);
+  constexpr uint32_t kIdescS = idesc16(Num<T>::kFormat, kTile, kStep, false);
+  constexpr uint32_t kIdescO = idesc16(Num<T>::kFormat, kTile, HD, true);
+  extern __shared__ __align__(1024) uint8_t qbuf[];  // queries, then the rings
+  uint8_t* kring = qbuf + BLOCKS * kStage;
+  uint8_t* vring = kring + NK * kStage;
+  using Control = ChunkControl<NK, NV, Q8>;
+  Control& sh = *reinterpret_cast<Control*>(vring + NV * kStage);
+  volatile int* abort_flag = &sh.abort_flag;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int group = a.n_q_heads / a.n_kv_heads, grid = gridDim.x;
+
+  // ---- this CTA's range -------------------------------------------------------
+  if (warp == 1) tmem_alloc(&sh.tmem, 512);
+  if (tid == 0) {
+    if (!Q8) {
+      tma_prefetch_desc(&kmap);
+      tma_prefetch_desc(&vmap);
+    }
+#pragma unroll 1
+    for (int i = 0; i < NK; ++i) { mbar_init(sh.k_full + i, 1); mbar_init(sh.k_empty + i, 1); mbar_init(sh.k_fit + i, kConvWarps); }
+#pragma unroll 1
+    for (int i = 0; i < NV; ++i) { mbar_init(sh.v_full + i, 1); mbar_init(sh.v_empty + i, 1); mbar_init(sh.fixed + i, Q8 ? kConvWarps : 1); }
+#pragma unroll 1
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(sh.s_full[i], 1); mbar_init(sh.s_full[i] + 1, 1); mbar_init(sh.p_full[i], 4); mbar_init(sh.p_full[i] + 1, 4);
+      mbar_init(sh.o_full[i], 1); mbar_init(sh.o_full[i] + 1, 1); mbar_init(sh.ready + i, 4); mbar_init(sh.met + i, 4);
+    }
+    mbar_init(&sh.pair, 8);
+    mbar_init(&sh.drain, 1);
+    fence_barrier_init();
+    *abort_flag = 0;
+  }
+  pdl_trigger();
+  pdl_wait();
+  const uint32_t stalled = reinterpret_cast<const volatile uint32_t*>(a.workspace)[kStalledWord];
+  // The share's form and, in ranges, this CTA's first place: two rounds over the
+  // sequences, their sum and then the place in it; both are one round of a
+  // single step for up to as many sequences as threads.
+  Ranges ranges;
+  int lo = 0, hi = 0, units = 0, longest = 0;
+  bool single = true;  // no sequence has more than one block
+#pragma unroll 1
+  for (int round = 0; round < 2; ++round) {
+    int run = 0;
+#pragma unroll 1
+    for (int b0 = 0; b0 < a.batch; b0 += kThreads) {
+      const int b = b0 + tid;
+      int3 v = make_int3(0, 0, 0);
+      if (b < a.batch) v = make_int3(a.ctx_len[b], a.starts[b], a.starts[b + 1]);
+      if (b < kSeqHeld && b < a.batch) {
+        sh.seq[b] = make_int2(v.x, v.y);
+        if (b == kSeqHeld - 1 || b == a.batch - 1) sh.seq[b + 1] = make_int2(0, v.z);
+      }
+      const Chunk s = chunk_of(a, v.x, v.y, v.z, kRows);
+      int places = 0, tiles = 0;  // of a head
+      if (s.blocks == 1) {
+        tiles = span_of(a, s, 0, kRows).tiles;
+        places = tiles + kStart;
+      }
+      for (uint32_t m = __ballot_sync(0xffffffffu, s.blocks > 1); m; m &= m - 1) {  // the warp adds up one's blocks
+        const int from = __ffs(m) - 1;
+        const Chunk o = chunk_of(a, __shfl_sync(0xffffffffu, v.x, from), __shfl_sync(0xffffffffu, v.y, from),
+                                 __shfl_sync(0xffffffffu, v.z, from), kRows);
+        int part = 0;
+        for (int i = lane; i < o.blocks; i += 32) part += span_of(a, o, i, kRows).tiles + kStart;
+        part = __reduce_add_sync(0xffffffffu, part);
+        if (lane == from) places = part;
+      }
+      const int cost = places * a.n_kv_heads;
+      int inc = cost;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int t = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += t;
+      }
+      const int u = __reduce_add_sync(0xffffffffu, a.n_kv_heads * s.blocks);
+      const int most = __reduce_max_sync(0xffffffffu, tiles);
+      if (lane == 31) { sh.sum[warp] = inc; sh.units[warp] = u; sh.most[warp] = most; }
+      single &= !__syncthreads_or(s.blocks > 1);
+      const bool is = lane < kThreads / 32;
+      const int of = is ? sh.sum[lane] : 0, step = __reduce_add_sync(0xffffffffu, of);
+      inc += run + __reduce_add_sync(0xffffffffu, lane < warp ? of : 0);
+      units += __reduce_add_sync(0xffffffffu, is ? sh.units[lane] : 0);
+      longest = max(longest, __reduce_max_sync(0xffffffffu, is ? sh.most[lane] : 0));
+      run += step;
+      if (a.batch <= kThreads) {
+        ranges.set(run, grid);
+        lo = ranges.at(blockIdx.x);
+        hi = ranges.at(blockIdx.x + 1);
+        round = 1;
+      }
+      if (round && inc > lo && inc - cost <= lo) {
+        const int off = lo - (inc - cost);
+        sh.start_b = b;
+        sh.start_head = off / places;
+        sh.start_off = off % places;
+      }
+      __syncthreads();
+    }
+    if (!round) {
+      ranges.set(run, grid);
+      lo = ranges.at(blockIdx.x);
+      hi = ranges.at(blockIdx.x + 1);
+    }
+  }
+  const bool one_part = single && a.batch <= kSeqHeld && units <= grid;
+  if (!one_part && warp == 0 && hi > lo) {  // the block that the first place lies in
+    const int b = sh.start_b, rest = sh.start_off;
+    const Chunk s = chunk_of(a, a.ctx_len[b], a.starts[b], a.starts[b + 1], kRows);
+    int before = 0;
+#pragma unroll 1
+    for (int i0 = 0; i0 < s.blocks; i0 += 32) {
+      const int len = i0 + lane < s.blocks ? span_of(a, s, i0 + lane, kRows).tiles + kStart : 0;
+      int inc = len;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int t = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += t;
+      }
+      const uint32_t past = __ballot_sync(0xffffffffu, before + inc > rest);
+      if (past) {
+        if (lane == __ffs(past) - 1) { sh.start_block = i0 + lane; sh.start_off = rest - (before + inc - len); }
+        break;
+      }
+      before += __shfl_sync(0xffffffffu, inc, 31);
+    }
+  }
+  if (!one_part) __syncthreads();
+  ChunkWalk& w = sh.walk[warp];
+  auto begin = [&] {  // of a walk in ranges
+    w.left = hi - lo;  // 0: more CTAs than places
+    w.b = hi > lo ? sh.start_b : 0;
+    w.head = hi > lo ? sh.start_head : 0;
+    w.block = hi > lo ? sh.start_block : 0;
+    w.off = hi > lo ? sh.start_off : 0;
+    w.at = lo - w.off;
+    w.load(a, sh.seq, kRows);
+    if (hi > lo) w.g = span_of(a, w.s, w.block, kRows);
+  };
+  if (one_part) {
+    // the fewest tiles a part that the CTAs are enough for; two sequences a lane
+    static_assert(kSeqHeld == 64, "two sequences a lane");
+    int tiles[2], mine[2];
+    const int all_tiles = ranges.total - units * kStart;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int b = 2 * lane + e;
+      tiles[e] = mine[e] = 0;
+      if (b < a.batch) {
+        const Chunk s = chunk_of(a, sh.seq[b].x, sh.seq[b].y, sh.seq[b + 1].y, kRows);
+        if (s.blocks) {
+          tiles[e] = span_of(a, s, 0, kRows).tiles;
+          mine[e] = a.n_kv_heads;
+        }
+      }
+    }
+    // (a unit's parts are less than one more than its tiles / most)
+    int least = max(1, all_tiles / grid), most = max(least, min(longest, all_tiles / (grid - units + 1) + 1));
+#pragma unroll 1
+    while (least < most) {
+      const int mid = (least + most) / 2;
+      const int need = __reduce_add_sync(0xffffffffu, mine[0] * parts_of(tiles[0], mid) + mine[1] * parts_of(tiles[1], mid));
+      if (need <= grid) most = mid; else least = mid + 1;
+    }
+    int inc = 0;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) { mine[e] *= parts_of(tiles[e], most); inc += mine[e]; }
+    const int own = inc;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int t = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += t;
+    }
+    if (lane == 0) w.left = 0;  // more CTAs than parts
+    __syncwarp();
+    int before = inc - own;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int at = (int)blockIdx.x - before;
+      if (at >= 0 && at < mine[e]) {
+        const int parts = parts_of(tiles[e], most);
+        w.left = 1;
+        w.b = 2 * lane + e;
+        w.load(a, sh.seq, kRows);
+        w.g = span_of(a, w.s, 0, kRows);
+        w.head = at / parts;
+        w.block = 0;
+        w.count = parts;
+        w.me = at - w.head * parts;
+        w.c0 = (int)blockIdx.x - w.me;
+        w.t0 = w.me * w.g.tiles / parts;
+        w.t1 = (w.me + 1) * w.g.tiles / parts;
+      }
+      before += mine[e];
+    }
+  } else if (lane == 0) {
+    begin();
+  }
+  __syncwarp();
+  const bool had_part = w.left > 0;
+  // the warp's next segment
+  auto next = [&]() -> bool {
+    __syncwarp();
+    bool some = false;
+    if (lane == 0) some = w.next(a, sh.seq, kRows, ranges, one_part);
+    return __shfl_sync(0xffffffffu, (int)some, 0);
+  };
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = sh.tmem;
+  int tile0 = 0;  // tiles of the segments before this one
+  bool ok = true;
+  // pages of a tile that hold keys the block may see
+  auto pages_of = [&](int tile) { return min(kTilePages, (w.g.end - 1) / kPageTok - tile * kTilePages + 1); };
+
+  if (warp < 4) {
+    if (warp == 0 || warp == 2) {
+      // ---- loads: keys by one warp, values by another --------------------------------
+      // Page ids are fetched 32 pages (four tiles) at a time, a block ahead of
+      // their use: a load from the table would be on every copy's path.
+      const bool v = warp == 2;
+      uint64_t *full = v ? sh.v_full : sh.k_full, *empty = v ? sh.v_empty : sh.k_empty;
+      uint8_t* to0 = v ? vring : kring;
+      const CUtensorMap* map = v ? &vmap : &kmap;
+      const int ns = v ? NV : NK;
+      int st = 0, phase = 0, issued = 0;  // stages are used in turn
+      while (ok && next()) {
+        const int n = w.t1 - w.t0, head = w.head;
+        const int32_t* row = a.page_table + (size_t)w.b * a.max_pages;
+        const int last_page = (w.g.end - 1) / kPageTok;
+        auto fetch = [&](int block) {
+          const int j = 4 * block + lane / kTilePages;
+          const int p = j < n ? w.g.tile(w.t0 + j) * kTilePages + lane % kTilePages : last_page + 1;
+          const int page = p <= last_page ? row[p] : 0;
+          return (uint32_t)page < (uint32_t)a.n_pages ? page : a.n_pages;  // out of the tensor: reads as zeros
+        };
+        int have = fetch(0), after = n > 4 ? fetch(1) : 0;
+#pragma unroll 1
+        for (int j = 0; j < n; ++j) {
+          const int pages = pages_of(w.g.tile(w.t0 + j));
+          if (j > 0 && (j & 3) == 0) {
+            have = after;
+            if (j + 4 < n) after = fetch(j / 4 + 1);
+          }
+          int page[kTilePages];
+#pragma unroll
+          for (int q = 0; q < kTilePages; ++q) page[q] = __shfl_sync(0xffffffffu, have, (j & 3) * kTilePages + q);
+          ok = warp_wait(empty + st, phase ^ 1, abort_flag);
+          if (!ok) break;
+          uint8_t* to = to0 + st * kStage;
+          if constexpr (Q8) {
+            // a page's codes where its last 16-bit entries go (see the conversion)
+            uint8_t* scale = (v ? sh.v_scale : sh.k_scale) + st * kTile;
+            constexpr int kCodes = HD * kPageTok;
+            uint8_t* codes = to + (HD == 128 ? kChunkBytes : kCodes);
+            int there = 0;
+#pragma unroll
+            for (int q = 0; q < kTilePages; ++q) {
+              if (q >= pages) continue;
+              if (page[q] < a.n_pages) {
+                ++there;
+              } else {  // no such page: zeros
+#pragma unroll 1
+                for (int i = lane; i < kCodes / 16; i += 32) reinterpret_cast<uint4*>(codes + q * kPageTok * 128)[i] = make_uint4(0, 0, 0, 0);
+                if (lane == 0) *reinterpret_cast<uint4*>(scale + q * kPageTok) = make_uint4(0, 0, 0, 0);
+              }
+            }
+            __syncwarp();
+            if (elect_one()) {
+              mbar_arrive_expect_tx(full + st, (uint32_t)there * (kCodes + kPageTok));
+              const uint8_t* from = reinterpret_cast<const uint8_t*>(v ? a.v_cache : a.k_cache) + (int64_t)head * kCodes;
+              const uint8_t* from_scale = (v ? a.v_scale : a.k_scale) + (int64_t)head * kPageTok;
+#pragma unroll
+              for (int q = 0; q < kTilePages; ++q)
+                if (q < pages && page[q] < a.n_pages) {
+                  bulk_load(codes + q * kPageTok * 128, from + page[q] * a.page_stride, kCodes, full + st);
+                  bulk_load(scale + q * kPageTok, from_scale + page[q] * a.scale_stride, kPageTok, full + st);
+                }
+            }
+          } else if (elect_one()) {
+            mbar_arrive_expect_tx(full + st, (uint32_t)pages * kChunks * kPageTok * 128);
+#pragma unroll
+            for (int q = 0; q < kTilePages; ++q)
+              if (q < pages) {
+#pragma unroll
+                for (int c = 0; c < kChunks; ++c)
+                  tma_load_4d(to + c * kChunkBytes + q * kPageTok * 128, map, full + st, c * 64, 0, head, page[q]);
+              }
+          }
+          __syncwarp();
+          ++issued;
+          if (++st == ns) { st = 0; phase ^= 1; }
+        }
+      }
+      if (!ok) {  // copies in flight write this CTA's shared memory: they land before it goes
+        *abort_flag = 1;
+        for (int i = max(0, issued - ns); i < issued; ++i) mbar_drain(full + i % ns, (i / ns) & 1);
+      }
+    } else if (warp == 1) {
+      // ---- products ---------------------------------------------------------------
+      uint32_t ph_p = 0, ph_ready = 0;
+      const uint32_t q_addr = smem_u32(qbuf), k_addr = smem_u32(kring), v_addr = smem_u32(vring);
+      uint64_t* keys_in = Q8 ? sh.k_fit : sh.k_full;
+      auto wait_k = [&](int i) { ok = ok && warp_wait(keys_in + i % NK, (i / NK) & 1, abort_flag); };
+      auto wait_v = [&](int i) { ok = ok && warp_wait(sh.fixed + i % NV, (i / NV) & 1, abort_flag); };
+      // Operand addresses go through a shuffle, which tells the compiler that they
+      // are the warp's and not a lane's, and steps add constants to a
+      // descriptor's low word: an issue then costs little beside its product.
+      auto uniform = [](uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); };
+      // Shared-memory descriptors, 128-byte swizzle.  Queries and keys: 128-byte
+      // rows along K, eight-row atoms 1024 bytes apart.  Values: 64 of a key's
+      // entries a row (N is contiguous), atoms of eight keys 1024 bytes apart along
+      // K, the next 64 entries a chunk further.
+      constexpr uint64_t kDescK = (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+      constexpr uint64_t kDescV = (uint64_t)(kChunkBytes >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+      // tensor memory: the groups' score buffers, then their accumulators
+      auto scores = [&](int g, int h, int buf, int i) {  // of half h of tile i
+        const uint32_t qa = uniform((q_addr + (BLOCKS == 2 ? g * kStage : 0)) >> 4);
+        const uint32_t kb = uniform((k_addr + (i % NK) * kStage + h * kStep * 128) >> 4);
+        const uint32_t d = uniform(tmem + g * kTile + buf * kStep);
+        if (elect_one()) {
+#pragma unroll
+          for (int k = 0; k < HD / 16; ++k) {
+            const uint32_t at = ((k / 4) * kChunkBytes + (k % 4) * 32) >> 4;
+            umma_ss(d, kDescK | (qa + at), kDescK | (kb + at), kIdescS, k > 0);
+          }
+          umma_commit(&sh.s_full[g][buf]);
+        }
+        __syncwarp();
+      };
+      auto outputs = [&](int g, int h, int buf, int i, bool first, int keys) {  // O += P V
+        const uint32_t vb = uniform((v_addr + (i % NV) * kStage + h * kStep * 128) >> 4);
+        const uint32_t o = uniform(tmem + 2 * kTile + g * HD), p = uniform(tmem + g * kTile + buf * kStep);
+        // keys past the end have probability 0: whole steps of 16 are left out, but
+        // for the first, which leaves zeros where there were none yet
+        const int steps = __shfl_sync(0xffffffffu, max(1, (keys - h * kStep + 15) / 16), 0);
+        const uint32_t bit = 2 * g + buf;
+        ok = ok && warp_wait(&sh.p_full[g][buf], ph_p >> bit & 1, abort_flag);
+        if (!ok) return;
+        ph_p ^= 1u << bit;
+        tc_fence_after();
+        if (elect_one()) {
+#pragma unroll
+          for (int k = 0; k < kStep / 16; ++k)
+            if (k < steps) umma_ts(o, p + k * 8, kDescV | (vb + k * 128), kIdescO, !first || k > 0);
+          umma_commit(&sh.o_full[g][buf]);
+        }
+        __syncwarp();
+      };
+      auto commit = [&](uint64_t* bar) {
+        if (elect_one()) umma_commit(bar);
+        __syncwarp();
+      };
+      while (ok && next()) {
+        const int n = w.t1 - w.t0;
+        auto keys_from = [&](int j) { return w.g.end - w.g.tile(w.t0 + j) * kTile; };  // of tile j's first on
+        ok = warp_wait(sh.ready + 0, ph_ready, abort_flag) && warp_wait(sh.ready + 1, ph_ready, abort_flag);
+        ph_ready ^= 1;
+        tc_fence_after();
+        // tile j's outputs, and the scores that go where its probabilities were:
+        // two blocks, of the next tile's same half; one, of the same half two tiles on
+        constexpr int kAhead = BLOCKS == 2 ? 1 : 2;
+#pragma unroll 1
+        for (int j = -kAhead; j < n && ok; ++j) {
+          const int i = tile0 + j, keys = j >= 0 ? keys_from(j) : 0;
+          const bool more = j + kAhead < n;
+          if (j >= 0) wait_v(i);
+          if (!ok) break;
+#pragma unroll
+          for (int e = 0; e < 2 * BLOCKS; ++e) {
+            const int g = e & 1, h = BLOCKS == 2 ? e >> 1 : g, buf = BLOCKS == 2 ? h : (j & 1);
+            if (j >= 0) outputs(g, h, buf, i, j == 0 && (BLOCKS == 1 || h == 0), keys);
+            // (asked for here, since the load of a stage that has just come free is
+            // what a step would wait for)
+            if (more && e == 0) wait_k(i + kAhead);
+            if (!ok) break;
+            if (more) scores(g, h, buf, i + kAhead);
+          }
+          if (!ok) break;
+          if (j >= 0) commit(sh.v_empty + i % NV);
+          if (more) commit(sh.k_empty + (i + kAhead) % NK);
+        }
+        tile0 += n;
+      }
+      if (!ok) *abort_flag = 1;
+      // products in flight read shared memory and write tensor memory: let them end
+      commit(&sh.drain);
+      mbar_drain(&sh.drain, 0);
+    } else if (!Q8) {
+      // ---- values of tiles that some row does not see whole ----------------------------
+      while (ok && next()) {
+        const int n = w.t1 - w.t0;
+#pragma unroll 1
+        for (int j = 0; j < n; ++j) {
+          const int st = (tile0 + j) % NV;
+          ok = warp_wait(sh.v_full + st, ((tile0 + j) / NV) & 1, abort_flag);
+          if (!ok) break;
+          const int k0 = w.g.tile(w.t0 + j) * kTile;
+          if (!all_see(a, w.s, w.g.p_lo, w.g.p_hi, k0, k0 + kTile)) {
+            const int end = w.g.end - k0;
+            // the products take 16 keys at a time, and each half's first 16 in any case
+            const int used = min(kTile, max(kStep + 16, (end + 15) & ~15));
+            constexpr int kPieces = HD / 8;
+            bool any = false;
+#pragma unroll 4
+            for (int p = lane; p < used * kPieces; p += 32) {
+              const int r = p / kPieces, c = p % kPieces;
+              if (all_see(a, w.s, w.g.p_lo, w.g.p_hi, k0 + r, k0 + r + 1)) continue;
+              uint4* at = reinterpret_cast<uint4*>(vring + st * kStage + (c / 8) * kChunkBytes + r * 128 + (((c % 8) ^ (r & 7)) << 4));
+              const uint4 v = *at;
+              const uint4 f = r >= end ? make_uint4(0, 0, 0, 0)
+                                       : make_uint4(finite_of<T>(v.x), finite_of<T>(v.y), finite_of<T>(v.z), finite_of<T>(v.w));
+              if (f.x != v.x || f.y != v.y || f.z != v.z || f.w != v.w) {
+                *at = f;
+                any |= r < end;
+              }
+            }
+            fence_proxy_async_all();
+            any = __any_sync(0xffffffffu, any);
+            if (lane == 0) sh.odd[st] = any;
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(sh.fixed + st);
+        }
+        tile0 += n;
+      }
+      if (!ok) *abort_flag = 1;
+    }
+  } else if (warp < 12) {
+    // ---- softmax: group g, a thread a row --------------------------------------------
+    const int g = (warp - 4) >> 2, t = tid - 128 - g * kTile;  // t: row of the score tile = lane of tensor memory
+    const uint32_t my = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+    const uint32_t s_addr = my + g * kTile, o_addr = my + 2 * kTile + g * HD;
+    const float sl2 = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1e-30f);  // a masked score stays -inf at scale 0
+    const bool wide_out = (reinterpret_cast<uintptr_t>(a.out) & 31) == 0;
+    uint32_t ph_s = 0, ph_pair = 0, ph_met = 0;
+    int handed[2] = {0, 0};  // probabilities handed over so far, by buffer
+    auto meet = [&] {  // both groups, 256 threads
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.pair);
+      ok = warp_wait(&sh.pair, ph_pair, abort_flag);
+      ph_pair ^= 1;
+    };
+    auto group_meet = [&] {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(sh.met + g);
+      ok = warp_wait(sh.met + g, ph_met, abort_flag);
+      ph_met ^= 1;
+    };
+    while (ok && next()) {
+      const int n = w.t1 - w.t0;
+      const int row_base = w.block * kRows + (BLOCKS == 2 ? g * kTile : 0);  // row of the unit that lane 0 of the group has
+      const int row = row_base + t, rows = w.s.rows;
+      // queries into shared memory, swizzled; one block: each group lays out half
+      {
+        constexpr int kPieces = HD / 8, kMine = BLOCKS == 2 ? kTile : kTile / 2, kStep = kTile / kPieces;
+        const uint32_t sign = a.scale < 0.f ? 0x80008000u : 0u;  // a negative scale turns the queries' signs
+        const int c = t % kPieces, r0 = t / kPieces + (BLOCKS == 2 ? 0 : g * kMine);
+        const T* q = reinterpret_cast<const T*>(a.q) + (int64_t)w.s.row0 * a.q_stride + (int64_t)w.head * group * HD + c * 8;
+        uint8_t* dst = qbuf + (BLOCKS == 2 ? g * kStage : 0) + (c / 8) * kChunkBytes;
+        uint4 v[kMine / kStep];  // all loads are out before the first is stored
+#pragma unroll
+        for (int i = 0; i < kMine / kStep; ++i) {
+          const int r = row_base + r0 + i * kStep, token = r / group;
+          v[i] = make_uint4(0, 0, 0, 0);
+          if (r < rows) v[i] = *reinterpret_cast<const uint4*>(q + (int64_t)token * a.q_stride + (r - token * group) * HD);
+        }
+#pragma unroll
+        for (int i = 0; i < kMine / kStep; ++i) {
+          const int r = r0 + i * kStep;
+          v[i].x ^= sign; v[i].y ^= sign; v[i].z ^= sign; v[i].w ^= sign;
+          *reinterpret_cast<uint4*>(dst + r * 128 + (((c % 8) ^ (r & 7)) << 4)) = v[i];
+        }
+        fence_proxy_async_all();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(sh.ready + g);
+      }
+      const int token = min(row, rows - 1) / group, p = w.s.ctx + token;
+      const int see_end = min(p + 1, w.s.keys), see_from = window_from(a, p);
+      // positions of the group's first and last rows
+      const int g_lo = w.s.ctx + min(row_base, rows - 1) / group, g_hi = w.s.ctx + min(row_base + kTile - 1, rows - 1) / group;
+      auto page_flag = [&](int j) -> uint32_t {  // this lane's page of tile j is one of the pool
+        const int at = w.g.tile(w.t0 + j) * kTilePages + lane;
+        if (lane >= kTilePages || at * kPageTok >= w.g.end) return 1;
+        return (uint32_t)a.page_table[(size_t)w.b * a.max_pages + at] < (uint32_t)a.n_pages;
+      };
+      float m_ref = -INFINITY, sum = 0.f;
+      bool patch = false;  // values that the rows who see them get back in the epilogue
+      // The product with the last probabilities handed over from a buffer is done (the
+      // one before it was before the buffer's scores came again, so that a barrier's
+      // one bit tells them apart).
+      auto o_done = [&](int buf) {
+        const bool done = handed[buf] == 0 || warp_wait(&sh.o_full[g][buf], (handed[buf] & 1) ^ 1, abort_flag);
+        tc_fence_after();
+        return done;
+      };
+      uint32_t flag = page_flag(0);
+#pragma unroll 1
+      for (int j = 0; j < n; ++j) {
+        const uint32_t flags = __ballot_sync(0xffffffffu, flag);
+        if (j + 1 < n) flag = page_flag(j + 1);
+        const int k0 = w.g.tile(w.t0 + j) * kTile;
+        const bool partly = !all_see(a, w.s, w.g.p_lo, w.g.p_hi, k0, k0 + kTile);
+#pragma unroll 1
+        for (int e = 0; e < BLOCKS; ++e) {
+          const int h = BLOCKS == 2 ? e : g, buf = BLOCKS == 2 ? e : (j & 1), key = k0 + h * kStep;
+          const uint32_t there = flags >> (4 * h) & 15u;
+          const bool masked = there != 15u || !all_see(a, w.s, g_lo, g_hi, key, key + kStep);
+          const uint32_t s_at = s_addr + buf * kStep;
+          ok = warp_wait(&sh.s_full[g][buf], ph_s >> buf & 1, abort_flag);
+          if (!ok) break;
+          ph_s ^= 1u << buf;
+          tc_fence_after();
+          uint32_t v[kStep];
+          tm_ld32(s_at, v);
+          tm_ld32(s_at + 32, v + 32);
+          tm_landed<kStep>(v);
+          if (masked) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              const uint32_t m = seen32(key + 32 * c, see_end, see_from, a.sinks) &
+                                 ((there >> (2 * c) & 1 ? 0xFFFFu : 0u) | (there >> (2 * c + 1) & 1 ? 0xFFFF0000u : 0u));
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (!(m >> i & 1)) v[32 * c + i] = 0xFF800000u;
+            }
+          }
+          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int i = 0; i < kStep; i += 2)
+            mx[i >> 1 & 3] = fmaxf(fmaxf(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), mx[i >> 1 & 3]);
+          // what probabilities are taken against: 2^kRaise below the largest
+          const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * sl2 - Num<T>::kRaise;
+          if (j == 0 && e == 0) {
+            m_ref = top;
+          } else if (__any_sync(0xffffffffu, top > m_ref + kLazy)) {
+            const float m_new = fmaxf(m_ref, top);
+            const float alpha = m_new == m_ref ? 1.0f : ex2(m_ref - m_new);
+            m_ref = m_new;
+            sum *= alpha;
+            ok = o_done(buf ^ 1);
+            if (!ok) break;
+            scale_row<HD>(o_addr, alpha);
+          }
+          const float base = m_ref == -INFINITY ? 0.f : m_ref;
+          const uint64_t scale2 = pair_of(__float_as_uint(sl2), __float_as_uint(sl2));
+          const uint64_t base2 = pair_of(__float_as_uint(-base), __float_as_uint(-base));
+          uint64_t acc[2] = {0, 0};
+          // in place: the pair at 2 i becomes entry i
+#pragma unroll
+          for (int i = 0; i < kStep / 2; ++i) {
+            const float2 f = floats_of(fma2(pair_of(v[2 * i], v[2 * i + 1]), scale2, base2));
+            const float x = ex2(f.x), y = ex2(f.y);
+            acc[i & 1] = add2(acc[i & 1], pair_of(__float_as_uint(x), __float_as_uint(y)));
+            v[i] = Num<T>::pack(x, y);
+          }
+          tm_st32(s_at, v);
+          tm_wait_st();
+          const float2 acc2 = floats_of(add2(acc[0], acc[1]));
+          sum += acc2.x + acc2.y;
+          if (partly) {  // the stage is not refilled before these probabilities are used
+            const int st = (tile0 + j) % NV;
+            ok = warp_wait(sh.fixed + st, ((tile0 + j) / NV) & 1, abort_flag);
+            if (!ok) break;
+            patch |= sh.odd[st] != 0;
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sh.p_full[g][buf]);
+          ++handed[buf];
+        }
+        if (!ok) break;
+      }
+      if (!ok) break;
+      ok = o_done(0) && o_done(1);
+      if (!ok) break;
+      // ---- epilogue: a group's own accumulator, or half the columns of both groups' ----
+      float w0 = 1.f, w1 = 0.f;
+      if (BLOCKS == 1) {
+        float4* ml = reinterpret_cast<float4*>(qbuf);  // the queries have been read
+        ml[g * kTile + t] = make_float4(m_ref, sum, patch ? 1.f : 0.f, 0.f);
+        meet();
+        if (!ok) break;
+        const float4 x = ml[t], y = ml[kTile + t];
+        patch = x.z + y.z > 0.f;
+        m_ref = fmaxf(x.x, y.x);
+        w0 = x.x == -INFINITY ? 0.f : ex2(x.x - m_ref);
+        w1 = y.x == -INFINITY ? 0.f : ex2(y.x - m_ref);
+        sum = x.y * w0 + y.y * w1;
+      }
+      constexpr int kCols = BLOCKS == 2 ? HD : HD / 2;
+      const int col0 = BLOCKS == 2 ? 0 : g * kCols, in_block = (BLOCKS == 2 ? g * kTile : 0) + t;
+      const bool whole = w.t0 == 0 && w.t1 == w.g.tiles, on = row < rows;
+      // A unit's contributors are consecutive CTAs.  All but the last to arrive
+      // leave their partial; that one joins them, in tile order (see
+      // tree_attention.cu).
+      const int count = whole ? 1 : w.count, me = w.me, c0 = w.c0;
+      uint32_t* arrived = reinterpret_cast<uint32_t*>(a.workspace) + 2 * c0 + g;
+      const Partial mine = slot_of(a, 2 * (c0 + me) + (w.t0 > 0 ? 0 : 1), HD, BLOCKS);
+      bool two = false;
+      if (count == 2) {
+        if (t == 0) sh.last_in[g] = ld_acquire(arrived) == 1;
+        group_meet();
+        if (!ok) break;
+        two = sh.last_in[g];
+      }
+      T* unit = reinterpret_cast<T*>(a.out) + ((int64_t)w.s.row0 * a.n_q_heads + (int64_t)w.head * group) * HD;
+      T* out = unit + ((int64_t)token * a.n_q_heads + (row - token * group)) * HD;
+      if (!two) {
+        const float inv = sum > 0.f ? 1.0f / sum : 0.f;
+#pragma unroll 1
+        for (int c = col0; c < col0 + kCols; c += 32) {
+          uint32_t o[32];
+          own_columns<HD, BLOCKS>(o, my + 2 * kTile + (BLOCKS == 2 ? g * HD : 0) + c, w0, w1, true);
+          if (!on) continue;
+          if (whole) {
+            store_columns<T>(out + c, o, inv, wide_out);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              *mine.o(c / 4 + i, in_block) = make_float4(__uint_as_float(o[4 * i]), __uint_as_float(o[4 * i + 1]),
+                                                         __uint_as_float(o[4 * i + 2]), __uint_as_float(o[4 * i + 3]));
+          }
+        }
+        if (patch && on) patch_chunk<T, HD, Q8>(a, w, p, col0, kCols, whole ? out : nullptr, mine, in_block);
+        if (!whole) {
+          *mine.stats(HD, g, in_block) = make_float2(m_ref, sum);
+          // written before the group meets, read after, and written again only when
+          // all of it has been through another tile
+#pragma unroll 1
+          for (int i = t; i < count; i += kTile)
+            sh.slots[g][i] = (uint16_t)(2 * (c0 + i) + (i == 0 ? 1 : 0));
+          fence_gpu();
+          group_meet();
+          if (!ok) break;
+          if (t == 0) sh.last_in[g] = arrive_acq_rel(arrived) == (uint32_t)count - 1;
+          group_meet();
+          if (!ok) break;
+          if (sh.last_in[g]) {
+            if (count == 2) {
+              two = true;
+            } else {
+              fence_gpu();
+              const int live = min(kTile, rows - row_base);
+              join<T, HD, BLOCKS>(a, sh.slots[g], count, g, t, in_block - t, live, col0 / 4, kCols / 4, unit, row_base);
+              if (t == 0) *arrived = 0;  // as the next call wants it
+            }
+          }
+        }
+      }
+      if (two) {
+        const Partial other = slot_of(a, 2 * (c0 + 1 - me) + me, HD, BLOCKS);
+        join_two<T, HD, BLOCKS>(other, my + 2 * kTile + (BLOCKS == 2 ? g * HD : 0), g, in_block, me == 0, m_ref, sum, w0,
+                                w1, true, col0, on, out, wide_out);
+        if (patch && on) patch_chunk<T, HD, Q8>(a, w, p, col0, kCols, out, mine, in_block);
+        if (t == 0) *arrived = 0;
+      }
+      if (BLOCKS == 1) {  // the queries' place holds the sums, and each group reads both accumulators
+        meet();
+        if (!ok) break;
+      }
+      tile0 += n;
+    }
+    if (!ok) *abort_flag = 1;
+  } else if constexpr (Q8) {
+    // ---- codes into 16-bit entries, in place -------------------------------------------
+    // A page's codes lie in the half of its place that its last 16-bit entries take
+    // (hd 128: the second 64 entries', hd 64: the last eight tokens'); the warp that
+    // has the page holds all of them before it writes.
+    constexpr int kCodes = HD * kPageTok, kHeld = kCodes / 512, kRowPieces = HD / 16;
+    const int cw = warp - 12;
+    while (ok && next()) {
+      const int n = w.t1 - w.t0;
+#pragma unroll 1
+      for (int jj = 0; jj < 2 * n; ++jj) {  // keys, then values of a tile
+        const bool v = jj & 1;
+        const int i = tile0 + (jj >> 1), tile = w.g.tile(w.t0 + (jj >> 1)), k0 = tile * kTile;
+        const int st = v ? i % NV : i % NK;
+        ok = v ? warp_wait(sh.v_full + st, (i / NV) & 1, abort_flag) : warp_wait(sh.k_full + st, (i / NK) & 1, abort_flag);
+        if (!ok) break;
+        uint8_t* stage = (v ? vring : kring) + st * kStage;
+        const uint8_t* scale = (v ? sh.v_scale : sh.k_scale) + st * kTile;
+        const bool clean = v && !all_see(a, w.s, w.g.p_lo, w.g.p_hi, k0, k0 + kTile);
+        const int pages = pages_of(tile);
+        bool any = false;
+#pragma unroll 1
+        for (int q = cw; q < pages; q += kConvWarps) {
+          const uint4* codes = reinterpret_cast<const uint4*>(stage + (HD == 128 ? kChunkBytes : kCodes) + q * kPageTok * 128);
+          uint4 x[kHeld];
+          Widen<T> by[kHeld];
+          uint32_t odd = 0;
+          bool far = false;
+#pragma unroll
+          for (int e = 0; e < kHeld; ++e) {
+            x[e] = codes[e * 32 + lane];
+            by[e].set(scale[q * kPageTok + (e * 32 + lane) / kRowPieces]);
+            far |= by[e].far;
+            odd |= Widen<T>::odd(x[e].x) | Widen<T>::odd(x[e].y) | Widen<T>::odd(x[e].z) | Widen<T>::odd(x[e].w);
+          }
+          far = __any_sync(0xffffffffu, far || odd);  // (and every lane holds its codes)
+#pragma unroll
+          for (int e = 0; e < kHeld; ++e) {
+            const int r = q * kPageTok + (e * 32 + lane) / kRowPieces, c16 = lane % kRowPieces;
+            const uint32_t in[4] = {x[e].x, x[e].y, x[e].z, x[e].w};
+            uint32_t y[8];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              if (far) by[e].four_far(in[k], y[2 * k], y[2 * k + 1]);
+              else by[e].four(in[k], y[2 * k], y[2 * k + 1]);
+            }
+            if (clean && !all_see(a, w.s, w.g.p_lo, w.g.p_hi, k0 + r, k0 + r + 1)) {
+#pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                const uint32_t f = k0 + r >= w.g.end ? 0u : finite_of<T>(y[k]);
+                any |= k0 + r < w.g.end && f != y[k];
+                y[k] = f;
+              }
+            }
+            // two pieces of eight entries; the lanes of a row's second half write theirs
+            // the other way round, so that eight lanes reach all banks
+            uint8_t* to = stage + (c16 / 4) * kChunkBytes + r * 128;
+            const int c = (2 * c16) % 8, turn = HD == 128 ? c16 / 4 : 0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const bool second = (h ^ turn) != 0;
+              *reinterpret_cast<uint4*>(to + (((c + (second ? 1 : 0)) ^ (r & 7)) << 4)) =
+                  second ? make_uint4(y[4], y[5], y[6], y[7]) : make_uint4(y[0], y[1], y[2], y[3]);
+            }
+          }
+        }
+        if (v && cw == 0 && pages <= kTilePages / 2) {  // the second half's first 16, which are multiplied in any case
+#pragma unroll 1
+          for (int e = lane; e < kPageTok * HD / 8; e += 32)
+            *reinterpret_cast<uint4*>(stage + (e / (kPageTok * 8)) * kChunkBytes + kStep * 128 + e % (kPageTok * 8) * 16) = make_uint4(0, 0, 0, 0);
+        }
+        fence_proxy_async_all();
+        if (v) {
+          any = __any_sync(0xffffffffu, any);
+          if (lane == 0) reinterpret_cast<uint8_t*>(sh.odd + st)[cw] = any;
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(v ? sh.fixed + st : sh.k_fit + st);
+      }
+      tile0 += n;
+    }
+    if (!ok) *abort_flag = 1;
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) tmem_dealloc(tmem, 512);
+  if (*abort_flag || stalled) {
+    // A wait ran out, now or in an earlier call with this workspace (whose
+    // arrivals are then not to be trusted): every unit of the range becomes NaN,
+    // never numbers that look right, until the workspace is zeroed again.
+    if (tid == 0) {
+      reinterpret_cast<volatile uint32_t*>(a.workspace)[kStalledWord] = 1;
+      if (one_part) w.left = had_part; else begin();
+    }
+    __syncthreads();
+    const ChunkWalk& u = sh.walk[0];
+    while (true) {
+      __syncthreads();
+      if (tid == 0) sh.odd[0] = sh.walk[0].next(a, sh.seq, kRows, ranges, one_part);
+      __syncthreads();
+      if (!sh.odd[0]) break;
+#pragma unroll 1
+      for (int r = u.block * kRows + tid; r < min((u.block + 1) * kRows, u.s.rows); r += kThreads) {
+        const int token = r / group;
+        T* out = reinterpret_cast<T*>(a.out) +
+                 (((int64_t)u.s.row0 + token) * a.n_q_heads + (int64_t)u.head * group + (r - token * group)) * HD;
+#pragma unroll 1
+        for (int e = 0; e < HD; e += 2) *reinterpret_cast<uint32_t*>(out + e) = 0x7FFF7FFFu;
+      }
+    }
+  }
+}
+
+namespace {
+
+// Blocks of 256 query vectors where a sequence has more than 128 of them on
+// average: two groups with rows of their own reuse each tile twice; with fewer,
+// both work on the same rows.
+int chunk_blocks(int n_tokens, int batch, int group) { return (int64_t)n_tokens * group <= (int64_t)batch * kTile ? 1 : 2; }
+
+template <typename T, int HD, int BLOCKS, bool Q8>
+void run_chunk(const ChunkAttnArgs& a, cudaStream_t s) {
+  constexpr int smem = chunk_smem<HD, BLOCKS, Q8>();
+  auto* kernel = chunk_attention_kernel<T, HD, BLOCKS, Q8>;
+  static OncePerDevice ctas;
+  const int dev = current_device(), sms = ctas.get(dev, [&] {
+    allow_shared(kernel, smem);
+    int n = 0;
+    const cudaError_t e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess) throw e;
+    return n;
+  });
+  const int grid = sms < kMaxGrid ? sms : kMaxGrid;
+  CUtensorMap km, vm;
+  if (Q8) {
+    std::memset(&km, 0, sizeof(km));
+    vm = km;
+  } else {
+    km = cache_map(a, a.k_cache);
+    vm = cache_map(a, a.v_cache);
+  }
+  launch_in_turn(kernel, dim3(grid), chunk_threads(Q8), smem, 0, s, a, km, vm);
+}
+
+// the caches' width is the translation unit's
+template <bool Q8, typename T, int HD>
+void run_chunk_sized(const ChunkAttnArgs& a, cudaStream_t s) {
+  if (chunk_blocks(a.n_tokens, a.batch, a.n_q_heads / a.n_kv_heads) == 1) run_chunk<T, HD, 1, Q8>(a, s);
+  else run_chunk<T, HD, 2, Q8>(a, s);
+}
+template <bool Q8>
+void run_chunk_attention(const ChunkAttnArgs& a, cudaStream_t s) {
+  if (a.dtype == DT_BF16) {
+    if (a.head_dim == 128) run_chunk_sized<Q8, __nv_bfloat16, 128>(a, s); else run_chunk_sized<Q8, __nv_bfloat16, 64>(a, s);
+  } else {
+    if (a.head_dim == 128) run_chunk_sized<Q8, __half, 128>(a, s); else run_chunk_sized<Q8, __half, 64>(a, s);
+  }
+}
+
+}  // namespace
+
+}  // namespace pard

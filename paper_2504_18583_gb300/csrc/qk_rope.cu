@@ -22,6 +22,14 @@
 // position 65536.  Here each frequency becomes a whole number of 2^-64 turns,
 // once a thread, and the product with the position, modulo 2^64, is the exact
 // phase of that number; its top 32 bits go through sincospif.
+//
+// An 8-bit cache holds e4m3 codes and, for each token's head, the biased exponent
+// of a power of two: the smallest under which no finite entry passes 448, e4m3's
+// largest.  Codes are rounded from the 32-bit values, so an entry is rounded once;
+// a power of two moves no bit, so a reader's 16-bit copy of an entry is exact.
+// Infinities and NaN become NaN and do not count for the exponent.  It costs the
+// row's largest entry (three or four shuffles) and four conversions a lane, and
+// saves half of the caches' bytes.
 #include <cuda_fp16.h>
 
 #include "common.cuh"
@@ -75,6 +83,19 @@ __device__ __forceinline__ uint64_t turns_per_position(float f) {
   return f < 0.f ? 0 - t : t;
 }
 
+// The biased exponent of the smallest power of two p with most <= 448 p, in [1, 254].
+__device__ __forceinline__ uint32_t scale_exponent(float most) {
+  const uint32_t u = __float_as_uint(most);  // 448 is 1.75 * 2^8
+  const int e = (int)(u >> 23) - 8 + ((u & 0x7FFFFF) > 0x600000 ? 1 : 0);
+  return (uint32_t)max(e, 1);
+}
+// Two values as e4m3 codes, x in the low byte; what is not finite becomes NaN.
+__device__ __forceinline__ uint32_t e4m3_pair(float x, float y) {
+  uint16_t v;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %2, %1;" : "=h"(v) : "f"(x), "f"(y));
+  return v;
+}
+
 __device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
 
@@ -82,7 +103,7 @@ __device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
 
 // A CTA has U heads of every lane group, those of its blockIdx.y, and walks over
 // tokens: the next one's loads are out while it works on one.
-template <typename T, int HD, int U>
+template <typename T, int HD, int U, bool Q8>
 __global__ void __launch_bounds__(kRopeThreads, U == 1 ? 5 : 4) qk_rope_kernel(const __grid_constant__ QkRopeArgs a) {
   constexpr int kGroup = HD / 8;                      // lanes of one head
   constexpr int kGroups = kRopeThreads / kGroup;      // heads a CTA takes at once
@@ -138,6 +159,7 @@ __global__ void __launch_bounds__(kRopeThreads, U == 1 ? 5 : 4) qk_rope_kernel(c
       reinterpret_cast<float2*>(s_turn[buf][tk])[((te % 8 / 2) * kGroup + te / 8) * 2 + (te & 1)] =
           t_turns ? make_float2(t_own * (a.amplitude * cs), (t_odd ? t_far : -t_far) * (a.amplitude * sn)) : make_float2(t_own, 0.f);
     }
+    const int64_t slot_now = slot;
     const bool write = slot >= 0 && slot < (int64_t)a.n_pages * kPageTok;
     const int64_t cache_at = (int64_t)(uint32_t)(slot >> 4) * a.page_stride + (int)(slot & (kPageTok - 1)) * HD + e0;
     __syncthreads();  // (the other buffer's readers are past it: they arrived here)
@@ -156,9 +178,11 @@ __global__ void __launch_bounds__(kRopeThreads, U == 1 ? 5 : 4) qk_rope_kernel(c
       const bool is_q = h < a.n_q_heads, is_v = h >= a.n_q_heads + a.n_kv_heads;
       const uint4 raw = x[e];
       uint4 out = raw;
+      float v[8];
+      if (Q8) unpack<T>(raw, v);
       if (__any_sync(0xffffffffu, on && !is_v)) {
-        float v[8], t[8];
-        unpack<T>(raw, v);
+        float t[8];
+        if (!Q8) unpack<T>(raw, v);
         float r = 1.f;
         if (__any_sync(0xffffffffu, is_q ? q_norm : k_norm)) {
           float ss = 0.f;
@@ -200,13 +224,35 @@ __global__ void __launch_bounds__(kRopeThreads, U == 1 ? 5 : 4) qk_rope_kernel(c
           }
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = t[i] * r;
+        for (int i = 0; i < 8; ++i)
+          if (!Q8 || !is_v) v[i] = t[i] * r;
         if (!is_v)
           out = make_uint4(Pack<T>::from(v[0], v[1]), Pack<T>::from(v[2], v[3]), Pack<T>::from(v[4], v[5]),
                            Pack<T>::from(v[6], v[7]));
       }
+      const uint4 q_out = out;
+      if (Q8 && __any_sync(0xffffffffu, on && !is_q)) {
+        float most = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float m = fabsf(v[i]);
+          if (m < INFINITY) most = fmaxf(most, m); else v[i] = __int_as_float(0x7FFFFFFF);
+        }
+#pragma unroll
+        for (int d = kGroup / 2; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+        const uint32_t code = scale_exponent(most);
+        const float inv = __uint_as_float((254u - code) << 23);
+        out.x = e4m3_pair(v[0] * inv, v[1] * inv) | e4m3_pair(v[2] * inv, v[3] * inv) << 16;
+        out.y = e4m3_pair(v[4] * inv, v[5] * inv) | e4m3_pair(v[6] * inv, v[7] * inv) << 16;
+        out.z = code;
+      }
       if (on && is_q) {
-        *reinterpret_cast<uint4*>(q_row + e * kGroups * HD) = out;
+        *reinterpret_cast<uint4*>(q_row + e * kGroups * HD) = q_out;
+      } else if (Q8 && on && write) {
+        const int kh = h - a.n_q_heads - (is_v ? a.n_kv_heads : 0);
+        uint8_t* cache = reinterpret_cast<uint8_t*>(is_v ? a.v_cache : a.k_cache);
+        *reinterpret_cast<uint2*>(cache + cache_at + kh * (kPageTok * HD)) = make_uint2(out.x, out.y);
+        if (l == 0) (is_v ? a.v_scale : a.k_scale)[(slot_now >> 4) * a.scale_stride + kh * kPageTok + (slot_now & (kPageTok - 1))] = (uint8_t)out.z;
       } else if (on && write) {
         const int kh = h - a.n_q_heads - (is_v ? a.n_kv_heads : 0);
         T* cache = reinterpret_cast<T*>(is_v ? a.v_cache : a.k_cache);
@@ -219,26 +265,31 @@ __global__ void __launch_bounds__(kRopeThreads, U == 1 ? 5 : 4) qk_rope_kernel(c
   }
 }
 
-template <typename T, int HD, int U>
+template <typename T, int HD, int U, bool Q8>
 static void launch_items(const QkRopeArgs& a, int most, cudaStream_t s) {
   constexpr int kTake = U * kRopeThreads / (HD / 8);
   const int chunks = (a.n_q_heads + 2 * a.n_kv_heads + kTake - 1) / kTake;
   const int across = most / chunks < 1 ? 1 : most / chunks;
-  launch_in_turn(qk_rope_kernel<T, HD, U>, dim3(a.n_tokens < across ? a.n_tokens : across, chunks), kRopeThreads, 0, 0, s, a);
+  launch_in_turn(qk_rope_kernel<T, HD, U, Q8>, dim3(a.n_tokens < across ? a.n_tokens : across, chunks), kRopeThreads, 0, 0, s, a);
 }
 
-template <typename T, int HD>
+template <typename T, int HD, bool Q8>
 static void run_rope(const QkRopeArgs& a, cudaStream_t s) {
   // few tokens: a head a lane group, so that no thread works in turns; many: as
   // many as a lane can have in flight
-  if (a.n_tokens <= 304) launch_items<T, HD, 1>(a, 152 * 5, s); else launch_items<T, HD, kRopeHeads>(a, 152 * 4, s);
+  if (a.n_tokens <= 304) launch_items<T, HD, 1, Q8>(a, 152 * 5, s); else launch_items<T, HD, kRopeHeads, Q8>(a, 152 * 4, s);
+}
+
+template <typename T, int HD>
+static void run_cache(const QkRopeArgs& a, cudaStream_t s) {
+  if (a.k_scale) run_rope<T, HD, true>(a, s); else run_rope<T, HD, false>(a, s);
 }
 
 void launch_qk_rope(const QkRopeArgs& a, cudaStream_t s) {
   if (a.dtype == DT_BF16) {
-    if (a.head_dim == 128) run_rope<__nv_bfloat16, 128>(a, s); else run_rope<__nv_bfloat16, 64>(a, s);
+    if (a.head_dim == 128) run_cache<__nv_bfloat16, 128>(a, s); else run_cache<__nv_bfloat16, 64>(a, s);
   } else {
-    if (a.head_dim == 128) run_rope<__half, 128>(a, s); else run_rope<__half, 64>(a, s);
+    if (a.head_dim == 128) run_cache<__half, 128>(a, s); else run_cache<__half, 64>(a, s);
   }
 }
 

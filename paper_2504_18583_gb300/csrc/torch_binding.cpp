@@ -17,11 +17,12 @@
 #include <string>
 #include <utility>
 
-#include "pard.h"
+#include "pard_serve.h"
 
 namespace {
 
 constexpr int64_t kPage = 16;
+constexpr int64_t kHead = 4096;  // bytes of the chunk attention's workspace that have to be zero at first
 PyObject* g_error = nullptr;  // pard.PardError
 
 struct Refuse {  // becomes a ValueError
@@ -80,6 +81,33 @@ int64_t cache_stride(const at::Tensor& t, const char* name, at::ScalarType type,
     throw Refuse{std::string(name) + ": each page must be a contiguous [kv_heads, 16, head_dim] block"};
   return t.size(0) > 1 ? t.stride(0) : std::max(t.stride(0), h * kPage * d);
 }
+
+// exponents of an 8-bit cache [pages, kv_heads, 16], whose pages may lie apart: bytes from one to the next
+int64_t scale_stride_of(const at::Tensor& t, const char* name, const at::Tensor& cache, const Where& w) {
+  if (t.dim() != 3 || (t.scalar_type() != at::kFloat8_e8m0fnu && t.scalar_type() != at::kByte) || !t.is_cuda() ||
+      t.get_device() != w.dev || t.size(0) != cache.size(0) || t.size(1) != cache.size(1) || t.size(2) != kPage)
+    throw Refuse{std::string(name) + ": want [pages, kv_heads, 16] of float8_e8m0fnu or uint8 on the same device"};
+  if (t.stride(2) != 1 || (t.size(1) > 1 && t.stride(1) != kPage))
+    throw Refuse{std::string(name) + ": each page must be a contiguous [kv_heads, 16] block"};
+  return t.size(0) > 1 ? t.stride(0) : std::max(t.stride(0), t.size(1) * kPage);
+}
+// A pair of caches, of `type` or of 8 bits with their exponents.
+struct Caches {
+  int64_t stride, scale_stride = 0;
+  uint8_t *k_scale = nullptr, *v_scale = nullptr;
+  Caches(const at::Tensor& kc, const at::Tensor& vc, PyObject* ks, PyObject* vs, at::ScalarType type, const Where& w) {
+    if ((ks == Py_None) != (vs == Py_None)) throw Refuse{"k_scale and v_scale: want both or neither"};
+    if (ks != Py_None) type = at::kFloat8_e4m3fn;
+    stride = cache_stride(kc, "k_cache", type, w);
+    if (cache_stride(vc, "v_cache", type, w) != stride || vc.sizes() != kc.sizes()) throw Refuse{"the caches disagree on heads, head_dim, pages or page stride"};
+    if (ks == Py_None) return;
+    const at::Tensor &k = tensor_of(ks, "k_scale"), &v = tensor_of(vs, "v_scale");
+    scale_stride = scale_stride_of(k, "k_scale", kc, w);
+    if (scale_stride_of(v, "v_scale", kc, w) != scale_stride) throw Refuse{"k_scale and v_scale disagree on page stride"};
+    k_scale = static_cast<uint8_t*>(k.data_ptr());
+    v_scale = static_cast<uint8_t*>(v.data_ptr());
+  }
+};
 
 long whole(PyObject* o, const char* name) {
   const long v = PyLong_AsLong(o);
@@ -150,7 +178,7 @@ PyObject* tree_plan(PyObject* const* a, Py_ssize_t n) {
 }
 
 PyObject* qk_norm_rope(PyObject* const* a, Py_ssize_t n) {
-  count_is(n, 13);
+  count_is(n, 15);
   const at::Tensor& qkv = tensor_of(a[0], "qkv");
   const Where w(qkv, "qkv");
   const at::ScalarType type = qkv.scalar_type();
@@ -159,10 +187,9 @@ PyObject* qk_norm_rope(PyObject* const* a, Py_ssize_t n) {
   const int64_t T = qkv.size(0), width = qkv.size(1);
   const long Hq = whole(a[1], "n_q_heads"), Hkv = whole(a[2], "n_kv_heads");
   const at::Tensor &kc = tensor_of(a[5], "k_cache"), &vc = tensor_of(a[6], "v_cache");
-  const int64_t stride = cache_stride(kc, "k_cache", type, w);
+  const Caches c(kc, vc, a[13], a[14], type, w);
   const int64_t hd = kc.size(3);
-  if (cache_stride(vc, "v_cache", type, w) != stride || vc.sizes() != kc.sizes() || kc.size(1) != Hkv ||
-      width != (Hq + 2 * Hkv) * hd)
+  if (kc.size(1) != Hkv || width != (Hq + 2 * Hkv) * hd)
     throw Refuse{"qkv and caches disagree on heads, head_dim, pages or page stride"};
   int64_t half = 0;
   if (a[7] != Py_None) {
@@ -178,10 +205,17 @@ PyObject* qk_norm_rope(PyObject* const* a, Py_ssize_t n) {
   const int interleaved = PyObject_IsTrue(a[11]);
   if (interleaved < 0) throw Raised{};
   at::Tensor q = at::empty({T, Hq, hd}, w.options(type));
-  done(pard_qk_norm_rope(qkv.data_ptr(), T > 1 ? qkv.stride(0) : std::max(width, qkv.stride(0)), code, T, Hq, Hkv, hd, d_qg,
-                         d_kg, (float)eps, d_pos, d_slots, d_freq, 2 * half, interleaved, (float)amplitude, q.data_ptr(),
-                         Hq * hd, kc.data_ptr(), vc.data_ptr(), stride, kc.size(0), w.stream),
-       "pard_qk_norm_rope");
+  const int64_t row = T > 1 ? qkv.stride(0) : std::max(width, qkv.stride(0));
+  if (c.k_scale)
+    done(pard_qk_norm_rope_quantized(qkv.data_ptr(), row, code, T, Hq, Hkv, hd, d_qg, d_kg, (float)eps, d_pos, d_slots, d_freq,
+                                     2 * half, interleaved, (float)amplitude, q.data_ptr(), Hq * hd, kc.data_ptr(),
+                                     vc.data_ptr(), c.stride, c.k_scale, c.v_scale, c.scale_stride, kc.size(0), w.stream),
+         "pard_qk_norm_rope_quantized");
+  else
+    done(pard_qk_norm_rope(qkv.data_ptr(), row, code, T, Hq, Hkv, hd, d_qg, d_kg, (float)eps, d_pos, d_slots, d_freq, 2 * half,
+                           interleaved, (float)amplitude, q.data_ptr(), Hq * hd, kc.data_ptr(), vc.data_ptr(), c.stride,
+                           kc.size(0), w.stream),
+         "pard_qk_norm_rope");
   return wrap(std::move(q));
 }
 
@@ -239,6 +273,103 @@ PyObject* tree_attention(PyObject* const* a, Py_ssize_t n) {
                            d_table, P, d_ctx, d_nodes, reinterpret_cast<const uint64_t*>(d_mask), (float)scale,
                            out.data_ptr(), workspace.data_ptr(), workspace.nbytes(), w.stream),
        "pard_tree_attention");
+  return wrap(std::move(out));
+}
+
+PyObject* chunk_attention(PyObject* const* a, Py_ssize_t n) {
+  count_is(n, 14);
+  const at::Tensor& q = tensor_of(a[0], "q");
+  const Where w(q, "q");
+  const at::ScalarType type = q.scalar_type();
+  const int code = type_code(type, false, "q");
+  dim_of(q, 3, "q");
+  const int64_t T = q.size(0), Hq = q.size(1), hd = q.size(2), token = T > 1 ? q.stride(0) : Hq * hd;
+  if (q.stride(2) != 1 || (Hq > 1 && q.stride(1) != hd)) throw Refuse{"q: a token's heads must be contiguous"};
+  const at::Tensor &kc = tensor_of(a[1], "k_cache"), &vc = tensor_of(a[2], "v_cache");
+  const Caches c(kc, vc, a[9], a[10], type, w);
+  if (kc.size(3) != hd) throw Refuse{"q and caches disagree on head_dim"};
+  dim_of(tensor_of(a[3], "page_table"), 2, "page_table");
+  const int64_t B = THPVariable_Unpack(a[3]).size(0), P = THPVariable_Unpack(a[3]).size(1), Hkv = kc.size(1);
+  const auto* d_table = w.want<int32_t>(a[3], "page_table", at::kInt, {B, P});
+  const auto* d_starts = w.want<int32_t>(a[4], "starts", at::kInt, {B + 1});
+  const auto* d_ctx = w.want<int32_t>(a[5], "ctx_len", at::kInt, {B});
+  const double scale = a[6] == Py_None ? 1.0 / std::sqrt((double)hd) : real(a[6]);
+  const long window = whole(a[7], "window"), sinks = whole(a[8], "sinks");
+  at::Tensor out, workspace;
+  if (a[11] == Py_None) out = at::empty({T, Hq, hd}, w.options(type));
+  else { w.want(a[11], "out", type, {T, Hq, hd}); out = THPVariable_Unpack(a[11]); }
+  const int64_t need = std::max<int64_t>((int64_t)pard_chunk_attention_workspace_bytes(T, B, Hq, Hkv, hd), kHead);
+  const int capturing = PyObject_IsTrue(a[13]);
+  if (a[12] != Py_None) {
+    workspace = tensor_of(a[12], "workspace");
+    if (!workspace.is_cuda() || workspace.get_device() != w.dev || !workspace.is_contiguous())
+      throw Refuse{"workspace: want a contiguous tensor on the same device"};
+  } else if (capturing) {  // a graph may run beside later calls: its calls have their own
+    workspace = at::empty({need}, w.options(at::kByte));
+    workspace.narrow(0, 0, kHead).zero_();
+  } else {
+    at::Tensor& shared = workspace_of(w.dev, w.stream);
+    if (!shared.defined() || shared.numel() < need) shared = at::zeros({need}, w.options(at::kByte));
+    workspace = shared;
+  }
+  done(pard_chunk_attention(q.data_ptr(), token, code, T, B, Hq, Hkv, hd, kc.data_ptr(), vc.data_ptr(), c.stride, c.k_scale,
+                            c.v_scale, c.scale_stride, kc.size(0), d_table, P, d_starts, d_ctx, window, sinks, (float)scale,
+                            out.data_ptr(), workspace.data_ptr(), workspace.nbytes(), w.stream),
+       "pard_chunk_attention");
+  return wrap(std::move(out));
+}
+
+PyObject* adjust_logits(PyObject* const* a, Py_ssize_t n) {
+  count_is(n, 13);
+  const at::Tensor& z = tensor_of(a[0], "logits");
+  const Where w(z, "logits");
+  const at::ScalarType type = z.scalar_type();
+  const int code = type_code(type, true, "logits");
+  if (z.dim() != 2 || z.stride(1) != 1) throw Refuse{"logits: want [rows, vocab] with contiguous rows"};
+  const int64_t R = z.size(0), V = z.size(1);
+  // how many sequences the rows belong to: what is given a sequence says so, else one a row
+  static const char* const names[] = {"logits", "history", "hist_len", "prompt_len", "repetition", "frequency", "presence",
+                                      "bias_ids", "bias", "allowed", "tokens", "mask", "out"};
+  int64_t B = R;
+  for (int i : {1, 2, 3, 4, 5, 6, 7, 8, 10, 11})
+    if (a[i] != Py_None) {
+      const at::Tensor& t = tensor_of(a[i], names[i]);
+      if (t.dim() < 1) throw Refuse{std::string(names[i]) + ": want its first dimension to count sequences"};
+      B = t.size(0);
+      break;
+    }
+  if (B < 1 ? R != 0 : R % B != 0) throw Refuse{"logits: " + std::to_string(R) + " rows are no multiple of " + std::to_string(B) + " sequences"};
+  const int64_t N = B < 1 ? 0 : R / B;
+  int64_t L = 0, M = 0;
+  if ((a[1] == Py_None) != (a[2] == Py_None)) throw Refuse{"history and hist_len: want both or neither"};
+  if ((a[7] == Py_None) != (a[8] == Py_None)) throw Refuse{"bias_ids and bias: want both or neither"};
+  if ((a[10] == Py_None) != (a[11] == Py_None)) throw Refuse{"tokens and mask: want both or neither"};
+  if (a[1] != Py_None) { dim_of(tensor_of(a[1], "history"), 2, "history"); L = THPVariable_Unpack(a[1]).size(1); }
+  if (a[7] != Py_None) { dim_of(tensor_of(a[7], "bias_ids"), 2, "bias_ids"); M = THPVariable_Unpack(a[7]).size(1); }
+  const auto* d_history = w.want_or_none<int32_t>(a[1], "history", at::kInt, {B, L});
+  const auto* d_len = w.want_or_none<int32_t>(a[2], "hist_len", at::kInt, {B});
+  const auto* d_prompt = w.want_or_none<int32_t>(a[3], "prompt_len", at::kInt, {B});
+  const auto* d_rep = w.want_or_none<float>(a[4], "repetition", at::kFloat, {B});
+  const auto* d_freq = w.want_or_none<float>(a[5], "frequency", at::kFloat, {B});
+  const auto* d_pres = w.want_or_none<float>(a[6], "presence", at::kFloat, {B});
+  const auto* d_ids = w.want_or_none<int32_t>(a[7], "bias_ids", at::kInt, {B, M});
+  const auto* d_bias = w.want_or_none<float>(a[8], "bias", at::kFloat, {B, M});
+  const auto* d_allowed = w.want_or_none<int32_t>(a[9], "allowed", at::kInt, {R, (V + 31) / 32});
+  const auto* d_tokens = w.want_or_none<int32_t>(a[10], "tokens", at::kInt, {B, N});
+  const auto* d_mask = w.want_or_none<int64_t>(a[11], "mask", at::kLong, {B, N, (N + 63) / 64});
+  at::Tensor out;
+  if (a[12] == Py_None) {
+    out = at::empty({R, V}, w.options(type));
+  } else {
+    out = tensor_of(a[12], "out");
+    if (out.scalar_type() != type || out.sizes() != z.sizes() || !out.is_cuda() || out.get_device() != w.dev || out.stride(1) != 1)
+      throw Refuse{"out: want contiguous rows of the logits' type and shape on the same device"};
+  }
+  done(pard_adjust_logits(z.data_ptr(), R > 1 ? z.stride(0) : std::max(V, z.stride(0)), code, B, N, V, d_history, L, d_len,
+                          d_prompt, d_rep, d_freq, d_pres, d_ids, d_bias, M, reinterpret_cast<const uint32_t*>(d_allowed),
+                          d_tokens, reinterpret_cast<const uint64_t*>(d_mask), out.data_ptr(),
+                          R > 1 ? out.stride(0) : std::max(V, out.stride(0)), w.stream),
+       "pard_adjust_logits");
   return wrap(std::move(out));
 }
 
@@ -305,6 +436,8 @@ PyMethodDef g_methods[] = {method<tree_plan>("tree_plan"),
                            method<qk_norm_rope>("qk_norm_rope"),
                            method<tree_attention>("tree_attention"),
                            method<shared_workspace>("shared_workspace"),
+                           method<chunk_attention>("chunk_attention"),
+                           method<adjust_logits>("adjust_logits"),
                            method<sample>("sample"),
                            method<tree_commit>("tree_commit"),
                            {"set_error", set_error, METH_O, nullptr},

@@ -79,6 +79,9 @@ struct QkRopeArgs {
   const float* inv_freq;
   void *q, *k_cache, *v_cache;
   int64_t q_stride, page_stride;
+  // an 8-bit cache's exponents, [page][head][16] bytes (null: the caches are of `dtype`)
+  uint8_t *k_scale = nullptr, *v_scale = nullptr;
+  int64_t scale_stride = 0;
 };
 void launch_qk_rope(const QkRopeArgs& a, cudaStream_t s);
 

@@ -98,11 +98,19 @@ def lib() -> ctypes.CDLL:
         L.pard_sample.argtypes = [vp, i64, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp]
         L.pard_tree_commit.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, vp, i64, i64, i64, i32, i32, i32, i32,
                                        vp, vp, vp, vp]
+        L.pard_qk_norm_rope_quantized.argtypes = [vp, i64, i32, i32, i32, i32, i32, vp, vp, f32, vp, vp, vp, i32, i32, f32,
+                                                  vp, i64, vp, vp, i64, vp, vp, i64, i32, vp]
+        L.pard_chunk_attention_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
+        L.pard_chunk_attention_workspace_bytes.restype = sz
+        L.pard_chunk_attention.argtypes = [vp, i64, i32, i32, i32, i32, i32, i32, vp, vp, i64, vp, vp, i64, i32, vp, i32,
+                                           vp, vp, i32, i32, f32, vp, vp, sz, vp]
+        L.pard_adjust_logits.argtypes = [vp, i64, i32, i32, i32, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp,
+                                         vp, i64, vp]
         for name in ("pard_load_weights", "pard_prefill", "pard_draft", "pard_draft_sequential", "pard_verify",
                      "pard_accept_commit", "pard_set_mask_ids", "pard_selftest_stalled_wait", "pard_cod_select",
                      "pard_set_logits", "pard_set_draft_logits", "pard_get_state", "pard_read_kv", "pard_last_status",
                      "pard_tree_plan", "pard_qk_norm_rope", "pard_tree_attention", "pard_sample",
-                     "pard_tree_commit"):
+                     "pard_tree_commit", "pard_qk_norm_rope_quantized", "pard_chunk_attention", "pard_adjust_logits"):
             getattr(L, name).restype = ctypes.c_int
         _lib = L
     return _lib

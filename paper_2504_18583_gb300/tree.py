@@ -14,6 +14,12 @@ head_dim] (bf16 or fp16)::
     accept_len, emitted, ctx_len = tree_commit(token.view(batch, width), tokens, parents, n_nodes, ctx_len,
                                                page_table, pool)
 
+Beside the tree, what a serving loop needs around that step: ``chunk_attention``
+reads prompts in pieces (or decodes token by token) over the same cache, with a
+sliding window and first tokens that stay visible; ``quantized_cache`` is an 8-bit
+form of it that ``qk_norm_rope`` writes and ``chunk_attention`` reads; and
+``adjust_logits`` applies penalties, biases and grammar masks before ``sample``.
+
 Every call enqueues its work on torch's current stream of the current device
 and allocates nothing but its outputs (and the attention's workspace, unless
 one is passed) from torch.  Tensors of another stream need torch's own
@@ -98,16 +104,31 @@ def rope_frequencies(rot_dim: int, theta: float = 10000.0, scaling: Optional[str
 
 
 def qk_norm_rope(qkv, n_q_heads: int, n_kv_heads: int, pos, slots, k_cache, v_cache, inv_freq, q_gain=None,
-                 k_gain=None, eps: float = 1e-6, interleaved: bool = False, amplitude: float = 1.0):
+                 k_gain=None, eps: float = 1e-6, interleaved: bool = False, amplitude: float = 1.0, k_scale=None,
+                 v_scale=None):
     """Norm and rotate the query and key heads of QKV rows, write keys and
     values to the paged caches (pard_qk_norm_rope).
 
     qkv [T, (Hq + 2 Hkv) * hd] bf16 or fp16, rows may lie apart; pos [T] int32;
     slots [T] int64; caches [pages, Hkv, 16, hd]; inv_freq [rot / 2] fp32
-    (rot_dim = 2 * its length; None: no rotation); gains [hd] or None.  Returns
-    the queries [T, Hq, hd]."""
+    (rot_dim = 2 * its length; None: no rotation); gains [hd] or None.  With
+    k_scale and v_scale [pages, Hkv, 16] (float8_e8m0fnu or uint8) the caches are
+    float8_e4m3fn and a token's head is stored as codes and a power of two
+    (pard_qk_norm_rope_quantized; quantized_cache makes one); tokens of a call
+    then need slots of their own.  Returns the queries [T, Hq, hd]."""
     return _ops.qk_norm_rope(qkv, n_q_heads, n_kv_heads, pos, slots, k_cache, v_cache, inv_freq, q_gain, k_gain, eps,
-                             interleaved, amplitude)
+                             interleaved, amplitude, k_scale, v_scale)
+
+
+def quantized_cache(n_pages: int, n_kv_heads: int, head_dim: int, device="cuda"):
+    """One layer's 8-bit cache: k_cache, v_cache [pages, Hkv, 16, hd] float8_e4m3fn, k_scale, v_scale [pages, Hkv, 16]
+    float8_e8m0fnu, all zeros (a token's head takes hd + 1 bytes of each; the entry is its code times its scale)."""
+    def zeros(*shape):
+        return torch.zeros(shape, dtype=torch.uint8, device=device)
+    shape = (n_pages, n_kv_heads, 16)
+    k, v = (zeros(*shape, head_dim).view(torch.float8_e4m3fn) for _ in range(2))
+    k_scale, v_scale = (zeros(*shape).view(torch.float8_e8m0fnu) for _ in range(2))
+    return k, v, k_scale, v_scale
 
 
 def tree_attention_workspace(batch: int, width: int, n_q_heads: int, n_kv_heads: int, head_dim: int, device="cuda"):
@@ -119,7 +140,8 @@ def tree_attention_workspace(batch: int, width: int, n_q_heads: int, n_kv_heads:
 
 
 def shared_workspace():
-    """The workspace that tree_attention calls without one use on the current stream; None before the first.
+    """The workspace that tree_attention and chunk_attention calls without one use on the current stream; None before
+    the first.
 
     Should a wait inside the kernel ever run out (2 s), that call's output is NaN, and so is that of every later call
     with the same workspace.  Once the cause is gone, ``shared_workspace().zero_()`` makes it fit for use again (a
@@ -141,6 +163,55 @@ def tree_attention(q, k_cache, v_cache, page_table, ctx_len, n_nodes, mask, scal
     given saves that).  Returns [B, N, Hq, hd]."""
     return _ops.tree_attention(q, k_cache, v_cache, page_table, ctx_len, n_nodes, mask, scale, out, workspace,
                                workspace is None and torch.cuda.is_current_stream_capturing())
+
+
+def chunk_attention_workspace(n_tokens: int, batch: int, n_q_heads: int, n_kv_heads: int, head_dim: int, device="cuda"):
+    """A workspace for chunk_attention calls of these sizes (or smaller), one at a time."""
+    n = pard.lib().pard_chunk_attention_workspace_bytes(n_tokens, batch, n_q_heads, n_kv_heads, head_dim)
+    if n == 0:
+        raise ValueError("chunk_attention does not support these sizes")
+    return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+def chunk_attention(q, k_cache, v_cache, page_table, starts, ctx_len, scale: Optional[float] = None, window: int = 0,
+                    sinks: int = 0, k_scale=None, v_scale=None, out=None, workspace=None):
+    """Attention of a batch's new tokens over their sequences' paged caches
+    (pard_chunk_attention): pieces of prompts, single tokens, or both.
+
+    q [T, Hq, hd] bf16 or fp16 (tokens may lie apart), rows starts[b] to
+    starts[b + 1] - 1 sequence b's, at positions ctx_len[b], ctx_len[b] + 1, ...,
+    their own keys and values in the cache already (qk_norm_rope); caches [pages,
+    Hkv, 16, hd] of q's type, or float8_e4m3fn with k_scale and v_scale [pages,
+    Hkv, 16]; page_table [B, P], starts [B + 1], ctx_len [B] int32.  A token at
+    position p sees the keys j <= p; with window > 0 only those with
+    p - j < window or j < sinks.  scale: 1 / sqrt(hd) unless given; workspace: of
+    chunk_attention_workspace (without one, calls share the stream's with
+    tree_attention: shared_workspace; a call that a CUDA graph captures gets its
+    own).  Returns [T, Hq, hd]; rows of no sequence are not written."""
+    return _ops.chunk_attention(q, k_cache, v_cache, page_table, starts, ctx_len, scale, window, sinks, k_scale, v_scale,
+                                out, workspace, workspace is None and torch.cuda.is_current_stream_capturing())
+
+
+def adjust_logits(logits, history=None, hist_len=None, prompt_len=None, repetition=None, frequency=None, presence=None,
+                  bias_ids=None, bias=None, allowed=None, tokens=None, mask=None, out=None):
+    """What requests ask of their logits before a token is drawn
+    (pard_adjust_logits): penalties, biases and a grammar's mask.
+
+    logits [B * N, V] fp32, bf16 or fp16 (rows may lie apart), N rows a sequence:
+    its next token's, or its tree's nodes'.  For each sequence: history [B, L]
+    int32, of which the first hist_len [B] count and the first prompt_len [B] of
+    those are the prompt; repetition, frequency, presence [B] fp32; bias_ids
+    [B, M] int32 and bias [B, M] fp32.  For each row: allowed [B * N, ceil(V / 32)]
+    int32, a clear bit forbids the token; tokens [B, N] int32 and mask of
+    tree_plan: a node's branch counts as generated.  Each may be None.
+
+        z / r if z > 0 else z r   for tokens of the history
+        - frequency * count - presence * (count > 0)   of what was generated
+        + biases, then -inf where not allowed
+
+    Returns [B * N, V] of the logits' type, or writes `out`, which may be logits."""
+    return _ops.adjust_logits(logits, history, hist_len, prompt_len, repetition, frequency, presence, bias_ids, bias,
+                              allowed, tokens, mask, out)
 
 
 def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None):
