@@ -17,13 +17,12 @@
 //
 // Roles: warp 0 loads keys, warp 2 values, warp 1 issues the products, warp 3
 // looks after values that not every row sees; two warpgroups take the softmax, a
-// thread a row.  Work goes in steps of 64 keys, half a tile: each group has two
-// score buffers of 64 columns beside its accumulator, and the scores of its step
-// after the next are asked for as soon as a buffer's probabilities have been
-// multiplied.  So a group always has a step to work on while the products of the
-// one before run, and the tensor cores one to multiply.  With more than 128 query
-// vectors each group has its own 128 of them and takes both halves of a tile,
-// else both have the same rows and a half each (their sums are joined at the end).
+// thread a row, half a tile (64 keys) at a time, so that the first half's product
+// runs under the second's softmax.  With more than 128 query vectors each group has
+// its own 128 of them and a buffer of scores, and one group's products run under
+// the other's softmax; else both have the same rows and a half of each tile (their
+// sums are joined at the end), and the scores of the next tile but one are asked
+// for as soon as a buffer is free.
 //
 // Masks touch only tiles that some row does not see whole: a row sees a run of
 // columns up to its own position, less those between the first tokens and its
@@ -76,8 +75,11 @@ __device__ __forceinline__ Chunk chunk_of(const ChunkAttnArgs& a, int ctx, int f
   s.blocks = (s.rows + rows_per_block - 1) / rows_per_block;
   return s;
 }
+// n / group for rows of a block counted from a token's first: n below group + 256
+__device__ __forceinline__ int in_group(const ChunkAttnArgs& a, int n) { return a.group_magic ? (int)__umulhi((uint32_t)n, a.group_magic) : n; }
 // One block's positions and tiles: tiles [0, sink) then [sink + skip, sink + skip + tiles - sink).
 struct Span {
+  int token, rest;        // of the first row: its token in the chunk, and its place among that one's rows
   int p_lo, p_hi, end;    // first and last row's positions; keys that the last row may see
   int sink, skip, tiles;
   __device__ __forceinline__ int tile(int k) const { return k < sink ? k : k + skip; }
@@ -86,8 +88,10 @@ __device__ __forceinline__ int window_from(const ChunkAttnArgs& a, int p) { retu
 __device__ __forceinline__ Span span_of(const ChunkAttnArgs& a, const Chunk& s, int block, int rows_per_block) {
   Span g;
   const int group = a.n_q_heads / a.n_kv_heads, r0 = block * rows_per_block;
-  g.p_lo = s.ctx + r0 / group;
-  g.p_hi = s.ctx + (min(r0 + rows_per_block, s.rows) - 1) / group;
+  g.token = r0 / group;
+  g.rest = r0 - g.token * group;
+  g.p_lo = s.ctx + g.token;
+  g.p_hi = g.p_lo + in_group(a, g.rest + min(rows_per_block, s.rows - r0) - 1);
   g.end = min(g.p_hi + 1, s.keys);
   const int last = (g.end + kTile - 1) / kTile;  // tiles up to the end (one at least: a table has a page)
   const int first = min(window_from(a, g.p_lo) / kTile, last - 1);
@@ -173,6 +177,11 @@ __device__ __forceinline__ uint32_t seen32(int key, int end, int from, int sinks
   return low_bits(end - key) & (~low_bits(from - key) | low_bits(sinks - key));
 }
 
+// The type of the products' operands: an 8-bit cache's entries are made fp16 ones
+// whatever the queries' type.
+template <typename T, bool Q8> struct OperandOf { using type = T; };
+template <typename T> struct OperandOf<T, true> { using type = __half; };
+
 // A value's entry, of a 16-bit cache or an 8-bit one.
 template <typename T, int HD, bool Q8>
 __device__ __forceinline__ float value_at(const ChunkAttnArgs& a, int64_t page, int head, int tok, int c) {
@@ -180,13 +189,7 @@ __device__ __forceinline__ float value_at(const ChunkAttnArgs& a, int64_t page, 
     return Num<T>::get(reinterpret_cast<const T*>(a.v_cache) + page * a.page_stride + ((int64_t)head * kPageTok + tok) * HD + c);
   const uint32_t code = reinterpret_cast<const uint8_t*>(a.v_cache)[page * a.page_stride + ((int64_t)head * kPageTok + tok) * HD + c];
   const uint32_t e = a.v_scale[page * a.scale_stride + (int64_t)head * kPageTok + tok];
-  if ((code & 0x7F) == 0x7F || e == 255u) return __int_as_float(0x7FFFFFFF);
-  const int ex = code >> 3 & 15, m = code & 7;
-  float x = ldexpf(ex ? (float)(8 + m) : (float)m, max(ex, 1) - 10 + (int)e - 127);
-  if (Num<T>::kFormat == 0) x = fminf(x, 65504.f);  // fp16: held there, as the product's operand is
-  const uint32_t y = Num<T>::pack(code & 0x80 ? -x : x, 0.f);
-  const uint16_t z = (uint16_t)y;
-  return Num<T>::get(&z);
+  return (code & 0x7F) == 0x7F || e == 255u ? __int_as_float(0x7FFFFFFF) : 0.f;  // (finite: as an operand it is held to 65504)
 }
 
 // Adds the infinities and NaN of the values of a part's tiles that not every row
@@ -218,51 +221,17 @@ __device__ __noinline__ void patch_chunk(const ChunkAttnArgs& a, const ChunkWalk
 }
 
 // ---- 8-bit entries into 16-bit ones -------------------------------------------
-// What multiplies a row's codes: a power of two in steps that stay in range.
-template <typename T> struct Widen;
-template <> struct Widen<__nv_bfloat16> {
-  // A code's bits moved into a bf16's are the value times 2^-120, subnormal codes
-  // too; two factors bring it back, the second 1 but for rows above 448 * 2^7.
-  uint32_t m1, m2;
-  bool far;
-  __device__ __forceinline__ void set(uint32_t e) {
-    const uint32_t x = e == 255u ? 0x7FFFu : (min(e, 134u) + 120u) << 7, y = e > 134u && e != 255u ? (e - 7u) << 7 : 0x3F80u;
-    m1 = x | x << 16;
-    m2 = y | y << 16;
-    far = e > 134u;
-  }
-  static __device__ __forceinline__ uint32_t mul(uint32_t x, uint32_t y) {
-    const __nv_bfloat162 p = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&x), *reinterpret_cast<const __nv_bfloat162*>(&y));
-    return *reinterpret_cast<const uint32_t*>(&p);
-  }
-  static __device__ __forceinline__ uint32_t move(uint32_t x) { return (x & 0x80008000u) | (x >> 4 & 0x07F007F0u); }
-  // four codes
-  __device__ __forceinline__ void four(uint32_t w, uint32_t& lo, uint32_t& hi) const {
-    lo = mul(move(__byte_perm(w, 0, 0x1404)), m1);
-    hi = mul(move(__byte_perm(w, 0, 0x3424)), m1);
-  }
-  __device__ __forceinline__ void four_far(uint32_t w, uint32_t& lo, uint32_t& hi) const {
-    four(w, lo, hi);
-    lo = mul(lo, m2);
-    hi = mul(hi, m2);
-    // codes that are NaN
-    if ((w & 0x7Fu) == 0x7Fu) lo |= 0x7FFFu;
-    if ((w >> 8 & 0x7Fu) == 0x7Fu) lo |= 0x7FFF0000u;
-    if ((w >> 16 & 0x7Fu) == 0x7Fu) hi |= 0x7FFFu;
-    if ((w >> 24 & 0x7Fu) == 0x7Fu) hi |= 0x7FFF0000u;
-  }
-  static __device__ __forceinline__ uint32_t odd(uint32_t w) { return ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }
-};
-template <> struct Widen<__half> {
-  // Codes are fp16 values; the factor is one where no product leaves the normal
-  // range, else the product is taken in 32 bits and held to 65504.
-  uint32_t m1;
+// A row's codes times its power of two, as fp16.  The conversion gives codes as they
+// are (NaN too), and the product with a power of two from 2^-14 to 2^7 stays a normal
+// fp16 power of two's, exact down to 2^-24; beyond that it is taken in 32 bits and
+// held to 65504.  (As bf16, with the bits moved and two products, an entry took three
+// times the instructions, and the tiles of 128 keys 14000 clocks against HBM's 1400.)
+struct Widen {
+  uint32_t m;
   float s;
-  bool far;
-  __device__ __forceinline__ void set(uint32_t e) {
-    far = e < 113u || e > 134u;
-    const uint32_t x = (min(max(e, 113u), 134u) - 112u) << 10;
-    m1 = x | x << 16;
+  __device__ __forceinline__ static bool far(uint32_t e) { return e - 113u > 21u; }
+  __device__ __forceinline__ void set(uint32_t e) { m = (e - 112u) * 0x04000400u; }
+  __device__ __forceinline__ void set_far(uint32_t e) {
     s = e == 255u ? __int_as_float(0x7FFFFFFF) : __uint_as_float(e ? e << 23 : 1u << 22);
   }
   static __device__ __forceinline__ uint32_t codes(uint32_t two) {
@@ -270,25 +239,17 @@ template <> struct Widen<__half> {
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(v) : "h"((uint16_t)two));
     return v;
   }
-  static __device__ __forceinline__ uint32_t mul(uint32_t x, uint32_t y) {
-    const __half2 p = __hmul2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&y));
+  __device__ __forceinline__ uint32_t near_two(uint32_t two) const {
+    const uint32_t x = codes(two);
+    const __half2 p = __hmul2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&m));
     return *reinterpret_cast<const uint32_t*>(&p);
   }
-  __device__ __forceinline__ void four(uint32_t w, uint32_t& lo, uint32_t& hi) const {
-    lo = mul(codes(w), m1);
-    hi = mul(codes(w >> 16), m1);
-  }
-  __device__ __forceinline__ uint32_t wide(uint32_t two) const {
+  __device__ __forceinline__ uint32_t far_two(uint32_t two) const {
     const uint32_t h = codes(two);
     const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
     auto held = [&](float x) { x *= s; return x > 65504.f ? 65504.f : x < -65504.f ? -65504.f : x; };  // (NaN stays)
     return Num<__half>::pack(held(f.x), held(f.y));
   }
-  __device__ __forceinline__ void four_far(uint32_t w, uint32_t& lo, uint32_t& hi) const {
-    lo = wide(w);
-    hi = wide(w >> 16);
-  }
-  static __device__ __forceinline__ uint32_t odd(uint32_t) { return 0u; }  // the conversion knows NaN
 };
 
 // What a CTA keeps in shared memory behind the operands.
@@ -296,14 +257,16 @@ template <int NK, int NV, bool Q8>
 struct ChunkControl {
   uint64_t k_full[NK], k_empty[NK], v_full[NV], v_empty[NV];
   uint64_t k_fit[NK], fixed[NV];  // a stage's keys (8-bit caches), values are fit for the product
-  uint64_t s_full[2][2];   // scores of a group are in one of its buffers
-  uint64_t p_full[2][2];   // their probabilities are, and O is scaled
-  uint64_t o_full[2][2];   // the product with a buffer's probabilities is done
+  uint64_t s_full[2];      // a tile's scores are in one of the two buffers
+  uint64_t p_full[2][2];   // the probabilities of one of its halves are, and O is scaled
+  uint64_t o_full[2][2];   // two blocks: a group's product with a tile's first half is done, with all of a segment's;
+                           // one: the product with its probabilities of a buffer is
   uint64_t ready[2];       // the group has read O and laid out its queries
   uint64_t pair, met[2];   // the two groups meet, a group's warps do
   uint64_t drain;          // every product is done
   alignas(16) uint8_t k_scale[Q8 ? NK * kTile : 16], v_scale[Q8 ? NV * kTile : 16];
   int2 seq[kSeqHeld + 1];  // sequences' context lengths and first rows
+  uint8_t back[Q8 ? 2 * kTile : 16];  // exponents of the queries' rows, which were scaled by them
   uint32_t tmem, last_in[2], odd[NV];  // odd: a stage's values that not all rows see held infinities or NaN (a byte a warp)
   int abort_flag, start_b, start_head, start_block, start_off;
   int sum[16], units[16], most[16];
@@ -328,8 +291,10 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
                            const __grid_constant__ CUtensorMap vmap) {
   constexpr int NK = ck_stages(HD, BLOCKS, Q8), NV = cv_stages(HD, BLOCKS, Q8), kStage = stage_bytes(HD);
   constexpr int kChunks = HD / 64, kChunkBytes = kTile * 128, kRows = kTile * BLOCKS, kThreads = chunk_threads(Q8);
-  constexpr uint32_t kIdescS = idesc16(Num<T>::kFormat, kTile, kStep, false);
-  constexpr uint32_t kIdescO = idesc16(Num<T>::kFormat, kTile, HD, true);
+  using M = typename OperandOf<T, Q8>::type;
+  constexpr bool kRaised = sizeof(T) == sizeof(M) && Num<T>::kFormat != Num<M>::kFormat;  // bf16 queries become fp16 ones, row by row scaled
+  constexpr uint32_t kIdescS = idesc16(Num<M>::kFormat, kTile, kTile, false);
+  constexpr uint32_t kIdescO = idesc16(Num<M>::kFormat, kTile, HD, true);
   extern __shared__ __align__(1024) uint8_t qbuf[];  // queries, then the rings
   uint8_t* kring = qbuf + BLOCKS * kStage;
   uint8_t* vring = kring + NK * kStage;
@@ -352,7 +317,7 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
     for (int i = 0; i < NV; ++i) { mbar_init(sh.v_full + i, 1); mbar_init(sh.v_empty + i, 1); mbar_init(sh.fixed + i, Q8 ? kConvWarps : 1); }
 #pragma unroll 1
     for (int i = 0; i < 2; ++i) {
-      mbar_init(sh.s_full[i], 1); mbar_init(sh.s_full[i] + 1, 1); mbar_init(sh.p_full[i], 4); mbar_init(sh.p_full[i] + 1, 4);
+      mbar_init(sh.s_full + i, 1); mbar_init(sh.p_full[i], 4); mbar_init(sh.p_full[i] + 1, 4);
       mbar_init(sh.o_full[i], 1); mbar_init(sh.o_full[i] + 1, 1); mbar_init(sh.ready + i, 4); mbar_init(sh.met + i, 4);
     }
     mbar_init(&sh.pair, 8);
@@ -629,92 +594,109 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
       }
     } else if (warp == 1) {
       // ---- products ---------------------------------------------------------------
+      // One lane issues, all wait.  A tile takes 32 products (128 columns: 2048 clocks),
+      // and what lies between them is the warp's own time, so it is kept short: stages
+      // and phases are counted along, addresses made the warp's (by a shuffle: the
+      // compiler then keeps them in uniform registers) once a tile, and steps add
+      // constants to a descriptor's low word.
       uint32_t ph_p = 0, ph_ready = 0;
-      const uint32_t q_addr = smem_u32(qbuf), k_addr = smem_u32(kring), v_addr = smem_u32(vring);
+      int kst = 0, vst = 0;
+      uint32_t kph = 0, vph = 0;
+      const uint32_t q_addr = smem_u32(qbuf) >> 4, k_addr = smem_u32(kring) >> 4, v_addr = smem_u32(vring) >> 4;
       uint64_t* keys_in = Q8 ? sh.k_fit : sh.k_full;
-      auto wait_k = [&](int i) { ok = ok && warp_wait(keys_in + i % NK, (i / NK) & 1, abort_flag); };
-      auto wait_v = [&](int i) { ok = ok && warp_wait(sh.fixed + i % NV, (i / NV) & 1, abort_flag); };
-      // Operand addresses go through a shuffle, which tells the compiler that they
-      // are the warp's and not a lane's, and steps add constants to a
-      // descriptor's low word: an issue then costs little beside its product.
+      const bool leader = elect_one();
       auto uniform = [](uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); };
+      const uint32_t tm = uniform(tmem);
       // Shared-memory descriptors, 128-byte swizzle.  Queries and keys: 128-byte
       // rows along K, eight-row atoms 1024 bytes apart.  Values: 64 of a key's
       // entries a row (N is contiguous), atoms of eight keys 1024 bytes apart along
       // K, the next 64 entries a chunk further.
       constexpr uint64_t kDescK = (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
       constexpr uint64_t kDescV = (uint64_t)(kChunkBytes >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
-      // tensor memory: the groups' score buffers, then their accumulators
-      auto scores = [&](int g, int h, int buf, int i) {  // of half h of tile i
-        const uint32_t qa = uniform((q_addr + (BLOCKS == 2 ? g * kStage : 0)) >> 4);
-        const uint32_t kb = uniform((k_addr + (i % NK) * kStage + h * kStep * 128) >> 4);
-        const uint32_t d = uniform(tmem + g * kTile + buf * kStep);
-        if (elect_one()) {
+      // tensor memory: two buffers of scores (two blocks: a group each; one: tiles in
+      // turn), then the groups' accumulators
+      auto scores = [&](int x, uint32_t kb) {  // of the keys at kb into buffer x
+        const uint32_t qa = q_addr + (BLOCKS == 2 ? x * (kStage >> 4) : 0), d = tm + x * kTile;
+        if (leader) {
 #pragma unroll
           for (int k = 0; k < HD / 16; ++k) {
             const uint32_t at = ((k / 4) * kChunkBytes + (k % 4) * 32) >> 4;
             umma_ss(d, kDescK | (qa + at), kDescK | (kb + at), kIdescS, k > 0);
           }
-          umma_commit(&sh.s_full[g][buf]);
+          umma_commit(sh.s_full + x);
         }
-        __syncwarp();
       };
-      auto outputs = [&](int g, int h, int buf, int i, bool first, int keys) {  // O += P V
-        const uint32_t vb = uniform((v_addr + (i % NV) * kStage + h * kStep * 128) >> 4);
-        const uint32_t o = uniform(tmem + 2 * kTile + g * HD), p = uniform(tmem + g * kTile + buf * kStep);
-        // keys past the end have probability 0: whole steps of 16 are left out, but
-        // for the first, which leaves zeros where there were none yet
-        const int steps = __shfl_sync(0xffffffffu, max(1, (keys - h * kStep + 15) / 16), 0);
-        const uint32_t bit = 2 * g + buf;
-        ok = ok && warp_wait(&sh.p_full[g][buf], ph_p >> bit & 1, abort_flag);
+      // O += P V of half h, whose probabilities are in buffer x.  Keys past the end have
+      // probability 0: whole steps of 16 are left out, but for the first, which leaves
+      // zeros where there were none yet.
+      auto outputs = [&](int g, int x, int h, uint32_t vb, bool first, int keys) {
+        const uint32_t o = tm + 2 * kTile + g * HD, p = tm + x * kTile + h * kStep, bit = 2 * x + h;
+        ok = ok && warp_wait(&sh.p_full[x][h], ph_p >> bit & 1, abort_flag);
         if (!ok) return;
         ph_p ^= 1u << bit;
         tc_fence_after();
-        if (elect_one()) {
+        if (leader) {
+          umma_ts(o, p, kDescV | (vb + h * 4 * 128), kIdescO, !first);
+          if (keys >= (h + 1) * kStep) {
 #pragma unroll
-          for (int k = 0; k < kStep / 16; ++k)
-            if (k < steps) umma_ts(o, p + k * 8, kDescV | (vb + k * 128), kIdescO, !first || k > 0);
-          umma_commit(&sh.o_full[g][buf]);
+            for (int k = 1; k < kStep / 16; ++k) umma_ts(o, p + k * 8, kDescV | (vb + (h * 4 + k) * 128), kIdescO, 1);
+          } else {
+#pragma unroll 1
+            for (int k = 1; k < kStep / 16; ++k)
+              if (keys > h * kStep + k * 16) umma_ts(o, p + k * 8, kDescV | (vb + (h * 4 + k) * 128), kIdescO, 1);
+          }
+          if (BLOCKS == 1) umma_commit(&sh.o_full[g][x]); else if (h == 0) umma_commit(&sh.o_full[g][0]);
         }
-        __syncwarp();
       };
       auto commit = [&](uint64_t* bar) {
-        if (elect_one()) umma_commit(bar);
-        __syncwarp();
+        if (leader) umma_commit(bar);
       };
       while (ok && next()) {
         const int n = w.t1 - w.t0;
-        auto keys_from = [&](int j) { return w.g.end - w.g.tile(w.t0 + j) * kTile; };  // of tile j's first on
+        const int last_keys = w.t1 == w.g.tiles ? w.g.end - w.g.tile(w.t1 - 1) * kTile : kTile;  // of the last tile
         ok = warp_wait(sh.ready + 0, ph_ready, abort_flag) && warp_wait(sh.ready + 1, ph_ready, abort_flag);
         ph_ready ^= 1;
         tc_fence_after();
-        // tile j's outputs, and the scores that go where its probabilities were:
-        // two blocks, of the next tile's same half; one, of the same half two tiles on
+        // tile j's outputs, and the scores that go where its probabilities were: two
+        // blocks, of the next tile; one, of the tile after the next
         constexpr int kAhead = BLOCKS == 2 ? 1 : 2;
 #pragma unroll 1
         for (int j = -kAhead; j < n && ok; ++j) {
-          const int i = tile0 + j, keys = j >= 0 ? keys_from(j) : 0;
           const bool more = j + kAhead < n;
-          if (j >= 0) wait_v(i);
+          const int keys = j == n - 1 ? last_keys : kTile;
+          const uint32_t kb = uniform(k_addr + kst * (kStage >> 4)), vb = uniform(v_addr + vst * (kStage >> 4));
+          if (j >= 0) ok = warp_wait(sh.fixed + vst, vph, abort_flag);
           if (!ok) break;
 #pragma unroll
-          for (int e = 0; e < 2 * BLOCKS; ++e) {
-            const int g = e & 1, h = BLOCKS == 2 ? e >> 1 : g, buf = BLOCKS == 2 ? h : (j & 1);
-            if (j >= 0) outputs(g, h, buf, i, j == 0 && (BLOCKS == 1 || h == 0), keys);
+          for (int e = 0; e < BLOCKS; ++e) {
+            const int x = BLOCKS == 2 ? e : j & 1;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              if (j >= 0) outputs(BLOCKS == 2 ? e : h, x, h, vb, j == 0 && (BLOCKS == 1 || h == 0), keys);
             // (asked for here, since the load of a stage that has just come free is
             // what a step would wait for)
-            if (more && e == 0) wait_k(i + kAhead);
+            if (more && e == 0) ok = ok && warp_wait(keys_in + kst, kph, abort_flag);
             if (!ok) break;
-            if (more) scores(g, h, buf, i + kAhead);
+            if (more) scores(x, kb);
           }
           if (!ok) break;
-          if (j >= 0) commit(sh.v_empty + i % NV);
-          if (more) commit(sh.k_empty + (i + kAhead) % NK);
+          if (j >= 0) {
+            commit(sh.v_empty + vst);
+            if (++vst == NV) { vst = 0; vph ^= 1; }
+          }
+          if (more) {
+            commit(sh.k_empty + kst);
+            if (++kst == NK) { kst = 0; kph ^= 1; }
+          }
         }
-        tile0 += n;
+        if (BLOCKS == 2 && ok) {
+          commit(&sh.o_full[0][1]);
+          commit(&sh.o_full[1][1]);
+        }
       }
       if (!ok) *abort_flag = 1;
       // products in flight read shared memory and write tensor memory: let them end
+      __syncwarp();
       commit(&sh.drain);
       mbar_drain(&sh.drain, 0);
     } else if (!Q8) {
@@ -733,19 +715,26 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
             const int used = min(kTile, max(kStep + 16, (end + 15) & ~15));
             constexpr int kPieces = HD / 8;
             bool any = false;
-#pragma unroll 4
-            for (int p = lane; p < used * kPieces; p += 32) {
-              const int r = p / kPieces, c = p % kPieces;
-              if (all_see(a, w.s, w.g.p_lo, w.g.p_hi, k0 + r, k0 + r + 1)) continue;
-              uint4* at = reinterpret_cast<uint4*>(vring + st * kStage + (c / 8) * kChunkBytes + r * 128 + (((c % 8) ^ (r & 7)) << 4));
-              const uint4 v = *at;
-              const uint4 f = r >= end ? make_uint4(0, 0, 0, 0)
-                                       : make_uint4(finite_of<T>(v.x), finite_of<T>(v.y), finite_of<T>(v.z), finite_of<T>(v.w));
-              if (f.x != v.x || f.y != v.y || f.z != v.z || f.w != v.w) {
-                *at = f;
-                any |= r < end;
+            auto clean = [&](int r0, int r1) {
+#pragma unroll 8
+              for (int p = r0 * kPieces + lane; p < r1 * kPieces; p += 32) {
+                const int r = p / kPieces, c = p % kPieces;
+                uint4* at = reinterpret_cast<uint4*>(vring + st * kStage + (c / 8) * kChunkBytes + r * 128 + (((c % 8) ^ (r & 7)) << 4));
+                const uint4 v = *at;
+                const uint4 f = r >= end ? make_uint4(0, 0, 0, 0)
+                                         : make_uint4(finite_of<M>(v.x), finite_of<M>(v.y), finite_of<M>(v.z), finite_of<M>(v.w));
+                if (f.x != v.x || f.y != v.y || f.z != v.z || f.w != v.w) {
+                  *at = f;
+                  any |= r < end;
+                }
               }
-            }
+            };
+            // rows that the last of the block's rows has in its window, or that are among the first
+            // tokens, and that the first row's position reaches, are left alone
+            const int reach = min(max(min(w.g.p_lo + 1, w.s.keys) - k0, 0), used);
+            const int from = min(max(window_from(a, w.g.p_hi) - k0, 0), reach), sinks = min(max(a.sinks - k0, 0), from);
+            clean(sinks, from);
+            clean(reach, used);
             fence_proxy_async_all();
             any = __any_sync(0xffffffffu, any);
             if (lane == 0) sh.odd[st] = any;
@@ -761,11 +750,11 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
     // ---- softmax: group g, a thread a row --------------------------------------------
     const int g = (warp - 4) >> 2, t = tid - 128 - g * kTile;  // t: row of the score tile = lane of tensor memory
     const uint32_t my = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-    const uint32_t s_addr = my + g * kTile, o_addr = my + 2 * kTile + g * HD;
-    const float sl2 = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1e-30f);  // a masked score stays -inf at scale 0
+    const uint32_t o_addr = my + 2 * kTile + g * HD;
+    const float sl2_all = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1.2e-38f);  // a masked score stays -inf at scale 0
     const bool wide_out = (reinterpret_cast<uintptr_t>(a.out) & 31) == 0;
     uint32_t ph_s = 0, ph_pair = 0, ph_met = 0;
-    int handed[2] = {0, 0};  // probabilities handed over so far, by buffer
+    uint32_t ph_o[2] = {0, 0};  // phases of o_full that come next
     auto meet = [&] {  // both groups, 256 threads
       __syncwarp();
       if (lane == 0) mbar_arrive(&sh.pair);
@@ -782,23 +771,44 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
       const int n = w.t1 - w.t0;
       const int row_base = w.block * kRows + (BLOCKS == 2 ? g * kTile : 0);  // row of the unit that lane 0 of the group has
       const int row = row_base + t, rows = w.s.rows;
+      const bool live = row_base + (warp & 3) * 32 < rows;  // the warp has a row at all
       // queries into shared memory, swizzled; one block: each group lays out half
       {
-        constexpr int kPieces = HD / 8, kMine = BLOCKS == 2 ? kTile : kTile / 2, kStep = kTile / kPieces;
+        constexpr int kPieces = HD / 8, kMine = BLOCKS == 2 ? kTile : kTile / 2, kEach = kTile / kPieces;
         const uint32_t sign = a.scale < 0.f ? 0x80008000u : 0u;  // a negative scale turns the queries' signs
-        const int c = t % kPieces, r0 = t / kPieces + (BLOCKS == 2 ? 0 : g * kMine);
-        const T* q = reinterpret_cast<const T*>(a.q) + (int64_t)w.s.row0 * a.q_stride + (int64_t)w.head * group * HD + c * 8;
+        const int c = t % kPieces, r0 = t / kPieces + (BLOCKS == 2 ? 0 : g * kMine), in_unit = BLOCKS == 2 ? g * kTile : 0;
+        const T* q = reinterpret_cast<const T*>(a.q) + ((int64_t)w.s.row0 + w.g.token) * a.q_stride + (int64_t)w.head * group * HD + c * 8;
         uint8_t* dst = qbuf + (BLOCKS == 2 ? g * kStage : 0) + (c / 8) * kChunkBytes;
-        uint4 v[kMine / kStep];  // all loads are out before the first is stored
+        uint4 v[kMine / kEach];  // all loads are out before the first is stored
 #pragma unroll
-        for (int i = 0; i < kMine / kStep; ++i) {
-          const int r = row_base + r0 + i * kStep, token = r / group;
+        for (int i = 0; i < kMine / kEach; ++i) {
+          const int n_row = w.g.rest + in_unit + r0 + i * kEach, tok = in_group(a, n_row);
           v[i] = make_uint4(0, 0, 0, 0);
-          if (r < rows) v[i] = *reinterpret_cast<const uint4*>(q + (int64_t)token * a.q_stride + (r - token * group) * HD);
+          if (row_base + r0 + i * kEach < rows) v[i] = *reinterpret_cast<const uint4*>(q + (int64_t)tok * a.q_stride + (n_row - tok * group) * HD);
         }
 #pragma unroll
-        for (int i = 0; i < kMine / kStep; ++i) {
-          const int r = r0 + i * kStep;
+        for (int i = 0; i < kMine / kEach; ++i) {
+          const int r = r0 + i * kEach;
+          if constexpr (kRaised) {
+            // bf16 queries as fp16, each row times the power of two that brings its
+            // largest entry into [2^14, 2^15): exact down to 2^-39 of it
+            float most = 0.f, f[8];
+            const uint32_t in[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              f[k] = __uint_as_float(k & 1 ? in[k / 2] & 0xFFFF0000u : in[k / 2] << 16);
+              const float m = fabsf(f[k]);
+              if (m < INFINITY) most = fmaxf(most, m);
+            }
+#pragma unroll
+            for (int d = kPieces / 2; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+            const int e = max((int)(__float_as_uint(most) >> 23), 15);  // biased exponent of the largest
+            const float up = __uint_as_float((uint32_t)(268 - e) << 23);  // 2^(14 - (e - 127))
+#pragma unroll
+            for (int k = 0; k < 8; ++k) f[k] *= up;
+            v[i] = make_uint4(Num<__half>::pack(f[0], f[1]), Num<__half>::pack(f[2], f[3]), Num<__half>::pack(f[4], f[5]), Num<__half>::pack(f[6], f[7]));
+            if (c == 0) sh.back[in_unit + r] = (uint8_t)e;
+          }
           v[i].x ^= sign; v[i].y ^= sign; v[i].z ^= sign; v[i].w ^= sign;
           *reinterpret_cast<uint4*>(dst + r * 128 + (((c % 8) ^ (r & 7)) << 4)) = v[i];
         }
@@ -807,10 +817,18 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
         __syncwarp();
         if (lane == 0) mbar_arrive(sh.ready + g);
       }
-      const int token = min(row, rows - 1) / group, p = w.s.ctx + token;
+      float sl2 = sl2_all;
+      if constexpr (kRaised) {
+        if (BLOCKS == 1) meet(); else group_meet();  // the rows' exponents are there
+        if (!ok) break;
+        sl2 = fmaxf(sl2_all * __uint_as_float((uint32_t)max((int)sh.back[BLOCKS == 2 ? g * kTile + t : t] - 14, 1) << 23), 1.2e-38f);
+      }
+      const int n_row = w.g.rest + min(row, rows - 1) - w.block * kRows, in_token = in_group(a, n_row);  // of the block's first token on
+      const int token = w.g.token + in_token, p = w.s.ctx + token;
       const int see_end = min(p + 1, w.s.keys), see_from = window_from(a, p);
       // positions of the group's first and last rows
-      const int g_lo = w.s.ctx + min(row_base, rows - 1) / group, g_hi = w.s.ctx + min(row_base + kTile - 1, rows - 1) / group;
+      auto position = [&](int r) { return w.g.p_lo + in_group(a, w.g.rest + min(r, rows - 1) - w.block * kRows); };
+      const int g_lo = position(row_base), g_hi = position(row_base + kTile - 1);
       auto page_flag = [&](int j) -> uint32_t {  // this lane's page of tile j is one of the pool
         const int at = w.g.tile(w.t0 + j) * kTilePages + lane;
         if (lane >= kTilePages || at * kPageTok >= w.g.end) return 1;
@@ -818,94 +836,104 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
       };
       float m_ref = -INFINITY, sum = 0.f;
       bool patch = false;  // values that the rows who see them get back in the epilogue
-      // The product with the last probabilities handed over from a buffer is done (the
-      // one before it was before the buffer's scores came again, so that a barrier's
-      // one bit tells them apart).
-      auto o_done = [&](int buf) {
-        const bool done = handed[buf] == 0 || warp_wait(&sh.o_full[g][buf], (handed[buf] & 1) ^ 1, abort_flag);
-        tc_fence_after();
-        return done;
-      };
       uint32_t flag = page_flag(0);
+      const uint64_t scale2 = pair_of(__float_as_uint(sl2), __float_as_uint(sl2));
+      const Chunk ws = w.s;
+      const Span wg = w.g;
 #pragma unroll 1
       for (int j = 0; j < n; ++j) {
         const uint32_t flags = __ballot_sync(0xffffffffu, flag);
         if (j + 1 < n) flag = page_flag(j + 1);
-        const int k0 = w.g.tile(w.t0 + j) * kTile;
-        const bool partly = !all_see(a, w.s, w.g.p_lo, w.g.p_hi, k0, k0 + kTile);
-#pragma unroll 1
-        for (int e = 0; e < BLOCKS; ++e) {
-          const int h = BLOCKS == 2 ? e : g, buf = BLOCKS == 2 ? e : (j & 1), key = k0 + h * kStep;
-          const uint32_t there = flags >> (4 * h) & 15u;
-          const bool masked = there != 15u || !all_see(a, w.s, g_lo, g_hi, key, key + kStep);
-          const uint32_t s_at = s_addr + buf * kStep;
-          ok = warp_wait(&sh.s_full[g][buf], ph_s >> buf & 1, abort_flag);
+        const int k0 = wg.tile(w.t0 + j) * kTile, x = BLOCKS == 2 ? g : j & 1;
+        const bool partly = !all_see(a, ws, wg.p_lo, wg.p_hi, k0, k0 + kTile);  // some row of the block does not see all of the tile,
+        const bool masked = flags != 0xFFFFFFFFu || !all_see(a, ws, g_lo, g_hi, k0, k0 + kTile);  // some row of the group
+        ok = warp_wait(sh.s_full + x, ph_s >> x & 1, abort_flag);
+        if (!ok) break;
+        ph_s ^= 1u << x;
+        tc_fence_after();
+        if (partly) {  // the stage is not refilled before these probabilities are used
+          const int st = (tile0 + j) % NV;
+          ok = warp_wait(sh.fixed + st, ((tile0 + j) / NV) & 1, abort_flag);
           if (!ok) break;
-          ph_s ^= 1u << buf;
-          tc_fence_after();
-          uint32_t v[kStep];
-          tm_ld32(s_at, v);
-          tm_ld32(s_at + 32, v + 32);
-          tm_landed<kStep>(v);
-          if (masked) {
+          patch |= sh.odd[st] != 0;
+        }
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              const uint32_t m = seen32(key + 32 * c, see_end, see_from, a.sinks) &
-                                 ((there >> (2 * c) & 1 ? 0xFFFFu : 0u) | (there >> (2 * c + 1) & 1 ? 0xFFFF0000u : 0u));
+        for (int e = 0; e < BLOCKS; ++e) {
+          const int h = BLOCKS == 2 ? e : g;
+          const uint32_t s_at = my + x * kTile + h * kStep;
+          if (live) {
+            uint32_t v[kStep];
+            tm_ld32(s_at, v);
+            tm_ld32(s_at + 32, v + 32);
+            tm_landed<kStep>(v);
+            if (masked) {
 #pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (!(m >> i & 1)) v[32 * c + i] = 0xFF800000u;
+              for (int c = 0; c < 2; ++c) {
+                const uint32_t there = flags >> (4 * h + 2 * c);
+                const uint32_t m = seen32(k0 + h * kStep + 32 * c, see_end, see_from, a.sinks) &
+                                   ((there & 1 ? 0xFFFFu : 0u) | (there & 2 ? 0xFFFF0000u : 0u));
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                  if (!(m >> i & 1)) v[32 * c + i] = 0xFF800000u;
+              }
             }
-          }
-          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int i = 0; i < kStep; i += 2)
-            mx[i >> 1 & 3] = fmaxf(fmaxf(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), mx[i >> 1 & 3]);
-          // what probabilities are taken against: 2^kRaise below the largest
-          const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * sl2 - Num<T>::kRaise;
-          if (j == 0 && e == 0) {
-            m_ref = top;
-          } else if (__any_sync(0xffffffffu, top > m_ref + kLazy)) {
-            const float m_new = fmaxf(m_ref, top);
-            const float alpha = m_new == m_ref ? 1.0f : ex2(m_ref - m_new);
-            m_ref = m_new;
-            sum *= alpha;
-            ok = o_done(buf ^ 1);
-            if (!ok) break;
-            scale_row<HD>(o_addr, alpha);
-          }
-          const float base = m_ref == -INFINITY ? 0.f : m_ref;
-          const uint64_t scale2 = pair_of(__float_as_uint(sl2), __float_as_uint(sl2));
-          const uint64_t base2 = pair_of(__float_as_uint(-base), __float_as_uint(-base));
-          uint64_t acc[2] = {0, 0};
-          // in place: the pair at 2 i becomes entry i
+            for (int i = 0; i < kStep; i += 2)
+              mx[i >> 1 & 3] = fmaxf(fmaxf(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), mx[i >> 1 & 3]);
+            // what probabilities are taken against: 2^kRaise below the largest
+            const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * sl2 - Num<M>::kRaise;
+            if (j == 0 && e == 0) {
+              m_ref = top;
+            } else if (__any_sync(0xffffffffu, top > m_ref + kLazy)) {
+              const float m_new = fmaxf(m_ref, top);
+              const float alpha = m_new == m_ref ? 1.0f : ex2(m_ref - m_new);
+              m_ref = m_new;
+              sum *= alpha;
+              // The products before this one are done: two blocks, those of earlier tiles
+              // when the scores came, this tile's first half's by its barrier; one, those of
+              // the buffer when its scores came again, the other's by that one's barrier.
+              if (BLOCKS == 2 ? e == 1 : j > 0) {
+                ok = BLOCKS == 2 ? warp_wait(&sh.o_full[g][0], ph_o[0], abort_flag) : warp_wait(&sh.o_full[g][x ^ 1], (x ? ph_o[0] : ph_o[1]) ^ 1, abort_flag);
+                tc_fence_after();
+                if (!ok) break;
+              }
+              scale_row<HD>(o_addr, alpha);
+            }
+            const float base = m_ref == -INFINITY ? 0.f : m_ref;
+            const uint64_t base2 = pair_of(__float_as_uint(-base), __float_as_uint(-base));
+            uint64_t acc[2] = {0, 0};
+            // in place: the pair at 2 i becomes entry i
 #pragma unroll
-          for (int i = 0; i < kStep / 2; ++i) {
-            const float2 f = floats_of(fma2(pair_of(v[2 * i], v[2 * i + 1]), scale2, base2));
-            const float x = ex2(f.x), y = ex2(f.y);
-            acc[i & 1] = add2(acc[i & 1], pair_of(__float_as_uint(x), __float_as_uint(y)));
-            v[i] = Num<T>::pack(x, y);
-          }
-          tm_st32(s_at, v);
-          tm_wait_st();
-          const float2 acc2 = floats_of(add2(acc[0], acc[1]));
-          sum += acc2.x + acc2.y;
-          if (partly) {  // the stage is not refilled before these probabilities are used
-            const int st = (tile0 + j) % NV;
-            ok = warp_wait(sh.fixed + st, ((tile0 + j) / NV) & 1, abort_flag);
-            if (!ok) break;
-            patch |= sh.odd[st] != 0;
+            for (int i = 0; i < kStep / 2; ++i) {
+              const float2 f = floats_of(fma2(pair_of(v[2 * i], v[2 * i + 1]), scale2, base2));
+              const float y = ex2(f.x), z = ex2(f.y);
+              acc[i & 1] = add2(acc[i & 1], pair_of(__float_as_uint(y), __float_as_uint(z)));
+              v[i] = Num<M>::pack(y, z);
+            }
+            tm_st32(s_at, v);
+            tm_wait_st();
+            const float2 acc2 = floats_of(add2(acc[0], acc[1]));
+            sum += acc2.x + acc2.y;
           }
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(&sh.p_full[g][buf]);
-          ++handed[buf];
+          if (lane == 0) mbar_arrive(&sh.p_full[x][h]);
         }
         if (!ok) break;
+        // a product more of its kind is on the way
+        if (BLOCKS == 2 || x == 0) ph_o[0] ^= 1; else ph_o[1] ^= 1;
       }
       if (!ok) break;
-      ok = o_done(0) && o_done(1);
+      // all of the segment's products
+      if (BLOCKS == 2) {
+        ok = warp_wait(&sh.o_full[g][1], ph_o[1], abort_flag);
+        ph_o[1] ^= 1;
+      } else {
+        ok = warp_wait(&sh.o_full[g][0], ph_o[0] ^ 1, abort_flag) && (n == 1 || warp_wait(&sh.o_full[g][1], ph_o[1] ^ 1, abort_flag));
+      }
       if (!ok) break;
+      tc_fence_after();
       // ---- epilogue: a group's own accumulator, or half the columns of both groups' ----
       float w0 = 1.f, w1 = 0.f;
       if (BLOCKS == 1) {
@@ -1019,44 +1047,57 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
         for (int q = cw; q < pages; q += kConvWarps) {
           const uint4* codes = reinterpret_cast<const uint4*>(stage + (HD == 128 ? kChunkBytes : kCodes) + q * kPageTok * 128);
           uint4 x[kHeld];
-          Widen<T> by[kHeld];
-          uint32_t odd = 0;
+          uint32_t by[kHeld];
           bool far = false;
 #pragma unroll
           for (int e = 0; e < kHeld; ++e) {
             x[e] = codes[e * 32 + lane];
-            by[e].set(scale[q * kPageTok + (e * 32 + lane) / kRowPieces]);
-            far |= by[e].far;
-            odd |= Widen<T>::odd(x[e].x) | Widen<T>::odd(x[e].y) | Widen<T>::odd(x[e].z) | Widen<T>::odd(x[e].w);
+            by[e] = scale[q * kPageTok + (e * 32 + lane) / kRowPieces];
+            far |= Widen::far(by[e]);
           }
-          far = __any_sync(0xffffffffu, far || odd);  // (and every lane holds its codes)
-#pragma unroll
-          for (int e = 0; e < kHeld; ++e) {
-            const int r = q * kPageTok + (e * 32 + lane) / kRowPieces, c16 = lane % kRowPieces;
-            const uint32_t in[4] = {x[e].x, x[e].y, x[e].z, x[e].w};
-            uint32_t y[8];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              if (far) by[e].four_far(in[k], y[2 * k], y[2 * k + 1]);
-              else by[e].four(in[k], y[2 * k], y[2 * k + 1]);
-            }
-            if (clean && !all_see(a, w.s, w.g.p_lo, w.g.p_hi, k0 + r, k0 + r + 1)) {
-#pragma unroll
-              for (int k = 0; k < 8; ++k) {
-                const uint32_t f = k0 + r >= w.g.end ? 0u : finite_of<T>(y[k]);
-                any |= k0 + r < w.g.end && f != y[k];
-                y[k] = f;
-              }
-            }
-            // two pieces of eight entries; the lanes of a row's second half write theirs
-            // the other way round, so that eight lanes reach all banks
-            uint8_t* to = stage + (c16 / 4) * kChunkBytes + r * 128;
-            const int c = (2 * c16) % 8, turn = HD == 128 ? c16 / 4 : 0;
+          far = __any_sync(0xffffffffu, far);  // (and every lane holds its codes)
+          // eight entries of row r: two pieces of a row's sixteen codes, and the lanes of a
+          // row's second half write theirs the other way round, so that eight lanes reach
+          // all banks
+          const int c16 = lane % kRowPieces, turn = HD == 128 ? c16 / 4 : 0;
+          uint8_t* to = stage + (c16 / 4) * kChunkBytes + (q * kPageTok + lane / kRowPieces) * 128;
+          auto put = [&](int e, const uint32_t (&y)[8]) {
+            const int r = lane / kRowPieces + e * (32 / kRowPieces), c = (2 * c16) % 8;
+            uint8_t* at = to + e * (32 / kRowPieces) * 128;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               const bool second = (h ^ turn) != 0;
-              *reinterpret_cast<uint4*>(to + (((c + (second ? 1 : 0)) ^ (r & 7)) << 4)) =
+              *reinterpret_cast<uint4*>(at + (((c + (second ? 1 : 0)) ^ (r & 7)) << 4)) =
                   second ? make_uint4(y[4], y[5], y[6], y[7]) : make_uint4(y[0], y[1], y[2], y[3]);
+            }
+          };
+          if (!far && !clean) {
+#pragma unroll
+            for (int e = 0; e < kHeld; ++e) {
+              Widen w8;
+              w8.set(by[e]);
+              const uint32_t y[8] = {w8.near_two(x[e].x), w8.near_two(x[e].x >> 16), w8.near_two(x[e].y), w8.near_two(x[e].y >> 16),
+                                     w8.near_two(x[e].z), w8.near_two(x[e].z >> 16), w8.near_two(x[e].w), w8.near_two(x[e].w >> 16)};
+              put(e, y);
+            }
+          } else {
+#pragma unroll 1
+            for (int e = 0; e < kHeld; ++e) {
+              Widen w8;
+              const uint4 xe = e == 0 ? x[0] : e == 1 ? x[1] : e == 2 ? x[kHeld > 2 ? 2 : 0] : x[kHeld > 3 ? 3 : 0];
+              w8.set_far(e == 0 ? by[0] : e == 1 ? by[1] : e == 2 ? by[kHeld > 2 ? 2 : 0] : by[kHeld > 3 ? 3 : 0]);
+              uint32_t y[8] = {w8.far_two(xe.x), w8.far_two(xe.x >> 16), w8.far_two(xe.y), w8.far_two(xe.y >> 16),
+                               w8.far_two(xe.z), w8.far_two(xe.z >> 16), w8.far_two(xe.w), w8.far_two(xe.w >> 16)};
+              const int key = k0 + q * kPageTok + lane / kRowPieces + e * (32 / kRowPieces);
+              if (clean && !all_see(a, w.s, w.g.p_lo, w.g.p_hi, key, key + 1)) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                  const uint32_t f = key >= w.g.end ? 0u : finite_of<__half>(y[k]);
+                  any |= key < w.g.end && f != y[k];
+                  y[k] = f;
+                }
+              }
+              put(e, y);
             }
           }
         }
@@ -1145,7 +1186,9 @@ void run_chunk_sized(const ChunkAttnArgs& a, cudaStream_t s) {
   else run_chunk<T, HD, 2, Q8>(a, s);
 }
 template <bool Q8>
-void run_chunk_attention(const ChunkAttnArgs& a, cudaStream_t s) {
+void run_chunk_attention(ChunkAttnArgs a, cudaStream_t s) {
+  const uint32_t group = a.n_q_heads / a.n_kv_heads;
+  a.group_magic = group > 1 ? 0xFFFFFFFFu / group + 1 : 0;
   if (a.dtype == DT_BF16) {
     if (a.head_dim == 128) run_chunk_sized<Q8, __nv_bfloat16, 128>(a, s); else run_chunk_sized<Q8, __nv_bfloat16, 64>(a, s);
   } else {
