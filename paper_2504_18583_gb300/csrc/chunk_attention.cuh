@@ -51,14 +51,18 @@ constexpr int kSeqHeld = 64;                    // sequences whose lengths a CTA
 constexpr int kStep = kTile / 2;                // keys of a step
 constexpr int kConvWarps = 4;                   // warps that convert an 8-bit cache's tiles
 
+constexpr int kAheadSegs = 4;                   // segments that are worked out ahead
+
 __host__ __device__ constexpr int chunk_threads(bool q8) { return q8 ? 384 + 32 * kConvWarps : 384; }
-// tiles of keys, and of values, in flight: what shared memory holds beside the queries
+// Tiles of keys, and of values, in shared memory beside the queries; of an 8-bit
+// cache also as they lie, on their way into those.
 __host__ __device__ constexpr int ck_stages(int hd, int blocks, bool q8) {
-  return hd == 128 ? (blocks == 1 ? 3 : 2) : (blocks == 1 ? 6 : 5);
+  return q8 ? (hd == 128 ? 2 : 3) : hd == 128 ? (blocks == 1 ? 3 : 2) : (blocks == 1 ? 6 : 5);
 }
 __host__ __device__ constexpr int cv_stages(int hd, int blocks, bool q8) {
-  return hd == 128 ? (q8 ? 2 : 3) : (blocks == 1 ? 6 : 5);
+  return q8 ? (hd == 128 ? 2 : 3) : hd == 128 ? 3 : (blocks == 1 ? 6 : 5);
 }
+__host__ __device__ constexpr int raw_stages(int hd, int blocks, bool q8) { return !q8 ? 0 : hd == 128 ? (blocks == 1 ? 2 : 1) : 4; }
 
 // A sequence of the batch.
 struct Chunk {
@@ -106,16 +110,18 @@ __device__ __forceinline__ bool all_see(const ChunkAttnArgs& a, const Chunk& s, 
   return key1 <= min(lo + 1, s.keys) && (window_from(a, hi) <= key0 || key1 <= a.sinks);
 }
 
-// A warp's walk over its CTA's share: one segment (part of a unit) after the
-// other, in shared memory.
-struct ChunkWalk {
-  int left;            // places to go; in the one-part form 1, then 0
-  int b, off;          // sequence, and place within the unit
-  int at;              // place of the whole pass where the unit begins
+// A segment, part of a unit: tiles [t0, t1) (none: there are no more).
+struct Segment {
   Chunk s;
   Span g;
-  int head, block, t0, t1;
+  int b, head, block, t0, t1;
   int count, me, c0;   // the unit's contributors, this CTA's place among them, the first of them (among CTAs with a place)
+};
+// The walk over a CTA's share, one segment after the other, in shared memory.
+struct ChunkWalk : Segment {
+  int left;            // places to go; in the one-part form 1, then 0
+  int off;             // place within the unit
+  int at;              // place of the whole pass where the unit begins
   __device__ __forceinline__ void load(const ChunkAttnArgs& a, const int2* held, int rows_per_block) {
     if (b < kSeqHeld) s = chunk_of(a, held[b].x, held[b].y, held[b + 1].y, rows_per_block);
     else s = chunk_of(a, a.ctx_len[b], a.starts[b], a.starts[b + 1], rows_per_block);
@@ -195,7 +201,7 @@ __device__ __forceinline__ float value_at(const ChunkAttnArgs& a, int64_t page, 
 // Adds the infinities and NaN of the values of a part's tiles that not every row
 // of the block sees back to a row that sees them: to the output, or to a partial.
 template <typename T, int HD, bool Q8>
-__device__ __noinline__ void patch_chunk(const ChunkAttnArgs& a, const ChunkWalk& w, int p, int col0, int cols, T* out,
+__device__ __noinline__ void patch_chunk(const ChunkAttnArgs& a, const Segment& w, int p, int col0, int cols, T* out,
                                          Partial part, int row) {
   const int end = min(p + 1, w.s.keys), from = window_from(a, p);
   for (int k = w.t0; k < w.t1; ++k) {
@@ -253,56 +259,73 @@ struct Widen {
 };
 
 // What a CTA keeps in shared memory behind the operands.
-template <int NK, int NV, bool Q8>
+template <int NK, int NV, int NR>
 struct ChunkControl {
-  uint64_t k_full[NK], k_empty[NK], v_full[NV], v_empty[NV];
-  uint64_t k_fit[NK], fixed[NV];  // a stage's keys (8-bit caches), values are fit for the product
+  static constexpr bool Q8 = NR > 0;
+  uint64_t k_full[NK], k_empty[NK], v_full[NV], v_empty[NV];  // stages (8-bit: v_full unused)
+  uint64_t fixed[NV];      // a stage's values are fit for the product
+  uint64_t raw_full[2][NR + 1], raw_empty[2][NR + 1];         // keys', values' codes
   uint64_t s_full[2];      // a tile's scores are in one of the two buffers
   uint64_t p_full[2][2];   // the probabilities of one of its halves are, and O is scaled
   uint64_t o_full[2][2];   // two blocks: a group's product with a tile's first half is done, with all of a segment's;
                            // one: the product with its probabilities of a buffer is
-  uint64_t ready[2];       // the group has read O and laid out its queries
+  uint64_t ready[2];       // the group has read O of the segment before
+  uint64_t q_full, q_free; // a segment's queries are there; one block: their place is no longer read
+  uint64_t seg_full[kAheadSegs], seg_free[kAheadSegs];
   uint64_t pair, met[2];   // the two groups meet, a group's warps do
   uint64_t drain;          // every product is done
-  alignas(16) uint8_t k_scale[Q8 ? NK * kTile : 16], v_scale[Q8 ? NV * kTile : 16];
-  int2 seq[kSeqHeld + 1];  // sequences' context lengths and first rows
+  alignas(16) uint8_t scale[2][Q8 ? NR * kTile : 16];  // of the codes
   uint8_t back[Q8 ? 2 * kTile : 16];  // exponents of the queries' rows, which were scaled by them
+  int2 seq[kSeqHeld + 1];  // sequences' context lengths and first rows
   uint32_t tmem, last_in[2], odd[NV];  // odd: a stage's values that not all rows see held infinities or NaN (a byte a warp)
   int abort_flag, start_b, start_head, start_block, start_off;
   int sum[16], units[16], most[16];
-  ChunkWalk walk[Q8 ? 16 : 12];
+  ChunkWalk walk;
+  Segment seg[kAheadSegs];
   uint16_t slots[2][kMaxGrid];
 };
 template <int HD, int BLOCKS, bool Q8>
 constexpr int chunk_smem() {
-  return (BLOCKS + ck_stages(HD, BLOCKS, Q8) + cv_stages(HD, BLOCKS, Q8)) * stage_bytes(HD) +
-         (int)sizeof(ChunkControl<ck_stages(HD, BLOCKS, Q8), cv_stages(HD, BLOCKS, Q8), Q8>);
+  constexpr int nk = ck_stages(HD, BLOCKS, Q8), nv = cv_stages(HD, BLOCKS, Q8), nr = raw_stages(HD, BLOCKS, Q8);
+  return (BLOCKS + nk + nv + nr) * stage_bytes(HD) + (int)sizeof(ChunkControl<nk, nv, nr>);
 }
 static_assert(chunk_smem<128, 1, false>() <= 227 * 1024 && chunk_smem<128, 2, false>() <= 227 * 1024, "shared memory of one CTA");
 static_assert(chunk_smem<64, 1, false>() <= 227 * 1024 && chunk_smem<64, 2, false>() <= 227 * 1024, "shared memory of one CTA");
 static_assert(chunk_smem<128, 1, true>() <= 227 * 1024 && chunk_smem<128, 2, true>() <= 227 * 1024, "shared memory of one CTA");
 static_assert(chunk_smem<64, 1, true>() <= 227 * 1024 && chunk_smem<64, 2, true>() <= 227 * 1024, "shared memory of one CTA");
 
+__device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* m, uint64_t* bar, int c0, int c1, int c2) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+          smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(m)), "r"(c0), "r"(c1), "r"(c2), "r"(smem_u32(bar))
+      : "memory");
+}
+
 }  // namespace
 
+// by_tma: queries come by tensor copies (qmap), else by the softmax warps' loads
 template <typename T, int HD, int BLOCKS, bool Q8>
 __global__ void __launch_bounds__(chunk_threads(Q8), 1)
     chunk_attention_kernel(const __grid_constant__ ChunkAttnArgs a, const __grid_constant__ CUtensorMap kmap,
-                           const __grid_constant__ CUtensorMap vmap) {
-  constexpr int NK = ck_stages(HD, BLOCKS, Q8), NV = cv_stages(HD, BLOCKS, Q8), kStage = stage_bytes(HD);
+                           const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CUtensorMap qmap) {
+  constexpr int NK = ck_stages(HD, BLOCKS, Q8), NV = cv_stages(HD, BLOCKS, Q8), NR = raw_stages(HD, BLOCKS, Q8);
+  constexpr int kStage = stage_bytes(HD), kRaw = kStage / 2, kConsumers = Q8 ? 15 : 11;
   constexpr int kChunks = HD / 64, kChunkBytes = kTile * 128, kRows = kTile * BLOCKS, kThreads = chunk_threads(Q8);
   using M = typename OperandOf<T, Q8>::type;
-  constexpr bool kRaised = sizeof(T) == sizeof(M) && Num<T>::kFormat != Num<M>::kFormat;  // bf16 queries become fp16 ones, row by row scaled
+  constexpr bool kRaised = Num<T>::kFormat != Num<M>::kFormat;  // bf16 queries become fp16 ones, row by row scaled
   constexpr uint32_t kIdescS = idesc16(Num<M>::kFormat, kTile, kTile, false);
   constexpr uint32_t kIdescO = idesc16(Num<M>::kFormat, kTile, HD, true);
   extern __shared__ __align__(1024) uint8_t qbuf[];  // queries, then the rings
   uint8_t* kring = qbuf + BLOCKS * kStage;
   uint8_t* vring = kring + NK * kStage;
-  using Control = ChunkControl<NK, NV, Q8>;
-  Control& sh = *reinterpret_cast<Control*>(vring + NV * kStage);
+  uint8_t* raw_rings = vring + NV * kStage;  // keys' codes, values' codes
+  using Control = ChunkControl<NK, NV, NR>;
+  Control& sh = *reinterpret_cast<Control*>(raw_rings + NR * kStage);
   volatile int* abort_flag = &sh.abort_flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int group = a.n_q_heads / a.n_kv_heads, grid = gridDim.x;
+  const bool by_tma = !Q8 && a.q_by_tma;
 
   // ---- this CTA's range -------------------------------------------------------
   if (warp == 1) tmem_alloc(&sh.tmem, 512);
@@ -310,16 +333,26 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
     if (!Q8) {
       tma_prefetch_desc(&kmap);
       tma_prefetch_desc(&vmap);
+      if (by_tma) tma_prefetch_desc(&qmap);
     }
 #pragma unroll 1
-    for (int i = 0; i < NK; ++i) { mbar_init(sh.k_full + i, 1); mbar_init(sh.k_empty + i, 1); mbar_init(sh.k_fit + i, kConvWarps); }
+    for (int i = 0; i < NK; ++i) { mbar_init(sh.k_full + i, Q8 ? kConvWarps / 2 : 1); mbar_init(sh.k_empty + i, 1); }
 #pragma unroll 1
-    for (int i = 0; i < NV; ++i) { mbar_init(sh.v_full + i, 1); mbar_init(sh.v_empty + i, 1); mbar_init(sh.fixed + i, Q8 ? kConvWarps : 1); }
+    for (int i = 0; i < NV; ++i) { mbar_init(sh.v_full + i, 1); mbar_init(sh.v_empty + i, 1); mbar_init(sh.fixed + i, Q8 ? kConvWarps / 2 : 1); sh.odd[i] = 0; }
+#pragma unroll 1
+    for (int i = 0; i < NR; ++i) {
+      mbar_init(sh.raw_full[0] + i, 1); mbar_init(sh.raw_full[1] + i, 1);
+      mbar_init(sh.raw_empty[0] + i, kConvWarps / 2); mbar_init(sh.raw_empty[1] + i, kConvWarps / 2);
+    }
 #pragma unroll 1
     for (int i = 0; i < 2; ++i) {
       mbar_init(sh.s_full + i, 1); mbar_init(sh.p_full[i], 4); mbar_init(sh.p_full[i] + 1, 4);
       mbar_init(sh.o_full[i], 1); mbar_init(sh.o_full[i] + 1, 1); mbar_init(sh.ready + i, 4); mbar_init(sh.met + i, 4);
     }
+#pragma unroll 1
+    for (int i = 0; i < kAheadSegs; ++i) { mbar_init(sh.seg_full + i, 1); mbar_init(sh.seg_free + i, kConsumers); }
+    mbar_init(&sh.q_full, by_tma ? 1 : 8);
+    mbar_init(&sh.q_free, 8);
     mbar_init(&sh.pair, 8);
     mbar_init(&sh.drain, 1);
     fence_barrier_init();
@@ -390,7 +423,7 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
         sh.start_head = off / places;
         sh.start_off = off % places;
       }
-      __syncthreads();
+      if (a.batch > kThreads) __syncthreads();  // what the next step writes has been read
     }
     if (!round) {
       ranges.set(run, grid);
@@ -399,30 +432,8 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
     }
   }
   const bool one_part = single && a.batch <= kSeqHeld && units <= grid;
-  if (!one_part && warp == 0 && hi > lo) {  // the block that the first place lies in
-    const int b = sh.start_b, rest = sh.start_off;
-    const Chunk s = chunk_of(a, a.ctx_len[b], a.starts[b], a.starts[b + 1], kRows);
-    int before = 0;
-#pragma unroll 1
-    for (int i0 = 0; i0 < s.blocks; i0 += 32) {
-      const int len = i0 + lane < s.blocks ? span_of(a, s, i0 + lane, kRows).tiles + kStart : 0;
-      int inc = len;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int t = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += t;
-      }
-      const uint32_t past = __ballot_sync(0xffffffffu, before + inc > rest);
-      if (past) {
-        if (lane == __ffs(past) - 1) { sh.start_block = i0 + lane; sh.start_off = rest - (before + inc - len); }
-        break;
-      }
-      before += __shfl_sync(0xffffffffu, inc, 31);
-    }
-  }
-  if (!one_part) __syncthreads();
-  ChunkWalk& w = sh.walk[warp];
-  auto begin = [&] {  // of a walk in ranges
+  ChunkWalk& w = sh.walk;
+  auto begin = [&] {  // the walk in ranges, from its first place
     w.left = hi - lo;  // 0: more CTAs than places
     w.b = hi > lo ? sh.start_b : 0;
     w.head = hi > lo ? sh.start_head : 0;
@@ -432,148 +443,108 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
     w.load(a, sh.seq, kRows);
     if (hi > lo) w.g = span_of(a, w.s, w.block, kRows);
   };
-  if (one_part) {
-    // the fewest tiles a part that the CTAs are enough for; two sequences a lane
-    static_assert(kSeqHeld == 64, "two sequences a lane");
-    int tiles[2], mine[2];
-    const int all_tiles = ranges.total - units * kStart;
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int b = 2 * lane + e;
-      tiles[e] = mine[e] = 0;
-      if (b < a.batch) {
-        const Chunk s = chunk_of(a, sh.seq[b].x, sh.seq[b].y, sh.seq[b + 1].y, kRows);
-        if (s.blocks) {
-          tiles[e] = span_of(a, s, 0, kRows).tiles;
-          mine[e] = a.n_kv_heads;
-        }
-      }
-    }
-    // (a unit's parts are less than one more than its tiles / most)
-    int least = max(1, all_tiles / grid), most = max(least, min(longest, all_tiles / (grid - units + 1) + 1));
-#pragma unroll 1
-    while (least < most) {
-      const int mid = (least + most) / 2;
-      const int need = __reduce_add_sync(0xffffffffu, mine[0] * parts_of(tiles[0], mid) + mine[1] * parts_of(tiles[1], mid));
-      if (need <= grid) most = mid; else least = mid + 1;
-    }
-    int inc = 0;
-#pragma unroll
-    for (int e = 0; e < 2; ++e) { mine[e] *= parts_of(tiles[e], most); inc += mine[e]; }
-    const int own = inc;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int t = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += t;
-    }
-    if (lane == 0) w.left = 0;  // more CTAs than parts
-    __syncwarp();
-    int before = inc - own;
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int at = (int)blockIdx.x - before;
-      if (at >= 0 && at < mine[e]) {
-        const int parts = parts_of(tiles[e], most);
-        w.left = 1;
-        w.b = 2 * lane + e;
-        w.load(a, sh.seq, kRows);
-        w.g = span_of(a, w.s, 0, kRows);
-        w.head = at / parts;
-        w.block = 0;
-        w.count = parts;
-        w.me = at - w.head * parts;
-        w.c0 = (int)blockIdx.x - w.me;
-        w.t0 = w.me * w.g.tiles / parts;
-        w.t1 = (w.me + 1) * w.g.tiles / parts;
-      }
-      before += mine[e];
-    }
-  } else if (lane == 0) {
-    begin();
-  }
-  __syncwarp();
-  const bool had_part = w.left > 0;
-  // the warp's next segment
-  auto next = [&]() -> bool {
-    __syncwarp();
-    bool some = false;
-    if (lane == 0) some = w.next(a, sh.seq, kRows, ranges, one_part);
-    return __shfl_sync(0xffffffffu, (int)some, 0);
-  };
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = sh.tmem;
   int tile0 = 0;  // tiles of the segments before this one
   bool ok = true;
+  // a warp's next segment: what it has read of the one before may be written over
+  int taken = 0;
+  auto next = [&]() -> bool {
+    __syncwarp();
+    if (taken > 0 && lane == 0) mbar_arrive(sh.seg_free + (taken - 1) % kAheadSegs);
+    ok = ok && warp_wait(sh.seg_full + taken % kAheadSegs, (taken / kAheadSegs) & 1, abort_flag);
+    ++taken;
+    return ok && sh.seg[(taken - 1) % kAheadSegs].t1 > 0;
+  };
+  auto segment = [&]() -> const Segment& { return sh.seg[(taken - 1) % kAheadSegs]; };
   // pages of a tile that hold keys the block may see
-  auto pages_of = [&](int tile) { return min(kTilePages, (w.g.end - 1) / kPageTok - tile * kTilePages + 1); };
+  auto pages_of = [&](const Segment& u, int tile) { return min(kTilePages, (u.g.end - 1) / kPageTok - tile * kTilePages + 1); };
 
-  if (warp < 4) {
-    if (warp == 0 || warp == 2) {
-      // ---- loads: keys by one warp, values by another --------------------------------
-      // Page ids are fetched 32 pages (four tiles) at a time, a block ahead of
-      // their use: a load from the table would be on every copy's path.
-      const bool v = warp == 2;
-      uint64_t *full = v ? sh.v_full : sh.k_full, *empty = v ? sh.v_empty : sh.k_empty;
-      uint8_t* to0 = v ? vring : kring;
-      const CUtensorMap* map = v ? &vmap : &kmap;
-      const int ns = v ? NV : NK;
-      int st = 0, phase = 0, issued = 0;  // stages are used in turn
-      while (ok && next()) {
-        const int n = w.t1 - w.t0, head = w.head;
-        const int32_t* row = a.page_table + (size_t)w.b * a.max_pages;
-        const int last_page = (w.g.end - 1) / kPageTok;
-        auto fetch = [&](int block) {
-          const int j = 4 * block + lane / kTilePages;
-          const int p = j < n ? w.g.tile(w.t0 + j) * kTilePages + lane % kTilePages : last_page + 1;
-          const int page = p <= last_page ? row[p] : 0;
-          return (uint32_t)page < (uint32_t)a.n_pages ? page : a.n_pages;  // out of the tensor: reads as zeros
-        };
-        int have = fetch(0), after = n > 4 ? fetch(1) : 0;
+  if (warp == 0 || warp == 2) {
+    // ---- loads: keys by one warp, values by another ------------------------------------
+    // Page ids are fetched 32 pages (four tiles) at a time, a block ahead of
+    // their use: a load from the table would be on every copy's path.
+    const bool v = warp == 2;
+    uint64_t* full = Q8 ? sh.raw_full[v] : (v ? sh.v_full : sh.k_full);
+    uint64_t* empty = Q8 ? sh.raw_empty[v] : (v ? sh.v_empty : sh.k_empty);
+    uint8_t* to0 = Q8 ? raw_rings + (v ? NR * kRaw : 0) : (v ? vring : kring);
+    const CUtensorMap* map = v ? &vmap : &kmap;
+    const int ns = Q8 ? NR : v ? NV : NK;
+    int st = 0, phase = 0, issued = 0, last = 0;  // stages are used in turn
+    int q_out = 0;  // segments whose queries were asked for
+    while (next()) {
+      const Segment& u = segment();
+      const int n = u.t1 - u.t0, head = u.head;
+      const int32_t* row = a.page_table + (size_t)u.b * a.max_pages;
+      const int last_page = (u.g.end - 1) / kPageTok;
+      auto fetch = [&](int block) {
+        const int j = 4 * block + lane / kTilePages;
+        const int p = j < n ? u.g.tile(u.t0 + j) * kTilePages + lane % kTilePages : last_page + 1;
+        const int page = p <= last_page ? row[p] : 0;
+        return (uint32_t)page < (uint32_t)a.n_pages ? page : a.n_pages;  // out of the tensor: reads as zeros
+      };
+      // The segment's queries, once the products of the one before have read theirs:
+      // two blocks, when its last scores are there; one, when the softmax no longer
+      // uses their place.
+      auto queries = [&] {
+        if (taken > 1) {
+          if (BLOCKS == 1) ok = ok && warp_wait(&sh.q_free, taken & 1, abort_flag);
+          else ok = ok && warp_wait(empty + last % ns, (last / ns) & 1, abort_flag);
+        }
+        if (ok && elect_one()) {
+          mbar_arrive_expect_tx(&sh.q_full, BLOCKS * kStage);
+#pragma unroll
+          for (int i = 0; i < BLOCKS; ++i)
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c)
+              tma_load_3d(qbuf + i * kStage + c * kChunkBytes, &qmap, &sh.q_full, c * 64, head * group,
+                          u.s.row0 + u.g.token + i * (kTile / group));
+        }
+        __syncwarp();
+        ++q_out;
+      };
+      if (!Q8 && by_tma && !v && taken == 1) queries();
+      const int last_before = last;
+      int have = fetch(0), after = n > 4 ? fetch(1) : 0;
 #pragma unroll 1
-        for (int j = 0; j < n; ++j) {
-          const int pages = pages_of(w.g.tile(w.t0 + j));
-          if (j > 0 && (j & 3) == 0) {
-            have = after;
-            if (j + 4 < n) after = fetch(j / 4 + 1);
+      for (int j = 0; j < n && ok; ++j) {
+        const int pages = pages_of(u, u.g.tile(u.t0 + j));
+        if (j > 0 && (j & 3) == 0) {
+          have = after;
+          if (j + 4 < n) after = fetch(j / 4 + 1);
+        }
+        ok = ok && warp_wait(empty + st, phase ^ 1, abort_flag);
+        if (!ok) break;
+        uint8_t* to = to0 + st * (Q8 ? kRaw : kStage);
+        if constexpr (Q8) {
+          // lanes 0 to 7 copy a page's codes each, lanes 8 to 15 its exponents
+          uint8_t* scale = sh.scale[v] + st * kTile;
+          constexpr int kCodes = HD * kPageTok;
+          const int q = lane & 7, page = __shfl_sync(0xffffffffu, have, (j & 3) * kTilePages + q);
+          const bool mine = lane < 2 * kTilePages && q < pages, there = mine && page < a.n_pages;
+          if (mine && !there) {  // no such page: zeros
+            uint4* z = reinterpret_cast<uint4*>(lane < kTilePages ? to + q * kCodes : scale + q * kPageTok);
+#pragma unroll 1
+            for (int i = 0; i < (lane < kTilePages ? kCodes / 16 : 1); ++i) z[i] = make_uint4(0, 0, 0, 0);
           }
+          __syncwarp();
+          const uint32_t all = __popc(__ballot_sync(0xffffffffu, there && lane < kTilePages));
+          if (lane == 0) mbar_arrive_expect_tx(full + st, all * (kCodes + kPageTok));
+          __syncwarp();
+          if (there) {
+            if (lane < kTilePages)
+              bulk_load(to + q * kCodes, reinterpret_cast<const uint8_t*>(v ? a.v_cache : a.k_cache) + page * a.page_stride + (int64_t)head * kCodes,
+                        kCodes, full + st);
+            else
+              bulk_load(scale + q * kPageTok, (v ? a.v_scale : a.k_scale) + page * a.scale_stride + (int64_t)head * kPageTok, kPageTok, full + st);
+          }
+        } else {
           int page[kTilePages];
 #pragma unroll
           for (int q = 0; q < kTilePages; ++q) page[q] = __shfl_sync(0xffffffffu, have, (j & 3) * kTilePages + q);
-          ok = warp_wait(empty + st, phase ^ 1, abort_flag);
-          if (!ok) break;
-          uint8_t* to = to0 + st * kStage;
-          if constexpr (Q8) {
-            // a page's codes where its last 16-bit entries go (see the conversion)
-            uint8_t* scale = (v ? sh.v_scale : sh.k_scale) + st * kTile;
-            constexpr int kCodes = HD * kPageTok;
-            uint8_t* codes = to + (HD == 128 ? kChunkBytes : kCodes);
-            int there = 0;
-#pragma unroll
-            for (int q = 0; q < kTilePages; ++q) {
-              if (q >= pages) continue;
-              if (page[q] < a.n_pages) {
-                ++there;
-              } else {  // no such page: zeros
-#pragma unroll 1
-                for (int i = lane; i < kCodes / 16; i += 32) reinterpret_cast<uint4*>(codes + q * kPageTok * 128)[i] = make_uint4(0, 0, 0, 0);
-                if (lane == 0) *reinterpret_cast<uint4*>(scale + q * kPageTok) = make_uint4(0, 0, 0, 0);
-              }
-            }
-            __syncwarp();
-            if (elect_one()) {
-              mbar_arrive_expect_tx(full + st, (uint32_t)there * (kCodes + kPageTok));
-              const uint8_t* from = reinterpret_cast<const uint8_t*>(v ? a.v_cache : a.k_cache) + (int64_t)head * kCodes;
-              const uint8_t* from_scale = (v ? a.v_scale : a.k_scale) + (int64_t)head * kPageTok;
-#pragma unroll
-              for (int q = 0; q < kTilePages; ++q)
-                if (q < pages && page[q] < a.n_pages) {
-                  bulk_load(codes + q * kPageTok * 128, from + page[q] * a.page_stride, kCodes, full + st);
-                  bulk_load(scale + q * kPageTok, from_scale + page[q] * a.scale_stride, kPageTok, full + st);
-                }
-            }
-          } else if (elect_one()) {
+          if (elect_one()) {
             mbar_arrive_expect_tx(full + st, (uint32_t)pages * kChunks * kPageTok * 128);
 #pragma unroll
             for (int q = 0; q < kTilePages; ++q)
@@ -583,169 +554,296 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
                   tma_load_4d(to + c * kChunkBytes + q * kPageTok * 128, map, full + st, c * 64, 0, head, page[q]);
               }
           }
-          __syncwarp();
-          ++issued;
-          if (++st == ns) { st = 0; phase ^= 1; }
+        }
+        __syncwarp();
+        last = issued++;
+        if (++st == ns) { st = 0; phase ^= 1; }
+        if (!Q8 && by_tma && !v && j == 0 && taken > 1) {  // a tile first: its place came free before the queries'
+          const int mine = last;
+          last = last_before;
+          queries();
+          last = mine;
         }
       }
-      if (!ok) {  // copies in flight write this CTA's shared memory: they land before it goes
-        *abort_flag = 1;
-        for (int i = max(0, issued - ns); i < issued; ++i) mbar_drain(full + i % ns, (i / ns) & 1);
-      }
-    } else if (warp == 1) {
-      // ---- products ---------------------------------------------------------------
-      // One lane issues, all wait.  A tile takes 32 products (128 columns: 2048 clocks),
-      // and what lies between them is the warp's own time, so it is kept short: stages
-      // and phases are counted along, addresses made the warp's (by a shuffle: the
-      // compiler then keeps them in uniform registers) once a tile, and steps add
-      // constants to a descriptor's low word.
-      uint32_t ph_p = 0, ph_ready = 0;
-      int kst = 0, vst = 0;
-      uint32_t kph = 0, vph = 0;
-      const uint32_t q_addr = smem_u32(qbuf) >> 4, k_addr = smem_u32(kring) >> 4, v_addr = smem_u32(vring) >> 4;
-      uint64_t* keys_in = Q8 ? sh.k_fit : sh.k_full;
-      const bool leader = elect_one();
-      auto uniform = [](uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); };
-      const uint32_t tm = uniform(tmem);
-      // Shared-memory descriptors, 128-byte swizzle.  Queries and keys: 128-byte
-      // rows along K, eight-row atoms 1024 bytes apart.  Values: 64 of a key's
-      // entries a row (N is contiguous), atoms of eight keys 1024 bytes apart along
-      // K, the next 64 entries a chunk further.
-      constexpr uint64_t kDescK = (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
-      constexpr uint64_t kDescV = (uint64_t)(kChunkBytes >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
-      // tensor memory: two buffers of scores (two blocks: a group each; one: tiles in
-      // turn), then the groups' accumulators
-      auto scores = [&](int x, uint32_t kb) {  // of the keys at kb into buffer x
-        const uint32_t qa = q_addr + (BLOCKS == 2 ? x * (kStage >> 4) : 0), d = tm + x * kTile;
-        if (leader) {
+    }
+    if (!ok) {  // copies in flight write this CTA's shared memory: they land before it goes
+      *abort_flag = 1;
+      for (int i = max(0, issued - ns); i < issued; ++i) mbar_drain(full + i % ns, (i / ns) & 1);
+      if (q_out) mbar_drain(&sh.q_full, (q_out - 1) & 1);
+    }
+  } else if (warp == 1) {
+    // ---- products ---------------------------------------------------------------------
+    // One lane issues, all wait.  A tile takes 32 products (128 columns: 2048 clocks),
+    // and what lies between them is the warp's own time, so it is kept short: stages
+    // and phases are counted along, addresses made the warp's (by a shuffle: the
+    // compiler then keeps them in uniform registers) once a tile, and steps add
+    // constants to a descriptor's low word.
+    uint32_t ph_p = 0;
+    int kst = 0, vst = 0;
+    uint32_t kph = 0, vph = 0;
+    const uint32_t q_addr = smem_u32(qbuf) >> 4, k_addr = smem_u32(kring) >> 4, v_addr = smem_u32(vring) >> 4;
+    const bool leader = elect_one();
+    auto uniform = [](uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); };
+    const uint32_t tm = uniform(tmem);
+    // Shared-memory descriptors, 128-byte swizzle.  Queries and keys: 128-byte
+    // rows along K, eight-row atoms 1024 bytes apart.  Values: 64 of a key's
+    // entries a row (N is contiguous), atoms of eight keys 1024 bytes apart along
+    // K, the next 64 entries a chunk further.
+    constexpr uint64_t kDescK = (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+    constexpr uint64_t kDescV = (uint64_t)(kChunkBytes >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+    // tensor memory: two buffers of scores (two blocks: a group each; one: tiles in
+    // turn), then the groups' accumulators
+    auto scores = [&](int x, uint32_t kb) {  // of the keys at kb into buffer x
+      const uint32_t qa = q_addr + (BLOCKS == 2 ? x * (kStage >> 4) : 0), d = tm + x * kTile;
+      if (leader) {
 #pragma unroll
-          for (int k = 0; k < HD / 16; ++k) {
-            const uint32_t at = ((k / 4) * kChunkBytes + (k % 4) * 32) >> 4;
-            umma_ss(d, kDescK | (qa + at), kDescK | (kb + at), kIdescS, k > 0);
-          }
-          umma_commit(sh.s_full + x);
+        for (int k = 0; k < HD / 16; ++k) {
+          const uint32_t at = ((k / 4) * kChunkBytes + (k % 4) * 32) >> 4;
+          umma_ss(d, kDescK | (qa + at), kDescK | (kb + at), kIdescS, k > 0);
         }
-      };
-      // O += P V of half h, whose probabilities are in buffer x.  Keys past the end have
-      // probability 0: whole steps of 16 are left out, but for the first, which leaves
-      // zeros where there were none yet.
-      auto outputs = [&](int g, int x, int h, uint32_t vb, bool first, int keys) {
-        const uint32_t o = tm + 2 * kTile + g * HD, p = tm + x * kTile + h * kStep, bit = 2 * x + h;
-        ok = ok && warp_wait(&sh.p_full[x][h], ph_p >> bit & 1, abort_flag);
-        if (!ok) return;
-        ph_p ^= 1u << bit;
-        tc_fence_after();
-        if (leader) {
-          umma_ts(o, p, kDescV | (vb + h * 4 * 128), kIdescO, !first);
-          if (keys >= (h + 1) * kStep) {
+        umma_commit(sh.s_full + x);
+      }
+    };
+    // O += P V of half h, whose probabilities are in buffer x.  Keys past the end have
+    // probability 0: whole steps of 16 are left out, but for the first, which leaves
+    // zeros where there were none yet.
+    auto outputs = [&](int g, int x, int h, uint32_t vb, bool first, int keys) {
+      const uint32_t o = tm + 2 * kTile + g * HD, p = tm + x * kTile + h * kStep, bit = 2 * x + h;
+      ok = ok && warp_wait(&sh.p_full[x][h], ph_p >> bit & 1, abort_flag);
+      if (!ok) return;
+      ph_p ^= 1u << bit;
+      tc_fence_after();
+      if (leader) {
+        umma_ts(o, p, kDescV | (vb + h * 4 * 128), kIdescO, !first);
+        if (keys >= (h + 1) * kStep) {
 #pragma unroll
-            for (int k = 1; k < kStep / 16; ++k) umma_ts(o, p + k * 8, kDescV | (vb + (h * 4 + k) * 128), kIdescO, 1);
-          } else {
+          for (int k = 1; k < kStep / 16; ++k) umma_ts(o, p + k * 8, kDescV | (vb + (h * 4 + k) * 128), kIdescO, 1);
+        } else {
 #pragma unroll 1
-            for (int k = 1; k < kStep / 16; ++k)
-              if (keys > h * kStep + k * 16) umma_ts(o, p + k * 8, kDescV | (vb + (h * 4 + k) * 128), kIdescO, 1);
-          }
-          if (BLOCKS == 1) umma_commit(&sh.o_full[g][x]); else if (h == 0) umma_commit(&sh.o_full[g][0]);
+          for (int k = 1; k < kStep / 16; ++k)
+            if (keys > h * kStep + k * 16) umma_ts(o, p + k * 8, kDescV | (vb + (h * 4 + k) * 128), kIdescO, 1);
         }
-      };
-      auto commit = [&](uint64_t* bar) {
-        if (leader) umma_commit(bar);
-      };
-      while (ok && next()) {
-        const int n = w.t1 - w.t0;
-        const int last_keys = w.t1 == w.g.tiles ? w.g.end - w.g.tile(w.t1 - 1) * kTile : kTile;  // of the last tile
-        ok = warp_wait(sh.ready + 0, ph_ready, abort_flag) && warp_wait(sh.ready + 1, ph_ready, abort_flag);
-        ph_ready ^= 1;
-        tc_fence_after();
-        // tile j's outputs, and the scores that go where its probabilities were: two
-        // blocks, of the next tile; one, of the tile after the next
-        constexpr int kAhead = BLOCKS == 2 ? 1 : 2;
+        if (BLOCKS == 1) umma_commit(&sh.o_full[g][x]); else if (h == 0) umma_commit(&sh.o_full[g][0]);
+      }
+    };
+    auto commit = [&](uint64_t* bar) {
+      if (leader) umma_commit(bar);
+    };
+    while (next()) {
+      const Segment& u = segment();
+      const int n = u.t1 - u.t0;
+      const int last_keys = u.t1 == u.g.tiles ? u.g.end - u.g.tile(u.t1 - 1) * kTile : kTile;  // of the last tile
+      const uint32_t turn = (taken - 1) & 1;
+      ok = ok && warp_wait(&sh.q_full, turn, abort_flag);
+      if (!by_tma) tc_fence_after();
+      // tile j's outputs, and the scores that go where its probabilities were: two
+      // blocks, of the next tile; one, of the tile after the next.  The first scores
+      // need nothing of the segment before, the first outputs that its own were read.
+      constexpr int kAhead = BLOCKS == 2 ? 1 : 2;
 #pragma unroll 1
-        for (int j = -kAhead; j < n && ok; ++j) {
-          const bool more = j + kAhead < n;
-          const int keys = j == n - 1 ? last_keys : kTile;
-          const uint32_t kb = uniform(k_addr + kst * (kStage >> 4)), vb = uniform(v_addr + vst * (kStage >> 4));
-          if (j >= 0) ok = warp_wait(sh.fixed + vst, vph, abort_flag);
-          if (!ok) break;
+      for (int j = -kAhead; j < n && ok; ++j) {
+        const bool more = j + kAhead < n;
+        const int keys = j == n - 1 ? last_keys : kTile;
+        const uint32_t kb = uniform(k_addr + kst * (kStage >> 4)), vb = uniform(v_addr + vst * (kStage >> 4));
+        if (j >= 0) ok = warp_wait(sh.fixed + vst, vph, abort_flag);
+        if (BLOCKS == 1 && j == 0) ok = ok && warp_wait(sh.ready + 0, turn, abort_flag) && warp_wait(sh.ready + 1, turn, abort_flag);
+        if (!ok) break;
 #pragma unroll
-          for (int e = 0; e < BLOCKS; ++e) {
-            const int x = BLOCKS == 2 ? e : j & 1;
+        for (int e = 0; e < BLOCKS; ++e) {
+          const int x = BLOCKS == 2 ? e : j & 1;
+          if (BLOCKS == 2 && j == 0) ok = ok && warp_wait(sh.ready + e, turn, abort_flag);
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-              if (j >= 0) outputs(BLOCKS == 2 ? e : h, x, h, vb, j == 0 && (BLOCKS == 1 || h == 0), keys);
-            // (asked for here, since the load of a stage that has just come free is
-            // what a step would wait for)
-            if (more && e == 0) ok = ok && warp_wait(keys_in + kst, kph, abort_flag);
-            if (!ok) break;
-            if (more) scores(x, kb);
-          }
+          for (int h = 0; h < 2; ++h)
+            if (j >= 0) outputs(BLOCKS == 2 ? e : h, x, h, vb, j == 0 && (BLOCKS == 1 || h == 0), keys);
+          // (asked for here, since the load of a stage that has just come free is
+          // what a step would wait for)
+          if (more && e == 0) ok = ok && warp_wait(sh.k_full + kst, kph, abort_flag);
           if (!ok) break;
-          if (j >= 0) {
-            commit(sh.v_empty + vst);
-            if (++vst == NV) { vst = 0; vph ^= 1; }
-          }
-          if (more) {
-            commit(sh.k_empty + kst);
-            if (++kst == NK) { kst = 0; kph ^= 1; }
-          }
+          if (more) scores(x, kb);
         }
-        if (BLOCKS == 2 && ok) {
-          commit(&sh.o_full[0][1]);
-          commit(&sh.o_full[1][1]);
+        if (!ok) break;
+        if (j >= 0) {
+          commit(sh.v_empty + vst);
+          if (++vst == NV) { vst = 0; vph ^= 1; }
+        }
+        if (more) {
+          commit(sh.k_empty + kst);
+          if (++kst == NK) { kst = 0; kph ^= 1; }
         }
       }
-      if (!ok) *abort_flag = 1;
-      // products in flight read shared memory and write tensor memory: let them end
+      if (BLOCKS == 2 && ok) {
+        commit(&sh.o_full[0][1]);
+        commit(&sh.o_full[1][1]);
+      }
+    }
+    if (!ok) *abort_flag = 1;
+    // products in flight read shared memory and write tensor memory: let them end
+    __syncwarp();
+    commit(&sh.drain);
+    mbar_drain(&sh.drain, 0);
+  } else if (warp == 3) {
+    // ---- segments, worked out ahead of their use -----------------------------------------
+    if (one_part) {
+      // the fewest tiles a part that the CTAs are enough for; two sequences a lane
+      static_assert(kSeqHeld == 64, "two sequences a lane");
+      int tiles[2], mine[2];
+      const int all_tiles = ranges.total - units * kStart;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int b = 2 * lane + e;
+        tiles[e] = mine[e] = 0;
+        if (b < a.batch) {
+          const Chunk s = chunk_of(a, sh.seq[b].x, sh.seq[b].y, sh.seq[b + 1].y, kRows);
+          if (s.blocks) {
+            tiles[e] = span_of(a, s, 0, kRows).tiles;
+            mine[e] = a.n_kv_heads;
+          }
+        }
+      }
+      // (a unit's parts are less than one more than its tiles / most)
+      int least = max(1, all_tiles / grid), most = max(least, min(longest, all_tiles / (grid - units + 1) + 1));
+#pragma unroll 1
+      while (least < most) {
+        const int mid = (least + most) / 2;
+        const int need = __reduce_add_sync(0xffffffffu, mine[0] * parts_of(tiles[0], mid) + mine[1] * parts_of(tiles[1], mid));
+        if (need <= grid) most = mid; else least = mid + 1;
+      }
+      int inc = 0;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) { mine[e] *= parts_of(tiles[e], most); inc += mine[e]; }
+      const int own = inc;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int t = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += t;
+      }
+      if (lane == 0) w.left = 0;  // more CTAs than parts
       __syncwarp();
-      commit(&sh.drain);
-      mbar_drain(&sh.drain, 0);
-    } else if (!Q8) {
-      // ---- values of tiles that some row does not see whole ----------------------------
-      while (ok && next()) {
-        const int n = w.t1 - w.t0;
+      int before = inc - own;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int at = (int)blockIdx.x - before;
+        if (at >= 0 && at < mine[e]) {
+          const int parts = parts_of(tiles[e], most);
+          w.left = 1;
+          w.b = 2 * lane + e;
+          w.load(a, sh.seq, kRows);
+          w.g = span_of(a, w.s, 0, kRows);
+          w.head = at / parts;
+          w.block = 0;
+          w.count = parts;
+          w.me = at - w.head * parts;
+          w.c0 = (int)blockIdx.x - w.me;
+          w.t0 = w.me * w.g.tiles / parts;
+          w.t1 = (w.me + 1) * w.g.tiles / parts;
+        }
+        before += mine[e];
+      }
+    } else {
+      if (hi > lo) {  // the block that the first place lies in
+        const int b = sh.start_b, rest = sh.start_off;
+        const Chunk s = chunk_of(a, a.ctx_len[b], a.starts[b], a.starts[b + 1], kRows);
+        int before = 0;
+        __syncwarp();
 #pragma unroll 1
-        for (int j = 0; j < n; ++j) {
-          const int st = (tile0 + j) % NV;
-          ok = warp_wait(sh.v_full + st, ((tile0 + j) / NV) & 1, abort_flag);
-          if (!ok) break;
-          const int k0 = w.g.tile(w.t0 + j) * kTile;
-          if (!all_see(a, w.s, w.g.p_lo, w.g.p_hi, k0, k0 + kTile)) {
-            const int end = w.g.end - k0;
-            // the products take 16 keys at a time, and each half's first 16 in any case
-            const int used = min(kTile, max(kStep + 16, (end + 15) & ~15));
-            constexpr int kPieces = HD / 8;
-            bool any = false;
-            auto clean = [&](int r0, int r1) {
-#pragma unroll 8
-              for (int p = r0 * kPieces + lane; p < r1 * kPieces; p += 32) {
-                const int r = p / kPieces, c = p % kPieces;
-                uint4* at = reinterpret_cast<uint4*>(vring + st * kStage + (c / 8) * kChunkBytes + r * 128 + (((c % 8) ^ (r & 7)) << 4));
-                const uint4 v = *at;
-                const uint4 f = r >= end ? make_uint4(0, 0, 0, 0)
-                                         : make_uint4(finite_of<M>(v.x), finite_of<M>(v.y), finite_of<M>(v.z), finite_of<M>(v.w));
-                if (f.x != v.x || f.y != v.y || f.z != v.z || f.w != v.w) {
-                  *at = f;
-                  any |= r < end;
+        for (int i0 = 0; i0 < s.blocks; i0 += 32) {
+          const int len = i0 + lane < s.blocks ? span_of(a, s, i0 + lane, kRows).tiles + kStart : 0;
+          int inc = len;
+#pragma unroll
+          for (int o = 1; o < 32; o <<= 1) {
+            const int t = __shfl_up_sync(0xffffffffu, inc, o);
+            if (lane >= o) inc += t;
+          }
+          const uint32_t past = __ballot_sync(0xffffffffu, before + inc > rest);
+          if (past) {
+            if (lane == __ffs(past) - 1) { sh.start_block = i0 + lane; sh.start_off = rest - (before + inc - len); }
+            break;
+          }
+          before += __shfl_sync(0xffffffffu, inc, 31);
+        }
+        __syncwarp();
+      }
+      if (lane == 0) begin();
+    }
+    int made = 0;
+    bool more = true;
+    auto make = [&] {
+      if (!more || !ok) return;
+      const int slot = made % kAheadSegs;
+      if (made >= kAheadSegs) ok = warp_wait(sh.seg_free + slot, (made / kAheadSegs - 1) & 1, abort_flag);
+      if (!ok) return;
+      __syncwarp();
+      int some = 0;
+      if (lane == 0) {
+        some = w.next(a, sh.seq, kRows, ranges, one_part);
+        sh.seg[slot] = w;
+        if (!some) sh.seg[slot].t1 = 0;
+        mbar_arrive(sh.seg_full + slot);
+      }
+      more = __shfl_sync(0xffffffffu, some, 0) != 0;
+      ++made;
+    };
+    for (int cur = 0; ok; ++cur) {
+      while (ok && more && made < cur + kAheadSegs - 1) make();
+      if (!ok || cur >= made) break;
+      const Segment& u = sh.seg[cur % kAheadSegs];
+      const int n = u.t1 - u.t0;
+      if (u.t1 <= 0) break;
+      // ---- values of tiles that some row does not see whole ------------------------------
+#pragma unroll 1
+      for (int j = 0; j < n && !Q8; ++j) {
+        const int st = (tile0 + j) % NV;
+        ok = warp_wait(sh.v_full + st, ((tile0 + j) / NV) & 1, abort_flag);
+        if (!ok) break;
+        const int k0 = u.g.tile(u.t0 + j) * kTile;
+        if (!all_see(a, u.s, u.g.p_lo, u.g.p_hi, k0, k0 + kTile)) {
+          const int end = u.g.end - k0;  // keys of the tile
+          bool any = false;
+          constexpr int kPieces = HD / 8, kBatch = 8;
+          auto place = [&](int p) {
+            const int r = p / kPieces, c = p % kPieces;
+            return reinterpret_cast<uint4*>(vring + st * kStage + (c / 8) * kChunkBytes + r * 128 + (((c % 8) ^ (r & 7)) << 4));
+          };
+          // past the end: what the products, 16 keys at a time and each half's first
+          // 16 in any case, read
+          auto zero = [&](int r0, int r1) {
+#pragma unroll 1
+            for (int p = r0 * kPieces + lane; p < r1 * kPieces; p += 32) *place(p) = make_uint4(0, 0, 0, 0);
+          };
+          if (end < kTile) zero(end, (end + 15) & ~15);
+          if (end <= kStep) zero(kStep, kStep + 16);
+          // rows that the last of the block's rows has in its window, or that are among the first
+          // tokens, and that the first row's position reaches, are left alone
+          auto clean = [&](int r0, int r1) {
+#pragma unroll 1
+            for (int p0 = r0 * kPieces + lane; p0 < r1 * kPieces; p0 += 32 * kBatch) {
+              uint4 x[kBatch];
+#pragma unroll
+              for (int i = 0; i < kBatch; ++i) x[i] = *place(min(p0 + 32 * i, r1 * kPieces - 1));
+#pragma unroll
+              for (int i = 0; i < kBatch; ++i) {
+                const uint4 f = make_uint4(finite_of<M>(x[i].x), finite_of<M>(x[i].y), finite_of<M>(x[i].z), finite_of<M>(x[i].w));
+                if (p0 + 32 * i < r1 * kPieces && (f.x != x[i].x || f.y != x[i].y || f.z != x[i].z || f.w != x[i].w)) {
+                  *place(p0 + 32 * i) = f;
+                  any = true;
                 }
               }
-            };
-            // rows that the last of the block's rows has in its window, or that are among the first
-            // tokens, and that the first row's position reaches, are left alone
-            const int reach = min(max(min(w.g.p_lo + 1, w.s.keys) - k0, 0), used);
-            const int from = min(max(window_from(a, w.g.p_hi) - k0, 0), reach), sinks = min(max(a.sinks - k0, 0), from);
-            clean(sinks, from);
-            clean(reach, used);
-            fence_proxy_async_all();
-            any = __any_sync(0xffffffffu, any);
-            if (lane == 0) sh.odd[st] = any;
-          }
-          __syncwarp();
-          if (lane == 0) mbar_arrive(sh.fixed + st);
+            }
+          };
+          const int reach = min(max(min(u.g.p_lo + 1, u.s.keys) - k0, 0), min(end, kTile));
+          const int from = min(max(window_from(a, u.g.p_hi) - k0, 0), reach), sinks = min(max(a.sinks - k0, 0), from);
+          clean(sinks, from);
+          clean(reach, min(end, kTile));
+          fence_proxy_async_all();
+          any = __any_sync(0xffffffffu, any);
+          if (lane == 0) sh.odd[st] = any;
         }
-        tile0 += n;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(sh.fixed + st);
       }
-      if (!ok) *abort_flag = 1;
+      tile0 += n;
     }
+    if (!ok) *abort_flag = 1;
   } else if (warp < 12) {
     // ---- softmax: group g, a thread a row --------------------------------------------
     const int g = (warp - 4) >> 2, t = tid - 128 - g * kTile;  // t: row of the score tile = lane of tensor memory
@@ -767,22 +865,29 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
       ok = warp_wait(sh.met + g, ph_met, abort_flag);
       ph_met ^= 1;
     };
-    while (ok && next()) {
-      const int n = w.t1 - w.t0;
-      const int row_base = w.block * kRows + (BLOCKS == 2 ? g * kTile : 0);  // row of the unit that lane 0 of the group has
-      const int row = row_base + t, rows = w.s.rows;
+    auto arrive = [&](uint64_t* bar) {
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar);
+    };
+    while (next()) {
+      const Segment& u = segment();
+      arrive(sh.ready + g);  // O of the segment before has been read
+      const int n = u.t1 - u.t0;
+      const int row_base = u.block * kRows + (BLOCKS == 2 ? g * kTile : 0);  // row of the unit that lane 0 of the group has
+      const int row = row_base + t, rows = u.s.rows;
       const bool live = row_base + (warp & 3) * 32 < rows;  // the warp has a row at all
       // queries into shared memory, swizzled; one block: each group lays out half
-      {
+      if (!by_tma) {
         constexpr int kPieces = HD / 8, kMine = BLOCKS == 2 ? kTile : kTile / 2, kEach = kTile / kPieces;
         const uint32_t sign = a.scale < 0.f ? 0x80008000u : 0u;  // a negative scale turns the queries' signs
         const int c = t % kPieces, r0 = t / kPieces + (BLOCKS == 2 ? 0 : g * kMine), in_unit = BLOCKS == 2 ? g * kTile : 0;
-        const T* q = reinterpret_cast<const T*>(a.q) + ((int64_t)w.s.row0 + w.g.token) * a.q_stride + (int64_t)w.head * group * HD + c * 8;
+        const T* q = reinterpret_cast<const T*>(a.q) + ((int64_t)u.s.row0 + u.g.token) * a.q_stride + (int64_t)u.head * group * HD + c * 8;
         uint8_t* dst = qbuf + (BLOCKS == 2 ? g * kStage : 0) + (c / 8) * kChunkBytes;
         uint4 v[kMine / kEach];  // all loads are out before the first is stored
 #pragma unroll
         for (int i = 0; i < kMine / kEach; ++i) {
-          const int n_row = w.g.rest + in_unit + r0 + i * kEach, tok = in_group(a, n_row);
+          const int n_row = u.g.rest + in_unit + r0 + i * kEach, tok = in_group(a, n_row);
           v[i] = make_uint4(0, 0, 0, 0);
           if (row_base + r0 + i * kEach < rows) v[i] = *reinterpret_cast<const uint4*>(q + (int64_t)tok * a.q_stride + (n_row - tok * group) * HD);
         }
@@ -813,9 +918,7 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
           *reinterpret_cast<uint4*>(dst + r * 128 + (((c % 8) ^ (r & 7)) << 4)) = v[i];
         }
         fence_proxy_async_all();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(sh.ready + g);
+        arrive(&sh.q_full);
       }
       float sl2 = sl2_all;
       if constexpr (kRaised) {
@@ -823,40 +926,35 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
         if (!ok) break;
         sl2 = fmaxf(sl2_all * __uint_as_float((uint32_t)max((int)sh.back[BLOCKS == 2 ? g * kTile + t : t] - 14, 1) << 23), 1.2e-38f);
       }
-      const int n_row = w.g.rest + min(row, rows - 1) - w.block * kRows, in_token = in_group(a, n_row);  // of the block's first token on
-      const int token = w.g.token + in_token, p = w.s.ctx + token;
-      const int see_end = min(p + 1, w.s.keys), see_from = window_from(a, p);
+      const int n_row = u.g.rest + min(row, rows - 1) - u.block * kRows, in_token = in_group(a, n_row);  // of the block's first token on
+      const int token = u.g.token + in_token, p = u.s.ctx + token;
+      const int see_end = min(p + 1, u.s.keys), see_from = window_from(a, p);
       // positions of the group's first and last rows
-      auto position = [&](int r) { return w.g.p_lo + in_group(a, w.g.rest + min(r, rows - 1) - w.block * kRows); };
+      auto position = [&](int r) { return u.g.p_lo + in_group(a, u.g.rest + min(r, rows - 1) - u.block * kRows); };
       const int g_lo = position(row_base), g_hi = position(row_base + kTile - 1);
       auto page_flag = [&](int j) -> uint32_t {  // this lane's page of tile j is one of the pool
-        const int at = w.g.tile(w.t0 + j) * kTilePages + lane;
-        if (lane >= kTilePages || at * kPageTok >= w.g.end) return 1;
-        return (uint32_t)a.page_table[(size_t)w.b * a.max_pages + at] < (uint32_t)a.n_pages;
+        const int at = u.g.tile(u.t0 + j) * kTilePages + lane;
+        if (lane >= kTilePages || at * kPageTok >= u.g.end) return 1;
+        return (uint32_t)a.page_table[(size_t)u.b * a.max_pages + at] < (uint32_t)a.n_pages;
       };
       float m_ref = -INFINITY, sum = 0.f;
       bool patch = false;  // values that the rows who see them get back in the epilogue
       uint32_t flag = page_flag(0);
       const uint64_t scale2 = pair_of(__float_as_uint(sl2), __float_as_uint(sl2));
-      const Chunk ws = w.s;
-      const Span wg = w.g;
+      const Chunk us = u.s;
+      const Span ug = u.g;
+      const int first_tile = u.t0;
 #pragma unroll 1
       for (int j = 0; j < n; ++j) {
         const uint32_t flags = __ballot_sync(0xffffffffu, flag);
         if (j + 1 < n) flag = page_flag(j + 1);
-        const int k0 = wg.tile(w.t0 + j) * kTile, x = BLOCKS == 2 ? g : j & 1;
-        const bool partly = !all_see(a, ws, wg.p_lo, wg.p_hi, k0, k0 + kTile);  // some row of the block does not see all of the tile,
-        const bool masked = flags != 0xFFFFFFFFu || !all_see(a, ws, g_lo, g_hi, k0, k0 + kTile);  // some row of the group
+        const int k0 = ug.tile(first_tile + j) * kTile, x = BLOCKS == 2 ? g : j & 1;
+        const bool partly = !all_see(a, us, ug.p_lo, ug.p_hi, k0, k0 + kTile);  // some row of the block does not see all of the tile,
+        const bool masked = flags != 0xFFFFFFFFu || !all_see(a, us, g_lo, g_hi, k0, k0 + kTile);  // some row of the group
         ok = warp_wait(sh.s_full + x, ph_s >> x & 1, abort_flag);
         if (!ok) break;
         ph_s ^= 1u << x;
         tc_fence_after();
-        if (partly) {  // the stage is not refilled before these probabilities are used
-          const int st = (tile0 + j) % NV;
-          ok = warp_wait(sh.fixed + st, ((tile0 + j) / NV) & 1, abort_flag);
-          if (!ok) break;
-          patch |= sh.odd[st] != 0;
-        }
 #pragma unroll
         for (int e = 0; e < BLOCKS; ++e) {
           const int h = BLOCKS == 2 ? e : g;
@@ -916,9 +1014,13 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
             const float2 acc2 = floats_of(add2(acc[0], acc[1]));
             sum += acc2.x + acc2.y;
           }
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&sh.p_full[x][h]);
+          if (partly && e == BLOCKS - 1) {  // the stage is not refilled before these probabilities are used
+            const int st = (tile0 + j) % NV;
+            ok = warp_wait(sh.fixed + st, ((tile0 + j) / NV) & 1, abort_flag);
+            if (!ok) break;
+            patch |= sh.odd[st] != 0;
+          }
+          arrive(&sh.p_full[x][h]);
         }
         if (!ok) break;
         // a product more of its kind is on the way
@@ -941,22 +1043,26 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
         ml[g * kTile + t] = make_float4(m_ref, sum, patch ? 1.f : 0.f, 0.f);
         meet();
         if (!ok) break;
-        const float4 x = ml[t], y = ml[kTile + t];
-        patch = x.z + y.z > 0.f;
-        m_ref = fmaxf(x.x, y.x);
-        w0 = x.x == -INFINITY ? 0.f : ex2(x.x - m_ref);
-        w1 = y.x == -INFINITY ? 0.f : ex2(y.x - m_ref);
-        sum = x.y * w0 + y.y * w1;
+        const float4 y = ml[t], z = ml[kTile + t];
+        patch = y.z + z.z > 0.f;
+        m_ref = fmaxf(y.x, z.x);
+        w0 = y.x == -INFINITY ? 0.f : ex2(y.x - m_ref);
+        w1 = z.x == -INFINITY ? 0.f : ex2(z.x - m_ref);
+        sum = y.y * w0 + z.y * w1;
+        fence_proxy_async_all();  // (a copy may write there next)
+        meet();
+        if (!ok) break;
+        arrive(&sh.q_free);
       }
       constexpr int kCols = BLOCKS == 2 ? HD : HD / 2;
       const int col0 = BLOCKS == 2 ? 0 : g * kCols, in_block = (BLOCKS == 2 ? g * kTile : 0) + t;
-      const bool whole = w.t0 == 0 && w.t1 == w.g.tiles, on = row < rows;
+      const bool whole = u.t0 == 0 && u.t1 == ug.tiles, on = row < rows;
       // A unit's contributors are consecutive CTAs.  All but the last to arrive
       // leave their partial; that one joins them, in tile order (see
       // tree_attention.cu).
-      const int count = whole ? 1 : w.count, me = w.me, c0 = w.c0;
+      const int count = whole ? 1 : u.count, me = u.me, c0 = u.c0;
       uint32_t* arrived = reinterpret_cast<uint32_t*>(a.workspace) + 2 * c0 + g;
-      const Partial mine = slot_of(a, 2 * (c0 + me) + (w.t0 > 0 ? 0 : 1), HD, BLOCKS);
+      const Partial mine = slot_of(a, 2 * (c0 + me) + (u.t0 > 0 ? 0 : 1), HD, BLOCKS);
       bool two = false;
       if (count == 2) {
         if (t == 0) sh.last_in[g] = ld_acquire(arrived) == 1;
@@ -964,12 +1070,15 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
         if (!ok) break;
         two = sh.last_in[g];
       }
-      T* unit = reinterpret_cast<T*>(a.out) + ((int64_t)w.s.row0 * a.n_q_heads + (int64_t)w.head * group) * HD;
-      T* out = unit + ((int64_t)token * a.n_q_heads + (row - token * group)) * HD;
+      T* unit = reinterpret_cast<T*>(a.out) + ((int64_t)us.row0 * a.n_q_heads + (int64_t)u.head * group) * HD;
+      const int in_chunk = row - u.block * kRows + u.g.rest - in_token * group;  // this row among its token's
+      T* out = unit + ((int64_t)token * a.n_q_heads + in_chunk) * HD;
+      const int unit_row0 = row_base;
       if (!two) {
         const float inv = sum > 0.f ? 1.0f / sum : 0.f;
 #pragma unroll 1
         for (int c = col0; c < col0 + kCols; c += 32) {
+          if (!live) break;
           uint32_t o[32];
           own_columns<HD, BLOCKS>(o, my + 2 * kTile + (BLOCKS == 2 ? g * HD : 0) + c, w0, w1, true);
           if (!on) continue;
@@ -982,7 +1091,7 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
                                                          __uint_as_float(o[4 * i + 2]), __uint_as_float(o[4 * i + 3]));
           }
         }
-        if (patch && on) patch_chunk<T, HD, Q8>(a, w, p, col0, kCols, whole ? out : nullptr, mine, in_block);
+        if (patch && on) patch_chunk<T, HD, Q8>(a, u, p, col0, kCols, whole ? out : nullptr, mine, in_block);
         if (!whole) {
           *mine.stats(HD, g, in_block) = make_float2(m_ref, sum);
           // written before the group meets, read after, and written again only when
@@ -1001,8 +1110,8 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
               two = true;
             } else {
               fence_gpu();
-              const int live = min(kTile, rows - row_base);
-              join<T, HD, BLOCKS>(a, sh.slots[g], count, g, t, in_block - t, live, col0 / 4, kCols / 4, unit, row_base);
+              const int live_rows = min(kTile, rows - row_base);
+              join<T, HD, BLOCKS>(a, sh.slots[g], count, g, t, in_block - t, live_rows, col0 / 4, kCols / 4, unit, unit_row0);
               if (t == 0) *arrived = 0;  // as the next call wants it
             }
           }
@@ -1012,10 +1121,10 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
         const Partial other = slot_of(a, 2 * (c0 + 1 - me) + me, HD, BLOCKS);
         join_two<T, HD, BLOCKS>(other, my + 2 * kTile + (BLOCKS == 2 ? g * HD : 0), g, in_block, me == 0, m_ref, sum, w0,
                                 w1, true, col0, on, out, wide_out);
-        if (patch && on) patch_chunk<T, HD, Q8>(a, w, p, col0, kCols, out, mine, in_block);
+        if (patch && on) patch_chunk<T, HD, Q8>(a, u, p, col0, kCols, out, mine, in_block);
         if (t == 0) *arrived = 0;
       }
-      if (BLOCKS == 1) {  // the queries' place holds the sums, and each group reads both accumulators
+      if (BLOCKS == 1) {  // each group reads both accumulators
         meet();
         if (!ok) break;
       }
@@ -1023,29 +1132,29 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
     }
     if (!ok) *abort_flag = 1;
   } else if constexpr (Q8) {
-    // ---- codes into 16-bit entries, in place -------------------------------------------
-    // A page's codes lie in the half of its place that its last 16-bit entries take
-    // (hd 128: the second 64 entries', hd 64: the last eight tokens'); the warp that
-    // has the page holds all of them before it writes.
+    // ---- codes into 16-bit entries: two warps for keys, two for values ----------------------
     constexpr int kCodes = HD * kPageTok, kHeld = kCodes / 512, kRowPieces = HD / 16;
-    const int cw = warp - 12;
-    while (ok && next()) {
-      const int n = w.t1 - w.t0;
+    const int v = (warp - 12) >> 1, cw = warp & 1, ns = v ? NV : NK;
+    uint8_t *from0 = raw_rings + v * NR * kRaw, *to0 = v ? vring : kring;
+    uint64_t *empty = v ? sh.v_empty : sh.k_empty, *full = v ? sh.fixed : sh.k_full;
+    int st = 0, rs = 0;
+    uint32_t ph = 0, rph = 0;
+    while (next()) {
+      const Segment& u = segment();
+      const int n = u.t1 - u.t0;
 #pragma unroll 1
-      for (int jj = 0; jj < 2 * n; ++jj) {  // keys, then values of a tile
-        const bool v = jj & 1;
-        const int i = tile0 + (jj >> 1), tile = w.g.tile(w.t0 + (jj >> 1)), k0 = tile * kTile;
-        const int st = v ? i % NV : i % NK;
-        ok = v ? warp_wait(sh.v_full + st, (i / NV) & 1, abort_flag) : warp_wait(sh.k_full + st, (i / NK) & 1, abort_flag);
+      for (int j = 0; j < n; ++j) {
+        const int tile = u.g.tile(u.t0 + j), k0 = tile * kTile;
+        ok = warp_wait(sh.raw_full[v] + rs, rph, abort_flag) && warp_wait(empty + st, ph ^ 1, abort_flag);
         if (!ok) break;
-        uint8_t* stage = (v ? vring : kring) + st * kStage;
-        const uint8_t* scale = (v ? sh.v_scale : sh.k_scale) + st * kTile;
-        const bool clean = v && !all_see(a, w.s, w.g.p_lo, w.g.p_hi, k0, k0 + kTile);
-        const int pages = pages_of(tile);
+        uint8_t* stage = to0 + st * kStage;
+        const uint8_t *raw = from0 + rs * kRaw, *scale = sh.scale[v] + rs * kTile;
+        const bool clean = v && !all_see(a, u.s, u.g.p_lo, u.g.p_hi, k0, k0 + kTile);
+        const int pages = pages_of(u, tile);
         bool any = false;
 #pragma unroll 1
-        for (int q = cw; q < pages; q += kConvWarps) {
-          const uint4* codes = reinterpret_cast<const uint4*>(stage + (HD == 128 ? kChunkBytes : kCodes) + q * kPageTok * 128);
+        for (int q = cw; q < pages; q += kConvWarps / 2) {
+          const uint4* codes = reinterpret_cast<const uint4*>(raw + q * kCodes);
           uint4 x[kHeld];
           uint32_t by[kHeld];
           bool far = false;
@@ -1055,7 +1164,6 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
             by[e] = scale[q * kPageTok + (e * 32 + lane) / kRowPieces];
             far |= Widen::far(by[e]);
           }
-          far = __any_sync(0xffffffffu, far);  // (and every lane holds its codes)
           // eight entries of row r: two pieces of a row's sixteen codes, and the lanes of a
           // row's second half write theirs the other way round, so that eight lanes reach
           // all banks
@@ -1071,7 +1179,7 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
                   second ? make_uint4(y[4], y[5], y[6], y[7]) : make_uint4(y[0], y[1], y[2], y[3]);
             }
           };
-          if (!far && !clean) {
+          if (!__any_sync(0xffffffffu, far) && !clean) {
 #pragma unroll
             for (int e = 0; e < kHeld; ++e) {
               Widen w8;
@@ -1084,16 +1192,16 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
 #pragma unroll 1
             for (int e = 0; e < kHeld; ++e) {
               Widen w8;
-              const uint4 xe = e == 0 ? x[0] : e == 1 ? x[1] : e == 2 ? x[kHeld > 2 ? 2 : 0] : x[kHeld > 3 ? 3 : 0];
-              w8.set_far(e == 0 ? by[0] : e == 1 ? by[1] : e == 2 ? by[kHeld > 2 ? 2 : 0] : by[kHeld > 3 ? 3 : 0]);
+              const uint4 xe = codes[e * 32 + lane];
+              w8.set_far(scale[q * kPageTok + (e * 32 + lane) / kRowPieces]);
               uint32_t y[8] = {w8.far_two(xe.x), w8.far_two(xe.x >> 16), w8.far_two(xe.y), w8.far_two(xe.y >> 16),
                                w8.far_two(xe.z), w8.far_two(xe.z >> 16), w8.far_two(xe.w), w8.far_two(xe.w >> 16)};
               const int key = k0 + q * kPageTok + lane / kRowPieces + e * (32 / kRowPieces);
-              if (clean && !all_see(a, w.s, w.g.p_lo, w.g.p_hi, key, key + 1)) {
+              if (clean && !all_see(a, u.s, u.g.p_lo, u.g.p_hi, key, key + 1)) {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                  const uint32_t f = key >= w.g.end ? 0u : finite_of<__half>(y[k]);
-                  any |= key < w.g.end && f != y[k];
+                  const uint32_t f = key >= u.g.end ? 0u : finite_of<__half>(y[k]);
+                  any |= key < u.g.end && f != y[k];
                   y[k] = f;
                 }
               }
@@ -1107,14 +1215,15 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
             *reinterpret_cast<uint4*>(stage + (e / (kPageTok * 8)) * kChunkBytes + kStep * 128 + e % (kPageTok * 8) * 16) = make_uint4(0, 0, 0, 0);
         }
         fence_proxy_async_all();
-        if (v) {
-          any = __any_sync(0xffffffffu, any);
-          if (lane == 0) reinterpret_cast<uint8_t*>(sh.odd + st)[cw] = any;
+        any = __any_sync(0xffffffffu, any);
+        if (lane == 0) {
+          if (v) reinterpret_cast<uint8_t*>(sh.odd + st)[cw] = any;
+          mbar_arrive(full + st);
+          mbar_arrive(sh.raw_empty[v] + rs);
         }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(v ? sh.fixed + st : sh.k_fit + st);
+        if (++st == ns) { st = 0; ph ^= 1; }
+        if (++rs == NR) { rs = 0; rph ^= 1; }
       }
-      tile0 += n;
     }
     if (!ok) *abort_flag = 1;
   }
@@ -1125,22 +1234,22 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
     // A wait ran out, now or in an earlier call with this workspace (whose
     // arrivals are then not to be trusted): every unit of the range becomes NaN,
     // never numbers that look right, until the workspace is zeroed again.
+    const bool part = sh.seg[0].t1 > 0;
+    __syncthreads();
     if (tid == 0) {
       reinterpret_cast<volatile uint32_t*>(a.workspace)[kStalledWord] = 1;
-      if (one_part) w.left = had_part; else begin();
+      if (one_part) w.left = part; else begin();
     }
-    __syncthreads();
-    const ChunkWalk& u = sh.walk[0];
     while (true) {
       __syncthreads();
-      if (tid == 0) sh.odd[0] = sh.walk[0].next(a, sh.seq, kRows, ranges, one_part);
+      if (tid == 0) sh.odd[0] = w.next(a, sh.seq, kRows, ranges, one_part);
       __syncthreads();
       if (!sh.odd[0]) break;
 #pragma unroll 1
-      for (int r = u.block * kRows + tid; r < min((u.block + 1) * kRows, u.s.rows); r += kThreads) {
+      for (int r = w.block * kRows + tid; r < min((w.block + 1) * kRows, w.s.rows); r += kThreads) {
         const int token = r / group;
         T* out = reinterpret_cast<T*>(a.out) +
-                 (((int64_t)u.s.row0 + token) * a.n_q_heads + (int64_t)u.head * group + (r - token * group)) * HD;
+                 (((int64_t)w.s.row0 + token) * a.n_q_heads + (int64_t)w.head * group + (r - token * group)) * HD;
 #pragma unroll 1
         for (int e = 0; e < HD; e += 2) *reinterpret_cast<uint32_t*>(out + e) = 0x7FFF7FFFu;
       }
@@ -1155,6 +1264,23 @@ namespace {
 // both work on the same rows.
 int chunk_blocks(int n_tokens, int batch, int group) { return (int64_t)n_tokens * group <= (int64_t)batch * kTile ? 1 : 2; }
 
+// The queries as [token][head][entry], boxes of some tokens x a key/value head's query heads x 64 entries.
+inline CUtensorMap query_map(const ChunkAttnArgs& a, int tokens) {
+  CUtensorMap m;
+  std::memset(&m, 0, sizeof(m));
+  auto enc = encoder();
+  if (!enc) throw cudaErrorNotSupported;
+  const cuuint64_t hd = a.head_dim;
+  const cuuint64_t dims[3] = {hd, (cuuint64_t)a.n_q_heads, (cuuint64_t)a.n_tokens};
+  const cuuint64_t strides[2] = {hd * 2, (cuuint64_t)a.q_stride * 2};
+  const cuuint32_t box[3] = {64, (cuuint32_t)(a.n_q_heads / a.n_kv_heads), (cuuint32_t)tokens}, es[3] = {1, 1, 1};
+  const CUresult r = enc(&m, a.dtype == DT_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
+                         const_cast<void*>(a.q), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) throw cudaErrorInvalidValue;
+  return m;
+}
+
 template <typename T, int HD, int BLOCKS, bool Q8>
 void run_chunk(const ChunkAttnArgs& a, cudaStream_t s) {
   constexpr int smem = chunk_smem<HD, BLOCKS, Q8>();
@@ -1168,15 +1294,21 @@ void run_chunk(const ChunkAttnArgs& a, cudaStream_t s) {
     return n;
   });
   const int grid = sms < kMaxGrid ? sms : kMaxGrid;
-  CUtensorMap km, vm;
-  if (Q8) {
-    std::memset(&km, 0, sizeof(km));
-    vm = km;
-  } else {
+  CUtensorMap km, vm, qm;
+  std::memset(&km, 0, sizeof(km));
+  vm = qm = km;
+  ChunkAttnArgs args = a;
+  const int group = a.n_q_heads / a.n_kv_heads;
+  args.group_magic = group > 1 ? 0xFFFFFFFFu / (uint32_t)group + 1 : 0;
+  if (!Q8) {
     km = cache_map(a, a.k_cache);
     vm = cache_map(a, a.v_cache);
+    // Queries come by tensor copies where a block's rows are whole tokens and need
+    // no other sign; the softmax warps' own loads take 4000 clocks before a unit's first scores.
+    args.q_by_tma = kTile % group == 0 && !(a.scale < 0.f);
+    if (args.q_by_tma) qm = query_map(a, kTile / group);
   }
-  launch_in_turn(kernel, dim3(grid), chunk_threads(Q8), smem, 0, s, a, km, vm);
+  launch_in_turn(kernel, dim3(grid), chunk_threads(Q8), smem, 0, s, args, km, vm, qm);
 }
 
 // the caches' width is the translation unit's
@@ -1186,9 +1318,7 @@ void run_chunk_sized(const ChunkAttnArgs& a, cudaStream_t s) {
   else run_chunk<T, HD, 2, Q8>(a, s);
 }
 template <bool Q8>
-void run_chunk_attention(ChunkAttnArgs a, cudaStream_t s) {
-  const uint32_t group = a.n_q_heads / a.n_kv_heads;
-  a.group_magic = group > 1 ? 0xFFFFFFFFu / group + 1 : 0;
+void run_chunk_attention(const ChunkAttnArgs& a, cudaStream_t s) {
   if (a.dtype == DT_BF16) {
     if (a.head_dim == 128) run_chunk_sized<Q8, __nv_bfloat16, 128>(a, s); else run_chunk_sized<Q8, __nv_bfloat16, 64>(a, s);
   } else {

@@ -34,7 +34,9 @@ struct ChunkAttnArgs {
   float scale;
   void* out;
   void* workspace;
-  uint32_t group_magic = 0;  // 2^32 / (query heads a key/value head), rounded up; 0 for one: the launcher's
+  // the launcher's
+  uint32_t group_magic = 0;  // 2^32 / (query heads a key/value head), rounded up; 0 for one
+  bool q_by_tma = false;
 };
 size_t chunk_attention_workspace(int n_tokens, int batch, int n_q_heads, int n_kv_heads, int head_dim);
 // places of the work ranges that a pass may have: below 2^31
