@@ -294,6 +294,9 @@ static_assert(chunk_smem<64, 1, false>() <= 227 * 1024 && chunk_smem<64, 2, fals
 static_assert(chunk_smem<128, 1, true>() <= 227 * 1024 && chunk_smem<128, 2, true>() <= 227 * 1024, "shared memory of one CTA");
 static_assert(chunk_smem<64, 1, true>() <= 227 * 1024 && chunk_smem<64, 2, true>() <= 227 * 1024, "shared memory of one CTA");
 
+// orders this thread's accesses to shared memory with copies' and products' ones
+__device__ __forceinline__ void fence_proxy_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
 __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* m, uint64_t* bar, int c0, int c1, int c2) {
   asm volatile(
       "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
@@ -822,9 +825,11 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
               for (int i = 0; i < kBatch; ++i) x[i] = *place(min(p0 + 32 * i, r1 * kPieces - 1));
 #pragma unroll
               for (int i = 0; i < kBatch; ++i) {
-                const uint4 f = make_uint4(finite_of<M>(x[i].x), finite_of<M>(x[i].y), finite_of<M>(x[i].z), finite_of<M>(x[i].w));
-                if (p0 + 32 * i < r1 * kPieces && (f.x != x[i].x || f.y != x[i].y || f.z != x[i].z || f.w != x[i].w)) {
-                  *place(p0 + 32 * i) = f;
+                // (an exponent of all ones carries into the bit above it)
+                constexpr uint32_t kExp = Num<M>::kExponent * 0x10001u, kOne = (0x8000u - Num<M>::kExponent) * 0x10001u;
+                const uint32_t bad = ((x[i].x & kExp) + kOne) | ((x[i].y & kExp) + kOne) | ((x[i].z & kExp) + kOne) | ((x[i].w & kExp) + kOne);
+                if ((bad & 0x80008000u) && p0 + 32 * i < r1 * kPieces) {
+                  *place(p0 + 32 * i) = make_uint4(finite_of<M>(x[i].x), finite_of<M>(x[i].y), finite_of<M>(x[i].z), finite_of<M>(x[i].w));
                   any = true;
                 }
               }
@@ -834,7 +839,7 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
           const int from = min(max(window_from(a, u.g.p_hi) - k0, 0), reach), sinks = min(max(a.sinks - k0, 0), from);
           clean(sinks, from);
           clean(reach, min(end, kTile));
-          fence_proxy_async_all();
+          fence_proxy_shared();
           any = __any_sync(0xffffffffu, any);
           if (lane == 0) sh.odd[st] = any;
         }
@@ -917,7 +922,7 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
           v[i].x ^= sign; v[i].y ^= sign; v[i].z ^= sign; v[i].w ^= sign;
           *reinterpret_cast<uint4*>(dst + r * 128 + (((c % 8) ^ (r & 7)) << 4)) = v[i];
         }
-        fence_proxy_async_all();
+        fence_proxy_shared();
         arrive(&sh.q_full);
       }
       float sl2 = sl2_all;
@@ -1049,7 +1054,7 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
         w0 = y.x == -INFINITY ? 0.f : ex2(y.x - m_ref);
         w1 = z.x == -INFINITY ? 0.f : ex2(z.x - m_ref);
         sum = y.y * w0 + z.y * w1;
-        fence_proxy_async_all();  // (a copy may write there next)
+        fence_proxy_shared();  // (a copy may write there next)
         meet();
         if (!ok) break;
         arrive(&sh.q_free);
@@ -1214,7 +1219,7 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
           for (int e = lane; e < kPageTok * HD / 8; e += 32)
             *reinterpret_cast<uint4*>(stage + (e / (kPageTok * 8)) * kChunkBytes + kStep * 128 + e % (kPageTok * 8) * 16) = make_uint4(0, 0, 0, 0);
         }
-        fence_proxy_async_all();
+        fence_proxy_shared();
         any = __any_sync(0xffffffffu, any);
         if (lane == 0) {
           if (v) reinterpret_cast<uint8_t*>(sh.odd + st)[cw] = any;
