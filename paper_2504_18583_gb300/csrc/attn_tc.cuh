@@ -36,6 +36,11 @@ template <> struct Num<__nv_bfloat16> {
     return *reinterpret_cast<uint32_t*>(&p);
   }
   static __device__ __forceinline__ float get(const void* p) { return __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(p)); }
+  // two values times zero, added: NaN where one was infinite or NaN
+  static __device__ __forceinline__ uint32_t times_zero(uint32_t x, uint32_t sum) {
+    asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(sum) : "r"(x), "r"(0u));
+    return sum;
+  }
 };
 template <> struct Num<__half> {
   static constexpr uint32_t kFormat = 0;
@@ -46,6 +51,10 @@ template <> struct Num<__half> {
     return *reinterpret_cast<uint32_t*>(&p);
   }
   static __device__ __forceinline__ float get(const void* p) { return __half2float(*reinterpret_cast<const __half*>(p)); }
+  static __device__ __forceinline__ uint32_t times_zero(uint32_t x, uint32_t sum) {
+    asm("fma.rn.f16x2 %0, %1, %2, %0;" : "+r"(sum) : "r"(x), "r"(0u));
+    return sum;
+  }
 };
 
 // Instruction descriptor, kind::f16, fp32 accumulator, A K-major; `flip`: B

@@ -801,23 +801,20 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
         const int k0 = u.g.tile(u.t0 + j) * kTile;
         if (!all_see(a, u.s, u.g.p_lo, u.g.p_hi, k0, k0 + kTile)) {
           const int end = u.g.end - k0;  // keys of the tile
-          bool any = false;
-          constexpr int kPieces = HD / 8, kBatch = 8;
+          constexpr int kPieces = HD / 8, kBatch = 4;
           auto place = [&](int p) {
             const int r = p / kPieces, c = p % kPieces;
             return reinterpret_cast<uint4*>(vring + st * kStage + (c / 8) * kChunkBytes + r * 128 + (((c % 8) ^ (r & 7)) << 4));
           };
-          // past the end: what the products, 16 keys at a time and each half's first
-          // 16 in any case, read
-          auto zero = [&](int r0, int r1) {
-#pragma unroll 1
-            for (int p = r0 * kPieces + lane; p < r1 * kPieces; p += 32) *place(p) = make_uint4(0, 0, 0, 0);
-          };
-          if (end < kTile) zero(end, (end + 15) & ~15);
-          if (end <= kStep) zero(kStep, kStep + 16);
-          // rows that the last of the block's rows has in its window, or that are among the first
-          // tokens, and that the first row's position reaches, are left alone
+          // Rows that the last of the block's rows has in its window, or that are among the
+          // first tokens, and that the first row's position reaches, are left alone; the
+          // others, and those past the end that the products read too (16 keys at a time and
+          // each half's first 16 in any case), lose what is not finite.  As a rule there is
+          // nothing: times zero, summed, it would be NaN.
+          bool any = false, wrote = false;
           auto clean = [&](int r0, int r1) {
+            if (r0 >= r1) return;
+            uint32_t acc[4] = {0, 0, 0, 0};
 #pragma unroll 1
             for (int p0 = r0 * kPieces + lane; p0 < r1 * kPieces; p0 += 32 * kBatch) {
               uint4 x[kBatch];
@@ -825,21 +822,28 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
               for (int i = 0; i < kBatch; ++i) x[i] = *place(min(p0 + 32 * i, r1 * kPieces - 1));
 #pragma unroll
               for (int i = 0; i < kBatch; ++i) {
-                // (an exponent of all ones carries into the bit above it)
-                constexpr uint32_t kExp = Num<M>::kExponent * 0x10001u, kOne = (0x8000u - Num<M>::kExponent) * 0x10001u;
-                const uint32_t bad = ((x[i].x & kExp) + kOne) | ((x[i].y & kExp) + kOne) | ((x[i].z & kExp) + kOne) | ((x[i].w & kExp) + kOne);
-                if ((bad & 0x80008000u) && p0 + 32 * i < r1 * kPieces) {
-                  *place(p0 + 32 * i) = make_uint4(finite_of<M>(x[i].x), finite_of<M>(x[i].y), finite_of<M>(x[i].z), finite_of<M>(x[i].w));
-                  any = true;
-                }
+                acc[0] = Num<M>::times_zero(x[i].x, acc[0]);
+                acc[1] = Num<M>::times_zero(x[i].y, acc[1]);
+                acc[2] = Num<M>::times_zero(x[i].z, acc[2]);
+                acc[3] = Num<M>::times_zero(x[i].w, acc[3]);
               }
+            }
+            if (!__any_sync(0xffffffffu, ((acc[0] | acc[1] | acc[2] | acc[3]) & 0x7FFF7FFFu) != 0)) return;
+            wrote = true;
+#pragma unroll 1
+            for (int p = r0 * kPieces + lane; p < r1 * kPieces; p += 32) {
+              const uint4 x = *place(p), f = make_uint4(finite_of<M>(x.x), finite_of<M>(x.y), finite_of<M>(x.z), finite_of<M>(x.w));
+              if (f.x == x.x && f.y == x.y && f.z == x.z && f.w == x.w) continue;
+              *place(p) = f;
+              any |= p < end * kPieces;
             }
           };
           const int reach = min(max(min(u.g.p_lo + 1, u.s.keys) - k0, 0), min(end, kTile));
           const int from = min(max(window_from(a, u.g.p_hi) - k0, 0), reach), sinks = min(max(a.sinks - k0, 0), from);
           clean(sinks, from);
-          clean(reach, min(end, kTile));
-          fence_proxy_shared();
+          clean(reach, min(kTile, (end + 15) & ~15));
+          if (end <= kStep) clean(kStep, kStep + 16);
+          if (wrote) fence_proxy_shared();
           any = __any_sync(0xffffffffu, any);
           if (lane == 0) sh.odd[st] = any;
         }
