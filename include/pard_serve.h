@@ -79,7 +79,7 @@ pard_status pard_chunk_attention(const void* d_q, int64_t q_stride, int32_t dtyp
  * r, f, p: d_repetition, d_frequency, d_presence [batch] (null: 1, 0, 0).  Biases:
  * d_bias_ids, d_bias [batch][n_bias] (at most 2047).  d_allowed [batch * width]
  * [ceil(vocab / 32)] (null: all): bit v mod 32 of word v / 32.  Tokens outside
- * [0, vocab) are passed over.  vocab <= 262144, max_history <= 1000000. */
+ * [0, vocab) are passed over.  vocab <= 262144, max_history <= 524000. */
 pard_status pard_adjust_logits(const void* d_logits, int64_t row_stride, int32_t dtype, int32_t batch, int32_t width,
                                int32_t vocab, const int32_t* d_history, int32_t max_history, const int32_t* d_hist_len,
                                const int32_t* d_prompt_len, const float* d_repetition, const float* d_frequency,

@@ -10,18 +10,24 @@
 //
 // A CTA has one sequence's slice of the vocabulary for some of its rows.  The
 // history is counted into a table of a word an entry in shared memory (whole
-// numbers: no order), which then stays for all rows; a row of a tree adds its
-// branch's tokens before it is worked on and takes them out after.  Biases are
-// numbered in the same word, those of one token summed in the list's order by
-// one thread.  So a row costs its own reading and writing, and each slice reads
-// the whole history from L2, 4 bytes a token.
+// numbers: no order), biases are numbered in the same words, those of one token
+// summed in the list's order by one thread, and the entries that have something
+// become a list.  That is done once; a row is then copied, with its mask, and the
+// list's entries are worked out from its logits and written over the copy.  (With
+// the table looked up for every entry instead, nearly every warp had an entry to
+// change in each of its pieces: 64 rows with 8000 tokens took 28.5 us, 464 rows of
+// trees, which also added and removed each branch's tokens in the table, 159.)  A
+// tree's tokens are in the list too; how often a row's branch has one is counted
+// where it is needed.
 //
 // What bounds it: HBM for many rows, and for one the chain history -> table ->
-// row; a row's loads go out before the history's are looked at, and the next
-// row's before this one is worked on.
+// list -> row; a row's loads go out before the history's are looked at, and the
+// next row's before this one is worked on.  Slices are as long as they may be
+// while the CTAs come out as whole waves of four an SM.
 #include <cuda_fp16.h>
 
 #include "common.cuh"
+#include "per_device.h"
 #include "serve.h"
 
 namespace pard {
@@ -29,11 +35,14 @@ namespace pard {
 namespace {
 
 constexpr int kAdjThreads = 256;
+constexpr int kAdjCtas = 4;                   // CTAs an SM
+constexpr int kAdjLongest = 6912;             // entries of a slice, six bytes of shared memory each
 constexpr int kAdjVectors = 4;                // 16-byte pieces of a row's slice that a thread has
-constexpr uint32_t kCount = (1u << 20) - 1;   // of a table's word: how often the token was generated,
+constexpr uint32_t kCount = (1u << 19) - 1;   // of a table's word: how often the token was generated,
+constexpr uint32_t kOnTree = 1u << 19;        // whether a node of the tree has it,
 constexpr uint32_t kInPrompt = 1u << 20;      // whether the prompt has it,
 constexpr int kBiasShift = 21;                // and the number of its bias (0: none)
-static_assert(kMaxHistory + kTreeMaxNodes < (1 << 20) && kMaxBiases < (1 << 11), "fields of a table's word");
+static_assert(kMaxHistory + kTreeMaxNodes < (1 << 19) && kMaxBiases < (1 << 11), "fields of a table's word");
 
 template <typename T> struct Entries;  // of 16 bytes
 template <> struct Entries<float> {
@@ -99,41 +108,48 @@ struct Piece {
 }  // namespace
 
 template <typename T, bool MASK>
-__global__ void __launch_bounds__(kAdjThreads, 4) adjust_kernel(const __grid_constant__ AdjustArgs a, int slice) {
+__global__ void __launch_bounds__(kAdjThreads, kAdjCtas) adjust_kernel(const __grid_constant__ AdjustArgs a, int slice) {
   constexpr int kN = Entries<T>::kN;
-  extern __shared__ __align__(16) uint32_t table[];  // a word an entry, the biases' sums, their doubles' marks
+  // a word an entry, the biases' sums, the list, the marks of biases that come again
+  extern __shared__ __align__(16) uint32_t table[];
   float* sums = reinterpret_cast<float*>(table + slice);
-  uint8_t* twice = reinterpret_cast<uint8_t*>(sums + a.n_bias);
+  uint16_t* list = reinterpret_cast<uint16_t*>(sums + a.n_bias);
+  uint8_t* twice = reinterpret_cast<uint8_t*>(list + slice);
+  __shared__ int s_listed;
+  __shared__ uint32_t s_words[2][kAdjLongest / 32 + 1];  // a row's mask, and the next one's
+  __shared__ int32_t s_tokens[kTreeMaxNodes];  // a tree's tokens, as places in the slice (others: -1)
   const int tid = threadIdx.x, b = blockIdx.y, lo = blockIdx.x * slice, n = min(slice, a.vocab - lo);
   const int words = (a.vocab + 31) / 32;
   pdl_trigger();
 #pragma unroll 4
   for (int i = tid; i < slice / 4; i += kAdjThreads) reinterpret_cast<uint4*>(table)[i] = make_uint4(0, 0, 0, 0);
   for (int i = tid; i < a.n_bias; i += kAdjThreads) twice[i] = 0;
+  if (tid == 0) s_listed = 0;
   pdl_wait();
-  // a row's pieces that this thread has, and the mask's words that cover them
+  // a row's pieces that this thread has, and a word of its mask, which goes to all
+  // through shared memory (each thread's own words from L1: 40 us of 128 for 464 rows)
   struct Held {
     uint4 x[kAdjVectors];
-    uint32_t w0[kAdjVectors], w1[kAdjVectors];
+    uint32_t word;
   };
+  static_assert(kAdjLongest / 32 <= kAdjThreads, "a word a thread");
   auto load = [&](int i, Held& h) {
     const int64_t row = (int64_t)b * a.width + i;
     const Piece<T> p(a, row, lo, n);
-    const uint32_t* allowed = a.allowed + row * words;
+    if (MASK && tid < (n + 31) / 32) h.word = __ldg(a.allowed + row * words + lo / 32 + tid);
 #pragma unroll
     for (int e = 0; e < kAdjVectors; ++e) {
       const int v = tid + e * kAdjThreads;
       if (v >= p.vectors) break;
       h.x[e] = __ldcs(reinterpret_cast<const uint4*>(p.in + p.head) + v);
-      if (MASK) {
-        const int at = lo + p.head + v * kN;
-        h.w0[e] = allowed[at >> 5];
-        h.w1[e] = allowed[(at + kN - 1) >> 5];
-      }
     }
   };
   Held now;
   load(blockIdx.z, now);
+  // the first to touch an entry puts it on the list
+  auto touched = [&](uint32_t old, uint32_t at) {
+    if (old == 0) list[atomicAdd(&s_listed, 1)] = (uint16_t)at;
+  };
   Asked ask{1.f, 0.f, 0.f, sums};
   if (a.repetition) ask.repetition = a.repetition[b];
   if (a.frequency) ask.frequency = a.frequency[b];
@@ -147,7 +163,7 @@ __global__ void __launch_bounds__(kAdjThreads, 4) adjust_kernel(const __grid_con
     const float* bias = a.bias + (int64_t)b * a.n_bias;
     for (int j = tid; j < a.n_bias; j += kAdjThreads) {
       const uint32_t at = (uint32_t)ids[j] - (uint32_t)lo;
-      if (at < (uint32_t)n) atomicMax(table + at, (uint32_t)(a.n_bias - j) << kBiasShift);
+      if (at < (uint32_t)n) touched(atomicMax(table + at, (uint32_t)(a.n_bias - j) << kBiasShift), at);
     }
     __syncthreads();
     for (int j = tid; j < a.n_bias; j += kAdjThreads) {
@@ -168,64 +184,83 @@ __global__ void __launch_bounds__(kAdjThreads, 4) adjust_kernel(const __grid_con
     __syncthreads();
   }
   {
+    // 16 bytes of the history at a time between its first and last boundary
     const int32_t* said = a.history + (int64_t)b * a.max_history;
-#pragma unroll 8
-    for (int i = tid; i < length; i += kAdjThreads) {
-      const uint32_t at = (uint32_t)said[i] - (uint32_t)lo;
-      if (at < (uint32_t)n) {
-        if (i < prompt) atomicOr(table + at, kInPrompt); else atomicAdd(table + at, 1u);
+    const int head = min(length, (int)((16 - (reinterpret_cast<uintptr_t>(said) & 15)) & 15) / 4), pieces = (length - head) / 4;
+    auto count = [&](int i, int32_t id) {
+      const uint32_t at = (uint32_t)id - (uint32_t)lo;
+      if (at < (uint32_t)n) touched(i < prompt ? atomicOr(table + at, kInPrompt) : atomicAdd(table + at, 1u), at);
+    };
+    for (int p0 = tid; p0 < pieces; p0 += 8 * kAdjThreads) {
+      int4 q[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (p0 + e * kAdjThreads < pieces) q[e] = __ldg(reinterpret_cast<const int4*>(said + head) + p0 + e * kAdjThreads);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int v = p0 + e * kAdjThreads, i = head + 4 * v;
+        if (v >= pieces) break;
+        count(i, q[e].x);
+        count(i + 1, q[e].y);
+        count(i + 2, q[e].z);
+        count(i + 3, q[e].w);
       }
     }
+    const int i = tid < head ? tid : head + 4 * pieces + tid - head;
+    if (i < length && (tid < head || i >= head + 4 * pieces)) count(i, __ldg(said + i));
   }
-  // the branch's token that this thread adds, if it lies in the slice
-  uint32_t mine = 0xFFFFFFFFu;
-  if (a.tokens && tid < a.width) {
+  const int nodes = a.tokens ? a.width : 0;
+  if (tid < nodes) {
     const uint32_t at = (uint32_t)a.tokens[(int64_t)b * a.width + tid] - (uint32_t)lo;
-    if (at < (uint32_t)n) mine = at;
+    s_tokens[tid] = at < (uint32_t)n ? (int)at : -1;
+    if (at < (uint32_t)n) touched(atomicOr(table + at, kOnTree), at);
   }
-  const bool branches = __syncthreads_or(mine != 0xFFFFFFFFu);
-  const int mask_words = (a.width + 63) / 64;
-  auto on_branch = [&](int i) -> bool {
-    return mine != 0xFFFFFFFFu && (a.mask[((int64_t)b * a.width + i) * mask_words + (tid >> 6)] >> (tid & 63) & 1);
+  if (MASK && tid < (n + 31) / 32) s_words[0][tid] = now.word;
+  __syncthreads();
+  const int listed = s_listed, mask_words = (a.width + 63) / 64;
+  // One entry of the list a thread, as a rule: its logit is asked for with the row's
+  // pieces, and which of the tree's nodes have it is found once.
+  const bool own = listed <= kAdjThreads, has = own && tid < listed;
+  const int mine = has ? list[tid] : 0;
+  const uint32_t held = has ? table[mine] : 0;
+  uint64_t nodes_with[kTreeMaxWords] = {0, 0, 0, 0};
+  if (held & kOnTree)
+    for (int j = 0; j < nodes; ++j)
+#pragma unroll
+      for (int w = 0; w < kTreeMaxWords; ++w)
+        if (s_tokens[j] == mine && j >> 6 == w) nodes_with[w] |= (uint64_t)1 << (j & 63);
+  auto load_own = [&](int i, T& z) {
+    if (has) z = reinterpret_cast<const T*>(a.logits)[((int64_t)b * a.width + i) * a.stride + lo + mine];
   };
+  T z{};
+  load_own(blockIdx.z, z);
 #pragma unroll 1
-  for (int i = blockIdx.z; i < a.width; i += gridDim.z) {
+  for (int i = blockIdx.z, buf = 0; i < a.width; i += gridDim.z, buf ^= 1) {
     const int64_t row = (int64_t)b * a.width + i;
-    Held next;
-    if (i + (int)gridDim.z < a.width) load(i + gridDim.z, next);
-    bool added = false;
-    if (branches) {
-      added = on_branch(i);
-      if (added) atomicAdd(table + mine, 1u);
-      __syncthreads();
-    }
     const Piece<T> p(a, row, lo, n);
-    const bool even = (p.head & 3) == 0;  // the table's words of a piece lie on 16-byte boundaries too
+    const uint32_t* allowed = s_words[buf];
+    auto allows = [&](int at) { return !MASK || (allowed[at >> 5] >> (at & 31) & 1); };
+    const bool mine_allowed = has && allows(mine);
+    uint32_t t = held;
+    if (held & kOnTree) {
+#pragma unroll
+      for (int w = 0; w < kTreeMaxWords; ++w)
+        if (w < mask_words) t += __popcll(a.mask[row * mask_words + w] & nodes_with[w]);
+    }
+    Held next;
+    T z_next{};
+    if (i + (int)gridDim.z < a.width) {
+      load(i + gridDim.z, next);
+      load_own(i + gridDim.z, z_next);
+    }
 #pragma unroll
     for (int e = 0; e < kAdjVectors; ++e) {
       const int v = tid + e * kAdjThreads;
       if (v >= p.vectors) break;
-      const int at = p.head + v * kN;
-      uint32_t x[4] = {now.x[e].x, now.x[e].y, now.x[e].z, now.x[e].w}, t[kN], any = 0;
-      if (even) {
-#pragma unroll
-        for (int k = 0; k < kN / 4; ++k) {
-          const uint4 q = *reinterpret_cast<const uint4*>(table + at + 4 * k);
-          t[4 * k] = q.x; t[4 * k + 1] = q.y; t[4 * k + 2] = q.z; t[4 * k + 3] = q.w;
-        }
-      } else {
-#pragma unroll
-        for (int k = 0; k < kN; ++k) t[k] = table[at + k];
-      }
-#pragma unroll
-      for (int k = 0; k < kN; ++k) any |= t[k];
-      if (any) {
-#pragma unroll
-        for (int k = 0; k < kN; ++k)
-          if (t[k]) Entries<T>::put(x, k, ask.of(Entries<T>::get(x, k), t[k]));
-      }
+      uint32_t x[4] = {now.x[e].x, now.x[e].y, now.x[e].z, now.x[e].w};
       if (MASK) {
-        const uint32_t bits = __funnelshift_r(now.w0[e], now.w1[e], (lo + at) & 31);
+        const int at = p.head + v * kN;
+        const uint32_t bits = __funnelshift_r(allowed[at >> 5], allowed[(at + kN - 1) >> 5], at & 31);
 #pragma unroll
         for (int k = 0; k < kN; ++k)
           if (!(bits >> k & 1)) Entries<T>::put(x, k, -INFINITY);
@@ -236,34 +271,51 @@ __global__ void __launch_bounds__(kAdjThreads, 4) adjust_kernel(const __grid_con
     const int tail0 = p.head + p.vectors * kN, loose = p.head + n - tail0;
     for (int k = tid; k < loose; k += kAdjThreads) {
       const int at = k < p.head ? k : tail0 + k - p.head;
-      float z = Entries<T>::one(p.in + at);
-      const uint32_t t = table[at];
-      if (MASK && !(a.allowed[row * words + ((lo + at) >> 5)] >> ((lo + at) & 31) & 1)) p.out[at] = Entries<T>::round(-INFINITY);
-      else if (t) p.out[at] = Entries<T>::round(ask.of(z, t));
-      else p.out[at] = p.in[at];
+      const T x = p.in[at];
+      p.out[at] = allows(at) ? x : Entries<T>::round(-INFINITY);
     }
-    if (branches) {
-      __syncthreads();
-      if (added) atomicSub(table + mine, 1u);
+    if (MASK && tid < (n + 31) / 32) s_words[buf ^ 1][tid] = next.word;
+    __syncthreads();  // the copy is there
+    if (own) {
+      if (mine_allowed) p.out[mine] = Entries<T>::round(ask.of(Entries<T>::one(&z), t));
+    } else {
+      // (in place, the copy has left what is allowed as it was)
+      for (int k = tid; k < listed; k += kAdjThreads) {
+        const int at = list[k];
+        if (MASK && !(a.allowed[row * words + ((lo + at) >> 5)] >> (at & 31) & 1)) continue;  // (the row after the next may be in `allowed`)
+        uint32_t tk = table[at];
+        if (tk & kOnTree)
+          for (int j = 0; j < nodes; ++j)
+            if (s_tokens[j] == at) tk += (uint32_t)(a.mask[row * mask_words + (j >> 6)] >> (j & 63) & 1);
+        p.out[at] = Entries<T>::round(ask.of(Entries<T>::one(p.in + at), tk));
+      }
     }
     now = next;
+    z = z_next;
   }
 }
 
 template <typename T>
 static void run_adjust(const AdjustArgs& a, cudaStream_t s) {
-  // Slices as long as a thread's pieces allow, shorter where that gives fewer CTAs
-  // than four an SM, down to one piece a thread; then rows are shared out too.
-  const int piece = kAdjThreads * Entries<T>::kN, want = 4 * 152;
-  int slice = kAdjVectors * piece;
-  while (slice > piece && (int64_t)a.batch * ((a.vocab + slice - 1) / slice) < want) slice /= 2;
+  // Slices as long as a thread's pieces and shared memory allow, shortened until the
+  // CTAs are whole waves, down to one piece a thread; where that leaves SMs
+  // without a CTA, rows are shared out too.
+  const int piece = kAdjThreads * Entries<T>::kN, wave = kAdjCtas * 152;
+  const int longest = kAdjVectors * piece < kAdjLongest ? kAdjVectors * piece : kAdjLongest;
+  const int64_t least = (int64_t)a.batch * ((a.vocab + longest - 1) / longest), waves = (least + wave - 1) / wave;
+  const int64_t slices_wanted = waves * wave / a.batch;
+  int64_t slice64 = slices_wanted > 0 ? (a.vocab + slices_wanted - 1) / slices_wanted : longest;
+  slice64 = (slice64 + 31) / 32 * 32;
+  const int slice = (int)(slice64 < piece ? piece : slice64 > longest ? longest : slice64);
   const int slices = (a.vocab + slice - 1) / slice;
   const int64_t ctas = (int64_t)a.batch * slices;
-  const int shares = ctas >= want ? 1 : (int)((want + ctas - 1) / ctas);
+  const int shares = ctas >= wave ? 1 : (int)(wave / ctas);
   const dim3 grid(slices, a.batch, shares < a.width ? shares : a.width);
-  const size_t smem = (size_t)slice * 4 + (size_t)a.n_bias * 5;
-  if (a.allowed) launch_in_turn(adjust_kernel<T, true>, grid, kAdjThreads, smem, 0, s, a, slice);
-  else launch_in_turn(adjust_kernel<T, false>, grid, kAdjThreads, smem, 0, s, a, slice);
+  const size_t smem = (size_t)slice * 6 + (size_t)a.n_bias * 5;
+  auto* kernel = a.allowed ? adjust_kernel<T, true> : adjust_kernel<T, false>;
+  static OncePerDevice allowed[2];
+  allowed[a.allowed ? 1 : 0].get(current_device(), [&] { return allow_shared(kernel, kAdjLongest * 6 + kMaxBiases * 5); });
+  launch_in_turn(kernel, grid, kAdjThreads, smem, 0, s, a, slice);
 }
 
 void launch_adjust_logits(const AdjustArgs& a, cudaStream_t s) {

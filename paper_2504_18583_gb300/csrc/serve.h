@@ -7,7 +7,7 @@
 
 namespace pard {
 
-constexpr int kMaxHistory = 1000000;  // tokens of a sequence that penalties count: 20 bits hold them and a branch's
+constexpr int kMaxHistory = 524000;   // tokens of a sequence that penalties count: 19 bits hold them and a branch's
 constexpr int kMaxBiases = 2047;      // biases of a sequence: 11 bits number them
 
 struct AdjustArgs {

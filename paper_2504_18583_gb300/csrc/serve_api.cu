@@ -114,7 +114,7 @@ pard_status pard_adjust_logits(const void* d_logits, int64_t row_stride, int32_t
   if (batch < 0 || batch > 65535 || width < 0 || (int64_t)batch * width > (1 << 24))
     return refuse(PARD_ERR_ARG, "adjust_logits: batch outside [0, 65535] or more than 2^24 rows");
   if (vocab < 1 || vocab > kSampleMaxVocab) return refuse(PARD_ERR_SHAPE, "adjust_logits: vocabulary outside [1, 262144]");
-  if (max_history < 0 || max_history > kMaxHistory) return refuse(PARD_ERR_ARG, "adjust_logits: history outside [0, 1000000]");
+  if (max_history < 0 || max_history > kMaxHistory) return refuse(PARD_ERR_ARG, "adjust_logits: history outside [0, 524000]");
   if (max_history > 0 && (!d_history || !d_hist_len)) return refuse(PARD_ERR_ARG, "adjust_logits: a history needs its tokens and lengths");
   if (n_bias < 0 || n_bias > kMaxBiases) return refuse(PARD_ERR_ARG, "adjust_logits: biases outside [0, 2047]");
   if (n_bias > 0 && (!d_bias_ids || !d_bias)) return refuse(PARD_ERR_ARG, "adjust_logits: biases need their tokens and values");
