@@ -116,6 +116,7 @@ __global__ void __launch_bounds__(kAdjThreads, kAdjCtas) adjust_kernel(const __g
   uint16_t* list = reinterpret_cast<uint16_t*>(sums + a.n_bias);
   uint8_t* twice = reinterpret_cast<uint8_t*>(list + slice);
   __shared__ int s_listed;
+  __shared__ uint16_t s_noted[kAdjThreads / 32][512];
   __shared__ uint32_t s_words[2][kAdjLongest / 32 + 1];  // a row's mask, and the next one's
   __shared__ int32_t s_tokens[kTreeMaxNodes];  // a tree's tokens, as places in the slice (others: -1)
   const int tid = threadIdx.x, b = blockIdx.y, lo = blockIdx.x * slice, n = min(slice, a.vocab - lo);
@@ -184,30 +185,54 @@ __global__ void __launch_bounds__(kAdjThreads, kAdjCtas) adjust_kernel(const __g
     __syncthreads();
   }
   {
-    // 16 bytes of the history at a time between its first and last boundary
+    // A warp takes 512 tokens at a time, 16 bytes a load between the history's first
+    // and last boundary, notes those of the slice and then counts what it noted: few
+    // tokens lie in it, but nearly every 32 have one, and counting on the way had each
+    // of them wait for a counter's old value.
     const int32_t* said = a.history + (int64_t)b * a.max_history;
     const int head = min(length, (int)((16 - (reinterpret_cast<uintptr_t>(said) & 15)) & 15) / 4), pieces = (length - head) / 4;
-    auto count = [&](int i, int32_t id) {
+    const int lane = tid & 31;
+    uint16_t* noted = s_noted[tid >> 5];
+    int count = 0;
+    auto note = [&](bool there, int i, int32_t id) {  // all lanes of the warp
       const uint32_t at = (uint32_t)id - (uint32_t)lo;
-      if (at < (uint32_t)n) touched(i < prompt ? atomicOr(table + at, kInPrompt) : atomicAdd(table + at, 1u), at);
+      const bool in = there && at < (uint32_t)n;
+      const uint32_t all = __ballot_sync(0xffffffffu, in);
+      if (in) noted[count + __popc(all & ((1u << lane) - 1))] = (uint16_t)(at | (i < prompt ? 0x8000u : 0u));
+      count += __popc(all);
     };
-    for (int p0 = tid; p0 < pieces; p0 += 8 * kAdjThreads) {
-      int4 q[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (p0 + e * kAdjThreads < pieces) q[e] = __ldg(reinterpret_cast<const int4*>(said + head) + p0 + e * kAdjThreads);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int v = p0 + e * kAdjThreads, i = head + 4 * v;
-        if (v >= pieces) break;
-        count(i, q[e].x);
-        count(i + 1, q[e].y);
-        count(i + 2, q[e].z);
-        count(i + 3, q[e].w);
+    auto tally = [&] {
+      __syncwarp();
+      for (int k = lane; k < count; k += 32) {
+        const uint32_t at = noted[k] & 0x7FFFu;
+        touched(noted[k] & 0x8000u ? atomicOr(table + at, kInPrompt) : atomicAdd(table + at, 1u), at);
       }
+      __syncwarp();
+      count = 0;
+    };
+    for (int p0 = tid - lane; p0 < pieces; p0 += 4 * kAdjThreads) {
+      int4 q[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int v = p0 + e * kAdjThreads + lane;
+        q[e] = v < pieces ? __ldg(reinterpret_cast<const int4*>(said + head) + v) : make_int4(-1, -1, -1, -1);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int v = p0 + e * kAdjThreads + lane, i = head + 4 * v;
+        note(v < pieces, i, q[e].x);
+        note(v < pieces, i + 1, q[e].y);
+        note(v < pieces, i + 2, q[e].z);
+        note(v < pieces, i + 3, q[e].w);
+      }
+      tally();
     }
-    const int i = tid < head ? tid : head + 4 * pieces + tid - head;
-    if (i < length && (tid < head || i >= head + 4 * pieces)) count(i, __ldg(said + i));
+    if (tid < 32) {  // fewer than eight tokens are left, before the first boundary and behind the last
+      const int i = lane < head ? lane : head + 4 * pieces + lane - head;
+      const bool there = i < length && lane < 8;
+      note(there, i, there ? __ldg(said + i) : -1);
+      tally();
+    }
   }
   const int nodes = a.tokens ? a.width : 0;
   if (tid < nodes) {
