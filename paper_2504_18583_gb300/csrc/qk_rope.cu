@@ -232,11 +232,16 @@ __global__ void __launch_bounds__(kRopeThreads, U == 1 ? 5 : 4) qk_rope_kernel(c
       }
       const uint4 q_out = out;
       if (Q8 && __any_sync(0xffffffffu, on && !is_q)) {
-        float most = 0.f;
+        float most = 0.f;  // (a NaN is no maximum, and its code is NaN)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float m = fabsf(v[i]);
-          if (m < INFINITY) most = fmaxf(most, m); else v[i] = __int_as_float(0x7FFFFFFF);
+        for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(v[i]));
+        if (__any_sync(0xffffffffu, most == INFINITY)) {
+          most = 0.f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float m = fabsf(v[i]);
+            if (m < INFINITY) most = fmaxf(most, m); else v[i] = __int_as_float(0x7FFFFFFF);
+          }
         }
 #pragma unroll
         for (int d = kGroup / 2; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
