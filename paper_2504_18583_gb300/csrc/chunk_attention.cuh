@@ -313,7 +313,7 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
     chunk_attention_kernel(const __grid_constant__ ChunkAttnArgs a, const __grid_constant__ CUtensorMap kmap,
                            const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CUtensorMap qmap) {
   constexpr int NK = ck_stages(HD, BLOCKS, Q8), NV = cv_stages(HD, BLOCKS, Q8), NR = raw_stages(HD, BLOCKS, Q8);
-  constexpr int kStage = stage_bytes(HD), kRaw = kStage / 2, kConsumers = Q8 ? 15 : 11;
+  constexpr int kStage = stage_bytes(HD), kRaw = kStage / 2, kConsumers = Q8 ? 11 + kConvWarps : 11;
   constexpr int kChunks = HD / 64, kChunkBytes = kTile * 128, kRows = kTile * BLOCKS, kThreads = chunk_threads(Q8);
   using M = typename OperandOf<T, Q8>::type;
   constexpr bool kRaised = Num<T>::kFormat != Num<M>::kFormat;  // bf16 queries become fp16 ones, row by row scaled
@@ -333,11 +333,9 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
   // ---- this CTA's range -------------------------------------------------------
   if (warp == 1) tmem_alloc(&sh.tmem, 512);
   if (tid == 0) {
-    if (!Q8) {
-      tma_prefetch_desc(&kmap);
-      tma_prefetch_desc(&vmap);
-      if (by_tma) tma_prefetch_desc(&qmap);
-    }
+    tma_prefetch_desc(&kmap);
+    tma_prefetch_desc(&vmap);
+    if (by_tma) tma_prefetch_desc(&qmap);
 #pragma unroll 1
     for (int i = 0; i < NK; ++i) { mbar_init(sh.k_full + i, Q8 ? kConvWarps / 2 : 1); mbar_init(sh.k_empty + i, 1); }
 #pragma unroll 1
@@ -511,6 +509,11 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
       if (!Q8 && by_tma && !v && taken == 1) queries();
       const int last_before = last;
       int have = fetch(0), after = n > 4 ? fetch(1) : 0;
+      auto exponents_of = [&](int page) {
+        const uint8_t* from = (v ? a.v_scale : a.k_scale) + page * a.scale_stride + (int64_t)head * kPageTok;
+        return lane < kTilePages && page < a.n_pages ? __ldg(reinterpret_cast<const uint4*>(from)) : make_uint4(0, 0, 0, 0);
+      };
+      uint4 exponents = Q8 ? exponents_of(__shfl_sync(0xffffffffu, have, lane & 7)) : make_uint4(0, 0, 0, 0);
 #pragma unroll 1
       for (int j = 0; j < n && ok; ++j) {
         const int pages = pages_of(u, u.g.tile(u.t0 + j));
@@ -522,26 +525,24 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
         if (!ok) break;
         uint8_t* to = to0 + st * (Q8 ? kRaw : kStage);
         if constexpr (Q8) {
-          // lanes 0 to 7 copy a page's codes each, lanes 8 to 15 its exponents
+          // codes by tensor copies, 16 bytes of exponents a page through registers, asked
+          // for a tile ahead
           uint8_t* scale = sh.scale[v] + st * kTile;
           constexpr int kCodes = HD * kPageTok;
-          const int q = lane & 7, page = __shfl_sync(0xffffffffu, have, (j & 3) * kTilePages + q);
-          const bool mine = lane < 2 * kTilePages && q < pages, there = mine && page < a.n_pages;
-          if (mine && !there) {  // no such page: zeros
-            uint4* z = reinterpret_cast<uint4*>(lane < kTilePages ? to + q * kCodes : scale + q * kPageTok);
-#pragma unroll 1
-            for (int i = 0; i < (lane < kTilePages ? kCodes / 16 : 1); ++i) z[i] = make_uint4(0, 0, 0, 0);
+          if (lane < pages) *reinterpret_cast<uint4*>(scale + lane * kPageTok) = exponents;
+          if (j + 1 < n) {
+            const int ahead = (j + 1) & 3;
+            exponents = exponents_of(__shfl_sync(0xffffffffu, ahead == 0 ? after : have, ahead * kTilePages + (lane & 7)));
           }
+          int page[kTilePages];
+#pragma unroll
+          for (int q = 0; q < kTilePages; ++q) page[q] = __shfl_sync(0xffffffffu, have, (j & 3) * kTilePages + q);
           __syncwarp();
-          const uint32_t all = __popc(__ballot_sync(0xffffffffu, there && lane < kTilePages));
-          if (lane == 0) mbar_arrive_expect_tx(full + st, all * (kCodes + kPageTok));
-          __syncwarp();
-          if (there) {
-            if (lane < kTilePages)
-              bulk_load(to + q * kCodes, reinterpret_cast<const uint8_t*>(v ? a.v_cache : a.k_cache) + page * a.page_stride + (int64_t)head * kCodes,
-                        kCodes, full + st);
-            else
-              bulk_load(scale + q * kPageTok, (v ? a.v_scale : a.k_scale) + page * a.scale_stride + (int64_t)head * kPageTok, kPageTok, full + st);
+          if (elect_one()) {
+            mbar_arrive_expect_tx(full + st, (uint32_t)pages * kCodes);
+#pragma unroll
+            for (int q = 0; q < kTilePages; ++q)
+              if (q < pages) tma_load_4d(to + q * kCodes, map, full + st, 0, 0, head, page[q]);
           }
         } else {
           int page[kTilePages];
@@ -1143,7 +1144,7 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
   } else if constexpr (Q8) {
     // ---- codes into 16-bit entries: two warps for keys, two for values ----------------------
     constexpr int kCodes = HD * kPageTok, kHeld = kCodes / 512, kRowPieces = HD / 16;
-    const int v = (warp - 12) >> 1, cw = warp & 1, ns = v ? NV : NK;
+    const int v = (warp - 12) / (kConvWarps / 2), cw = (warp - 12) % (kConvWarps / 2), ns = v ? NV : NK;
     uint8_t *from0 = raw_rings + v * NR * kRaw, *to0 = v ? vring : kring;
     uint64_t *empty = v ? sh.v_empty : sh.k_empty, *full = v ? sh.fixed : sh.k_full;
     int st = 0, rs = 0;
@@ -1273,6 +1274,23 @@ namespace {
 // both work on the same rows.
 int chunk_blocks(int n_tokens, int batch, int group) { return (int64_t)n_tokens * group <= (int64_t)batch * kTile ? 1 : 2; }
 
+// An 8-bit cache's codes as [page][head][token][entry], boxes of a page's 16 tokens of a head.
+inline CUtensorMap codes_map(const ChunkAttnArgs& a, const void* base) {
+  CUtensorMap m;
+  std::memset(&m, 0, sizeof(m));
+  auto enc = encoder();
+  if (!enc) throw cudaErrorNotSupported;
+  const cuuint64_t hd = a.head_dim;
+  const cuuint64_t dims[4] = {hd, (cuuint64_t)kPageTok, (cuuint64_t)a.n_kv_heads, (cuuint64_t)a.n_pages};
+  const cuuint64_t strides[3] = {hd, hd * kPageTok, (cuuint64_t)a.page_stride};
+  const cuuint32_t box[4] = {(cuuint32_t)hd, (cuuint32_t)kPageTok, 1, 1}, es[4] = {1, 1, 1, 1};
+  const CUresult r = enc(&m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(base), dims, strides, box, es,
+                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) throw cudaErrorInvalidValue;
+  return m;
+}
+
 // The queries as [token][head][entry], boxes of some tokens x a key/value head's query heads x 64 entries.
 inline CUtensorMap query_map(const ChunkAttnArgs& a, int tokens) {
   CUtensorMap m;
@@ -1309,7 +1327,10 @@ void run_chunk(const ChunkAttnArgs& a, cudaStream_t s) {
   ChunkAttnArgs args = a;
   const int group = a.n_q_heads / a.n_kv_heads;
   args.group_magic = group > 1 ? 0xFFFFFFFFu / (uint32_t)group + 1 : 0;
-  if (!Q8) {
+  if (Q8) {
+    km = codes_map(a, a.k_cache);
+    vm = codes_map(a, a.v_cache);
+  } else {
     km = cache_map(a, a.k_cache);
     vm = cache_map(a, a.v_cache);
     // Queries come by tensor copies where a block's rows are whole tokens and need
@@ -1320,8 +1341,8 @@ void run_chunk(const ChunkAttnArgs& a, cudaStream_t s) {
   launch_in_turn(kernel, dim3(grid), chunk_threads(Q8), smem, 0, s, args, km, vm, qm);
 }
 
-// the caches' width is the translation unit's
-template <bool Q8, typename T, int HD>
+// The caches' width is the translation unit's.
+template <typename T, int HD, bool Q8>
 void run_chunk_sized(const ChunkAttnArgs& a, cudaStream_t s) {
   if (chunk_blocks(a.n_tokens, a.batch, a.n_q_heads / a.n_kv_heads) == 1) run_chunk<T, HD, 1, Q8>(a, s);
   else run_chunk<T, HD, 2, Q8>(a, s);
@@ -1329,9 +1350,9 @@ void run_chunk_sized(const ChunkAttnArgs& a, cudaStream_t s) {
 template <bool Q8>
 void run_chunk_attention(const ChunkAttnArgs& a, cudaStream_t s) {
   if (a.dtype == DT_BF16) {
-    if (a.head_dim == 128) run_chunk_sized<Q8, __nv_bfloat16, 128>(a, s); else run_chunk_sized<Q8, __nv_bfloat16, 64>(a, s);
+    if (a.head_dim == 128) run_chunk_sized<__nv_bfloat16, 128, Q8>(a, s); else run_chunk_sized<__nv_bfloat16, 64, Q8>(a, s);
   } else {
-    if (a.head_dim == 128) run_chunk_sized<Q8, __half, 128>(a, s); else run_chunk_sized<Q8, __half, 64>(a, s);
+    if (a.head_dim == 128) run_chunk_sized<__half, 128, Q8>(a, s); else run_chunk_sized<__half, 64, Q8>(a, s);
   }
 }
 
