@@ -180,14 +180,16 @@ __device__ __forceinline__ uint32_t finite_of(uint32_t v) {
 }
 // Parts of a unit of so many tiles where a part has `most`: one that is longer
 // by less than a split costs stays whole.
+template <int SPLIT = kSplit>
 __device__ __forceinline__ int parts_of(int tiles, int most) {
   // (the quotient in floating point is exact: half a unit off any whole number)
-  return tiles <= most + kSplit ? 1 : (int)__fdividef((float)(tiles + most) - 0.5f, (float)most);
+  return tiles <= most + SPLIT ? 1 : (int)__fdividef((float)(tiles + most) - 0.5f, (float)most);
 }
 // Where CTA c's range begins: floor(total c / grid).  With fewer places than
 // CTAs a range is one place or none, and its beginning is then also the number
 // of CTAs before c that have one.
-struct Ranges {
+template <int SPLIT>
+struct RangesOf {
   int total, grid, each, rest;
   __device__ __forceinline__ void set(int n, int g) {
     total = n;
@@ -198,9 +200,10 @@ struct Ranges {
   __device__ __forceinline__ int at(int c) const { return c * each + c * rest / grid; }
   // a cut at place x of a unit of `len` places: near an end it moves there
   static __device__ __forceinline__ int cut(int x, int len) {
-    return x <= kSplit ? 0 : x >= len - kSplit ? len : x;
+    return x <= SPLIT ? 0 : x >= len - SPLIT ? len : x;
   }
 };
+using Ranges = RangesOf<kSplit>;
 
 // A slot holds one partial, rows = 128 * blocks: O as [HD / 4][rows] float4,
 // then each softmax group's maxima and sums.  Before the slots: arrivals at a

@@ -49,6 +49,10 @@ namespace {
 
 constexpr int kSeqHeld = 64;                    // sequences whose lengths a CTA keeps at hand
 constexpr int kStep = kTile / 2;                // keys of a step
+// what a unit's start, and splitting it, costs in tiles (2 and 6, 3 and 3, 4 and 3: within 3% of these on all cases but the
+// ragged ones, up to 12% slower there)
+constexpr int kUnitStart = 3, kUnitSplit = 4;
+using ChunkRanges = RangesOf<kUnitSplit>;
 constexpr int kConvWarps = 4;                   // warps that convert an 8-bit cache's tiles
 
 constexpr int kAheadSegs = 4;                   // segments that are worked out ahead
@@ -126,11 +130,11 @@ struct ChunkWalk : Segment {
     if (b < kSeqHeld) s = chunk_of(a, held[b].x, held[b].y, held[b + 1].y, rows_per_block);
     else s = chunk_of(a, a.ctx_len[b], a.starts[b], a.starts[b + 1], rows_per_block);
   }
-  __device__ __noinline__ bool next(const ChunkAttnArgs& a, const int2* held, int rows_per_block, const Ranges& ranges,
+  __device__ __noinline__ bool next(const ChunkAttnArgs& a, const int2* held, int rows_per_block, const ChunkRanges& ranges,
                                     bool one_part) {
     if (one_part) return left-- > 0;
     while (left > 0) {
-      const int len = g.tiles + kStart;
+      const int len = g.tiles + kUnitStart;
       if (off >= len) {  // the next unit
         at += len;
         off = 0;
@@ -147,20 +151,20 @@ struct ChunkWalk : Segment {
         g = span_of(a, s, block, rows_per_block);
         continue;
       }
-      const int x0 = Ranges::cut(off, len), x1 = off + left < len ? Ranges::cut(off + left, len) : len;
+      const int x0 = ChunkRanges::cut(off, len), x1 = off + left < len ? ChunkRanges::cut(off + left, len) : len;
       const int step = min(len - off, left);
       off += step;
       left -= step;
-      t0 = max(0, x0 - kStart);
-      t1 = x1 - kStart;
+      t0 = max(0, x0 - kUnitStart);
+      t1 = x1 - kUnitStart;
       if (t1 <= t0) continue;
       count = 1;
       me = 0;
       c0 = blockIdx.x;
       if (t0 > 0 || t1 < g.tiles) {  // who else has a part of it
-        while (c0 > 0 && ranges.at(c0) > at && Ranges::cut(ranges.at(c0) - at, len) > 0) --c0;
+        while (c0 > 0 && ranges.at(c0) > at && ChunkRanges::cut(ranges.at(c0) - at, len) > 0) --c0;
         int c1 = blockIdx.x;
-        while (c1 + 1 < ranges.grid && ranges.at(c1 + 1) < at + len && Ranges::cut(ranges.at(c1 + 1) - at, len) < len) ++c1;
+        while (c1 + 1 < ranges.grid && ranges.at(c1 + 1) < at + len && ChunkRanges::cut(ranges.at(c1 + 1) - at, len) < len) ++c1;
         me = blockIdx.x;
         if (ranges.each == 0) {  // those between them whose range is empty never arrive
           c0 = ranges.at(c0);
@@ -365,7 +369,7 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
   // The share's form and, in ranges, this CTA's first place: two rounds over the
   // sequences, their sum and then the place in it; both are one round of a
   // single step for up to as many sequences as threads.
-  Ranges ranges;
+  ChunkRanges ranges;
   int lo = 0, hi = 0, units = 0, longest = 0;
   bool single = true;  // no sequence has more than one block
 #pragma unroll 1
@@ -384,14 +388,14 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
       int places = 0, tiles = 0;  // of a head
       if (s.blocks == 1) {
         tiles = span_of(a, s, 0, kRows).tiles;
-        places = tiles + kStart;
+        places = tiles + kUnitStart;
       }
       for (uint32_t m = __ballot_sync(0xffffffffu, s.blocks > 1); m; m &= m - 1) {  // the warp adds up one's blocks
         const int from = __ffs(m) - 1;
         const Chunk o = chunk_of(a, __shfl_sync(0xffffffffu, v.x, from), __shfl_sync(0xffffffffu, v.y, from),
                                  __shfl_sync(0xffffffffu, v.z, from), kRows);
         int part = 0;
-        for (int i = lane; i < o.blocks; i += 32) part += span_of(a, o, i, kRows).tiles + kStart;
+        for (int i = lane; i < o.blocks; i += 32) part += span_of(a, o, i, kRows).tiles + kUnitStart;
         part = __reduce_add_sync(0xffffffffu, part);
         if (lane == from) places = part;
       }
@@ -691,7 +695,7 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
       // the fewest tiles a part that the CTAs are enough for; two sequences a lane
       static_assert(kSeqHeld == 64, "two sequences a lane");
       int tiles[2], mine[2];
-      const int all_tiles = ranges.total - units * kStart;
+      const int all_tiles = ranges.total - units * kUnitStart;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int b = 2 * lane + e;
@@ -709,12 +713,12 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
 #pragma unroll 1
       while (least < most) {
         const int mid = (least + most) / 2;
-        const int need = __reduce_add_sync(0xffffffffu, mine[0] * parts_of(tiles[0], mid) + mine[1] * parts_of(tiles[1], mid));
+        const int need = __reduce_add_sync(0xffffffffu, mine[0] * parts_of<kUnitSplit>(tiles[0], mid) + mine[1] * parts_of<kUnitSplit>(tiles[1], mid));
         if (need <= grid) most = mid; else least = mid + 1;
       }
       int inc = 0;
 #pragma unroll
-      for (int e = 0; e < 2; ++e) { mine[e] *= parts_of(tiles[e], most); inc += mine[e]; }
+      for (int e = 0; e < 2; ++e) { mine[e] *= parts_of<kUnitSplit>(tiles[e], most); inc += mine[e]; }
       const int own = inc;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -728,7 +732,7 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
       for (int e = 0; e < 2; ++e) {
         const int at = (int)blockIdx.x - before;
         if (at >= 0 && at < mine[e]) {
-          const int parts = parts_of(tiles[e], most);
+          const int parts = parts_of<kUnitSplit>(tiles[e], most);
           w.left = 1;
           w.b = 2 * lane + e;
           w.load(a, sh.seq, kRows);
@@ -751,7 +755,7 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
         __syncwarp();
 #pragma unroll 1
         for (int i0 = 0; i0 < s.blocks; i0 += 32) {
-          const int len = i0 + lane < s.blocks ? span_of(a, s, i0 + lane, kRows).tiles + kStart : 0;
+          const int len = i0 + lane < s.blocks ? span_of(a, s, i0 + lane, kRows).tiles + kUnitStart : 0;
           int inc = len;
 #pragma unroll
           for (int o = 1; o < 32; o <<= 1) {

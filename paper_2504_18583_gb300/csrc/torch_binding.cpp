@@ -10,6 +10,7 @@
 #include <ATen/ops/empty.h>
 #include <ATen/ops/zeros.h>
 #include <c10/cuda/CUDAFunctions.h>
+#include <c10/cuda/CUDAGraphsC10Utils.h>
 #include <c10/cuda/CUDAStream.h>
 
 #include <cmath>
@@ -277,7 +278,7 @@ PyObject* tree_attention(PyObject* const* a, Py_ssize_t n) {
 }
 
 PyObject* chunk_attention(PyObject* const* a, Py_ssize_t n) {
-  count_is(n, 14);
+  count_is(n, 13);
   const at::Tensor& q = tensor_of(a[0], "q");
   const Where w(q, "q");
   const at::ScalarType type = q.scalar_type();
@@ -299,12 +300,11 @@ PyObject* chunk_attention(PyObject* const* a, Py_ssize_t n) {
   if (a[11] == Py_None) out = at::empty({T, Hq, hd}, w.options(type));
   else { w.want(a[11], "out", type, {T, Hq, hd}); out = THPVariable_Unpack(a[11]); }
   const int64_t need = std::max<int64_t>((int64_t)pard_chunk_attention_workspace_bytes(T, B, Hq, Hkv, hd), kHead);
-  const int capturing = PyObject_IsTrue(a[13]);
   if (a[12] != Py_None) {
     workspace = tensor_of(a[12], "workspace");
     if (!workspace.is_cuda() || workspace.get_device() != w.dev || !workspace.is_contiguous())
       throw Refuse{"workspace: want a contiguous tensor on the same device"};
-  } else if (capturing) {  // a graph may run beside later calls: its calls have their own
+  } else if (c10::cuda::currentStreamCaptureStatusMayInitCtx() != c10::cuda::CaptureStatus::None) {  // a graph may run beside later calls: its calls have their own
     workspace = at::empty({need}, w.options(at::kByte));
     workspace.narrow(0, 0, kHead).zero_();
   } else {

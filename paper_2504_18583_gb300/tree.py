@@ -189,7 +189,7 @@ def chunk_attention(q, k_cache, v_cache, page_table, starts, ctx_len, scale: Opt
     tree_attention: shared_workspace; a call that a CUDA graph captures gets its
     own).  Returns [T, Hq, hd]; rows of no sequence are not written."""
     return _ops.chunk_attention(q, k_cache, v_cache, page_table, starts, ctx_len, scale, window, sinks, k_scale, v_scale,
-                                out, workspace, workspace is None and torch.cuda.is_current_stream_capturing())
+                                out, workspace)
 
 
 def adjust_logits(logits, history=None, hist_len=None, prompt_len=None, repetition=None, frequency=None, presence=None,
