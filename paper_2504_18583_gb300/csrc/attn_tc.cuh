@@ -210,8 +210,8 @@ using Ranges = RangesOf<kSplit>;
 // unit, by the CTA that has its first tile, for each group.
 struct Partial {
   float* base;
-  int rows;
-  __device__ __forceinline__ float4* o(int c4, int row) const { return reinterpret_cast<float4*>(base) + (size_t)c4 * rows + row; }
+  int rows, c4_step, row_step = 1;  // steps: of O
+  __device__ __forceinline__ float4* o(int c4, int row) const { return reinterpret_cast<float4*>(base) + (size_t)c4 * c4_step + (size_t)row * row_step; }
   __device__ __forceinline__ float2* stats(int hd, int g, int row) const {
     return reinterpret_cast<float2*>(base + (size_t)hd * rows) + (size_t)g * rows + row;
   }
@@ -223,7 +223,7 @@ template <typename Args>
 __device__ __forceinline__ Partial slot_of(const Args& a, int slot, int hd, int blocks) {
   return Partial{reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(a.workspace) + kArriveBytes) +
                      (size_t)slot * slot_floats(hd, blocks),
-                 kTile * blocks};
+                 kTile * blocks, kTile * blocks};
 }
 __device__ __forceinline__ uint32_t ld_acquire(const uint32_t* p) {
   uint32_t v;

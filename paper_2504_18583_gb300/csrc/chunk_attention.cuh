@@ -91,6 +91,8 @@ struct Span {
   int p_lo, p_hi, end;    // first and last row's positions; keys that the last row may see
   int sink, skip, tiles;
   __device__ __forceinline__ int tile(int k) const { return k < sink ? k : k + skip; }
+  // keys up to which a tile is looked at: of the first tokens', those
+  __device__ __forceinline__ int limit(const ChunkAttnArgs& a, int k) const { return k < sink ? min(a.sinks, end) : end; }
 };
 __device__ __forceinline__ int window_from(const ChunkAttnArgs& a, int p) { return a.window ? max(0, p - a.window + 1) : 0; }
 __device__ __forceinline__ Span span_of(const ChunkAttnArgs& a, const Chunk& s, int block, int rows_per_block) {
@@ -230,6 +232,83 @@ __device__ __noinline__ void patch_chunk(const ChunkAttnArgs& a, const Segment& 
   }
 }
 
+// A unit of up to eight rows (a single token's, as a rule in many parts) leaves its
+// partials row by row, and a warp joins a row: its lanes take the parts' maxima and sums
+// (32 at a time) and then the row's columns, in 32 / kCols4 shares of the parts that are
+// added up last.  (With O as [HD / 4][rows], a row's pieces 2048 bytes apart, sixteen
+// parts of four rows took 5000 clocks to load.)
+constexpr int kFewRows = 8;
+template <int HD>
+__device__ __forceinline__ Partial few_rows(Partial p) {
+  p.c4_step = 1;
+  p.row_step = HD / 4;
+  return p;
+}
+template <typename T, int HD, int BLOCKS>
+__device__ __noinline__ void join_few(const Partial first, const uint16_t* slots, int count, int g, int t, int row0, int rows,
+                                      int c4_0, T* out, int row_in_token, int group, int64_t token_step) {
+  constexpr int kCols4 = HD / 4 / (BLOCKS == 1 ? 2 : 1), kShares = 32 / kCols4, kBatch = 8;
+  constexpr int64_t kSlot = slot_floats(HD, BLOCKS);
+  const int lane = t & 31, c = lane % kCols4, share = lane / kCols4;
+#pragma unroll 1
+  for (int row = t >> 5; row < rows; row += 4) {
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float m = -INFINITY, l = 0.f;
+    const float4* o = few_rows<HD>(first).o(c4_0 + c, row0 + row);
+#pragma unroll 1
+    for (int i0 = 0; i0 < count; i0 += 32) {
+      const int n = min(32, count - i0), slot = lane < n ? slots[i0 + lane] : 0;
+      float2 st = make_float2(-INFINITY, 0.f);
+      if (lane < n) st = *reinterpret_cast<const float2*>(reinterpret_cast<const float*>(first.stats(HD, g, row0 + row)) + slot * kSlot);
+      float4 v[kBatch];
+      auto load = [&](int i) {
+#pragma unroll
+        for (int e = 0; e < kBatch; ++e) {
+          const int at = i + e * kShares + share, from = __shfl_sync(0xffffffffu, slot, at & 31);
+          v[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (at < n) v[e] = o[from * (kSlot / 4)];
+        }
+      };
+      load(0);
+      float top = fmaxf(m, st.x), sum;
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+      const float base = top == -INFINITY ? 0.f : top, old = ex2(m - base), w = ex2(st.x - base);
+      sum = st.y * w;
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+      l = l * old + sum;
+      m = top;
+      acc.x *= old; acc.y *= old; acc.z *= old; acc.w *= old;
+#pragma unroll 1
+      for (int i = 0; i < n; i += kShares * kBatch) {
+        if (i > 0) load(i);
+#pragma unroll
+        for (int e = 0; e < kBatch; ++e) {
+          const float by = __shfl_sync(0xffffffffu, w, (i + e * kShares + share) & 31);
+          acc.x = fmaf(v[e].x, by, acc.x);
+          acc.y = fmaf(v[e].y, by, acc.y);
+          acc.z = fmaf(v[e].z, by, acc.z);
+          acc.w = fmaf(v[e].w, by, acc.w);
+        }
+      }
+    }
+#pragma unroll
+    for (int d = kCols4; d < 32; d <<= 1) {
+      acc.x += __shfl_xor_sync(0xffffffffu, acc.x, d);
+      acc.y += __shfl_xor_sync(0xffffffffu, acc.y, d);
+      acc.z += __shfl_xor_sync(0xffffffffu, acc.z, d);
+      acc.w += __shfl_xor_sync(0xffffffffu, acc.w, d);
+    }
+    const float inv = l > 0.f ? 1.0f / l : 0.f;
+    const int r = row_in_token + row, token = r / group;
+    uint2 p;
+    p.x = Num<T>::pack(acc.x * inv, acc.y * inv);
+    p.y = Num<T>::pack(acc.z * inv, acc.w * inv);
+    if (share == 0) *reinterpret_cast<uint2*>(out + token * token_step + (r - token * group) * HD + (c4_0 + c) * 4) = p;
+  }
+}
+
 // ---- 8-bit entries into 16-bit ones -------------------------------------------
 // A row's codes times its power of two, as fp16.  The conversion gives codes as they
 // are (NaN too), and the product with a power of two from 2^-14 to 2^7 stays a normal
@@ -282,11 +361,15 @@ struct ChunkControl {
   uint8_t back[Q8 ? 2 * kTile : 16];  // exponents of the queries' rows, which were scaled by them
   int2 seq[kSeqHeld + 1];  // sequences' context lengths and first rows
   uint32_t tmem, last_in[2], odd[NV];  // odd: a stage's values that not all rows see held infinities or NaN (a byte a warp)
+  uint8_t pages[16];       // which of a tile's pages are the pool's, tiles in turn: keys are loaded fewer than 16 ahead of the softmax
   int abort_flag, start_b, start_head, start_block, start_off;
   int sum[16], units[16], most[16];
   ChunkWalk walk;
   Segment seg[kAheadSegs];
-  uint16_t slots[2][kMaxGrid];
+  union {
+    int tiles[kSeqHeld];            // of a sequence's block, where it has one: until the segments are worked out
+    uint16_t slots[2][kMaxGrid];
+  };
 };
 template <int HD, int BLOCKS, bool Q8>
 constexpr int chunk_smem() {
@@ -399,6 +482,7 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
         part = __reduce_add_sync(0xffffffffu, part);
         if (lane == from) places = part;
       }
+      if (b < kSeqHeld) sh.tiles[b] = tiles;
       const int cost = places * a.n_kv_heads;
       int inc = cost;
 #pragma unroll
@@ -465,7 +549,7 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
   };
   auto segment = [&]() -> const Segment& { return sh.seg[(taken - 1) % kAheadSegs]; };
   // pages of a tile that hold keys the block may see
-  auto pages_of = [&](const Segment& u, int tile) { return min(kTilePages, (u.g.end - 1) / kPageTok - tile * kTilePages + 1); };
+  auto pages_of = [&](const Segment& u, int k) { return min(kTilePages, (u.g.limit(a, k) - 1) / kPageTok - u.g.tile(k) * kTilePages + 1); };
 
   if (warp == 0 || warp == 2) {
     // ---- loads: keys by one warp, values by another ------------------------------------
@@ -520,13 +604,14 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
       uint4 exponents = Q8 ? exponents_of(__shfl_sync(0xffffffffu, have, lane & 7)) : make_uint4(0, 0, 0, 0);
 #pragma unroll 1
       for (int j = 0; j < n && ok; ++j) {
-        const int pages = pages_of(u, u.g.tile(u.t0 + j));
+        const int pages = pages_of(u, u.t0 + j);
         if (j > 0 && (j & 3) == 0) {
           have = after;
           if (j + 4 < n) after = fetch(j / 4 + 1);
         }
         ok = ok && warp_wait(empty + st, phase ^ 1, abort_flag);
         if (!ok) break;
+        const uint32_t in_pool = __ballot_sync(0xffffffffu, have < a.n_pages) >> ((j & 3) * kTilePages);
         uint8_t* to = to0 + st * (Q8 ? kRaw : kStage);
         if constexpr (Q8) {
           // codes by tensor copies, 16 bytes of exponents a page through registers, asked
@@ -543,6 +628,7 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
           for (int q = 0; q < kTilePages; ++q) page[q] = __shfl_sync(0xffffffffu, have, (j & 3) * kTilePages + q);
           __syncwarp();
           if (elect_one()) {
+            if (!v) sh.pages[issued & 15] = (uint8_t)in_pool;
             mbar_arrive_expect_tx(full + st, (uint32_t)pages * kCodes);
 #pragma unroll
             for (int q = 0; q < kTilePages; ++q)
@@ -553,6 +639,7 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
 #pragma unroll
           for (int q = 0; q < kTilePages; ++q) page[q] = __shfl_sync(0xffffffffu, have, (j & 3) * kTilePages + q);
           if (elect_one()) {
+            if (!v) sh.pages[issued & 15] = (uint8_t)in_pool;
             mbar_arrive_expect_tx(full + st, (uint32_t)pages * kChunks * kPageTok * 128);
 #pragma unroll
             for (int q = 0; q < kTilePages; ++q)
@@ -640,7 +727,7 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
     while (next()) {
       const Segment& u = segment();
       const int n = u.t1 - u.t0;
-      const int last_keys = u.t1 == u.g.tiles ? u.g.end - u.g.tile(u.t1 - 1) * kTile : kTile;  // of the last tile
+      const int last_keys = u.g.limit(a, u.t1 - 1) - u.g.tile(u.t1 - 1) * kTile;
       const uint32_t turn = (taken - 1) & 1;
       ok = ok && warp_wait(&sh.q_full, turn, abort_flag);
       if (!by_tma) tc_fence_after();
@@ -651,7 +738,8 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
 #pragma unroll 1
       for (int j = -kAhead; j < n && ok; ++j) {
         const bool more = j + kAhead < n;
-        const int keys = j == n - 1 ? last_keys : kTile;
+        int keys = j == n - 1 ? last_keys : kTile;  // of tile j
+        if (j >= 0 && u.t0 + j < u.g.sink) keys = u.g.limit(a, u.t0 + j) - (u.t0 + j) * kTile;
         const uint32_t kb = uniform(k_addr + kst * (kStage >> 4)), vb = uniform(v_addr + vst * (kStage >> 4));
         if (j >= 0) ok = warp_wait(sh.fixed + vst, vph, abort_flag);
         if (BLOCKS == 1 && j == 0) ok = ok && warp_wait(sh.ready + 0, turn, abort_flag) && warp_wait(sh.ready + 1, turn, abort_flag);
@@ -698,15 +786,8 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
       const int all_tiles = ranges.total - units * kUnitStart;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const int b = 2 * lane + e;
-        tiles[e] = mine[e] = 0;
-        if (b < a.batch) {
-          const Chunk s = chunk_of(a, sh.seq[b].x, sh.seq[b].y, sh.seq[b + 1].y, kRows);
-          if (s.blocks) {
-            tiles[e] = span_of(a, s, 0, kRows).tiles;
-            mine[e] = a.n_kv_heads;
-          }
-        }
+        tiles[e] = sh.tiles[2 * lane + e];
+        mine[e] = tiles[e] ? a.n_kv_heads : 0;
       }
       // (a unit's parts are less than one more than its tiles / most)
       int least = max(1, all_tiles / grid), most = max(least, min(longest, all_tiles / (grid - units + 1) + 1));
@@ -788,6 +869,7 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
         if (!some) sh.seg[slot].t1 = 0;
         mbar_arrive(sh.seg_full + slot);
       }
+      __syncwarp();
       more = __shfl_sync(0xffffffffu, some, 0) != 0;
       ++made;
     };
@@ -805,7 +887,7 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
         if (!ok) break;
         const int k0 = u.g.tile(u.t0 + j) * kTile;
         if (!all_see(a, u.s, u.g.p_lo, u.g.p_hi, k0, k0 + kTile)) {
-          const int end = u.g.end - k0;  // keys of the tile
+          const int end = u.g.limit(a, u.t0 + j) - k0;  // keys of the tile
           constexpr int kPieces = HD / 8, kBatch = 4;
           auto place = [&](int p) {
             const int r = p / kPieces, c = p % kPieces;
@@ -946,27 +1028,21 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
       // positions of the group's first and last rows
       auto position = [&](int r) { return u.g.p_lo + in_group(a, u.g.rest + min(r, rows - 1) - u.block * kRows); };
       const int g_lo = position(row_base), g_hi = position(row_base + kTile - 1);
-      auto page_flag = [&](int j) -> uint32_t {  // this lane's page of tile j is one of the pool
-        const int at = u.g.tile(u.t0 + j) * kTilePages + lane;
-        if (lane >= kTilePages || at * kPageTok >= u.g.end) return 1;
-        return (uint32_t)a.page_table[(size_t)u.b * a.max_pages + at] < (uint32_t)a.n_pages;
-      };
       float m_ref = -INFINITY, sum = 0.f;
       bool patch = false;  // values that the rows who see them get back in the epilogue
-      uint32_t flag = page_flag(0);
       const uint64_t scale2 = pair_of(__float_as_uint(sl2), __float_as_uint(sl2));
       const Chunk us = u.s;
       const Span ug = u.g;
       const int first_tile = u.t0;
 #pragma unroll 1
       for (int j = 0; j < n; ++j) {
-        const uint32_t flags = __ballot_sync(0xffffffffu, flag);
-        if (j + 1 < n) flag = page_flag(j + 1);
         const int k0 = ug.tile(first_tile + j) * kTile, x = BLOCKS == 2 ? g : j & 1;
         const bool partly = !all_see(a, us, ug.p_lo, ug.p_hi, k0, k0 + kTile);  // some row of the block does not see all of the tile,
-        const bool masked = flags != 0xFFFFFFFFu || !all_see(a, us, g_lo, g_hi, k0, k0 + kTile);  // some row of the group
+        bool masked = !all_see(a, us, g_lo, g_hi, k0, k0 + kTile);  // some row of the group
         ok = warp_wait(sh.s_full + x, ph_s >> x & 1, abort_flag);
         if (!ok) break;
+        const uint32_t flags = sh.pages[(tile0 + j) & 15];
+        masked |= flags != 0xFFu;
         ph_s ^= 1u << x;
         tc_fence_after();
 #pragma unroll
@@ -1076,7 +1152,9 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
       // tree_attention.cu).
       const int count = whole ? 1 : u.count, me = u.me, c0 = u.c0;
       uint32_t* arrived = reinterpret_cast<uint32_t*>(a.workspace) + 2 * c0 + g;
-      const Partial mine = slot_of(a, 2 * (c0 + me) + (u.t0 > 0 ? 0 : 1), HD, BLOCKS);
+      const bool few = rows - u.block * kRows <= kFewRows;
+      auto slot = [&](int i) { const Partial s = slot_of(a, i, HD, BLOCKS); return few ? few_rows<HD>(s) : s; };
+      const Partial mine = slot(2 * (c0 + me) + (u.t0 > 0 ? 0 : 1));
       bool two = false;
       if (count == 2) {
         if (t == 0) sh.last_in[g] = ld_acquire(arrived) == 1;
@@ -1125,14 +1203,15 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
             } else {
               fence_gpu();
               const int live_rows = min(kTile, rows - row_base);
-              join<T, HD, BLOCKS>(a, sh.slots[g], count, g, t, in_block - t, live_rows, col0 / 4, kCols / 4, unit, unit_row0);
+              if (few) join_few<T, HD, BLOCKS>(slot_of(a, 0, HD, BLOCKS), sh.slots[g], count, g, t, in_block - t, live_rows, col0 / 4, unit, unit_row0, group, (int64_t)a.n_q_heads * HD);
+              else join<T, HD, BLOCKS>(a, sh.slots[g], count, g, t, in_block - t, live_rows, col0 / 4, kCols / 4, unit, unit_row0);
               if (t == 0) *arrived = 0;  // as the next call wants it
             }
           }
         }
       }
       if (two) {
-        const Partial other = slot_of(a, 2 * (c0 + 1 - me) + me, HD, BLOCKS);
+        const Partial other = slot(2 * (c0 + 1 - me) + me);
         join_two<T, HD, BLOCKS>(other, my + 2 * kTile + (BLOCKS == 2 ? g * HD : 0), g, in_block, me == 0, m_ref, sum, w0,
                                 w1, true, col0, on, out, wide_out);
         if (patch && on) patch_chunk<T, HD, Q8>(a, u, p, col0, kCols, out, mine, in_block);
@@ -1164,7 +1243,7 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
         uint8_t* stage = to0 + st * kStage;
         const uint8_t *raw = from0 + rs * kRaw, *scale = sh.scale[v] + rs * kTile;
         const bool clean = v && !all_see(a, u.s, u.g.p_lo, u.g.p_hi, k0, k0 + kTile);
-        const int pages = pages_of(u, tile);
+        const int pages = pages_of(u, u.t0 + j), end = u.g.limit(a, u.t0 + j);
         bool any = false;
 #pragma unroll 1
         for (int q = cw; q < pages; q += kConvWarps / 2) {
@@ -1214,8 +1293,8 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
               if (clean && !all_see(a, u.s, u.g.p_lo, u.g.p_hi, key, key + 1)) {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                  const uint32_t f = key >= u.g.end ? 0u : finite_of<__half>(y[k]);
-                  any |= key < u.g.end && f != y[k];
+                  const uint32_t f = key >= end ? 0u : finite_of<__half>(y[k]);
+                  any |= key < end && f != y[k];
                   y[k] = f;
                 }
               }

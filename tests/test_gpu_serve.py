@@ -185,6 +185,20 @@ def test_windows_and_first_tokens(tree, eight, window, sinks):
 
 
 @pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_tiles_that_are_not_loaded_whole(tree, dtype, hd, eight):
+    """Behind what a tile needs of its pages lies what shared memory held before: NaN of another call's caches."""
+    before = Case(dtype, 32, 8, hd, [1] * 40, [2000] * 40, eight)
+    for x in (before.k, before.v):
+        x.view(torch.uint8).fill_(0x7F) if eight else x.fill_(float("nan"))
+    for new, ctx, window, sinks in (([1], [1023], 1, 1), ([1], [1000], 200, 112), ([40], [1007], 1, 64), ([150], [3000], 800, 200),
+                                    ([1, 1, 300], [111, 4095, 2047], 700, 17), ([5], [64], 0, 0)):
+        before.call(tree)
+        Case(dtype, 4, 2, hd, new, ctx, eight, seed=len(new)).check(tree, window, sinks)
+
+
+@pytest.mark.parametrize("eight", [False, True])
 @pytest.mark.parametrize("dtype,Hq,Hkv,hd,new,ctx", [
     (BF, 32, 8, 128, [1], [20000]),                       # parts of units, many to join
     (BF, 4, 1, 64, [1, 1], [30000, 100]),
