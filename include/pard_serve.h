@@ -44,9 +44,9 @@ pard_status pard_qk_norm_rope_quantized(const void* d_qkv, int64_t qkv_stride, i
  * the pool gets zeros.  Masked keys and values may hold infinities or NaN.
  * Caches of `dtype` (d_k_scale and d_v_scale null), or 8-bit ones as
  * pard_qk_norm_rope_quantized writes them: an entry is then its code times its
- * power of two, which is exact in bf16; in fp16 it is held to +-65504 and to
- * multiples of 2^-24.  Scores and sums are held in 32 bits; probabilities are
- * rounded to `dtype` before they multiply the values.  d_workspace:
+ * power of two, held to +-65504 and to multiples of 2^-24.  Scores and sums are
+ * held in 32 bits; probabilities are rounded to `dtype` (with an 8-bit cache to
+ * fp16) before they multiply the values.  d_out must not overlap d_q.  d_workspace:
  * pard_chunk_attention_workspace_bytes (0: invalid arguments) bytes, the first
  * 4096 of them zero before the first call; each call leaves them fit for the
  * next, of any sizes that they are enough for, and for pard_tree_attention

@@ -12,29 +12,57 @@
 // tiles in order (sequence, head, block) are cut into one even range a CTA, or,
 // where there are no more units than CTAs and a block a sequence, each CTA takes
 // one equal part of one unit.  CTAs work that out from the sequences' lengths,
-// which the host need not know.  How units are cut, parts joined and workspaces
-// kept is as in tree_attention.cu.
+// which the host need not know.  Parts of a unit leave partials in the workspace
+// and the last to arrive joins them, in tile order.
 //
-// Roles: warp 0 loads keys, warp 2 values, warp 1 issues the products, warp 3
-// looks after values that not every row sees; two warpgroups take the softmax, a
-// thread a row, half a tile (64 keys) at a time, so that the first half's product
-// runs under the second's softmax.  With more than 128 query vectors each group has
-// its own 128 of them and a buffer of scores, and one group's products run under
-// the other's softmax; else both have the same rows and a half of each tile (their
-// sums are joined at the end), and the scores of the next tile but one are asked
-// for as soon as a buffer is free.
+// Warp 0 loads keys and queries and warp 2 values, by tensor copies of a page's 16
+// tokens; warp 1 issues the products; warp 3 works out the CTA's next segments
+// (parts of units) while the others are at this one, and looks over values that not
+// every row sees.  Two warpgroups take the softmax, a thread a row, half a tile (64
+// keys) at a time, so that the first half's product runs under the second's softmax;
+// probabilities go over the scores in tensor memory.  With more than 128 query
+// vectors each group has its own 128 of them and a buffer of scores, and one group's
+// products run under the other's softmax; else both have the same rows and a half of
+// each tile (their sums are joined at the end), and the scores of the next tile but
+// one are asked for as soon as a buffer is free.
 //
 // Masks touch only tiles that some row does not see whole: a row sees a run of
 // columns up to its own position, less those between the first tokens and its
-// window.  There values may hold anything: what lies past the block's last
-// position is zeroed in shared memory, and so are infinities and NaN of keys that
-// not every row sees, which the epilogue adds back for the rows that do.
+// window.  There values may hold anything: what lies past the last key that a tile is
+// read for, and infinities and NaN of keys that not every row sees, are zeroed in
+// shared memory, and the epilogue adds the latter back for the rows that see them.
 //
-// An 8-bit cache (e4m3 codes, a power of two a token and head) is loaded as it
-// lies, half of a stage, and four more warps turn it into the 16-bit operand in
-// place, a page at a time: codes and powers of two make 16-bit entries without a
-// rounding (fp16: down to 2^-24, and up to 65504), so everything behind them is
-// as for a 16-bit cache.
+// An 8-bit cache (e4m3 codes, a power of two a token and head) is loaded as it lies
+// into rings of its own, and four more warps turn each tile into fp16 operands, exactly
+// (down to 2^-24, and held to 65504), so that everything behind them is as for a
+// 16-bit cache.  Queries and probabilities are then fp16 too, whatever the queries'
+// type: bf16 queries are scaled row by row by a power of two that the softmax's scale
+// takes back.
+//
+// What bounds it, as measured with the tiles in steady state:
+// - Long chunks, 256 query vectors a unit: a tile of 128 keys takes 2950 to 3140 clocks,
+//   its 32 products 2052 of them and the softmax of both groups, eight warps, nearly all
+//   the others': scores wait for the probabilities that lie where they go.  The clock
+//   falls to 1.8 GHz under the power limit.  2048 tokens behind 30000 (64 heads on 8 of
+//   128): 1.43 ms, 1.46 PFLOP/s, 1.58 ms in a long run.  A prompt of 8191: 408 us.
+// - Units' ends: 7000 to 8000 clocks from a unit's last scores to the next one's first
+//   probabilities.  Four pieces of up to 512 tokens: 72 us; 16 sequences, most of them
+//   single tokens, with a window (heads of 64): 54 us, 2800 to 3600 clocks a tile, where
+//   masked tiles are many.
+// - Single tokens, 16-bit cache: HBM.  32 of them over 264000 keys: 180 us, 90% of the
+//   copy rate.
+// - 8-bit cache: shared memory.  A pair of tiles is written once as it lies, read, written
+//   as fp16 and read by the products, 1800 clocks of its 2830 (HBM: 1400): 32 single
+//   tokens 204 us; 1000 tokens behind 16001 277 us, against 219 from a 16-bit cache.
+// - A single token with a window of 2048: 14.4 us, the chain lengths -> shares -> pages ->
+//   keys -> softmax -> partial -> join, 28000 clocks.
+//
+// Tried and slower: 64-column score products (2048 tokens behind 30000: 1417 -> 1631 us),
+// two threads a row (2075), the maximum only where the sum grows too large (8191 tokens:
+// 471 -> 540), a third buffer of scores for heads of 64 (a prompt of 4096: 108 -> 119),
+// the second group's products left out where it has no rows (a few percent, everywhere),
+// eight converting warps, codes turned by integer instructions (204 -> 240) or half of them
+// (222); without any arithmetic the conversion takes as long.
 // (A header, since 16-bit and 8-bit caches are compiled apart: a function that is
 // not inlined is given the registers of the kernels that call it, and those have 168
 // and 128.)
@@ -1148,8 +1176,7 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
       const int col0 = BLOCKS == 2 ? 0 : g * kCols, in_block = (BLOCKS == 2 ? g * kTile : 0) + t;
       const bool whole = u.t0 == 0 && u.t1 == ug.tiles, on = row < rows;
       // A unit's contributors are consecutive CTAs.  All but the last to arrive
-      // leave their partial; that one joins them, in tile order (see
-      // tree_attention.cu).
+      // leave their partial; that one joins them, in tile order.
       const int count = whole ? 1 : u.count, me = u.me, c0 = u.c0;
       uint32_t* arrived = reinterpret_cast<uint32_t*>(a.workspace) + 2 * c0 + g;
       const bool few = rows - u.block * kRows <= kFewRows;

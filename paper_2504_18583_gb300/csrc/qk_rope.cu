@@ -29,7 +29,9 @@
 // a power of two moves no bit, so a reader's 16-bit copy of an entry is exact.
 // Infinities and NaN become NaN and do not count for the exponent.  It costs the
 // row's largest entry (three or four shuffles) and four conversions a lane, and
-// saves half of the caches' bytes.
+// saves half of the caches' bytes; instructions bound it (8191 tokens as above: 44.4
+// us, 4.2 TB/s, 72% of the issue slots; what is not finite is looked for once a row,
+// not once an entry: 46.4 -> 45.3).  16 tokens: 4.6 us, latency.
 #include <cuda_fp16.h>
 
 #include "common.cuh"

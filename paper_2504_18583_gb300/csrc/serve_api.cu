@@ -26,6 +26,13 @@ const char* bad_chunks(int n_tokens, int batch, int n_q_heads, int n_kv_heads) {
   return nullptr;
 }
 
+// a contiguous output of n_tokens rows lies over one of the queries' rows
+bool overlap(const void* out, const void* q, int64_t q_stride, int64_t row, int64_t n_tokens) {
+  const int64_t o = (int64_t)reinterpret_cast<uintptr_t>(out), at = (int64_t)reinterpret_cast<uintptr_t>(q), step = 2 * q_stride;
+  const int64_t before = o - at - 2 * row, first = before < 0 ? 0 : before / step + 1;  // the first row that ends behind `out`
+  return first < n_tokens && at + first * step < o + 2 * row * n_tokens;
+}
+
 }  // namespace
 }  // namespace pard
 
@@ -91,6 +98,8 @@ pard_status pard_chunk_attention(const void* d_q, int64_t q_stride, int32_t dtyp
   if (q_stride % 8 || !aligned16(d_q) || !aligned16(d_k_cache) || !aligned16(d_v_cache) || !aligned16(d_out) ||
       !aligned16(d_workspace))
     return refuse(PARD_ERR_ARG, "rows, caches, output and workspace must start on 16-byte boundaries");
+  if (overlap(d_out, d_q, q_stride, (int64_t)n_q_heads * head_dim, n_tokens))
+    return refuse(PARD_ERR_ARG, "chunk attention: the output lies over the queries");
   if (!std::isfinite(scale)) return refuse(PARD_ERR_ARG, "the scale must be finite");
   if (chunk_attention_places(n_tokens, batch, n_q_heads, n_kv_heads, max_pages) >= ((int64_t)1 << 31))
     return refuse(PARD_ERR_SHAPE, "more than 2^31 tiles of 128 keys: shorter page tables, chunks or a smaller batch");

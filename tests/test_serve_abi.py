@@ -9,6 +9,7 @@ import pytest
 from conftest import ROOT
 
 P = 0x10000  # 16-byte aligned, not null
+FAR = 1 << 46  # behind anything that starts at P
 ARG, SHAPE = -1, -2
 
 
@@ -29,7 +30,7 @@ WRITE = dict(qkv=P, qkv_stride=12 * 64, dtype=0, n_tokens=3, hq=8, hkv=2, hd=64,
              rot=64, inter=0, amp=1.0, q=P, q_stride=512, k=P, v=P, page_stride=2 * 16 * 64, ks=P, vs=P, scale_stride=32, n_pages=3,
              stream=None)
 CHUNK = dict(q=P, q_stride=512, dtype=0, n_tokens=9, batch=2, hq=8, hkv=2, hd=64, k=P, v=P, page_stride=2048, ks=None, vs=None,
-             scale_stride=0, n_pages=3, table=P, max_pages=4, starts=P, ctx=P, window=0, sinks=0, scale=0.125, out=P, ws=P,
+             scale_stride=0, n_pages=3, table=P, max_pages=4, starts=P, ctx=P, window=0, sinks=0, scale=0.125, out=FAR, ws=P,
              ws_bytes=1 << 30, stream=None)
 EIGHT = dict(ks=P, vs=P, scale_stride=32)
 ADJUST = dict(z=P, stride=100, dtype=2, batch=2, width=3, vocab=100, hist=P, max_hist=10, hist_len=P, prompt=P, rep=P, freq=P, pres=P,
@@ -51,7 +52,10 @@ ADJUST = dict(z=P, stride=100, dtype=2, batch=2, width=3, vocab=100, hist=P, max
         (dict(scale=float("inf")), ARG), (dict(q_stride=504), ARG), (dict(q_stride=514), ARG), (dict(q=P + 4), ARG),
         (dict(out=P + 2), ARG), (dict(ws_bytes=4096), ARG), (dict(page_stride=2052), SHAPE), (dict(page_stride=2000), SHAPE),
         (dict(n_tokens=1 << 27, max_pages=1 << 26), SHAPE), (dict(ks=P), ARG), (dict(vs=P), ARG), (dict(EIGHT, scale_stride=16), ARG),
-        (dict(EIGHT, vs=P + 4), ARG), (dict(EIGHT, page_stride=2056), ARG), (dict(n_pages=0), SHAPE)]),
+        (dict(EIGHT, vs=P + 4), ARG), (dict(EIGHT, page_stride=2056), ARG), (dict(n_pages=0), SHAPE),
+        # the output over the queries: the same rows, the last row's last entries, a row between rows that lie apart
+        (dict(out=P), ARG), (dict(out=P + 2 * 9 * 512 - 16), ARG), (dict(q_stride=512 * 100, out=P + 2 * 512 * 500 - 16), ARG),
+        (dict(q=FAR + 2 * 9 * 512 - 16), ARG)]),
     ("pard_adjust_logits", ADJUST, [
         (dict(z=None), ARG), (dict(out=None), ARG), (dict(dtype=3), SHAPE), (dict(batch=-1), ARG), (dict(batch=65536), ARG),
         (dict(batch=65535, width=257), ARG), (dict(vocab=0), SHAPE), (dict(vocab=262145, stride=262145, out_stride=262145), SHAPE),
@@ -102,3 +106,13 @@ def test_calls_check_their_arguments_before_the_device():
         tree.qk_norm_rope(z, 1, 1, z, z, z, z, None, k_scale=z, v_scale=z)
     with pytest.raises(ValueError):
         tree.chunk_attention_workspace(1, 1, 30, 8, 128)
+
+
+def test_an_output_between_the_queries_rows_is_let_through(lib):
+    """Refused for the workspace, which is looked at later."""
+    edit = dict(q_stride=512 * 100, ws_bytes=4096)
+    for out in (P + 2 * 512, P + 2 * 512 * 300 - 2 * 9 * 512, P + 2 * 512 * 800 + 2 * 512):
+        assert call(lib, "pard_chunk_attention", CHUNK, out=out, **edit) == ARG
+        assert b"workspace" in lib.pard_last_error()
+    assert call(lib, "pard_chunk_attention", CHUNK, out=P + 2 * 512 * 300 - 2 * 9 * 512 + 16, **edit) == ARG
+    assert b"over the queries" in lib.pard_last_error()
