@@ -22,10 +22,10 @@
 //
 // What bounds it: HBM for many rows (464 of 128256 in fp32, of 16 trees, with
 // penalties, biases and masks: 84 us, 5.7 TB/s), and for few the chain history ->
-// table -> list -> row (64 of 128256 in bf16 with 8000 tokens each: 18 us; one: 4.6);
-// a row's loads go out before the history's are looked at, and the next row's before
-// this one is worked on.  Slices are as long as they may be while the CTAs come out as
-// whole waves of four an SM.
+// table -> list -> row (64 of 128256 in bf16 with 8000 tokens each: 17.3 us, 9 of them
+// without the tokens; one: 4.6); a row's loads go out before the history's are looked
+// at, and the next row's before this one is worked on.  Slices are as long as they may
+// be while the CTAs come out as whole waves of four an SM.
 #include <cuda_fp16.h>
 
 #include "common.cuh"
@@ -118,7 +118,6 @@ __global__ void __launch_bounds__(kAdjThreads, kAdjCtas) adjust_kernel(const __g
   uint16_t* list = reinterpret_cast<uint16_t*>(sums + a.n_bias);
   uint8_t* twice = reinterpret_cast<uint8_t*>(list + slice);
   __shared__ int s_listed;
-  __shared__ uint16_t s_noted[kAdjThreads / 32][512];
   __shared__ uint32_t s_words[2][kAdjLongest / 32 + 1];  // a row's mask, and the next one's
   __shared__ int32_t s_tokens[kTreeMaxNodes];  // a tree's tokens, as places in the slice (others: -1)
   const int tid = threadIdx.x, b = blockIdx.y, lo = blockIdx.x * slice, n = min(slice, a.vocab - lo);
@@ -187,54 +186,40 @@ __global__ void __launch_bounds__(kAdjThreads, kAdjCtas) adjust_kernel(const __g
     __syncthreads();
   }
   {
-    // A warp takes 512 tokens at a time, 16 bytes a load between the history's first
-    // and last boundary, notes those of the slice and then counts what it noted: few
-    // tokens lie in it, but nearly every 32 have one, and counting on the way had each
-    // of them wait for a counter's old value.
+    // Sixteen tokens a thread at a time, 16 bytes a load between the history's first and
+    // last boundary.  Few of them lie in the slice: first which ones do is noted in a
+    // mask, three instructions a token, then those are counted.  (Nearly every 32 tokens
+    // have one: counted on the way, each 32 waited for a counter's old value, 28.5 us for
+    // the 64 rows above; gathered by ballots and counts of bits, those took most of 18.)
     const int32_t* said = a.history + (int64_t)b * a.max_history;
     const int head = min(length, (int)((16 - (reinterpret_cast<uintptr_t>(said) & 15)) & 15) / 4), pieces = (length - head) / 4;
-    const int lane = tid & 31;
-    uint16_t* noted = s_noted[tid >> 5];
-    int count = 0;
-    auto note = [&](bool there, int i, int32_t id) {  // all lanes of the warp
-      const uint32_t at = (uint32_t)id - (uint32_t)lo;
-      const bool in = there && at < (uint32_t)n;
-      const uint32_t all = __ballot_sync(0xffffffffu, in);
-      if (in) noted[count + __popc(all & ((1u << lane) - 1))] = (uint16_t)(at | (i < prompt ? 0x8000u : 0u));
-      count += __popc(all);
+    auto count = [&](int i) {
+      const uint32_t at = (uint32_t)__ldg(said + i) - (uint32_t)lo;
+      if (at < (uint32_t)n) touched(i < prompt ? atomicOr(table + at, kInPrompt) : atomicAdd(table + at, 1u), at);
     };
-    auto tally = [&] {
-      __syncwarp();
-      for (int k = lane; k < count; k += 32) {
-        const uint32_t at = noted[k] & 0x7FFFu;
-        touched(noted[k] & 0x8000u ? atomicOr(table + at, kInPrompt) : atomicAdd(table + at, 1u), at);
-      }
-      __syncwarp();
-      count = 0;
-    };
-    for (int p0 = tid - lane; p0 < pieces; p0 += 4 * kAdjThreads) {
+    for (int p0 = tid; p0 < pieces; p0 += 4 * kAdjThreads) {
       int4 q[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int v = p0 + e * kAdjThreads + lane;
+        const int v = p0 + e * kAdjThreads;
         q[e] = v < pieces ? __ldg(reinterpret_cast<const int4*>(said + head) + v) : make_int4(-1, -1, -1, -1);
       }
+      uint32_t in = 0;
+      auto note = [&](int k, int32_t id) { if ((uint32_t)id - (uint32_t)lo < (uint32_t)n) in |= 1u << k; };
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int v = p0 + e * kAdjThreads + lane, i = head + 4 * v;
-        note(v < pieces, i, q[e].x);
-        note(v < pieces, i + 1, q[e].y);
-        note(v < pieces, i + 2, q[e].z);
-        note(v < pieces, i + 3, q[e].w);
+        note(4 * e, q[e].x);
+        note(4 * e + 1, q[e].y);
+        note(4 * e + 2, q[e].z);
+        note(4 * e + 3, q[e].w);
       }
-      tally();
+      for (; in; in &= in - 1) {
+        const int k = __ffs(in) - 1;
+        count(head + 4 * (p0 + (k >> 2) * kAdjThreads) + (k & 3));
+      }
     }
-    if (tid < 32) {  // fewer than eight tokens are left, before the first boundary and behind the last
-      const int i = lane < head ? lane : head + 4 * pieces + lane - head;
-      const bool there = i < length && lane < 8;
-      note(there, i, there ? __ldg(said + i) : -1);
-      tally();
-    }
+    const int loose = length - 4 * pieces;  // before the first boundary and behind the last
+    if (tid < loose) count(tid < head ? tid : 4 * pieces + tid);
   }
   const int nodes = a.tokens ? a.width : 0;
   if (tid < nodes) {
