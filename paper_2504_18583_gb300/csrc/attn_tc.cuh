@@ -191,13 +191,15 @@ __device__ __forceinline__ int parts_of(int tiles, int most) {
 template <int SPLIT>
 struct RangesOf {
   int total, grid, each, rest;
+  uint32_t magic;  // 2^32 / grid, rounded up: c rest < grid^2
   __device__ __forceinline__ void set(int n, int g) {
+    magic = 0xFFFFFFFFu / (uint32_t)g + 1;
     total = n;
     grid = g;
     each = n / g;
     rest = n - each * g;
   }
-  __device__ __forceinline__ int at(int c) const { return c * each + c * rest / grid; }
+  __device__ __forceinline__ int at(int c) const { return c * each + (int)__umulhi((uint32_t)(c * rest), magic); }
   // a cut at place x of a unit of `len` places: near an end it moves there
   static __device__ __forceinline__ int cut(int x, int len) {
     return x <= SPLIT ? 0 : x >= len - SPLIT ? len : x;

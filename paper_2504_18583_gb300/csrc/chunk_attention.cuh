@@ -107,12 +107,17 @@ __device__ __forceinline__ Chunk chunk_of(const ChunkAttnArgs& a, int ctx, int f
   s.ctx = min(max(ctx, 0), 1 << 30);
   const int64_t end = (int64_t)s.ctx + s.n, most = (int64_t)a.max_pages * kPageTok;
   s.keys = (int)(end < most ? end : most);
-  s.rows = s.n * (a.n_q_heads / a.n_kv_heads);
+  s.rows = s.n * a.group;
   s.blocks = (s.rows + rows_per_block - 1) / rows_per_block;
   return s;
 }
 // n / group for rows of a block counted from a token's first: n below group + 256
 __device__ __forceinline__ int in_group(const ChunkAttnArgs& a, int n) { return a.group_magic ? (int)__umulhi((uint32_t)n, a.group_magic) : n; }
+// n / group for any n: the product passes the quotient by less than one
+__device__ __forceinline__ int token_of(const ChunkAttnArgs& a, int n) {
+  const int q = in_group(a, n);
+  return q * a.group > n ? q - 1 : q;
+}
 // One block's positions and tiles: tiles [0, sink) then [sink + skip, sink + skip + tiles - sink).
 struct Span {
   int token, rest;        // of the first row: its token in the chunk, and its place among that one's rows
@@ -125,9 +130,9 @@ struct Span {
 __device__ __forceinline__ int window_from(const ChunkAttnArgs& a, int p) { return a.window ? max(0, p - a.window + 1) : 0; }
 __device__ __forceinline__ Span span_of(const ChunkAttnArgs& a, const Chunk& s, int block, int rows_per_block) {
   Span g;
-  const int group = a.n_q_heads / a.n_kv_heads, r0 = block * rows_per_block;
-  g.token = r0 / group;
-  g.rest = r0 - g.token * group;
+  const int r0 = block * rows_per_block;
+  g.token = token_of(a, r0);
+  g.rest = r0 - g.token * a.group;
   g.p_lo = s.ctx + g.token;
   g.p_hi = g.p_lo + in_group(a, g.rest + min(rows_per_block, s.rows - r0) - 1);
   g.end = min(g.p_hi + 1, s.keys);
@@ -442,7 +447,7 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
   Control& sh = *reinterpret_cast<Control*>(raw_rings + NR * kStage);
   volatile int* abort_flag = &sh.abort_flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int group = a.n_q_heads / a.n_kv_heads, grid = gridDim.x;
+  const int group = a.group, grid = gridDim.x;
   const bool by_tma = !Q8 && a.q_by_tma;
 
   // ---- this CTA's range -------------------------------------------------------
@@ -859,9 +864,12 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
     } else {
       if (hi > lo) {  // the block that the first place lies in
         const int b = sh.start_b, rest = sh.start_off;
-        const Chunk s = chunk_of(a, a.ctx_len[b], a.starts[b], a.starts[b + 1], kRows);
-        int before = 0;
+        if (lane == 0) w.b = b;
         __syncwarp();
+        w.load(a, sh.seq, kRows);
+        __syncwarp();
+        const Chunk s = w.s;
+        int before = 0;
 #pragma unroll 1
         for (int i0 = 0; i0 < s.blocks; i0 += 32) {
           const int len = i0 + lane < s.blocks ? span_of(a, s, i0 + lane, kRows).tiles + kUnitStart : 0;
@@ -1436,6 +1444,7 @@ void run_chunk(const ChunkAttnArgs& a, cudaStream_t s) {
   vm = qm = km;
   ChunkAttnArgs args = a;
   const int group = a.n_q_heads / a.n_kv_heads;
+  args.group = group;
   args.group_magic = group > 1 ? 0xFFFFFFFFu / (uint32_t)group + 1 : 0;
   if (Q8) {
     km = codes_map(a, a.k_cache);

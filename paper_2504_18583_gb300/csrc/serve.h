@@ -35,6 +35,7 @@ struct ChunkAttnArgs {
   void* out;
   void* workspace;
   // the launcher's
+  int group = 1;             // query heads a key/value head
   uint32_t group_magic = 0;  // 2^32 / (query heads a key/value head), rounded up; 0 for one
   bool q_by_tma = false;
 };
