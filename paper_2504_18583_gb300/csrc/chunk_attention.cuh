@@ -44,23 +44,23 @@
 //   its 32 products 2052 of them and the softmax of both groups, eight warps, nearly all
 //   the others': scores wait for the probabilities that lie where they go.  The clock
 //   falls to 1.8 GHz under the power limit.  2048 tokens behind 30000 (64 heads on 8 of
-//   128): 1.43 ms, 1.46 PFLOP/s, 1.58 ms in a long run.  A prompt of 8191: 408 us.
+//   128): 1.41 ms, 1.48 PFLOP/s, 1.58 ms in a long run.  A prompt of 8191: 405 us.
 // - Units' ends: 7000 to 8000 clocks from a unit's last scores to the next one's first
-//   probabilities.  Four pieces of up to 512 tokens: 72 us; 16 sequences, most of them
+//   probabilities.  Four pieces of up to 512 tokens: 71 us; 16 sequences, most of them
 //   single tokens, with a window (heads of 64): 54 us, 2800 to 3600 clocks a tile, where
 //   masked tiles are many.
 // - Single tokens, 16-bit cache: HBM.  32 of them over 264000 keys: 180 us, 90% of the
 //   copy rate.
 // - 8-bit cache: shared memory.  A pair of tiles is written once as it lies, read, written
 //   as fp16 and read by the products, 1800 clocks of its 2830 (HBM: 1400): 32 single
-//   tokens 204 us; 1000 tokens behind 16001 277 us, against 219 from a 16-bit cache.
+//   tokens 201 us; 1000 tokens behind 16001 274 us, against 214 from a 16-bit cache.
 // - A single token with a window of 2048: 14.4 us, the chain lengths -> shares -> pages ->
 //   keys -> softmax -> partial -> join, 28000 clocks.
 //
 // Tried and slower: 64-column score products (2048 tokens behind 30000: 1417 -> 1631 us),
 // two threads a row (2075), the maximum only where the sum grows too large (8191 tokens:
 // 471 -> 540), a third buffer of scores for heads of 64 (a prompt of 4096: 108 -> 119),
-// the second group's products left out where it has no rows (a few percent, everywhere),
+// the second group's products left out where it has no rows (8191 tokens: 402 -> 413),
 // eight converting warps, codes turned by integer instructions (204 -> 240) or half of them
 // (222); without any arithmetic the conversion takes as long.
 // (A header, since 16-bit and 8-bit caches are compiled apart: a function that is
@@ -478,6 +478,7 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
     mbar_init(&sh.drain, 1);
     fence_barrier_init();
     *abort_flag = 0;
+    sh.start_b = sh.start_head = sh.start_block = sh.start_off = 0;  // (starts that decrease may leave them: in bounds then)
   }
   pdl_trigger();
   pdl_wait();
@@ -1387,9 +1388,11 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
 
 namespace {
 
-// Blocks of 256 query vectors where a sequence has more than 128 of them on
-// average: two groups with rows of their own reuse each tile twice; with fewer,
-// both work on the same rows.
+// Blocks of 256 query vectors where a sequence has more than 128 of them on average:
+// two groups with rows of their own use each tile twice.  With fewer, both work on
+// the same rows.  8 sequences of 8000 keys, four query heads a key/value head, 32
+// tokens each: 64 us in blocks of 128 and 69 of 256; 40 tokens: 90 and 70 (8-bit
+// caches: 65 and 94; 106 and 97).
 int chunk_blocks(int n_tokens, int batch, int group) { return (int64_t)n_tokens * group <= (int64_t)batch * kTile ? 1 : 2; }
 
 // An 8-bit cache's codes as [page][head][token][entry], boxes of a page's 16 tokens of a head.
