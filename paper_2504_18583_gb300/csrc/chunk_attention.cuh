@@ -52,8 +52,8 @@
 // - Single tokens, 16-bit cache: HBM.  32 of them over 264000 keys: 180 us, 90% of the
 //   copy rate.
 // - 8-bit cache: shared memory.  A pair of tiles is written once as it lies, read, written
-//   as fp16 and read by the products, 1800 clocks of its 2830 (HBM: 1400): 32 single
-//   tokens 201 us; 1000 tokens behind 16001 274 us, against 214 from a 16-bit cache.
+//   as fp16 and read by the products, 1800 clocks of its 2800 (HBM: 1400): 32 single
+//   tokens 194 us; 1000 tokens behind 16001 274 us, against 214 from a 16-bit cache.
 // - A single token with a window of 2048: 14.4 us, the chain lengths -> shares -> pages ->
 //   keys -> softmax -> partial -> join, 28000 clocks.
 //
@@ -351,7 +351,8 @@ __device__ __noinline__ void join_few(const Partial first, const uint16_t* slots
 struct Widen {
   uint32_t m;
   float s;
-  __device__ __forceinline__ static bool far(uint32_t e) { return e - 113u > 21u; }
+  // one of four exponents is below 113 or above 134
+  __device__ __forceinline__ static uint32_t far4(uint32_t e) { return __vcmpltu4(e, 0x71717171u) | __vcmpgtu4(e, 0x86868686u); }
   __device__ __forceinline__ void set(uint32_t e) { m = (e - 112u) * 0x04000400u; }
   __device__ __forceinline__ void set_far(uint32_t e) {
     s = e == 255u ? __int_as_float(0x7FFFFFFF) : __uint_as_float(e ? e << 23 : 1u << 22);
@@ -391,6 +392,7 @@ struct ChunkControl {
   uint64_t pair, met[2];   // the two groups meet, a group's warps do
   uint64_t drain;          // every product is done
   alignas(16) uint8_t scale[2][Q8 ? NR * kTile : 16];  // of the codes
+  uint8_t far[2][NR + 1];  // a tile of keys or values has one that Widen::far4() tells (what lies past the last key counts)
   uint8_t back[Q8 ? 2 * kTile : 16];  // exponents of the queries' rows, which were scaled by them
   int2 seq[kSeqHeld + 1];  // sequences' context lengths and first rows
   uint32_t tmem, last_in[2], odd[NV];  // odd: a stage's values that not all rows see held infinities or NaN (a byte a warp)
@@ -653,6 +655,8 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
           uint8_t* scale = sh.scale[v] + st * kTile;
           constexpr int kCodes = HD * kPageTok;
           if (lane < pages) *reinterpret_cast<uint4*>(scale + lane * kPageTok) = exponents;
+          const bool far = __any_sync(0xffffffffu, lane < pages && (Widen::far4(exponents.x) | Widen::far4(exponents.y) |
+                                                                    Widen::far4(exponents.z) | Widen::far4(exponents.w)));
           if (j + 1 < n) {
             const int ahead = (j + 1) & 3;
             exponents = exponents_of(__shfl_sync(0xffffffffu, ahead == 0 ? after : have, ahead * kTilePages + (lane & 7)));
@@ -663,6 +667,7 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
           __syncwarp();
           if (elect_one()) {
             if (!v) sh.pages[issued & 15] = (uint8_t)in_pool;
+            sh.far[v][st] = far;
             mbar_arrive_expect_tx(full + st, (uint32_t)pages * kCodes);
 #pragma unroll
             for (int q = 0; q < kTilePages; ++q)
@@ -1068,14 +1073,17 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
       float m_ref = -INFINITY, sum = 0.f;
       bool patch = false;  // values that the rows who see them get back in the epilogue
       const uint64_t scale2 = pair_of(__float_as_uint(sl2), __float_as_uint(sl2));
-      const Chunk us = u.s;
-      const Span ug = u.g;
-      const int first_tile = u.t0;
+      // all_see() of a tile that begins at k0: k0 <= whole and (from <= k0 or the tile lies
+      // among the first tokens), of the block's rows and of the group's
+      const int whole_block = min(u.g.p_lo + 1, u.s.keys) - kTile, from_block = window_from(a, u.g.p_hi);
+      const int whole_group = min(g_lo + 1, u.s.keys) - kTile, from_group = window_from(a, g_hi);
+      const int first_tile = u.t0, sink_tiles = u.g.sink, skip = u.g.skip;
 #pragma unroll 1
       for (int j = 0; j < n; ++j) {
-        const int k0 = ug.tile(first_tile + j) * kTile, x = BLOCKS == 2 ? g : j & 1;
-        const bool partly = !all_see(a, us, ug.p_lo, ug.p_hi, k0, k0 + kTile);  // some row of the block does not see all of the tile,
-        bool masked = !all_see(a, us, g_lo, g_hi, k0, k0 + kTile);  // some row of the group
+        const int k = first_tile + j, k0 = (k < sink_tiles ? k : k + skip) * kTile, x = BLOCKS == 2 ? g : j & 1;
+        const bool among = k0 + kTile <= a.sinks;
+        const bool partly = k0 > whole_block || (from_block > k0 && !among);  // some row of the block does not see all of the tile,
+        bool masked = k0 > whole_group || (from_group > k0 && !among);        // some row of the group
         ok = warp_wait(sh.s_full + x, ph_s >> x & 1, abort_flag);
         if (!ok) break;
         const uint32_t flags = sh.pages[(tile0 + j) & 15];
@@ -1183,7 +1191,7 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
       }
       constexpr int kCols = BLOCKS == 2 ? HD : HD / 2;
       const int col0 = BLOCKS == 2 ? 0 : g * kCols, in_block = (BLOCKS == 2 ? g * kTile : 0) + t;
-      const bool whole = u.t0 == 0 && u.t1 == ug.tiles, on = row < rows;
+      const bool whole = u.t0 == 0 && u.t1 == u.g.tiles, on = row < rows;
       // A unit's contributors are consecutive CTAs.  All but the last to arrive
       // leave their partial; that one joins them, in tile order.
       const int count = whole ? 1 : u.count, me = u.me, c0 = u.c0;
@@ -1198,7 +1206,7 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
         if (!ok) break;
         two = sh.last_in[g];
       }
-      T* unit = reinterpret_cast<T*>(a.out) + ((int64_t)us.row0 * a.n_q_heads + (int64_t)u.head * group) * HD;
+      T* unit = reinterpret_cast<T*>(a.out) + ((int64_t)u.s.row0 * a.n_q_heads + (int64_t)u.head * group) * HD;
       const int in_chunk = row - u.block * kRows + u.g.rest - in_token * group;  // this row among its token's
       T* out = unit + ((int64_t)token * a.n_q_heads + in_chunk) * HD;
       const int unit_row0 = row_base;
@@ -1281,61 +1289,59 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
         const bool clean = v && !all_see(a, u.s, u.g.p_lo, u.g.p_hi, k0, k0 + kTile);
         const int pages = pages_of(u, u.t0 + j), end = u.g.limit(a, u.t0 + j);
         bool any = false;
-#pragma unroll 1
-        for (int q = cw; q < pages; q += kConvWarps / 2) {
-          const uint4* codes = reinterpret_cast<const uint4*>(raw + q * kCodes);
-          uint4 x[kHeld];
-          uint32_t by[kHeld];
-          bool far = false;
+        // eight entries of row r: two pieces of a row's sixteen codes, and the lanes of a
+        // row's second half write theirs the other way round, so that eight lanes reach
+        // all banks
+        const int c16 = lane % kRowPieces, turn = HD == 128 ? c16 / 4 : 0;
+        uint8_t* to = stage + (c16 / 4) * kChunkBytes + lane / kRowPieces * 128;
+        auto put = [&](int q, int e, const uint32_t (&y)[8]) {
+          const int r = lane / kRowPieces + e * (32 / kRowPieces), c = (2 * c16) % 8;
+          uint8_t* at = to + (q * kPageTok + e * (32 / kRowPieces)) * 128;
 #pragma unroll
-          for (int e = 0; e < kHeld; ++e) {
-            x[e] = codes[e * 32 + lane];
-            by[e] = scale[q * kPageTok + (e * 32 + lane) / kRowPieces];
-            far |= Widen::far(by[e]);
+          for (int h = 0; h < 2; ++h) {
+            const bool second = (h ^ turn) != 0;
+            *reinterpret_cast<uint4*>(at + (((c + (second ? 1 : 0)) ^ (r & 7)) << 4)) =
+                second ? make_uint4(y[4], y[5], y[6], y[7]) : make_uint4(y[0], y[1], y[2], y[3]);
           }
-          // eight entries of row r: two pieces of a row's sixteen codes, and the lanes of a
-          // row's second half write theirs the other way round, so that eight lanes reach
-          // all banks
-          const int c16 = lane % kRowPieces, turn = HD == 128 ? c16 / 4 : 0;
-          uint8_t* to = stage + (c16 / 4) * kChunkBytes + (q * kPageTok + lane / kRowPieces) * 128;
-          auto put = [&](int e, const uint32_t (&y)[8]) {
-            const int r = lane / kRowPieces + e * (32 / kRowPieces), c = (2 * c16) % 8;
-            uint8_t* at = to + e * (32 / kRowPieces) * 128;
+        };
+        if (!clean && !sh.far[v][rs]) {
+#pragma unroll 1
+          for (int q = cw; q < pages; q += kConvWarps / 2) {
+            uint4 x[kHeld];
+            uint32_t by[kHeld];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const bool second = (h ^ turn) != 0;
-              *reinterpret_cast<uint4*>(at + (((c + (second ? 1 : 0)) ^ (r & 7)) << 4)) =
-                  second ? make_uint4(y[4], y[5], y[6], y[7]) : make_uint4(y[0], y[1], y[2], y[3]);
+            for (int e = 0; e < kHeld; ++e) {
+              x[e] = reinterpret_cast<const uint4*>(raw + q * kCodes)[e * 32 + lane];
+              by[e] = scale[q * kPageTok + (e * 32 + lane) / kRowPieces];
             }
-          };
-          if (!__any_sync(0xffffffffu, far) && !clean) {
 #pragma unroll
             for (int e = 0; e < kHeld; ++e) {
               Widen w8;
               w8.set(by[e]);
               const uint32_t y[8] = {w8.near_two(x[e].x), w8.near_two(x[e].x >> 16), w8.near_two(x[e].y), w8.near_two(x[e].y >> 16),
                                      w8.near_two(x[e].z), w8.near_two(x[e].z >> 16), w8.near_two(x[e].w), w8.near_two(x[e].w >> 16)};
-              put(e, y);
+              put(q, e, y);
             }
-          } else {
+          }
+        } else {
 #pragma unroll 1
-            for (int e = 0; e < kHeld; ++e) {
-              Widen w8;
-              const uint4 xe = codes[e * 32 + lane];
-              w8.set_far(scale[q * kPageTok + (e * 32 + lane) / kRowPieces]);
-              uint32_t y[8] = {w8.far_two(xe.x), w8.far_two(xe.x >> 16), w8.far_two(xe.y), w8.far_two(xe.y >> 16),
-                               w8.far_two(xe.z), w8.far_two(xe.z >> 16), w8.far_two(xe.w), w8.far_two(xe.w >> 16)};
-              const int key = k0 + q * kPageTok + lane / kRowPieces + e * (32 / kRowPieces);
-              if (clean && !all_see(a, u.s, u.g.p_lo, u.g.p_hi, key, key + 1)) {
+          for (int qe = 0; qe < kHeld * ((pages - cw + kConvWarps / 2 - 1) / (kConvWarps / 2)); ++qe) {
+            const int q = cw + qe / kHeld * (kConvWarps / 2), e = qe % kHeld;
+            Widen w8;
+            const uint4 xe = reinterpret_cast<const uint4*>(raw + q * kCodes)[e * 32 + lane];
+            w8.set_far(scale[q * kPageTok + (e * 32 + lane) / kRowPieces]);
+            uint32_t y[8] = {w8.far_two(xe.x), w8.far_two(xe.x >> 16), w8.far_two(xe.y), w8.far_two(xe.y >> 16),
+                             w8.far_two(xe.z), w8.far_two(xe.z >> 16), w8.far_two(xe.w), w8.far_two(xe.w >> 16)};
+            const int key = k0 + q * kPageTok + lane / kRowPieces + e * (32 / kRowPieces);
+            if (clean && !all_see(a, u.s, u.g.p_lo, u.g.p_hi, key, key + 1)) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                  const uint32_t f = key >= end ? 0u : finite_of<__half>(y[k]);
-                  any |= key < end && f != y[k];
-                  y[k] = f;
-                }
+              for (int k = 0; k < 8; ++k) {
+                const uint32_t f = key >= end ? 0u : finite_of<__half>(y[k]);
+                any |= key < end && f != y[k];
+                y[k] = f;
               }
-              put(e, y);
             }
+            put(q, e, y);
           }
         }
         if (v && cw == 0 && pages <= kTilePages / 2) {  // the second half's first 16, which are multiplied in any case

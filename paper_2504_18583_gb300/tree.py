@@ -121,13 +121,13 @@ def qk_norm_rope(qkv, n_q_heads: int, n_kv_heads: int, pos, slots, k_cache, v_ca
 
 
 def quantized_cache(n_pages: int, n_kv_heads: int, head_dim: int, device="cuda"):
-    """One layer's 8-bit cache: k_cache, v_cache [pages, Hkv, 16, hd] float8_e4m3fn, k_scale, v_scale [pages, Hkv, 16]
-    float8_e8m0fnu, all zeros (a token's head takes hd + 1 bytes of each; the entry is its code times its scale)."""
-    def zeros(*shape):
-        return torch.zeros(shape, dtype=torch.uint8, device=device)
+    """One layer's 8-bit cache: k_cache, v_cache [pages, Hkv, 16, hd] float8_e4m3fn, zeros, and k_scale, v_scale [pages, Hkv, 16]
+    float8_e8m0fnu, ones (a token's head takes hd + 1 bytes of each; the entry is its code times its scale)."""
+    def bytes_of(value, *shape):
+        return torch.full(shape, value, dtype=torch.uint8, device=device)
     shape = (n_pages, n_kv_heads, 16)
-    k, v = (zeros(*shape, head_dim).view(torch.float8_e4m3fn) for _ in range(2))
-    k_scale, v_scale = (zeros(*shape).view(torch.float8_e8m0fnu) for _ in range(2))
+    k, v = (bytes_of(0, *shape, head_dim).view(torch.float8_e4m3fn) for _ in range(2))
+    k_scale, v_scale = (bytes_of(127, *shape).view(torch.float8_e8m0fnu) for _ in range(2))
     return k, v, k_scale, v_scale
 
 
@@ -187,7 +187,8 @@ def chunk_attention(q, k_cache, v_cache, page_table, starts, ctx_len, scale: Opt
     p - j < window or j < sinks.  scale: 1 / sqrt(hd) unless given; workspace: of
     chunk_attention_workspace (without one, calls share the stream's with
     tree_attention: shared_workspace; a call that a CUDA graph captures gets its
-    own).  Returns [T, Hq, hd]; rows of no sequence are not written."""
+    own); out must not lie over q.  Returns [T, Hq, hd]; rows of no sequence are not
+    written."""
     return _ops.chunk_attention(q, k_cache, v_cache, page_table, starts, ctx_len, scale, window, sinks, k_scale, v_scale,
                                 out, workspace)
 
