@@ -21,7 +21,7 @@ namespace {
 
 constexpr int kTile = 128;                      // keys a tile, rows a score tile
 constexpr int kTilePages = kTile / kPageTok;
-constexpr int kStart = 2, kSplit = 6;           // what a unit's start, and splitting it, costs in tiles
+constexpr int kSplit = 6;                       // what splitting a unit costs in tiles
 constexpr int kMaxGrid = 160;                   // workspace slots are sized for this many CTAs
 constexpr float kLazy = 8.0f;                   // growth of a maximum, in powers of two, that is let pass
 

@@ -6,7 +6,7 @@ namespace pard {
 int64_t chunk_attention_places(int n_tokens, int batch, int n_q_heads, int n_kv_heads, int max_pages) {
   const int group = n_q_heads / n_kv_heads, rows = kTile * chunk_blocks(n_tokens, batch, group);
   const int64_t blocks = (int64_t)n_tokens * group / rows + batch, tiles = ((int64_t)max_pages * kPageTok + kTile - 1) / kTile;
-  return blocks * n_kv_heads * (tiles + kStart);
+  return blocks * n_kv_heads * (tiles + kUnitStart);  // as the kernel counts them: its sums are 32-bit ones
 }
 
 size_t chunk_attention_workspace(int n_tokens, int batch, int n_q_heads, int n_kv_heads, int head_dim) {

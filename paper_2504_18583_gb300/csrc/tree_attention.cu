@@ -62,6 +62,7 @@ namespace {
 
 constexpr int kTaThreads = 384;
 constexpr int kSeqCache = 64;                   // sequences whose lengths a CTA keeps at hand
+constexpr int kStart = 2;                       // what a unit's start costs in tiles
 
 // tiles of keys, and of values, in flight: what shared memory holds beside the queries
 __host__ __device__ constexpr int k_stages(int hd, int blocks) { return hd == 128 ? (blocks == 1 ? 3 : 2) : (blocks == 1 ? 6 : 5); }

@@ -116,3 +116,23 @@ def test_an_output_between_the_queries_rows_is_let_through(lib):
         assert b"workspace" in lib.pard_last_error()
     assert call(lib, "pard_chunk_attention", CHUNK, out=P + 2 * 512 * 300 - 2 * 9 * 512 + 16, **edit) == ARG
     assert b"over the queries" in lib.pard_last_error()
+
+
+@pytest.mark.parametrize("T,batch,heads,group", [
+    (262145, 1, 32, 1),   # one long prompt, blocks of 256 query vectors
+    (49500, 49500, 1024, 1),  # a token a sequence, blocks of 128
+    (70000, 3, 8, 4),
+])
+def test_the_limit_on_tiles_is_where_the_kernels_sums_end(lib, T, batch, heads, group):
+    """A unit (a block of rows of a key/value head) counts its tiles of 128 keys and three more, and the sum over all
+    units is held in 32 bits: page tables up to the last tile that fits are let through (and refused for the workspace,
+    which is looked at later), one page more is refused for its size."""
+    rows = 128 if T * group <= batch * 128 else 256
+    units = (T * group // rows + batch) * heads
+    tiles = (2 ** 31 - 1) // units - 3
+    edit = dict(n_tokens=T, batch=batch, hq=heads * group, hkv=heads, q_stride=heads * group * 64, page_stride=heads * 16 * 64, ws_bytes=4096)
+    assert units * (tiles + 3) < 2 ** 31 <= units * (tiles + 4)
+    assert call(lib, "pard_chunk_attention", CHUNK, max_pages=tiles * 8, **edit) == ARG
+    assert b"workspace" in lib.pard_last_error()
+    assert call(lib, "pard_chunk_attention", CHUNK, max_pages=tiles * 8 + 1, **edit) == SHAPE
+    assert b"2^31" in lib.pard_last_error()
