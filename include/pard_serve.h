@@ -47,7 +47,8 @@ pard_status pard_qk_norm_rope_quantized(const void* d_qkv, int64_t qkv_stride, i
  * power of two, held to +-65504 and to multiples of 2^-24.  Scores and sums are
  * held in 32 bits; probabilities are rounded to `dtype` (with an 8-bit cache to
  * fp16) before they multiply the values.  d_out must not overlap d_q.  d_workspace:
- * pard_chunk_attention_workspace_bytes (0: invalid arguments) bytes, the first
+ * pard_chunk_attention_workspace_bytes (0: invalid arguments) bytes, which are
+ * enough for all calls with these heads and no more tokens and sequences, the first
  * 4096 of them zero before the first call; each call leaves them fit for the
  * next, of any sizes that they are enough for, and for pard_tree_attention
  * (whose workspace fits here too).  Calls that may overlap on the GPU need one

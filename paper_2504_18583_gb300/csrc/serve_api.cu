@@ -74,7 +74,8 @@ size_t pard_chunk_attention_workspace_bytes(int32_t n_tokens, int32_t batch, int
   if (bad_chunks(n_tokens, batch, n_q_heads, n_kv_heads) ||
       bad_cache(n_kv_heads, head_dim, (int64_t)n_kv_heads * kPageTok * head_dim, 1))
     return 0;
-  return chunk_attention_workspace(n_tokens, batch, n_q_heads, n_kv_heads, head_dim);
+  // as few sequences as the call may have: the same tokens in fewer of them may take larger blocks
+  return chunk_attention_workspace(n_tokens, 1, n_q_heads, n_kv_heads, head_dim);
 }
 
 pard_status pard_chunk_attention(const void* d_q, int64_t q_stride, int32_t dtype, int32_t n_tokens, int32_t batch,

@@ -166,7 +166,7 @@ def tree_attention(q, k_cache, v_cache, page_table, ctx_len, n_nodes, mask, scal
 
 
 def chunk_attention_workspace(n_tokens: int, batch: int, n_q_heads: int, n_kv_heads: int, head_dim: int, device="cuda"):
-    """A workspace for chunk_attention calls of these sizes (or smaller), one at a time."""
+    """A workspace for chunk_attention calls with these heads and no more tokens and sequences, one at a time."""
     n = pard.lib().pard_chunk_attention_workspace_bytes(n_tokens, batch, n_q_heads, n_kv_heads, head_dim)
     if n == 0:
         raise ValueError("chunk_attention does not support these sizes")

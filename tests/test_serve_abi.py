@@ -136,3 +136,14 @@ def test_the_limit_on_tiles_is_where_the_kernels_sums_end(lib, T, batch, heads, 
     assert b"workspace" in lib.pard_last_error()
     assert call(lib, "pard_chunk_attention", CHUNK, max_pages=tiles * 8 + 1, **edit) == SHAPE
     assert b"2^31" in lib.pard_last_error()
+
+
+@pytest.mark.parametrize("heads", [(32, 8, 128), (32, 32, 64), (64, 8, 128), (14, 2, 64), (64, 1, 64)])
+def test_a_workspace_is_enough_for_fewer_tokens_and_sequences(lib, heads):
+    """Many short sequences take blocks of 128 rows, fewer of them with as many tokens blocks of 256, whose partials are
+    twice as large: the size for the former has to be enough for the latter."""
+    f, sizes = lib.pard_chunk_attention_workspace_bytes, (1, 2, 4, 32, 33, 129, 256, 1000)
+    for T in sizes:
+        for batch in sizes:
+            whole = f(T, batch, *heads)
+            assert all(f(t, b, *heads) <= whole for t in sizes if t <= T for b in sizes if b <= batch)
