@@ -219,6 +219,15 @@ struct Partial {
   }
 };
 __host__ __device__ constexpr size_t slot_floats(int hd, int blocks) { return (size_t)(hd + 4) * kTile * blocks; }
+// Values that not every row sees are taken out of the products where they are infinite
+// or NaN; who has such says so as it arrives, and the last to arrive adds the whole
+// unit's to the output, behind the join: in a partial, a weight of zero would turn an
+// infinity into NaN.
+constexpr uint32_t kOddArrival = 1u << 16;       // in an arrival, beside the one that counts it
+// 1: those who have arrived are all of a unit's contributors but one, who is the last; 2: and one of them said so; else 0
+__device__ __forceinline__ uint32_t last_of(uint32_t arrived, int count) {
+  return (arrived & (kOddArrival - 1)) != (uint32_t)count - 1 ? 0u : arrived < kOddArrival ? 1u : 2u;
+}
 constexpr int kStalledWord = 2 * kMaxGrid;       // after the arrivals: a wait has run out in some call
 constexpr size_t kArriveBytes = (kStalledWord + 4) * sizeof(uint32_t);
 template <typename Args>
@@ -233,9 +242,9 @@ __device__ __forceinline__ uint32_t ld_acquire(const uint32_t* p) {
   return v;
 }
 __device__ __forceinline__ void fence_gpu() { asm volatile("fence.acq_rel.gpu;" ::: "memory"); }
-__device__ __forceinline__ uint32_t arrive_acq_rel(uint32_t* p) {
+__device__ __forceinline__ uint32_t arrive_acq_rel(uint32_t* p, bool odd) {
   uint32_t old;
-  asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(old) : "l"(p) : "memory");
+  asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], %2;" : "=r"(old) : "l"(p), "r"(odd ? kOddArrival + 1 : 1u) : "memory");
   return old;
 }
 

@@ -237,13 +237,19 @@ __device__ __forceinline__ float value_at(const ChunkAttnArgs& a, int64_t page, 
   return (code & 0x7F) == 0x7F || e == 255u ? __int_as_float(0x7FFFFFFF) : 0.f;  // (finite: as an operand it is held to 65504)
 }
 
-// Adds the infinities and NaN of the values of a part's tiles that not every row
-// of the block sees back to a row that sees them: to the output, or to a partial.
-template <typename T, int HD, bool Q8>
-__device__ __noinline__ void patch_chunk(const ChunkAttnArgs& a, const Segment& w, int p, int col0, int cols, T* out,
-                                         Partial part, int row) {
+// Adds the infinities and NaN of a unit's values that not every row of the block
+// sees back to the output of the row that has thread t of group g, where it sees
+// them: they stay what they are there.
+template <typename T, int HD, int BLOCKS, bool Q8>
+__device__ __noinline__ void patch_chunk(const ChunkAttnArgs& a, const Segment& w, int g, int t) {
+  constexpr int cols = BLOCKS == 2 ? HD : HD / 2;
+  const int r = (BLOCKS == 2 ? g * kTile : 0) + t, col0 = BLOCKS == 2 ? 0 : g * cols;
+  if (w.block * BLOCKS * kTile + r >= w.s.rows) return;
+  const int in_token = in_group(a, w.g.rest + r), token = w.g.token + in_token, p = w.s.ctx + token;
   const int end = min(p + 1, w.s.keys), from = window_from(a, p);
-  for (int k = w.t0; k < w.t1; ++k) {
+  T* out = reinterpret_cast<T*>(a.out) +
+           (((int64_t)w.s.row0 + token) * a.n_q_heads + (int64_t)w.head * a.group + (w.g.rest + r - in_token * a.group)) * HD;
+  for (int k = 0; k < w.g.tiles; ++k) {
     const int k0 = w.g.tile(k) * kTile;
     if (all_see(a, w.s, w.g.p_lo, w.g.p_hi, k0, k0 + kTile)) continue;
     for (int pos = k0; pos < min(k0 + kTile, end); ++pos) {
@@ -254,12 +260,8 @@ __device__ __noinline__ void patch_chunk(const ChunkAttnArgs& a, const Segment& 
       for (int c = col0; c < col0 + cols; ++c) {
         const float x = value_at<T, HD, Q8>(a, page, w.head, pos % kPageTok, c);
         if (fabsf(x) < INFINITY) continue;
-        if (out) {
-          const uint32_t y = Num<T>::pack(Num<T>::get(out + c) + x, 0.f);
-          *reinterpret_cast<uint16_t*>(out + c) = (uint16_t)y;
-        } else {
-          reinterpret_cast<float*>(part.o(c / 4, row))[c % 4] += x;
-        }
+        const uint32_t y = Num<T>::pack(Num<T>::get(out + c) + x, 0.f);
+        *reinterpret_cast<uint16_t*>(out + c) = (uint16_t)y;
       }
     }
   }
@@ -396,6 +398,7 @@ struct ChunkControl {
   uint8_t back[Q8 ? 2 * kTile : 16];  // exponents of the queries' rows, which were scaled by them
   int2 seq[kSeqHeld + 1];  // sequences' context lengths and first rows
   uint32_t tmem, last_in[2], odd[NV];  // odd: a stage's values that not all rows see held infinities or NaN (a byte a warp)
+  int odd_in[2];           // the last segment, counted from 1, in which a group met such
   uint8_t pages[16];       // which of a tile's pages are the pool's, tiles in turn: keys are loaded fewer than 16 ahead of the softmax
   int abort_flag, start_b, start_head, start_block, start_off;
   int sum[16], units[16], most[16];
@@ -479,7 +482,7 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
     mbar_init(&sh.pair, 8);
     mbar_init(&sh.drain, 1);
     fence_barrier_init();
-    *abort_flag = 0;
+    *abort_flag = sh.odd_in[0] = sh.odd_in[1] = 0;
     sh.start_b = sh.start_head = sh.start_block = sh.start_off = 0;  // (starts that decrease may leave them: in bounds then)
   }
   pdl_trigger();
@@ -1071,7 +1074,6 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
       auto position = [&](int r) { return u.g.p_lo + in_group(a, u.g.rest + min(r, rows - 1) - u.block * kRows); };
       const int g_lo = position(row_base), g_hi = position(row_base + kTile - 1);
       float m_ref = -INFINITY, sum = 0.f;
-      bool patch = false;  // values that the rows who see them get back in the epilogue
       const uint64_t scale2 = pair_of(__float_as_uint(sl2), __float_as_uint(sl2));
       // all_see() of a tile that begins at k0: k0 <= whole and (from <= k0 or the tile lies
       // among the first tokens), of the block's rows and of the group's
@@ -1153,7 +1155,7 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
             const int st = (tile0 + j) % NV;
             ok = warp_wait(sh.fixed + st, ((tile0 + j) / NV) & 1, abort_flag);
             if (!ok) break;
-            patch |= sh.odd[st] != 0;
+            if (sh.odd[st]) sh.odd_in[g] = taken;  // the rows who see them get them back in the epilogue
           }
           arrive(&sh.p_full[x][h]);
         }
@@ -1174,12 +1176,11 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
       // ---- epilogue: a group's own accumulator, or half the columns of both groups' ----
       float w0 = 1.f, w1 = 0.f;
       if (BLOCKS == 1) {
-        float4* ml = reinterpret_cast<float4*>(qbuf);  // the queries have been read
-        ml[g * kTile + t] = make_float4(m_ref, sum, patch ? 1.f : 0.f, 0.f);
+        float2* ml = reinterpret_cast<float2*>(qbuf);  // the queries have been read
+        ml[g * kTile + t] = make_float2(m_ref, sum);
         meet();
         if (!ok) break;
-        const float4 y = ml[t], z = ml[kTile + t];
-        patch = y.z + z.z > 0.f;
+        const float2 y = ml[t], z = ml[kTile + t];
         m_ref = fmaxf(y.x, z.x);
         w0 = y.x == -INFINITY ? 0.f : ex2(y.x - m_ref);
         w1 = z.x == -INFINITY ? 0.f : ex2(z.x - m_ref);
@@ -1200,11 +1201,12 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
       auto slot = [&](int i) { const Partial s = slot_of(a, i, HD, BLOCKS); return few ? few_rows<HD>(s) : s; };
       const Partial mine = slot(2 * (c0 + me) + (u.t0 > 0 ? 0 : 1));
       bool two = false;
+      auto odd = [&] { return sh.odd_in[g] == taken; };
       if (count == 2) {
-        if (t == 0) sh.last_in[g] = ld_acquire(arrived) == 1;
+        if (t == 0) sh.last_in[g] = last_of(ld_acquire(arrived), count);
         group_meet();
         if (!ok) break;
-        two = sh.last_in[g];
+        two = sh.last_in[g] != 0;
       }
       T* unit = reinterpret_cast<T*>(a.out) + ((int64_t)u.s.row0 * a.n_q_heads + (int64_t)u.head * group) * HD;
       const int in_chunk = row - u.block * kRows + u.g.rest - in_token * group;  // this row among its token's
@@ -1227,7 +1229,6 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
                                                          __uint_as_float(o[4 * i + 2]), __uint_as_float(o[4 * i + 3]));
           }
         }
-        if (patch && on) patch_chunk<T, HD, Q8>(a, u, p, col0, kCols, whole ? out : nullptr, mine, in_block);
         if (!whole) {
           *mine.stats(HD, g, in_block) = make_float2(m_ref, sum);
           // written before the group meets, read after, and written again only when
@@ -1238,7 +1239,7 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
           fence_gpu();
           group_meet();
           if (!ok) break;
-          if (t == 0) sh.last_in[g] = arrive_acq_rel(arrived) == (uint32_t)count - 1;
+          if (t == 0) sh.last_in[g] = last_of(arrive_acq_rel(arrived, odd()), count);
           group_meet();
           if (!ok) break;
           if (sh.last_in[g]) {
@@ -1258,8 +1259,12 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
         const Partial other = slot(2 * (c0 + 1 - me) + me);
         join_two<T, HD, BLOCKS>(other, my + 2 * kTile + (BLOCKS == 2 ? g * HD : 0), g, in_block, me == 0, m_ref, sum, w0,
                                 w1, true, col0, on, out, wide_out);
-        if (patch && on) patch_chunk<T, HD, Q8>(a, u, p, col0, kCols, out, mine, in_block);
         if (t == 0) *arrived = 0;
+      }
+      if (whole ? odd() : sh.last_in[g] == 2 || (sh.last_in[g] == 1 && odd())) {
+        group_meet();  // a row may have been joined by other threads
+        if (!ok) break;
+        patch_chunk<T, HD, BLOCKS, Q8>(a, segment(), g, t);
       }
       if (BLOCKS == 1) {  // each group reads both accumulators
         meet();

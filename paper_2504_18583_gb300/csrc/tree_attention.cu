@@ -785,7 +785,7 @@ __global__ void __launch_bounds__(kTaThreads, 1)
           fence_gpu();
           group_meet();
           if (!ok) break;
-          if (t == 0) sh.last_in[g] = arrive_acq_rel(arrived) == (uint32_t)count - 1;
+          if (t == 0) sh.last_in[g] = arrive_acq_rel(arrived, false) == (uint32_t)count - 1;
           group_meet();
           if (!ok) break;
           if (sh.last_in[g]) {
