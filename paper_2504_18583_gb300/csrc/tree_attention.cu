@@ -37,8 +37,8 @@
 // Masks touch only tiles that reach past the context: a row's 256 mask bits
 // select among its scores.  Values there may hold anything: what lies past the
 // sequence is zeroed in shared memory, and so are infinities and NaN of tree
-// nodes, which the epilogue adds back for the rows that see the node (0 x NaN
-// would reach every row otherwise).
+// nodes, which the CTA that writes the output adds back for the rows that see the
+// node (0 x NaN would reach every row otherwise).
 //
 // What bounds it, measured:
 //   8 sequences x 64 nodes at 4096, 64/8 heads of 128: 69 us; 36 us of products
@@ -161,26 +161,27 @@ __device__ __forceinline__ uint32_t allowed32(const uint32_t* row, int words32, 
   return some >= 32 ? m : some <= 0 ? 0u : m & ((1u << some) - 1u);
 }
 
-// Adds the infinities and NaN of the values at positions [from, end), tree
-// nodes', back to a row that sees them: to the output, or to a partial.  (In
-// the joined output they go on top of the sum, where they stay what they are.)
-template <typename T, int HD>
-__device__ __noinline__ void patch_row(const TreeAttnArgs& a, int b, int head, const Seq& s, int from, int end,
-                                       const uint32_t* mrow, int col0, int cols, T* out, Partial part, int row) {
-  for (int pos = from; pos < end; ++pos) {
-    const int node = pos - s.ctx, page = page_of(a.page_table + (size_t)b * a.max_pages, pos, a.max_pages, a.n_pages);
+// Adds the infinities and NaN of the tree nodes' values back to the output of the
+// row that has thread t of group g, where it sees them: on top of the joined sum
+// they stay what they are.
+template <typename T, int HD, int BLOCKS>
+__device__ __noinline__ void patch_row(const TreeAttnArgs& a, const Walk& w, int g, int t) {
+  constexpr int cols = BLOCKS == 2 ? HD : HD / 2;
+  const int group = a.n_q_heads / a.n_kv_heads, row = w.block * BLOCKS * kTile + (BLOCKS == 2 ? g * kTile : 0) + t, of = row / group;
+  const int col0 = BLOCKS == 2 ? 0 : g * cols;
+  if (row >= w.s.nodes * group) return;
+  const uint32_t* mrow = reinterpret_cast<const uint32_t*>(a.mask + ((size_t)w.b * a.width + of) * a.words);
+  T* out = reinterpret_cast<T*>(a.out) + (((int64_t)w.b * a.width + of) * a.n_q_heads + (int64_t)w.head * group + (row - of * group)) * HD;
+  for (int pos = w.s.ctx; pos < w.s.keys; ++pos) {
+    const int node = pos - w.s.ctx, page = page_of(a.page_table + (size_t)w.b * a.max_pages, pos, a.max_pages, a.n_pages);
     if (page < 0 || !(mrow[node >> 5] >> (node & 31) & 1)) continue;
-    const T* v = reinterpret_cast<const T*>(a.v_cache) + page * a.page_stride + ((int64_t)head * kPageTok + pos % kPageTok) * HD;
+    const T* v = reinterpret_cast<const T*>(a.v_cache) + page * a.page_stride + ((int64_t)w.head * kPageTok + pos % kPageTok) * HD;
 #pragma unroll 1
     for (int c = col0; c < col0 + cols; ++c) {
       const float x = Num<T>::get(v + c);
       if (fabsf(x) < INFINITY) continue;
-      if (out) {
-        const uint32_t y = Num<T>::pack(Num<T>::get(out + c) + x, 0.f);
-        *reinterpret_cast<uint16_t*>(out + c) = (uint16_t)y;
-      } else {
-        reinterpret_cast<float*>(part.o(c / 4, row))[c % 4] += x;
-      }
+      const uint32_t y = Num<T>::pack(Num<T>::get(out + c) + x, 0.f);
+      *reinterpret_cast<uint16_t*>(out + c) = (uint16_t)y;
     }
   }
 }
@@ -747,12 +748,13 @@ __global__ void __launch_bounds__(kTaThreads, 1)
       const int count = whole ? 1 : w.count, me = w.me, c0 = w.c0;
       uint32_t* arrived = reinterpret_cast<uint32_t*>(a.workspace) + 2 * c0 + g;
       const Partial mine = slot_of(a, 2 * (c0 + me) + (w.t0 > 0 ? 0 : 1), HD, BLOCKS);
-      bool two = false;
+      bool two = false, finish = whole;  // this CTA writes the unit's output
       if (count == 2) {
-        if (t == 0) sh.last_in[g] = ld_acquire(arrived) == 1;
+        if (t == 0) sh.last_in[g] = last_of(ld_acquire(arrived), count);
         group_meet();
         if (!ok) break;
-        two = sh.last_in[g];
+        two = finish = sh.last_in[g] != 0;
+        patch |= sh.last_in[g] == 2;
       }
       T* out = reinterpret_cast<T*>(a.out) +
                (((int64_t)w.b * a.width + node) * a.n_q_heads + (int64_t)w.head * group + (row - node * group)) * HD;
@@ -772,9 +774,6 @@ __global__ void __launch_bounds__(kTaThreads, 1)
                                                          __uint_as_float(o[4 * i + 2]), __uint_as_float(o[4 * i + 3]));
           }
         }
-        if (patch && on)
-          patch_row<T, HD>(a, w.b, w.head, w.s, max(w.t0 * kTile, w.s.ctx), min(w.t1 * kTile, w.s.keys), mrow, col0, kCols,
-                           whole ? out : nullptr, mine, in_block);
         if (!whole) {
           *mine.stats(HD, g, in_block) = make_float2(m_ref, sum);
           // written before the group meets, read after, and written again only when
@@ -785,10 +784,12 @@ __global__ void __launch_bounds__(kTaThreads, 1)
           fence_gpu();
           group_meet();
           if (!ok) break;
-          if (t == 0) sh.last_in[g] = arrive_acq_rel(arrived, false) == (uint32_t)count - 1;
+          if (t == 0) sh.last_in[g] = last_of(arrive_acq_rel(arrived, patch), count);
           group_meet();
           if (!ok) break;
-          if (sh.last_in[g]) {
+          patch |= sh.last_in[g] == 2;
+          finish = sh.last_in[g] != 0;
+          if (finish) {
             if (count == 2) {
               two = true;
             } else {
@@ -805,10 +806,12 @@ __global__ void __launch_bounds__(kTaThreads, 1)
         const Partial other = slot_of(a, 2 * (c0 + 1 - me) + me, HD, BLOCKS);
         join_two<T, HD, BLOCKS>(other, my + 2 * kTile + (BLOCKS == 2 ? g * HD : 0), g, in_block, me == 0, m_ref, sum, w0,
                                 n > 1 ? w1 : 0.f, n > 1, col0, on, out, wide_out);
-        if (patch && on)
-          patch_row<T, HD>(a, w.b, w.head, w.s, max(w.t0 * kTile, w.s.ctx), min(w.t1 * kTile, w.s.keys), mrow, col0, kCols,
-                           out, mine, in_block);
         if (t == 0) *arrived = 0;
+      }
+      if (finish && patch) {
+        group_meet();  // a row may have been joined by other threads
+        if (!ok) break;
+        patch_row<T, HD, BLOCKS>(a, w, g, t);
       }
       if (BLOCKS == 1) {  // the queries' place holds the sums, and each group reads both accumulators
         meet();
