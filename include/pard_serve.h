@@ -67,7 +67,7 @@ pard_status pard_chunk_attention(const void* d_q, int64_t q_stride, int32_t dtyp
 /* What requests ask of their logits before a token is drawn.  d_logits [batch *
  * width][row_stride]: `width` rows a sequence (1, or the nodes of its tree), fp32,
  * bf16 or fp16; d_out the same type and rows out_stride apart, may be d_logits
- * (other overlaps: undefined).  In 32 bits, in this order, rounded once:
+ * row for row (other overlaps are refused).  In 32 bits, in this order, rounded once:
  *   z = z / r where z > 0, else z r       tokens of the row's history
  *   z = z - f c - p [c > 0]               c: how often the token was generated
  *   z = z + its biases                    summed in the list's order

@@ -33,6 +33,22 @@ bool overlap(const void* out, const void* q, int64_t q_stride, int64_t row, int6
   return first < n_tokens && at + first * step < o + 2 * row * n_tokens;
 }
 
+// rows of `row` bytes, each side's a step of its own (at least a row) apart, share a byte
+bool overlap_apart(const void* x, int64_t x_step, const void* y, int64_t y_step, int64_t row, int64_t rows) {
+  const int64_t a = (int64_t)reinterpret_cast<uintptr_t>(x), b = (int64_t)reinterpret_cast<uintptr_t>(y);
+  if (x_step == y_step) {  // y's row i ends or begins in the nearest of x's rows, or the next
+    const int64_t d = b < a ? a - b : b - a, k = d / x_step, r = d - k * x_step;
+    return (r < row && k < rows) || (x_step - r < row && k + 1 < rows);
+  }
+  for (int64_t i = 0, j = 0; i < rows && j < rows;) {
+    const int64_t p = a + i * x_step, q = b + j * y_step;
+    if (p + row <= q) i += (q - row - p) / x_step + 1;  // the first row that ends behind q
+    else if (q + row <= p) j += (p - row - q) / y_step + 1;
+    else return true;
+  }
+  return false;
+}
+
 }  // namespace
 }  // namespace pard
 
@@ -128,10 +144,13 @@ pard_status pard_adjust_logits(const void* d_logits, int64_t row_stride, int32_t
   if (max_history > 0 && (!d_history || !d_hist_len)) return refuse(PARD_ERR_ARG, "adjust_logits: a history needs its tokens and lengths");
   if (n_bias < 0 || n_bias > kMaxBiases) return refuse(PARD_ERR_ARG, "adjust_logits: biases outside [0, 2047]");
   if (n_bias > 0 && (!d_bias_ids || !d_bias)) return refuse(PARD_ERR_ARG, "adjust_logits: biases need their tokens and values");
+  if (row_stride < vocab || out_stride < vocab) return refuse(PARD_ERR_ARG, "rows overlap: row stride too small");
+  const int64_t size = dtype == DT_F32 ? 4 : 2, rows = (int64_t)batch * width;
+  if (!(d_out == d_logits && (out_stride == row_stride || rows == 1)) &&
+      overlap_apart(d_logits, row_stride * size, d_out, out_stride * size, vocab * size, rows))
+    return refuse(PARD_ERR_ARG, "adjust_logits: the output lies over the logits, but not in place");
   if (!d_tokens != !d_mask) return refuse(PARD_ERR_ARG, "adjust_logits: a tree needs its tokens and its mask");
   if (d_tokens && width > kTreeMaxNodes) return refuse(PARD_ERR_ARG, "tree width outside [1, 256]");
-  if (row_stride < vocab || out_stride < vocab) return refuse(PARD_ERR_ARG, "rows overlap: row stride too small");
-  const uintptr_t size = dtype == DT_F32 ? 4 : 2;
   if (reinterpret_cast<uintptr_t>(d_logits) % size || reinterpret_cast<uintptr_t>(d_out) % size)
     return refuse(PARD_ERR_ARG, "adjust_logits: logits not aligned to their type");
   const AdjustArgs a{d_logits, row_stride, out_stride, dtype, batch, width, vocab, max_history, n_bias,

@@ -210,7 +210,7 @@ def adjust_logits(logits, history=None, hist_len=None, prompt_len=None, repetiti
         - frequency * count - presence * (count > 0)   of what was generated
         + biases, then -inf where not allowed
 
-    Returns [B * N, V] of the logits' type, or writes `out`, which may be logits."""
+    Returns [B * N, V] of the logits' type, or writes `out`, which may be logits (but not lie over others of its entries)."""
     return _ops.adjust_logits(logits, history, hist_len, prompt_len, repetition, frequency, presence, bias_ids, bias,
                               allowed, tokens, mask, out)
 

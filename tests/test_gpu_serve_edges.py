@@ -64,3 +64,17 @@ def test_infinities_in_a_part_of_far_lower_scores(tree, dtype, Hq, Hkv, hd, n, w
         assert torch.equal(got[odd].nan_to_num(nan=1.0), want[odd].nan_to_num(nan=1.0))
         fine = torch.isfinite(want)
         assert ((got - want).abs() <= tol)[fine].all()
+
+
+# ---- adjusted logits ------------------------------------------------------------------
+def test_adjusted_logits_over_others_are_refused(tree):  # noqa: F811
+    from paper_2504_18583_gb300.pard import PardError
+    z = torch.randn((5, 240), device="cuda")
+    kept, flat = z.clone(), z.view(-1)
+    for at, out in ((z[:, :200], z[:, 1:201]), (z[1:, :200], z[:4, :200]), (flat[:200].view(1, 200), flat[199:399].view(1, 200)),
+                    (z[:, :200], flat[:1000].view(5, 200))):
+        with pytest.raises(PardError):
+            tree.adjust_logits(at, out=out)
+    assert torch.equal(z, kept)
+    tree.adjust_logits(z[:, :120], out=z[:, 120:])  # beside each other
+    assert torch.equal(z[:, 120:], kept[:, :120]) and torch.equal(z[:, :120], kept[:, :120])

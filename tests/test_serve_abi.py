@@ -147,3 +147,40 @@ def test_a_workspace_is_enough_for_fewer_tokens_and_sequences(lib, heads):
         for batch in sizes:
             whole = f(T, batch, *heads)
             assert all(f(t, b, *heads) <= whole for t in sizes if t <= T for b in sizes if b <= batch)
+
+
+# six rows of 100 floats (ADJUST)
+@pytest.mark.parametrize("edit,over", [
+    (dict(out=P + 4), True),                                   # an entry further
+    (dict(z=P + 4, out=P), True),
+    (dict(out=P + 5 * 400 + 396), True),                       # the last entry of all
+    (dict(out=P + 6 * 400), False),
+    (dict(z=P + 6 * 400, out=P), False),
+    (dict(z=P + 5 * 400 + 396, out=P), True),
+    (dict(out=P + 400), True),                                 # a row further
+    (dict(out_stride=200), True),                              # the first row in place, the others not
+    (dict(stride=200, out=P + 400, out_stride=200), False),    # rows between rows
+    (dict(stride=200, out=P + 404, out_stride=200), True),
+    (dict(stride=200, out=P + 396, out_stride=200), True),
+    (dict(stride=200, out=P, out_stride=200), False),          # in place, rows apart
+    (dict(stride=200, out=P + 800 * 3, out_stride=200), True),
+    (dict(stride=300, out=P + 400, out_stride=150), True),     # rows 0 and 1 lie between rows, row 2 on one
+    (dict(stride=400, out=P + 400, out_stride=800), False),    # at 400, 3600, 6800, ... against 0, 1600, 3200, ...
+    (dict(batch=1, width=1, out=P + 400, out_stride=1000), False),
+    (dict(batch=1, width=1, out=P, out_stride=1000), False),   # one row in place, whatever its stride
+    (dict(batch=1, width=1, out=P + 396), True),
+    (dict(dtype=0, out=P + 200), True),                        # 16-bit rows are half as long
+    (dict(dtype=0, out=P + 1200), False),
+])
+def test_adjusted_logits_over_others(lib, edit, over):
+    """An output that lies over other entries of the logits than its own is refused; in place, between the rows and apart
+    from them it is not (and goes on to be refused for its tree, which is looked at later)."""
+    args = {**ADJUST, "mask": None, **edit}
+    size, rows = 4 if args["dtype"] == 2 else 2, args["batch"] * args["width"]
+    of = {args["z"] + (r * args["stride"] + i) * size + b: (r, i) for r in range(rows) for i in range(100) for b in range(size)}
+    hits = [of.get(args["out"] + (r * args["out_stride"] + i) * size + b, (r, i)) != (r, i) for r in range(rows) for i in range(100)
+            for b in range(size)]
+    hit = any(hits)
+    assert hit == over
+    assert call(lib, "pard_adjust_logits", args) == ARG
+    assert (b"over the logits" if over else b"its mask") in lib.pard_last_error()
