@@ -1,9 +1,10 @@
 """Edges of the serving operators: against the 64-bit forms of test_gpu_serve.py,
 with its tolerances where no other is derived here."""
+import numpy as np
 import pytest
 import torch
 
-from test_gpu_serve import BF, FP, PAGE, Case, tree  # noqa: F401
+from test_gpu_serve import BF, FP, PAGE, Case, check_adjust, tree, tree_mask, words_of  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -78,3 +79,30 @@ def test_adjusted_logits_over_others_are_refused(tree):  # noqa: F811
     assert torch.equal(z, kept)
     tree.adjust_logits(z[:, :120], out=z[:, 120:])  # beside each other
     assert torch.equal(z[:, 120:], kept[:, :120]) and torch.equal(z[:, :120], kept[:, :120])
+
+
+@pytest.mark.parametrize("grammar,branch,inplace", [(False, False, False), (True, False, True), (True, True, False), (False, True, True)])
+@pytest.mark.parametrize("dtype,B,N,V,L", [
+    (torch.float32, 600, 2, 4096, 900),   # slices of 4096: four pieces a thread; a CTA has both rows
+    (BF, 64, 1, 128256, 8000),            # slices of 6752
+    (FP, 64, 3, 128256, 6000),
+    (torch.float32, 5, 29, 2048, 1500),   # rows shared out over CTAs
+    (torch.float32, 1, 300, 700, 600),    # a CTA a row or two
+])
+def test_adjust_more_entries_than_threads(tree, dtype, B, N, V, L, grammar, branch, inplace):  # noqa: F811
+    """Slices of which more than 256 entries change, so that threads take them in turns; long slices; several rows a CTA;
+    in place too."""
+    if branch and N > 256:
+        branch = False
+    rs = np.random.RandomState(V + N)
+    z = (4 * torch.randn((B * N, V), generator=torch.Generator(device="cuda").manual_seed(V), device="cuda")).to(dtype)
+    kw = dict(hist=rs.randint(-1, V + 1, (B, L)), hist_len=rs.randint(L - 50, L + 3, B), prompt_len=rs.randint(0, L, B),
+              rep=rs.uniform(0.7, 1.5, B), freq=rs.uniform(-0.5, 0.5, B), pres=rs.uniform(-1, 1, B), ids=rs.randint(0, V, (B, 40)),
+              bias=rs.uniform(-5, 5, (B, 40)), allowed=words_of(rs.rand(B * N, V) < 0.6) if grammar else None)
+    if branch:
+        kw.update(tokens=kw["hist"][:, :N] % V, mask=tree_mask(rs, B, N))  # a branch's tokens are in the history too
+    if inplace:  # (check_adjust takes the values from z before the call)
+        got = check_adjust(tree, z, N, out=z, **kw)
+        assert got.data_ptr() == z.data_ptr()
+    else:
+        check_adjust(tree, z, N, **kw)
