@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_serve import BF, FP, PAGE, Case, check_adjust, tree, tree_mask, words_of  # noqa: F401
+from test_gpu_serve import BF, FP, PAGE, Case, check_adjust, dev, tree, tree_mask, words_of  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -65,6 +65,47 @@ def test_infinities_in_a_part_of_far_lower_scores(tree, dtype, Hq, Hkv, hd, n, w
         assert torch.equal(got[odd].nan_to_num(nan=1.0), want[odd].nan_to_num(nan=1.0))
         fine = torch.isfinite(want)
         assert ((got - want).abs() <= tol)[fine].all()
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_a_prompt_in_pieces_row_by_row(tree, eight, dtype):  # noqa: F811
+    """A prompt read whole, in uneven pieces and token by token: every output against 64 bits over the cache that was
+    written.  In fp16 the tolerance tells a window that begins one key later, or one first token fewer, in every row (in
+    bf16 its probabilities' rounding is as much as a key in some)."""
+    Hq, Hkv, hd, T, window, sinks = 8, 2, 64, 333, 150, 4
+    c = Case(dtype, Hq, Hkv, hd, [T, T], [0, 0], eight, seed=2)
+    qkv = torch.randn((2 * T, (Hq + 2 * Hkv) * hd), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(dtype)
+    freq, amp = tree.rope_frequencies(hd, 1e4)
+
+    def read(pieces):
+        if eight:
+            c.k, c.v, c.ks, c.vs = tree.quantized_cache(c.n_pages, Hkv, hd)
+        else:
+            c.k, c.v = (torch.zeros((c.n_pages, Hkv, PAGE, hd), dtype=dtype, device="cuda") for _ in range(2))
+        out, q, done = torch.empty_like(c.q), torch.empty_like(c.q), np.zeros(2, int)
+        for new in pieces:
+            rows = dev(np.concatenate([b * T + done[b] + np.arange(new[b]) for b in range(2)]), torch.int64)
+            pos = [done[b] + np.arange(new[b]) for b in range(2)]
+            slots = np.concatenate([c.table[b, p // PAGE] * PAGE + p % PAGE for b, p in enumerate(pos)])
+            q[rows] = tree.qk_norm_rope(qkv[rows], Hq, Hkv, dev(np.concatenate(pos)), dev(slots, torch.int64), c.k, c.v, freq,
+                                        amplitude=amp, k_scale=c.ks, v_scale=c.vs)
+            out[rows] = tree.chunk_attention(q[rows], c.k, c.v, dev(c.table), dev(np.cumsum([0] + list(new))), dev(done), window=window,
+                                             sinks=sinks, k_scale=c.ks, v_scale=c.vs)
+            done += new
+        assert (done == T).all()
+        return out.double(), q
+
+    for i, pieces in enumerate(([(T, T)], [(100, 1), (1, 231), (200, 1), (31, 1), (1, T - 234)], [(1, 2)] * 160 + [(T - 160, T - 320)])):
+        got, c.q = read(pieces)
+        if i == 0:
+            if eight:
+                c.ks, c.vs = c.ks.view(torch.uint8), c.vs.view(torch.uint8)
+            want, tol = c.reference(window, sinks)
+            late = torch.arange(2 * T, device="cuda") % T >= window + sinks
+            for wrong in (c.reference(window - 1, sinks)[0], c.reference(window, sinks - 1)[0]) if dtype == FP else ():
+                assert ((wrong - want).abs() > 2 * tol)[late].flatten(1).any(1).all()
+        assert ((got - want).abs() <= tol).all(), float(((got - want).abs() / tol).max())
 
 
 # ---- adjusted logits ------------------------------------------------------------------
