@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_serve import BF, FP, PAGE, Case, check_adjust, dev, tree, tree_mask, words_of  # noqa: F401
+from test_gpu_serve import BF, FP, PAGE, ROUND, Case, check_adjust, dev, tree, tree_mask, words_of  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -13,9 +13,9 @@ pytestmark = pytest.mark.gpu
 @pytest.mark.parametrize("eight", [False, True])
 def test_a_workspace_of_a_larger_batch(tree, eight):  # noqa: F811
     """Made for many single tokens, used for a piece of a prompt of as many tokens and fewer, and for the batch again."""
-    ws = tree.chunk_attention_workspace(256, 256, 32, 8, 128)
+    ws = tree.chunk_attention_workspace(256, 256, 8, 2, 128)
     for new, ctx in (([33], [700]), ([1] * 256, [40] * 256), ([256], [0]), ([200, 3], [9000, 4]), ([1], [3000])):
-        Case(BF, 32, 8, 128, new, ctx, eight, seed=len(new)).check(tree, workspace=ws)
+        Case(BF, 8, 2, 128, new, ctx, eight, seed=len(new)).check(tree, workspace=ws)
     assert int(ws[:1296].sum()) == 0
 
 
@@ -106,6 +106,27 @@ def test_a_prompt_in_pieces_row_by_row(tree, eight, dtype):  # noqa: F811
             for wrong in (c.reference(window - 1, sinks)[0], c.reference(window, sinks - 1)[0]) if dtype == FP else ():
                 assert ((wrong - want).abs() > 2 * tol)[late].flatten(1).any(1).all()
         assert ((got - want).abs() <= tol).all(), float(((got - want).abs() / tol).max())
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("n,ctx", [(1, 2 ** 30 - 1), (1, 128 * (152 * 55188 - 1) - 1), (1, 128 * (152 * 54002 - 1) - 1), (300, 2 ** 30 - 300)])
+def test_the_longest_contexts(tree, eight, n, ctx):  # noqa: F811
+    """Positions up to 2^30, over a page table that names one page again and again: all 16 keys count alike, but for the
+    last few.  A part's sums add up to 8 products a tile, each off by 2^-23 of the sum."""
+    c = Case(BF, 1, 1, 64, [n], [16], eight, seed=3)
+    page, end = int(c.table[0, 0]), ctx + n
+    c.ctx = [ctx]
+    c.table = torch.full((1, -(-end // PAGE)), page, dtype=torch.int32, device="cuda")
+    out = torch.full_like(c.q, float("nan"))
+    got = tree.chunk_attention(c.q, c.k, c.v, c.table, dev(c.starts), dev(c.ctx), k_scale=c.ks, v_scale=c.vs, out=out)[:, 0].double()
+    k, v = (c.values(w, [page])[0] for w in "kv")
+    pos = torch.arange(ctx, end, device="cuda")[:, None]
+    times = (pos - torch.arange(PAGE, device="cuda")) // PAGE + 1
+    w = torch.exp((c.q[:, 0].double() @ k.T) / 8) * times
+    w /= w.sum(1, keepdim=True)
+    want, mag = w @ v, w @ v.abs()
+    tol = ROUND[BF] * (want.abs() + 2 * mag) + end / 128 / 100 * 8 * 2.0 ** -23 * mag
+    assert ((got - want).abs() <= tol).all(), float(((got - want).abs() / tol).max())
 
 
 # ---- adjusted logits ------------------------------------------------------------------
