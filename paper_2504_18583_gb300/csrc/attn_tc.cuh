@@ -182,7 +182,10 @@ __device__ __forceinline__ uint32_t finite_of(uint32_t v) {
 // by less than a split costs stays whole.
 template <int SPLIT = kSplit>
 __device__ __forceinline__ int parts_of(int tiles, int most) {
-  // (the quotient in floating point is exact: half a unit off any whole number)
+  // Exact below 2^21 tiles: the quotient is 0.5 / most off any whole number, and
+  // __fdividef off by two units in the last place at most, 2^-22 (tiles + most) / most.
+  // Above, with the numerator's own rounding, it is off by up to 4 / most: a part more or
+  // less, which those who look for `most` leave room for.
   return tiles <= most + SPLIT ? 1 : (int)__fdividef((float)(tiles + most) - 0.5f, (float)most);
 }
 // Where CTA c's range begins: floor(total c / grid).  With fewer places than

@@ -831,8 +831,9 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
         tiles[e] = sh.tiles[2 * lane + e];
         mine[e] = tiles[e] ? a.n_kv_heads : 0;
       }
-      // (a unit's parts are less than one more than its tiles / most)
-      int least = max(1, all_tiles / grid), most = max(least, min(longest, all_tiles / (grid - units + 1) + 1));
+      // (a unit's parts are less than one more than its tiles / most, or, of millions of
+      // tiles, than its tiles and four / most)
+      int least = max(1, all_tiles / grid), most = max(least, min(longest, all_tiles / (grid - units + 1) + 5));
 #pragma unroll 1
       while (least < most) {
         const int mid = (least + most) / 2;

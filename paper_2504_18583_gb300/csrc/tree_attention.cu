@@ -314,8 +314,9 @@ __global__ void __launch_bounds__(kTaThreads, 1)
       tiles[e] = s.tiles;
       mine[e] = s.tiles ? a.n_kv_heads * s.blocks : 0;
     }
-    // (a unit's parts are less than one more than its tiles / most)
-    int least = max(1, all_tiles / grid), most = max(least, min(longest, all_tiles / (grid - units + 1) + 1));
+    // (a unit's parts are less than one more than its tiles / most, or, of millions of
+    // tiles, than its tiles and four / most)
+    int least = max(1, all_tiles / grid), most = max(least, min(longest, all_tiles / (grid - units + 1) + 5));
 #pragma unroll 1
     while (least < most) {
       const int mid = (least + most) / 2;

@@ -109,7 +109,8 @@ def test_a_prompt_in_pieces_row_by_row(tree, eight, dtype):  # noqa: F811
 
 
 @pytest.mark.parametrize("eight", [False, True])
-@pytest.mark.parametrize("n,ctx", [(1, 2 ** 30 - 1), (1, 128 * (152 * 55188 - 1) - 1), (1, 128 * (152 * 54002 - 1) - 1), (300, 2 ** 30 - 300)])
+@pytest.mark.parametrize("n,ctx", [(1, 2 ** 30 - 1), (1, 128 * (152 * 55188 - 1) - 1), (1, 128 * (152 * 54002 - 1) - 1), (300, 2 ** 30 - 300),
+                                   (1, 128 * 8378391 - 1)])  # as many parts as CTAs, and no more
 def test_the_longest_contexts(tree, eight, n, ctx):  # noqa: F811
     """Positions up to 2^30, over a page table that names one page again and again: all 16 keys count alike, but for the
     last few.  A part's sums add up to 8 products a tile, each off by 2^-23 of the sum."""

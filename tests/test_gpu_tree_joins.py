@@ -1,9 +1,10 @@
-"""Infinities in tree nodes' values, joined from parts: against test_gpu_tree.py's
-64-bit forms, with its tolerances."""
+"""Tree attention joined from parts: infinities in nodes' values, and contexts up to
+the largest, against test_gpu_tree.py's 64-bit forms, with its tolerances where no
+other is derived here."""
 import pytest
 import torch
 
-from test_gpu_tree import PAGE, run_attention, tree  # noqa: F401
+from test_gpu_tree import PAGE, ROUND, dev, run_attention, tree  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -29,3 +30,20 @@ def test_infinities_of_nodes_with_far_lower_scores(tree, dtype, Hq, Hkv, hd, n, 
             fine = torch.ones_like(got, dtype=torch.bool)
             fine[sight, :, 7] = fine[sight, :, hd - 1] = False
             assert ((got.double() - want).abs() <= tol)[fine].all()
+
+
+@pytest.mark.parametrize("keys", [2 ** 30, 128 * 8378391])  # the second: as many parts as CTAs, and no more
+def test_the_longest_contexts(tree, keys):  # noqa: F811
+    """Contexts up to 2^30, over a page table that names one page again and again: its 16 keys count alike.  A part's sums
+    add up to 8 products a tile, each off by 2^-23 of the sum."""
+    hd, n = 64, 1
+    g = torch.Generator().manual_seed(1)
+    pool, q = (torch.randn(shape, generator=g).bfloat16().cuda() for shape in ((3, 2, 1, PAGE, hd), (1, n, 1, hd)))
+    table = torch.full((1, keys // PAGE), 1, dtype=torch.int32, device="cuda")
+    out = torch.full_like(q, float("nan"))
+    tree.tree_attention(q, pool[:, 0], pool[:, 1], table, dev([keys - n]), dev([n]), dev([[[1]]], torch.int64), out=out)
+    k, v = pool[1, 0, 0].double(), pool[1, 1, 0].double()
+    w = torch.softmax(q[0, 0].double() @ k.T / 8, -1)
+    want, mag = w @ v, w @ v.abs()
+    tol = ROUND[torch.bfloat16] * (want.abs() + 2 * mag) + keys / 128 / 100 * 8 * 2.0 ** -23 * mag
+    assert ((out[0, 0].double() - want).abs() <= tol).all()
