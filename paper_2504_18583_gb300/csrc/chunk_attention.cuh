@@ -905,7 +905,13 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
     auto make = [&] {
       if (!more || !ok) return;
       const int slot = made % kAheadSegs;
-      if (made >= kAheadSegs) ok = warp_wait(sh.seg_free + slot, (made / kAheadSegs - 1) & 1, abort_flag);
+      if (made >= kAheadSegs) {
+        // An 8-bit cache's tiles pass this warp by, and it waits for as long as the others
+        // take for a segment: up to 10 min, since a wait of theirs that runs out ends this one.
+        const int tries = Q8 ? 300 : 1;
+        ok = false;
+        for (int i = 0; i < tries && !ok && !*abort_flag; ++i) ok = warp_wait(sh.seg_free + slot, (made / kAheadSegs - 1) & 1, abort_flag);
+      }
       if (!ok) return;
       __syncwarp();
       int some = 0;

@@ -130,6 +130,24 @@ def test_the_longest_contexts(tree, eight, n, ctx):  # noqa: F811
     assert ((got - want).abs() <= tol).all(), float(((got - want).abs() / tol).max())
 
 
+def test_a_unit_that_takes_longer_than_a_wait_may(tree):  # noqa: F811
+    """8-bit caches, a sequence of 2^29 keys: the CTA that comes to the short one's heads has been at its first part for
+    three seconds then, longer than a wait inside the kernel may last, and has many more parts after it."""
+    heads, hd, keys = torch.cuda.get_device_properties(0).multi_processor_count, 64, 2 ** 29
+    c = Case(BF, heads, heads, hd, [1, 1], [15, 5], True, seed=4)
+    want, tol = c.reference()
+    c.ctx = [keys - 1, 5]
+    table = torch.zeros((2, keys // PAGE), dtype=torch.int32, device="cuda")
+    table[0], table[1, 0] = int(c.table[0, 0]), int(c.table[1, 0])
+    c.table = table
+    got = tree.chunk_attention(c.q, c.k, c.v, c.table, dev(c.starts), dev(c.ctx), k_scale=c.ks, v_scale=c.vs,
+                               out=torch.full_like(c.q, float("nan"))).double()
+    assert ((got[1] - want[1]).abs() <= tol[1]).all()
+    # the long one's sums pass what 32 bits tell apart: a weighted mean of its 16 values all the same
+    v = c.values("v", [int(table[0, 0])])
+    assert ((got[0] > 2 * v.amin(1) - 1) & (got[0] < 2 * v.amax(1) + 1)).all()
+
+
 # ---- adjusted logits ------------------------------------------------------------------
 def test_adjusted_logits_over_others_are_refused(tree):  # noqa: F811
     from paper_2504_18583_gb300.pard import PardError
