@@ -769,7 +769,6 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
     while (next()) {
       const Segment& u = segment();
       const int n = u.t1 - u.t0;
-      const int last_keys = u.g.limit(a, u.t1 - 1) - u.g.tile(u.t1 - 1) * kTile;
       const uint32_t turn = (taken - 1) & 1;
       ok = ok && warp_wait(&sh.q_full, turn, abort_flag);
       if (!by_tma) tc_fence_after();
@@ -780,8 +779,11 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
 #pragma unroll 1
       for (int j = -kAhead; j < n && ok; ++j) {
         const bool more = j + kAhead < n;
-        int keys = j == n - 1 ? last_keys : kTile;  // of tile j
-        if (j >= 0 && u.t0 + j < u.g.sink) keys = u.g.limit(a, u.t0 + j) - (u.t0 + j) * kTile;
+        // Keys of tile j, all tiles by one formula.  (As a choice by j, of the last tile's
+        // count, that of the first tokens' last and kTile, CUDA 13.0.88 compiles the kernels
+        // of one block to kTile where a traced j equals the first tokens' index: stale rows of
+        // shared memory are multiplied then, which test_tiles_that_are_not_loaded_whole sees.)
+        const int keys = min(kTile, u.g.limit(a, u.t0 + j) - u.g.tile(u.t0 + j) * kTile);
         const uint32_t kb = uniform(k_addr + kst * (kStage >> 4)), vb = uniform(v_addr + vst * (kStage >> 4));
         if (j >= 0) ok = warp_wait(sh.fixed + vst, vph, abort_flag);
         if (BLOCKS == 1 && j == 0) ok = ok && warp_wait(sh.ready + 0, turn, abort_flag) && warp_wait(sh.ready + 1, turn, abort_flag);
