@@ -54,6 +54,8 @@
 //     110000 clocks near HBM's rate, 15000 before, 6500 to write a part and 9000
 //     to 12000 for the last to join ten or eleven.
 //   1 node at 512: 12 us, all of it dependent steps.
+#include <type_traits>
+
 #include "attn_tc.cuh"
 
 namespace pard {
@@ -314,9 +316,15 @@ __global__ void __launch_bounds__(kTaThreads, 1)
       tiles[e] = s.tiles;
       mine[e] = s.tiles ? a.n_kv_heads * s.blocks : 0;
     }
-    // (a unit's parts are less than one more than its tiles / most, or, of millions of
-    // tiles, than its tiles and four / most)
-    int least = max(1, all_tiles / grid), most = max(least, min(longest, all_tiles / (grid - units + 1) + 5));
+    // (A unit's parts are less than one more than its tiles / most, or, of millions of
+    // tiles, than its tiles and four / most: a CTA fewer to share out is room for that.
+    // Signed or unsigned, the quotients are the same, but what the compiler makes of the
+    // whole kernel is not: with signed ones two trees of 13 nodes at 65000 take 59.8 us
+    // instead of 57.6, one node at 512 12.7 instead of 12.4; with unsigned ones the kernels
+    // of two blocks take 68.2 instead of 67.0 for 8 x 64 nodes at 4096.)
+    using Whole = std::conditional_t<BLOCKS == 1, uint32_t, int>;
+    int least = max(1, (int)((Whole)all_tiles / (Whole)grid));
+    int most = max(least, min(longest, (int)((Whole)all_tiles / (Whole)max(grid - units, 1)) + 1));
 #pragma unroll 1
     while (least < most) {
       const int mid = (least + most) / 2;
