@@ -20,8 +20,10 @@ extern "C" {
  * 16).  For each token and head b is the smallest in [1, 254] with |x| <= 448 *
  * 2^(b - 127) for all its finite entries, and a code is x / 2^(b - 127) rounded
  * to the nearest, ties to even, from the 32-bit x (queries are rounded to `dtype`
- * as there).  Infinities and NaN are stored as NaN.  No two tokens of a call may
- * have the same slot (but negative ones). */
+ * as there).  Infinities and NaN are stored as NaN.  The cache holds what fp32
+ * does, but pard_chunk_attention reads entries as fp16: larger ones than 65504 come
+ * back as 65504, and what lies between multiples of 2^-24 rounded to them.  No two
+ * tokens of a call may have the same slot (but negative ones). */
 pard_status pard_qk_norm_rope_quantized(const void* d_qkv, int64_t qkv_stride, int32_t dtype, int32_t n_tokens,
                                         int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, const void* d_q_gain,
                                         const void* d_k_gain, float eps, const int32_t* d_pos, const int64_t* d_slots,
@@ -46,12 +48,13 @@ pard_status pard_qk_norm_rope_quantized(const void* d_qkv, int64_t qkv_stride, i
  * pard_qk_norm_rope_quantized writes them: an entry is then its code times its
  * power of two, held to +-65504 and to multiples of 2^-24.  Scores and sums are
  * held in 32 bits; probabilities are rounded to `dtype` (with an 8-bit cache to
- * fp16) before they multiply the values.  d_out must not overlap d_q.  d_workspace:
- * pard_chunk_attention_workspace_bytes (0: invalid arguments) bytes, which are
- * enough for all calls with these heads and no more tokens and sequences, the first
- * 4096 of them zero before the first call; each call leaves them fit for the
- * next, of any sizes that they are enough for, and for pard_tree_attention
- * (whose workspace fits here too).  Calls that may overlap on the GPU need one
+ * fp16) before they multiply the values.  An infinity in a value makes the outputs
+ * of the tokens that see it infinite, or NaN where its weight is 0 in 32 bits.
+ * d_out must not overlap d_q.  d_workspace: pard_chunk_attention_workspace_bytes
+ * (0: invalid arguments) bytes, which are enough for all calls with these heads and
+ * no more tokens and sequences, the first 4096 of them zero before the first call;
+ * each call leaves them fit for the next, of any sizes that they are enough for,
+ * and for pard_tree_attention (whose workspace fits here too).  Calls that may overlap on the GPU need one
  * each.  Should a wait inside the kernel ever run out (2 s), the output is NaN,
  * and so is that of later calls until those bytes are zeroed again. */
 size_t pard_chunk_attention_workspace_bytes(int32_t n_tokens, int32_t batch, int32_t n_q_heads, int32_t n_kv_heads,
@@ -80,7 +83,8 @@ pard_status pard_chunk_attention(const void* d_q, int64_t q_stride, int32_t dtyp
  * r, f, p: d_repetition, d_frequency, d_presence [batch] (null: 1, 0, 0).  Biases:
  * d_bias_ids, d_bias [batch][n_bias] (at most 2047).  d_allowed [batch * width]
  * [ceil(vocab / 32)] (null: all): bit v mod 32 of word v / 32.  Tokens outside
- * [0, vocab) are passed over.  vocab <= 262144, max_history <= 524000. */
+ * [0, vocab) are passed over.  vocab <= 262144, max_history <= 524000, batch <=
+ * 65535, batch * width <= 2^24. */
 pard_status pard_adjust_logits(const void* d_logits, int64_t row_stride, int32_t dtype, int32_t batch, int32_t width,
                                int32_t vocab, const int32_t* d_history, int32_t max_history, const int32_t* d_hist_len,
                                const int32_t* d_prompt_len, const float* d_repetition, const float* d_frequency,

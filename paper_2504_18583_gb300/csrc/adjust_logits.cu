@@ -21,9 +21,9 @@
 // where it is needed.
 //
 // What bounds it: HBM for many rows (464 of 128256 in fp32, of 16 trees, with
-// penalties, biases and masks: 84 us, 5.7 TB/s), and for few the chain history ->
-// table -> list -> row (64 of 128256 in bf16 with 8000 tokens each: 17.3 us, 9 of them
-// without the tokens; one: 4.6); a row's loads go out before the history's are looked
+// penalties, biases and masks: 86 us, 5.6 TB/s), and for few the chain history ->
+// table -> list -> row (64 of 128256 in bf16 with 8000 tokens each: 17.4 us, 9 of them
+// without the tokens; one: 4.2); a row's loads go out before the history's are looked
 // at, and the next row's before this one is worked on.  Slices are as long as they may
 // be while the CTAs come out as whole waves of four an SM.
 #include <cuda_fp16.h>

@@ -30,7 +30,8 @@
 // columns up to its own position, less those between the first tokens and its
 // window.  There values may hold anything: what lies past the last key that a tile is
 // read for, and infinities and NaN of keys that not every row sees, are zeroed in
-// shared memory, and the epilogue adds the latter back for the rows that see them.
+// shared memory, and the CTA that writes a unit's output adds the latter back for the
+// rows that see them.
 //
 // An 8-bit cache (e4m3 codes, a power of two a token and head) is loaded as it lies
 // into rings of its own, and four more warps turn each tile into fp16 operands, exactly
@@ -44,17 +45,20 @@
 //   its 32 products 2052 of them and the softmax of both groups, eight warps, nearly all
 //   the others': scores wait for the probabilities that lie where they go.  The clock
 //   falls to 1.8 GHz under the power limit.  2048 tokens behind 30000 (64 heads on 8 of
-//   128): 1.41 ms, 1.48 PFLOP/s, 1.58 ms in a long run.  A prompt of 8191: 405 us.
+//   128): 1.40 ms, 1.49 PFLOP/s, 1.58 ms in a long run.  A prompt of 8191: 401 us, 412 in
+//   a long run.
 // - Units' ends: 7000 to 8000 clocks from a unit's last scores to the next one's first
-//   probabilities.  Four pieces of up to 512 tokens: 71 us; 16 sequences, most of them
-//   single tokens, with a window (heads of 64): 54 us, 2800 to 3600 clocks a tile, where
+//   probabilities.  Four pieces of up to 512 tokens: 70 us; 16 sequences, most of them
+//   single tokens, with a window (heads of 64): 52 us, 2800 to 3600 clocks a tile, where
 //   masked tiles are many.
-// - Single tokens, 16-bit cache: HBM.  32 of them over 264000 keys: 180 us, 90% of the
+// - Single tokens, 16-bit cache: HBM.  32 of them over 264000 keys: 179 us, 90% of the
 //   copy rate.
-// - 8-bit cache: shared memory.  A pair of tiles is written once as it lies, read, written
-//   as fp16 and read by the products, 1800 clocks of its 2800 (HBM: 1400): 32 single
-//   tokens 194 us; 1000 tokens behind 16001 274 us, against 214 from a 16-bit cache.
-// - A single token with a window of 2048: 14.4 us, the chain lengths -> shares -> pages ->
+// - 8-bit cache: the chain copy -> conversion -> products, two tiles deep, which is what
+//   fits beside the 16-bit operands: 2800 clocks a pair of tiles, where HBM would take
+//   1400 and shared memory, which has the bytes four times, 1800.  No unit is full: shared
+//   memory's pipe 32%, issue slots 41%, tensor pipe 34%, HBM 37%.  32 single tokens 192 us,
+//   more than from a 16-bit cache; 1000 tokens behind 16001 276 us, 214 from a 16-bit one.
+// - A single token with a window of 2048: 14.5 us, the chain lengths -> shares -> pages ->
 //   keys -> softmax -> partial -> join, 28000 clocks.
 //
 // Tried and slower: 64-column score products (2048 tokens behind 30000: 1417 -> 1631 us),
@@ -77,8 +81,8 @@ namespace {
 
 constexpr int kSeqHeld = 64;                    // sequences whose lengths a CTA keeps at hand
 constexpr int kStep = kTile / 2;                // keys of a step
-// what a unit's start, and splitting it, costs in tiles (2 and 6, 3 and 3, 4 and 3: within 3% of these on all cases but the
-// ragged ones, up to 12% slower there)
+// What a unit's start, and splitting it, costs in tiles.  (2 and 6: four ragged pieces 73 us instead of 70.5; but 1000 tokens
+// behind 16001 202 instead of 213, in an 8-bit cache 268 instead of 276; others within 1%.)
 constexpr int kUnitStart = 3, kUnitSplit = 4;
 using ChunkRanges = RangesOf<kUnitSplit>;
 constexpr int kConvWarps = 4;                   // warps that convert an 8-bit cache's tiles

@@ -41,7 +41,7 @@
 // node (0 x NaN would reach every row otherwise).
 //
 // What bounds it, measured:
-//   8 sequences x 64 nodes at 4096, 64/8 heads of 128: 69 us; 36 us of products
+//   8 sequences x 64 nodes at 4096, 64/8 heads of 128: 68 us; 36 us of products
 //     at the peak.  Its 128 units stay whole, so 24 of 152 CTAs have no part.  A
 //     pair of tiles takes 3300 clocks: 2100 of products, and the chain softmax
 //     (1310) -> P V -> scores of one group, of which the issuing warp's waits and

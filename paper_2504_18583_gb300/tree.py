@@ -115,7 +115,8 @@ def qk_norm_rope(qkv, n_q_heads: int, n_kv_heads: int, pos, slots, k_cache, v_ca
     k_scale and v_scale [pages, Hkv, 16] (float8_e8m0fnu or uint8) the caches are
     float8_e4m3fn and a token's head is stored as codes and a power of two
     (pard_qk_norm_rope_quantized; quantized_cache makes one); tokens of a call
-    then need slots of their own.  Returns the queries [T, Hq, hd]."""
+    then need slots of their own.  chunk_attention reads such entries as fp16: held
+    to 65504 and to multiples of 2^-24.  Returns the queries [T, Hq, hd]."""
     return _ops.qk_norm_rope(qkv, n_q_heads, n_kv_heads, pos, slots, k_cache, v_cache, inv_freq, q_gain, k_gain, eps,
                              interleaved, amplitude, k_scale, v_scale)
 
