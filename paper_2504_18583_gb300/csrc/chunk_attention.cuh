@@ -915,8 +915,10 @@ __global__ void __launch_bounds__(chunk_threads(Q8), 1)
         // An 8-bit cache's tiles pass this warp by, and it waits for as long as the others
         // take for a segment: up to 10 min, since a wait of theirs that runs out ends this one.
         const int tries = Q8 ? 300 : 1;
-        ok = false;
-        for (int i = 0; i < tries && !ok && !*abort_flag; ++i) ok = warp_wait(sh.seg_free + slot, (made / kAheadSegs - 1) & 1, abort_flag);
+        for (int i = 1;; ++i) {  // (all lanes leave together)
+          ok = warp_wait(sh.seg_free + slot, (made / kAheadSegs - 1) & 1, abort_flag);
+          if (ok || i == tries || __any_sync(0xffffffffu, *abort_flag)) break;
+        }
       }
       if (!ok) return;
       __syncwarp();
